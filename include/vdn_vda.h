@@ -276,6 +276,102 @@ vdn_status vdn_vda_prepare(vdn_vda_t h, const void* q_in, const void* k_in, cons
                            void* k_out, void* v_out, int B, int T, int F, int H, int d,
                            const vdn_vda_prep_params* p, void* cuda_stream);
 
+/* Token-wise gated delta rule (Eq. 2): the rule whose frame-wise form is the layer above, for tokens that do have an
+ * order -- a prompt, whose final state is the text state s0 of vdn_vda_forward_ex, or a causal layer token by token.
+ * Per value head, with alpha_t = exp(log_alpha_t):
+ *      S <- alpha_t S,    S <- S + beta_t (v_t - S k_t) k_t^T,    o_t = scale * S q_t
+ * Two entry points share the struct: vdn_vda_token_scan for whole sequences packed one behind another, vdn_vda_token_step
+ * for one token or a few of each request of a batch, the requests' states staying in a pool.
+ *
+ *   q, k    [N, key_heads, d] of cfg.io_dtype, DEVICE, 16-byte aligned.  Value head h reads key head
+ *           h / (heads / key_heads); key_heads divides heads.
+ *   v, out  [N, heads, d] of cfg.io_dtype.  out must not alias an input.
+ *   beta    [N, heads] float: write gate, already through the sigmoid.
+ *   p->log_alpha  [N, heads] float or NULL (= 0, no decay): natural logarithm of the decay gate, <= 0; -infinity forgets the
+ *           state.
+ *   p->q_stride, k_stride, v_stride, out_stride   elements from one token to the next, 0 = dense (heads of a token are
+ *           always dense): q, k, v may be slices of one projected tensor.  Multiples of 16 bytes.
+ *   p->l2_eps     0: q and k are used as they are.  > 0: x / sqrt(sum_j x_j^2 + l2_eps) first.
+ *   p->scale      factor on the read-out.
+ * States are float [.., heads, d_v, d_k], the orientation of s0 above, whatever io_dtype is.
+ *
+ * vdn_vda_token_scan: sequence s is the rows cu_seqlens[s] .. cu_seqlens[s+1]-1 (any length, zero too).
+ *   p->cu_seqlens int32 [n_seqs + 1], DEVICE, not decreasing, from 0 up to at most n_tokens; NULL only with n_seqs = 1: all
+ *           rows.  Rows behind the last sequence are neither read into a result nor written.  Offsets beyond the tensor are
+ *           clamped to it (wrong rows, but no access outside).
+ *   p->s0         [n_seqs, heads, d, d] or NULL (= 0): state before each sequence.
+ *   p->state      [n_seqs, heads, d, d] or NULL: receives the state after each sequence (s0 for an empty one); may be s0.
+ *   p->index, p->n_slots: must be NULL / 0.
+ *   workspace     DEVICE, 256-byte aligned, at least vdn_vda_token_scan_workspace_bytes (0 where none is needed; NULL is fine
+ *           then).  It is an argument and not the handle's, so that calls that may overlap, or captured graphs, can each
+ *           have their own; nothing in it outlives the call.
+ *   bf16 with d = 128 runs on the tensor cores in chunks of 64 tokens: the state, its products and the chunk's
+ *   triangular inverse keep 16 significant bits or more of every factor and fp32 sums (state within 1e-5 of a 64-bit
+ *   evaluation, relative to its norm); the rest, and VDN_FLAG_FORCE_SIMT, token by token in plain fp32.
+ * vdn_vda_token_step: request s is rows s * per .. (s + 1) * per - 1 of n_requests * per.
+ *   p->state      [n_slots, heads, d, d]: the pool, updated in place.
+ *   p->index      int32 [n_requests], DEVICE, or NULL (= s): the request's state.  A negative or too large index marks a
+ *           padding entry: its rows of out and every state are left as they were.  An index that an earlier request has
+ *           already is skipped the same way and vdn_vda_status reports VDN_ERR_INVALID_ARG.
+ *   p->cu_seqlens, p->s0: must be NULL.
+ * Both enqueue on cuda_stream and return; neither synchronises.  n_tokens = 0 / n_requests = 0 is a valid call. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(vdn_vda_token_params), checked */
+  int32_t heads, key_heads;
+  int32_t n_seqs;            /* vdn_vda_token_scan */
+  float scale, l2_eps;
+  const int32_t* cu_seqlens;
+  const int32_t* index;
+  const float* log_alpha;
+  const float* s0;
+  float* state;
+  int64_t n_slots;           /* vdn_vda_token_step */
+  int64_t q_stride, k_stride, v_stride, out_stride;
+} vdn_vda_token_params;
+size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p);
+vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
+                              long long n_tokens, const vdn_vda_token_params* p, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream);
+vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
+                              int n_requests, int per, const vdn_vda_token_params* p, void* cuda_stream);
+
+/* Rotary positions on three axes (time, height, width), for the queries and keys of the Softmax branch that runs beside
+ * the layer (the linear branch takes none, Sec. 2.3).  Pair p of a head's channels is turned by the angle
+ * position(token, axis[p]) * freq[p]:   (x, y) -> (x cos - y sin, x sin + y cos).
+ *
+ *   q_in, q_out   [B,T,F,H,d] of cfg.io_dtype, DEVICE, 16-byte aligned; q_out may be q_in.
+ *   k_in, k_out   [B,T,F,key_heads,d], likewise; both NULL: queries only.
+ *   p->pairs      rotated pairs, 1 .. d/2; the channels beyond them pass through.
+ *   p->flags      VDN_ROTARY_HALF: pair p is the channels (p, p + pairs), pairs a multiple of 8; otherwise (2p, 2p + 1).
+ *                 VDN_ROTARY_INVERSE: by the opposite angle (undoes the rotation; applied to a gradient it gives the
+ *                 gradient of the input).  Not together with norm_eps.
+ *   p->freq       double [pairs], DEVICE: angle per position.   p->axis  int32 [pairs], DEVICE: 0 time, 1 height, 2 width; a
+ *                 pair with any other value is left as it is.
+ *   p->positions  int32 [3][B*T*F], DEVICE, or NULL: token (t, u) of each clip stands at time t0 + t, height u / X, width u % X
+ *                 (F = Y * X; Y and X are not looked at when positions are given).
+ *   p->norm_eps   0: none.  > 0: each head's channels are first divided by sqrt(mean_j x_j^2 + norm_eps) and multiplied by
+ *                 q_weight / k_weight (float [d], DEVICE, or NULL = 1).
+ *   p->q_stride, k_stride, q_out_stride, k_out_stride   elements from one token to the next, 0 = dense.
+ * Angles are formed in 64 bits, everything else in 32; one rounding to io_dtype.  Needs no workspace.  Enqueues on
+ * cuda_stream and returns; does not synchronise. */
+#define VDN_ROTARY_HALF 1u
+#define VDN_ROTARY_INVERSE 2u
+typedef struct {
+  uint32_t struct_size;      /* sizeof(vdn_vda_rotary_params), checked */
+  uint32_t flags;
+  int32_t pairs, key_heads;
+  int32_t Y, X, t0;
+  float norm_eps;
+  const double* freq;
+  const int32_t* axis;
+  const int32_t* positions;
+  const float* q_weight;
+  const float* k_weight;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+} vdn_vda_rotary_params;
+vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void* q_out, void* k_out, int B, int T, int F,
+                          int H, int d, const vdn_vda_rotary_params* p, void* cuda_stream);
+
 /* The same layer for callers whose tensors live in HOST memory (pinned memory recommended; with pageable
  * memory the copies are not asynchronous).  All six tensor pointers are HOST pointers.  The staging buffer is a
  * caller-owned DEVICE buffer of at least vdn_vda_staging_bytes, set beforehand.  The copies in run on an input
@@ -356,7 +452,8 @@ vdn_status vdn_vda_scan_static(const float* stats, const float* inv, float* read
 
 /* Plumbing (no passage of the paper to cite).  Last device-side status recorded by this handle's kernels: VDN_OK,
  * VDN_ERR_TIMEOUT (a wait inside a kernel ran out; that kernel's CTA stopped early and the outputs of the call are
- * incomplete) or VDN_ERR_INTERNAL.  Does not synchronise: call it after synchronising the stream.  The word is
+ * incomplete), VDN_ERR_INTERNAL or VDN_ERR_INVALID_ARG (vdn_vda_token_step skipped a request whose state an earlier one of
+ * the same call has).  Does not synchronise: call it after synchronising the stream.  The word is
  * sticky: reading it clears nothing, and no forward call clears it, so that an error is not lost between a call
  * and the moment the caller looks.  vdn_vda_clear_status resets it. */
 vdn_status vdn_vda_status(vdn_vda_t h);

@@ -16,7 +16,7 @@ LIB_PATH = os.environ.get("VDN_VDA_LIB") or os.path.join(_HERE, "libvdn_vda.so")
 VDN_OK = 0
 STATUS_NAMES = {0: "VDN_OK", 1: "VDN_ERR_INVALID_ARG", 2: "VDN_ERR_UNSUPPORTED", 3: "VDN_ERR_WORKSPACE",
                 4: "VDN_ERR_CUDA", 5: "VDN_ERR_ARCH", 6: "VDN_ERR_TIMEOUT", 7: "VDN_ERR_INTERNAL"}
-VDN_ERR_TIMEOUT, VDN_ERR_INTERNAL = 6, 7
+VDN_ERR_INVALID_ARG, VDN_ERR_TIMEOUT, VDN_ERR_INTERNAL = 1, 6, 7
 VDN_F32, VDN_BF16 = 0, 1
 VDN_FLAG_FORCE_SIMT = 1
 VDN_FLAG_ADDITIVE_RULE = 4
@@ -24,11 +24,13 @@ VDN_FLAG_SCAN_CHUNKWISE = 8
 VDN_FLAG_SCAN_FRAMEWISE = 16
 VDN_FLAG_EXACT_STATS = 32
 VDN_FLAG_FP32_RESOLVE = 64
+VDN_ROTARY_HALF, VDN_ROTARY_INVERSE = 1, 2
 VIEW_STATS, VIEW_INV, VIEW_FWD, VIEW_READ, VIEW_INV_SPLIT, VIEW_READ_FWD, VIEW_READ_BWD, VIEW_COMP_M, VIEW_COMP_J = range(9)
 
 EXPORTS = (
     "vdn_vda_create", "vdn_vda_workspace_bytes", "vdn_vda_set_workspace", "vdn_vda_forward", "vdn_vda_forward_ex",
     "vdn_vda_forward_opt", "vdn_vda_workspace_bytes_opt", "vdn_vda_prepare",
+    "vdn_vda_token_scan_workspace_bytes", "vdn_vda_token_scan", "vdn_vda_token_step", "vdn_vda_rotate",
     "vdn_vda_staging_bytes", "vdn_vda_staging_bytes_opt", "vdn_vda_set_staging", "vdn_vda_forward_host",
     "vdn_vda_forward_host_opt", "vdn_vda_workspace_view",
     "vdn_vda_last_launch_count", "vdn_vda_profile", "vdn_vda_kernel_times", "vdn_vda_scan_static", "vdn_vda_status",
@@ -53,6 +55,24 @@ class VdnPrepParams(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("Y", ctypes.c_int32), ("X", ctypes.c_int32),
                 ("anchors", ctypes.c_int32), ("l2_eps", ctypes.c_float), ("wk_spatial", ctypes.c_void_p),
                 ("wk_temporal", ctypes.c_void_p), ("wv_spatial", ctypes.c_void_p), ("wv_temporal", ctypes.c_void_p)]
+
+
+class VdnTokenParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("heads", ctypes.c_int32), ("key_heads", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("scale", ctypes.c_float), ("l2_eps", ctypes.c_float),
+                ("cu_seqlens", ctypes.c_void_p), ("index", ctypes.c_void_p), ("log_alpha", ctypes.c_void_p),
+                ("s0", ctypes.c_void_p), ("state", ctypes.c_void_p), ("n_slots", ctypes.c_int64),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64)]
+
+
+class VdnRotaryParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("pairs", ctypes.c_int32),
+                ("key_heads", ctypes.c_int32), ("Y", ctypes.c_int32), ("X", ctypes.c_int32), ("t0", ctypes.c_int32),
+                ("norm_eps", ctypes.c_float), ("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64),
+                ("k_out_stride", ctypes.c_int64)]
 
 
 class VdnError(RuntimeError):
@@ -97,6 +117,15 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.vdn_vda_workspace_bytes_opt.restype = sz
     lib.vdn_vda_prepare.argtypes = [vp, vp, vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnPrepParams), vp]
     lib.vdn_vda_prepare.restype = ci
+    tok, i64 = ctypes.POINTER(VdnTokenParams), ctypes.c_longlong
+    lib.vdn_vda_token_scan_workspace_bytes.argtypes = [vp, i64, tok]
+    lib.vdn_vda_token_scan_workspace_bytes.restype = sz
+    lib.vdn_vda_token_scan.argtypes = [vp, vp, vp, vp, vp, vp, i64, tok, vp, sz, vp]
+    lib.vdn_vda_token_scan.restype = ci
+    lib.vdn_vda_token_step.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, tok, vp]
+    lib.vdn_vda_token_step.restype = ci
+    lib.vdn_vda_rotate.argtypes = [vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnRotaryParams), vp]
+    lib.vdn_vda_rotate.restype = ci
     lib.vdn_vda_forward_host.argtypes = fwd_args
     lib.vdn_vda_forward_host.restype = ci
     lib.vdn_vda_forward_host_opt.argtypes = [vp, vp, vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnOptions), vp]
@@ -213,6 +242,72 @@ def validate_layer_args(io_dtype, d_handle, device_index, q, k, v, beta, gate, o
     if norm_weight is not None:
         _require("norm_weight", norm_weight, (H, d), f32, on_cuda, device_index)
     return B, T, F, H, d
+
+
+def _require_rows(name, x, lead, heads, d, dtype, on_cuda, device_index):
+    """A tensor [*lead, heads, d] whose tokens may lie apart: the heads of a token dense, one distance between all tokens,
+    a multiple of 16 bytes.  Returns that distance in elements."""
+    if x is None:
+        raise ValueError(f"{name} is missing")
+    if tuple(x.shape) != (*lead, heads, d):
+        raise ValueError(f"{name} must have shape {(*lead, heads, d)}, got {tuple(x.shape)}")
+    if x.is_contiguous():
+        _require(name, x, x.shape, dtype, on_cuda, device_index)
+        return heads * d
+    st = x.stride()
+    n, step, ok = 1, None, (d == 1 or st[-1] == 1) and (heads == 1 or st[-2] == d)
+    for size, stride in zip(reversed(lead), reversed(st[:-2])):
+        if size != 1:
+            step = stride if step is None else step
+            ok = ok and stride == step * n
+        n *= size
+    step = heads * d if step is None else step
+    if not ok or step < heads * d or (step * x.element_size()) % 16:
+        raise ValueError(f"{name}: the heads of a token must be contiguous and its tokens evenly spaced, by a multiple of 16 bytes")
+    if bool(x.is_cuda) != on_cuda:
+        raise ValueError(f"{name} must be a {'CUDA' if on_cuda else 'host'} tensor")
+    if on_cuda and (x.device.index or 0) != device_index:
+        raise ValueError(f"{name} is on cuda:{x.device.index}, the handle is bound to cuda:{device_index}")
+    if x.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+    return step
+
+
+def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=None, log_alpha=None, on_cuda=True):
+    """Checks the token tensors of token_scan / token_step: q, k [..., Hk, d], v, out [..., H, d], beta, log_alpha [..., H].
+    Returns (leading shape, H, Hk, strides of q, k, v, out)."""
+    import torch
+    if v is None or v.dim() < 3:
+        raise ValueError("v must have shape [tokens, heads, d]")
+    if q is None or q.dim() != v.dim():
+        raise ValueError("q must have as many dimensions as v")
+    lead, H, Hk, d = tuple(int(n) for n in v.shape[:-2]), int(v.shape[-2]), int(q.shape[-2]), int(v.shape[-1])
+    if d != d_handle:
+        raise ValueError(f"v must have head dimension {d_handle}, got {d}")
+    if H == 0 or Hk == 0 or H % Hk:
+        raise ValueError(f"q must have a number of heads that divides the {H} of v, got {Hk}")
+    strides = [_require_rows(n, x, lead, c, d, io_dtype, on_cuda, device_index)
+               for n, x, c in (("q", q, Hk), ("k", k, Hk), ("v", v, H))]
+    _require("beta", beta, (*lead, H), torch.float32, on_cuda, device_index)
+    if log_alpha is not None:
+        _require("log_alpha", log_alpha, (*lead, H), torch.float32, on_cuda, device_index)
+    strides.append(H * d if out is None else _require_rows("out", out, lead, H, d, io_dtype, on_cuda, device_index))
+    return lead, H, Hk, strides
+
+
+def rotary_tables(sections, theta=10000.0, shared_ladder=False):
+    """(freq, axis) of rotate() for pairs that are `sections` = (time, height, width) pairs, one axis behind another (host
+    tensors).  Each axis has its own ladder theta^(-i / n) over its n pairs; with shared_ladder pair p of all n pairs has
+    theta^(-p / n) whatever its axis."""
+    import torch
+    if len(sections) != 3 or any(int(n) != n or n < 0 for n in sections) or sum(sections) == 0:
+        raise ValueError("sections must be three numbers of pairs, not all zero")
+    axis = torch.repeat_interleave(torch.arange(3, dtype=torch.int32), torch.tensor([int(n) for n in sections]))
+    if shared_ladder:
+        e = torch.arange(len(axis), dtype=torch.float64) / len(axis)
+    else:
+        e = torch.cat([torch.arange(int(n), dtype=torch.float64) / max(1, int(n)) for n in sections])
+    return theta ** -e, axis
 
 
 class Vda:
@@ -337,6 +432,132 @@ class Vda:
         self._check(self.lib.vdn_vda_prepare(self.h, p(q), p(k), p(v), p(qo), p(ko), p(vo), B, T, F, H, d,
                                              ctypes.byref(prm), self._stream(stream)))
         return qo, ko, vo
+
+    # -- token-wise rule, rotary positions ----------------------------------------------------
+    def _new(self, stream, make):
+        """Memory made for a call that runs on `stream`: taken on that stream, so that the allocator does not hand it on
+        while the call still runs; what the caller gets back is also marked as in use on the current stream."""
+        torch = self._torch
+        here = torch.cuda.current_stream(self.device)
+        if stream is None or stream == here:
+            with torch.cuda.device(self.device):
+                return make()
+        with torch.cuda.stream(stream):
+            x = make()
+        x.record_stream(here)
+        return x
+
+    def token_scan(self, q, k, v, beta, log_alpha=None, cu_seqlens=None, s0=None, out=None, state=None, scale=1.0,
+                   l2_eps=0.0, stream=None):
+        """vdn_vda_token_scan: the gated delta rule over packed sequences.  Returns (out, state).
+
+        q, k [N,Hk,d], v [N,H,d], beta, log_alpha [N,H] (float), cu_seqlens int32 [S+1] (CUDA; None: one sequence of all N
+        rows), s0 [S,H,d,d] (float, state before each sequence).  state [S,H,d,d] after each sequence, in s0's orientation
+        and that of forward(s0=...); `state` may be s0 itself.  Rows behind the last sequence are not written: a fresh `out`
+        holds whatever was there.
+        """
+        torch = self._torch
+        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
+        if len(lead) != 1:
+            raise ValueError("v must have shape [tokens, heads, d]")
+        n, d, S = lead[0], self.d, 1
+        if cu_seqlens is not None:
+            if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
+                raise ValueError("cu_seqlens must have shape [sequences + 1]")
+            S = int(cu_seqlens.numel()) - 1
+            _require("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, True, self.device)
+        for name, x in (("s0", s0), ("state", state)):
+            if x is not None:
+                _require(name, x, (S, H, d, d), torch.float32, True, self.device)
+        dev = v.device
+        if out is None:
+            out = self._new(stream, lambda: torch.empty(n, H, d, dtype=self.torch_dtype, device=dev))
+        if state is None:
+            state = self._new(stream, lambda: torch.empty(S, H, d, d, dtype=torch.float32, device=dev))
+        p = lambda x: x.data_ptr() if x is not None else None
+        prm = VdnTokenParams(ctypes.sizeof(VdnTokenParams), H, Hk, S, scale, l2_eps, p(cu_seqlens), None, p(log_alpha),
+                             p(s0), p(state), 0, *st)
+        need = int(self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, ctypes.byref(prm)))
+        ws = self._new(stream, lambda: torch.empty(need, dtype=torch.uint8, device=dev)) if need else None
+        self._check(self.lib.vdn_vda_token_scan(self.h, p(q), p(k), p(v), p(beta), p(out), n, ctypes.byref(prm), p(ws), need,
+                                                self._stream(stream)))
+        return out, state
+
+    def token_step(self, q, k, v, beta, state, log_alpha=None, index=None, out=None, scale=1.0, l2_eps=0.0, stream=None):
+        """vdn_vda_token_step: the same rule for one token or a few of each request; `state` is updated in place.
+
+        q, k [R,Hk,d] or [R,L,Hk,d] for R requests of L tokens, v [.., H,d], beta, log_alpha [.., H]; state [slots,H,d,d]
+        (float); index int32 [R] (CUDA): each request's slot, None: request r has slot r.  Requests with an index outside
+        the pool are padding: their rows of `out` are not written.
+        """
+        torch = self._torch
+        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
+        if len(lead) > 2 or (len(lead) == 2 and lead[1] == 0):
+            raise ValueError("v must have shape [requests, heads, d] or [requests, tokens, heads, d]")
+        R, per, d = lead[0], lead[1] if len(lead) == 2 else 1, self.d
+        if state is None or state.dim() != 4:
+            raise ValueError("state must have shape [slots, heads, d, d]")
+        _require("state", state, (state.shape[0], H, d, d), torch.float32, True, self.device)
+        if index is not None:
+            _require("index", index, (R,), torch.int32, True, self.device)
+        if out is None:
+            out = self._new(stream, lambda: torch.empty(*lead, H, d, dtype=self.torch_dtype, device=v.device))
+        p = lambda x: x.data_ptr() if x is not None else None
+        prm = VdnTokenParams(ctypes.sizeof(VdnTokenParams), H, Hk, 0, scale, l2_eps, None, p(index), p(log_alpha), None,
+                             p(state), state.shape[0], *st)
+        self._check(self.lib.vdn_vda_token_step(self.h, p(q), p(k), p(v), p(beta), p(out), R, per, ctypes.byref(prm),
+                                                self._stream(stream)))
+        return out
+
+    def rotate(self, q, k, freq, axis, Y=None, X=None, t0=0, positions=None, half=False, inverse=False, q_weight=None,
+               k_weight=None, norm_eps=0.0, out=None, stream=None):
+        """vdn_vda_rotate: rotary positions on (time, height, width) for q [B,T,F,H,d] and k [B,T,F,Hk,d] (or None).
+
+        freq [pairs] (float64) and axis [pairs] (int32, 0 time / 1 height / 2 width) as CUDA tensors (rotary_tables makes
+        them).  Positions are (t0 + t, u // X, u % X) of token u of frame t, F = Y * X, or positions int32 [3, B*T*F].  With
+        norm_eps > 0 each head is RMS-normalised first (weights [d], float).  `out` = optional (q_out, k_out); each may be
+        its input.  Returns (q', k').
+        """
+        torch = self._torch
+        if q is None or q.dim() != 5:
+            raise ValueError("q must have shape [B, T, F, H, d]")
+        B, T, F, H, d = (int(n) for n in q.shape)
+        lead = (B, T, F)
+        rows = lambda n, x, c: _require_rows(n, x, lead, c, d, self.torch_dtype, True, self.device)
+        qs, ks, Hk = rows("q", q, H), 0, 0
+        if k is not None:
+            if k.dim() != 5:
+                raise ValueError("k must have shape [B, T, F, Hk, d]")
+            Hk = int(k.shape[3])
+            ks = rows("k", k, Hk)
+        if freq is None or freq.dim() != 1:
+            raise ValueError("freq must have shape [pairs]")
+        n = int(freq.numel())
+        _require("freq", freq, (n,), torch.float64, True, self.device)
+        _require("axis", axis, (n,), torch.int32, True, self.device)
+        if positions is not None:
+            _require("positions", positions, (3, B * T * F), torch.int32, True, self.device)
+        elif Y is None or X is None:
+            raise ValueError("either Y and X or positions are needed")
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                _require(name, w, (d,), torch.float32, True, self.device)
+        qo, ko = out if out is not None else (None, None)
+        if qo is None:
+            qo = self._new(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
+        if k is None:
+            if ko is not None:
+                raise ValueError("out has keys, but there are none to rotate")
+        elif ko is None:
+            ko = self._new(stream, lambda: torch.empty(k.shape, dtype=k.dtype, device=k.device))
+        qos, kos = rows("q_out", qo, H), rows("k_out", ko, Hk) if k is not None else 0
+        p = lambda x: x.data_ptr() if x is not None else None
+        prm = VdnRotaryParams(ctypes.sizeof(VdnRotaryParams),
+                              (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0), n, Hk, Y or 0, X or 0,
+                              t0, norm_eps, p(freq), p(axis), p(positions), p(q_weight), p(k_weight), qs, ks, qos, kos)
+        self._check(self.lib.vdn_vda_rotate(self.h, p(q), p(k), p(qo), p(ko), B, T, F, H, d, ctypes.byref(prm),
+                                            self._stream(stream)))
+        return qo, ko
 
     def forward_host(self, q, k, v, beta, gate, out, stream=None, alpha=None, s0=None, chunk=1, radius=0,
                      anchors=False, gate_elem=None, norm_weight=None, q_l2_eps=0.0):

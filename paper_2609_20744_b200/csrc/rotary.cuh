@@ -1,0 +1,170 @@
+// Rotary positions on three axes (time, height, width) for queries and keys, with an optional RMSNorm of each head's
+// channels before the rotation.
+//
+// Pair p of a head's channels is turned by the angle  position(token, axis[p]) * freq[p].  The angle is formed in 64
+// bits, as turns, and only its fraction of a turn is rounded to 32 bits: at position 10^5 a 32-bit product would be off by
+// up to 4e-3 radians.  A CTA first writes the cosines and sines of its tokens to shared memory -- they are the same for
+// all heads of the queries and the keys -- and then streams the heads through registers: a lane holds two 16-byte
+// pieces, which are the two halves of its pairs (HALF) or hold whole neighbouring pairs.  Bound by HBM: each tensor is
+// read once and written once.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace vdn {
+
+struct RotaryArgs {
+  const void* in[2];         // queries, keys (or null)
+  void* out[2];
+  const float* weight[2];    // [d] or null
+  long long in_stride[2], out_stride[2];   // elements from one token to the next
+  int heads[2];              // 0 for keys left out
+  const double* freq;        // [pairs]
+  const int* axis;           // [pairs]; anything but 0, 1, 2 leaves the pair as it is
+  const int* positions;      // [3][n_tokens] or null: frame t0 + t, row, column of the token's grid place
+  long long n_tokens;
+  int pairs, T, F, X, t0, tile;
+  float norm_eps;            // > 0: RMSNorm first
+  float sign;                // -1: rotate back
+};
+
+struct Rotary {
+  static constexpr int THREADS = 256;
+  static constexpr int MAX_TILE = 32;      // tokens a CTA covers
+  static constexpr int UNROLL = 4;         // head rows a lane has in flight
+};
+
+// 16 bytes of a head's channels as floats, and back
+__device__ __forceinline__ void unpack16(const uint4& r, float (&x)[4], const float*) {
+  x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void unpack16(const uint4& r, float (&x)[8], const __nv_bfloat16*) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 pack16(const float (&x)[4], const float*) {
+  return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+__device__ __forceinline__ uint4 pack16(const float (&x)[8], const __nv_bfloat16*) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+template <typename Tio, int D, bool HALF>
+__global__ void __launch_bounds__(Rotary::THREADS) rotary_kernel(const RotaryArgs a) {
+  constexpr int VEC = 16 / (int)sizeof(Tio);       // channels of a 16-byte piece
+  constexpr int LPH = D / (2 * VEC);               // lanes of a head
+  constexpr int NP = VEC;                          // pairs of a lane
+  constexpr int P4 = NP / 2;                       // float4's (two pairs each) of a lane's cosines and sines
+  // [token][pair / 2 mod P4][lane][cos, sin, cos, sin]: the lanes of a head read 16-byte pieces side by side
+  extern __shared__ float4 table[];
+  const long long n0 = (long long)blockIdx.x * a.tile;
+  const int nt = (int)min((long long)a.tile, a.n_tokens - n0);
+
+  // ---- cosines and sines
+  for (int e = threadIdx.x; e < nt * (D / 2); e += Rotary::THREADS) {
+    const int j = e / (D / 2), lp = e % (D / 2);   // token of the tile; lane * NP + pair of the lane
+    const int l = lp / NP, i = lp % NP;
+    // the pair that slot lp stands for; HALF: lanes past the rotated channels pass theirs through
+    const int p = HALF ? (l * VEC < a.pairs ? lp : a.pairs) : lp;
+    float c = 1.f, s = 0.f;
+    if (p < a.pairs) {
+      const int ax = a.axis[p];
+      if (ax >= 0 && ax <= 2) {
+        const long long n = n0 + j;
+        int pos;
+        if (a.positions) {
+          pos = a.positions[(size_t)ax * a.n_tokens + n];
+        } else {
+          const int u = (int)(n % a.F);
+          pos = ax == 0 ? a.t0 + (int)((n / a.F) % a.T) : ax == 1 ? u / a.X : u % a.X;
+        }
+        const double turns = (double)pos * (a.freq[p] * 0.15915494309189533577);   // 1 / (2 pi)
+        sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
+        s *= a.sign;
+      }
+    }
+    float* t = reinterpret_cast<float*>(&table[(j * P4 + i / 2) * LPH + l]);
+    t[(i & 1) * 2] = c;
+    t[(i & 1) * 2 + 1] = s;
+  }
+  __syncthreads();
+
+  // ---- heads: task = (token of the tile, head row of queries then keys, lane)
+  const int rows = a.heads[0] + a.heads[1];
+  const int tasks = nt * rows;
+  const int l = threadIdx.x % LPH;
+  constexpr int STEP = Rotary::THREADS / LPH;      // tasks side by side
+  // first channel of the lane's two pieces
+  int c0 = 2 * l * VEC, c1 = c0 + VEC;
+  if (HALF && l * VEC < a.pairs) { c0 = l * VEC; c1 = c0 + a.pairs; }
+  for (int t0 = 0; t0 < tasks; t0 += STEP * Rotary::UNROLL) {
+    uint4 x0[Rotary::UNROLL], x1[Rotary::UNROLL];
+#pragma unroll
+    for (int u = 0; u < Rotary::UNROLL; ++u) {
+      const int t = t0 + u * STEP + (int)threadIdx.x / LPH;
+      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+      if (t < tasks) {
+        const int j = t / rows, r = t % rows, w = r >= a.heads[0];
+        const Tio* src = static_cast<const Tio*>(a.in[w]) + (size_t)(n0 + j) * a.in_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
+        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
+        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < Rotary::UNROLL; ++u) {
+      const int t = t0 + u * STEP + (int)threadIdx.x / LPH;
+      const bool live = t < tasks;
+      const int j = live ? t / rows : 0, r = live ? t % rows : 0, w = r >= a.heads[0];
+      float y0[VEC], y1[VEC];
+      unpack16(x0[u], y0, static_cast<const Tio*>(nullptr));
+      unpack16(x1[u], y1, static_cast<const Tio*>(nullptr));
+      if (a.norm_eps > 0.f) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) ss += y0[i] * y0[i] + y1[i] * y1[i];
+#pragma unroll
+        for (int m = 1; m < LPH; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
+        const float rn = rsqrtf(ss * (1.f / D) + a.norm_eps);
+        const float* wt = a.weight[w];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+          y0[i] *= wt ? rn * wt[c0 + i] : rn;
+          y1[i] *= wt ? rn * wt[c1 + i] : rn;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < NP; i += 2) {
+        const float4 cs = table[(j * P4 + i / 2) * LPH + l];
+        if (HALF) {
+          const float p0 = y0[i], p1 = y0[i + 1], z0 = y1[i], z1 = y1[i + 1];
+          y0[i] = p0 * cs.x - z0 * cs.y;     y1[i] = p0 * cs.y + z0 * cs.x;
+          y0[i + 1] = p1 * cs.z - z1 * cs.w; y1[i + 1] = p1 * cs.w + z1 * cs.z;
+        } else {
+          // pairs i, i + 1 of the lane are channels 2i .. 2i + 3 of its 2 VEC neighbouring channels
+          float* y = 2 * i < VEC ? &y0[(2 * i) % VEC] : &y1[(2 * i) % VEC];
+          const float p0 = y[0], z0 = y[1], p1 = y[2], z1 = y[3];
+          y[0] = p0 * cs.x - z0 * cs.y; y[1] = p0 * cs.y + z0 * cs.x;
+          y[2] = p1 * cs.z - z1 * cs.w; y[3] = p1 * cs.w + z1 * cs.z;
+        }
+      }
+      if (live) {
+        Tio* dst = static_cast<Tio*>(a.out[w]) + (size_t)(n0 + j) * a.out_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
+        *reinterpret_cast<uint4*>(dst + c0) = pack16(y0, static_cast<const Tio*>(nullptr));
+        *reinterpret_cast<uint4*>(dst + c1) = pack16(y1, static_cast<const Tio*>(nullptr));
+      }
+    }
+  }
+}
+
+}  // namespace vdn

@@ -22,8 +22,10 @@
 #include "readout_tc.cuh"
 #include "resolve.cuh"
 #include "resolve_tc.cuh"
+#include "rotary.cuh"
 #include "scan.cuh"
 #include "scan_tc.cuh"
+#include "token_rule.cuh"
 #include "wait_selftest.cuh"
 
 namespace {
@@ -1101,7 +1103,7 @@ vdn_status vdn_vda_status(vdn_vda_t h) {
   if (!h) return VDN_ERR_INVALID_ARG;
   const int v = *const_cast<volatile int*>(h->status_host);
   if (v == 0) return VDN_OK;
-  return v == VDN_ERR_INTERNAL ? VDN_ERR_INTERNAL : VDN_ERR_TIMEOUT;
+  return v == VDN_ERR_INTERNAL || v == VDN_ERR_INVALID_ARG ? static_cast<vdn_status>(v) : VDN_ERR_TIMEOUT;
 }
 
 vdn_status vdn_vda_clear_status(vdn_vda_t h) {
@@ -1192,6 +1194,207 @@ vdn_status vdn_vda_destroy(vdn_vda_t h) {
   }
   if (h->status_host) cudaFreeHost(h->status_host);
   delete h;
+  return VDN_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The pairs of tensors below are told apart by their first bytes only, as everywhere in this library.
+bool stride_ok(int64_t stride, long long dense, size_t es) {
+  return stride == 0 || (stride >= dense && stride <= (1LL << 40) && (stride * (long long)es) % 16 == 0);
+}
+
+// What both entry points of the token-wise rule ask of their arguments; fills the kernel's.
+vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
+                      long long n_tokens, const vdn_vda_token_params* p, vdn::TokenArgs& a) {
+  if (!p || p->struct_size != sizeof(vdn_vda_token_params))
+    return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_token_params missing or of the wrong struct_size");
+  if (p->heads <= 0 || p->key_heads <= 0 || p->heads % p->key_heads != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "key_heads must divide heads");
+  if (p->heads > 65535) return fail(h, VDN_ERR_UNSUPPORTED, "more than 65535 heads");
+  if (n_tokens < 0 || n_tokens > 0x7fffffffLL / 2)
+    return fail(h, VDN_ERR_INVALID_ARG, "the number of tokens must lie between 0 and 2^30");
+  if (n_tokens > 0 && (!q || !k || !v || !beta || !out)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(p->s0) || !aligned16(p->state))
+    return fail(h, VDN_ERR_INVALID_ARG, "q, k, v, out and the states must be 16-byte aligned");
+  if (out && (out == q || out == k || out == v)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias an input");
+  if (!(p->l2_eps >= 0.f) || p->l2_eps > 1e30f || !std::isfinite(p->scale))
+    return fail(h, VDN_ERR_INVALID_ARG, "scale must be finite, l2_eps a finite non-negative number");
+  const long long dk = (long long)p->key_heads * h->cfg.d, dv = (long long)p->heads * h->cfg.d;
+  const size_t es = elem_size(h);
+  if (!stride_ok(p->q_stride, dk, es) || !stride_ok(p->k_stride, dk, es) || !stride_ok(p->v_stride, dv, es) ||
+      !stride_ok(p->out_stride, dv, es))
+    return fail(h, VDN_ERR_INVALID_ARG, "token strides must cover a token's heads and be multiples of 16 bytes");
+  a = vdn::TokenArgs{};
+  a.q = q; a.k = k; a.v = v; a.beta = beta; a.out = out;
+  a.log_alpha = p->log_alpha;
+  a.q_stride = p->q_stride ? p->q_stride : dk;
+  a.k_stride = p->k_stride ? p->k_stride : dk;
+  a.v_stride = p->v_stride ? p->v_stride : dv;
+  a.out_stride = p->out_stride ? p->out_stride : dv;
+  a.n_tokens = n_tokens;
+  a.H = p->heads; a.Hk = p->key_heads;
+  a.scale = p->scale; a.l2_eps = p->l2_eps;
+  a.status = h->status_dev;
+  return VDN_OK;
+}
+
+vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t st) {
+  const int d = h->cfg.d;
+  const long long ctas = (long long)a.S * a.H * (d / 32);
+  if (ctas > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
+  prof_begin(h, st);
+  const unsigned grid = (unsigned)ctas;
+  if (h->cfg.io_dtype == VDN_F32) {
+    if (d == 64) vdn::token_rule_kernel<float, 64><<<grid, 256, 0, st>>>(a);
+    else vdn::token_rule_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+  } else {
+    if (d == 64) vdn::token_rule_kernel<__nv_bfloat16, 64><<<grid, 256, 0, st>>>(a);
+    else vdn::token_rule_kernel<__nv_bfloat16, 128><<<grid, 256, 0, st>>>(a);
+  }
+  prof_mark(h, st, 0, "token_rule");
+  h->launches = 1;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
+template <typename Tio, int D>
+void launch_rotary(const vdn::RotaryArgs& a, bool half, unsigned grid, size_t smem, cudaStream_t st) {
+  if (half) vdn::rotary_kernel<Tio, D, true><<<grid, vdn::Rotary::THREADS, smem, st>>>(a);
+  else vdn::rotary_kernel<Tio, D, false><<<grid, vdn::Rotary::THREADS, smem, st>>>(a);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
+  (void)n_tokens;
+  if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params)) return 0;
+  return 0;
+}
+
+vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
+                              long long n_tokens, const vdn_vda_token_params* p, void* workspace, size_t workspace_bytes,
+                              void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  vdn::TokenArgs a;
+  vdn_status r = plan_token(h, q, k, v, beta, out, n_tokens, p, a);
+  if (r != VDN_OK) return r;
+  if (p->n_seqs <= 0) return fail(h, VDN_ERR_INVALID_ARG, "n_seqs must be positive");
+  if (!p->cu_seqlens && p->n_seqs != 1) return fail(h, VDN_ERR_INVALID_ARG, "more than one sequence needs cu_seqlens");
+  if (p->index || p->n_slots) return fail(h, VDN_ERR_INVALID_ARG, "index and n_slots belong to vdn_vda_token_step");
+  if (out && (out == p->s0 || out == p->state)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias a state");
+  (void)workspace; (void)workspace_bytes;
+  a.cu_seqlens = p->cu_seqlens;
+  a.S = p->n_seqs;
+  a.per = (int)n_tokens;
+  a.slots = p->n_seqs;
+  a.state_in = p->s0;
+  a.state_out = p->state;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  return launch_token_rule(h, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
+                              int n_requests, int per, const vdn_vda_token_params* p, void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  if (n_requests < 0 || per <= 0) return fail(h, VDN_ERR_INVALID_ARG, "n_requests must not be negative, per must be positive");
+  vdn::TokenArgs a;
+  vdn_status r = plan_token(h, q, k, v, beta, out, (long long)n_requests * per, p, a);
+  if (r != VDN_OK) return r;
+  if (p->cu_seqlens || p->s0) return fail(h, VDN_ERR_INVALID_ARG, "cu_seqlens and s0 belong to vdn_vda_token_scan");
+  if (!p->state || p->n_slots <= 0) return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_token_step needs a pool of states");
+  if (p->n_slots > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "more than 2^31 - 1 states");
+  if (!p->index && p->n_slots < n_requests)
+    return fail(h, VDN_ERR_INVALID_ARG, "without an index the pool must hold a state for each request");
+  if (out && out == p->state) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias a state");
+  if (n_requests == 0) { h->launches = 0; return VDN_OK; }
+  a.index = p->index;
+  a.S = n_requests;
+  a.per = per;
+  a.slots = p->n_slots;
+  a.state_in = p->state;
+  a.state_out = p->state;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  return launch_token_rule(h, a, static_cast<cudaStream_t>(cuda_stream));
+}
+
+vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void* q_out, void* k_out, int B, int T, int F,
+                          int H, int d, const vdn_vda_rotary_params* p, void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  if (!p || p->struct_size != sizeof(vdn_vda_rotary_params))
+    return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_rotary_params missing or of the wrong struct_size");
+  if (!q_in || !q_out || (k_in == nullptr) != (k_out == nullptr) || !p->freq || !p->axis)
+    return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
+  if (!aligned16(q_in) || !aligned16(k_in) || !aligned16(q_out) || !aligned16(k_out))
+    return fail(h, VDN_ERR_INVALID_ARG, "q and k must be 16-byte aligned");
+  if (k_in && (q_out == k_in || k_out == q_in || q_out == k_out))
+    return fail(h, VDN_ERR_INVALID_ARG, "an output may only alias its own input");
+  if (d != h->cfg.d) return fail(h, VDN_ERR_INVALID_ARG, "d differs from the handle's configured head dimension");
+  if (B <= 0 || T <= 0 || F <= 0 || H <= 0 || (k_in && p->key_heads <= 0))
+    return fail(h, VDN_ERR_INVALID_ARG, "B, T, F, H and key_heads must be positive");
+  if (H > 65535 || p->key_heads > 65535) return fail(h, VDN_ERR_UNSUPPORTED, "more than 65535 heads");
+  const long long n = (long long)B * T;
+  if (n > 0x7fffffffLL / F) return fail(h, VDN_ERR_INVALID_ARG, "B*T*F exceeds the 32-bit token index range");
+  if (p->flags & ~(VDN_ROTARY_HALF | VDN_ROTARY_INVERSE)) return fail(h, VDN_ERR_INVALID_ARG, "unknown rotary flag");
+  const bool half = (p->flags & VDN_ROTARY_HALF) != 0, inverse = (p->flags & VDN_ROTARY_INVERSE) != 0;
+  if (p->pairs <= 0 || p->pairs > d / 2) return fail(h, VDN_ERR_INVALID_ARG, "pairs must lie between 1 and d/2");
+  if (half && p->pairs % 8 != 0) return fail(h, VDN_ERR_INVALID_ARG, "VDN_ROTARY_HALF needs a multiple of 8 pairs");
+  if (!(p->norm_eps >= 0.f) || p->norm_eps > 1e30f)
+    return fail(h, VDN_ERR_INVALID_ARG, "norm_eps must be a finite non-negative number");
+  if (inverse && p->norm_eps > 0.f) return fail(h, VDN_ERR_INVALID_ARG, "the inverse rotation takes no norm");
+  if (!(p->norm_eps > 0.f) && (p->q_weight || p->k_weight))
+    return fail(h, VDN_ERR_INVALID_ARG, "a norm weight needs norm_eps > 0");
+  if (!p->positions) {
+    if (p->Y <= 0 || p->X <= 0 || (long long)p->Y * p->X != F) return fail(h, VDN_ERR_INVALID_ARG, "Y * X must equal F");
+    if ((long long)p->t0 + T - 1 > 0x7fffffffLL) return fail(h, VDN_ERR_INVALID_ARG, "t0 + T exceeds 32 bits");
+  }
+  const size_t es = elem_size(h);
+  const long long dq = (long long)H * d, dk = (long long)p->key_heads * d;
+  if (!stride_ok(p->q_stride, dq, es) || !stride_ok(p->q_out_stride, dq, es) ||
+      (k_in && (!stride_ok(p->k_stride, dk, es) || !stride_ok(p->k_out_stride, dk, es))))
+    return fail(h, VDN_ERR_INVALID_ARG, "token strides must cover a token's heads and be multiples of 16 bytes");
+  vdn::RotaryArgs a{};
+  a.in[0] = q_in; a.in[1] = k_in; a.out[0] = q_out; a.out[1] = k_out;
+  a.weight[0] = p->q_weight; a.weight[1] = p->k_weight;
+  a.in_stride[0] = p->q_stride ? p->q_stride : dq;   a.out_stride[0] = p->q_out_stride ? p->q_out_stride : dq;
+  a.in_stride[1] = p->k_stride ? p->k_stride : dk;   a.out_stride[1] = p->k_out_stride ? p->k_out_stride : dk;
+  if ((q_in == q_out && a.in_stride[0] != a.out_stride[0]) || (k_in && k_in == k_out && a.in_stride[1] != a.out_stride[1]))
+    return fail(h, VDN_ERR_INVALID_ARG, "in place, input and output need the same stride");
+  a.heads[0] = H; a.heads[1] = k_in ? p->key_heads : 0;
+  a.freq = p->freq; a.axis = p->axis; a.positions = p->positions;
+  a.n_tokens = n * F;
+  a.pairs = p->pairs; a.T = T; a.F = F; a.X = p->X > 0 ? p->X : 1; a.t0 = p->t0;
+  a.norm_eps = p->norm_eps;
+  a.sign = inverse ? -1.f : 1.f;
+  // Tokens a CTA covers: enough that its lanes have two full turns of unrolled loads (fewer heads, more tokens), but no
+  // more than leave every SM several CTAs.
+  const int lanes = d * (int)es / 32, rows = a.heads[0] + a.heads[1];
+  long long tile = (2LL * vdn::Rotary::UNROLL * vdn::Rotary::THREADS / lanes + rows - 1) / rows;
+  const long long spread = a.n_tokens / (4LL * h->sm_count);
+  if (tile > spread) tile = spread;
+  a.tile = (int)(tile < 1 ? 1 : tile > vdn::Rotary::MAX_TILE ? vdn::Rotary::MAX_TILE : tile);
+  const unsigned grid = (unsigned)((a.n_tokens + a.tile - 1) / a.tile);
+  const size_t smem = (size_t)a.tile * (d / 2) * 8;
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  prof_begin(h, st);
+  if (h->cfg.io_dtype == VDN_F32) {
+    if (d == 64) launch_rotary<float, 64>(a, half, grid, smem, st);
+    else launch_rotary<float, 128>(a, half, grid, smem, st);
+  } else {
+    if (d == 64) launch_rotary<__nv_bfloat16, 64>(a, half, grid, smem, st);
+    else launch_rotary<__nv_bfloat16, 128>(a, half, grid, smem, st);
+  }
+  prof_mark(h, st, 0, "rotary");
+  h->launches = 1;
+  VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
 }
 
