@@ -26,6 +26,7 @@
 #include "scan.cuh"
 #include "scan_tc.cuh"
 #include "token_rule.cuh"
+#include "token_tc.cuh"
 #include "wait_selftest.cuh"
 
 namespace {
@@ -100,6 +101,7 @@ struct vdn_vda_s {
   int last_nseg = 0;
   bool attrs_set = false;
   bool tc_attrs_set = false;
+  bool token_attrs_set = false;
   unsigned ro_attrs_set = 0;       // read-out instantiations whose shared-memory attribute has been set
   int ro_short = 1;                // use the short-frame read-out layout where it applies (VDN_RO_SHORT=0 turns it off)
   // More scan chains than SMs: the surplus chains run on a side stream beside the read-out of the others
@@ -1260,6 +1262,74 @@ vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t 
   return VDN_OK;
 }
 
+// Workspace of the chunked rule: per (place, head) the chunk's two operators and its factors.
+struct TokenLayout {
+  long long places;
+  size_t e, p, f, total;
+};
+TokenLayout make_token_layout(long long n_tokens, int n_seqs, int heads) {
+  TokenLayout L;
+  L.places = n_tokens / vdn::TokenTc::C + n_seqs;
+  const size_t units = (size_t)L.places * heads;
+  size_t off = 0;
+  L.e = off; off += align_up(units * vdn::TokenTc::E_BYTES);
+  L.p = off; off += align_up(units * vdn::TokenTc::P_BYTES);
+  L.f = off; off += align_up(units * vdn::TokenTc::F_BYTES);
+  L.total = off;
+  return L;
+}
+
+bool token_on_tensor_cores(const vdn_vda_s* h, long long n_tokens, int n_seqs) {
+  (void)n_seqs;
+  return use_tensor_cores(h, h->cfg.d) && n_tokens > 0;
+}
+
+// Rows of `width` bf16 elements, `stride` elements apart, as a 2-D map with a (box, 64) box.
+vdn_status make_rows_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, long long rows, long long width, long long stride,
+                         unsigned box_width, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
+  const cuuint32_t box[2] = {box_width, 64};
+  const cuuint32_t estr[2] = {1, 1};
+  CUresult r = h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (token rows) failed: " + std::to_string((int)r));
+  return VDN_OK;
+}
+
+vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* ws, cudaStream_t st) {
+  if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  if (!h->token_attrs_set) {
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_prep_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vdn::TokenPrep::SMEM_BYTES));
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vdn::TokenChain::SMEM_BYTES));
+    h->token_attrs_set = true;
+  }
+  const TokenLayout L = make_token_layout(t.n_tokens, t.S, t.H);
+  if (L.places * t.H > 0x7fffffffLL || (long long)t.S * t.H > 0x7fffffffLL)
+    return fail(h, VDN_ERR_UNSUPPORTED, "too many (chunk, head) pairs for one call");
+  CUtensorMap tmK, tmQ, tmV;
+  const long long wk = (long long)t.Hk * 128, wv = (long long)t.H * 128;
+  vdn_status r;
+  if ((r = make_rows_map(h, &tmK, t.k, t.n_tokens, wk, t.k_stride, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmQ, t.q, t.n_tokens, wk, t.q_stride, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmV, t.v, t.n_tokens, wv, t.v_stride, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != VDN_OK) return r;
+  vdn::TokenTcArgs a;
+  a.t = t;
+  a.e = ws + L.e; a.p = ws + L.p; a.f = ws + L.f;
+  a.places = L.places;
+  prof_begin(h, st);
+  vdn::token_prep_kernel<<<(unsigned)(L.places * t.H), vdn::TokenPrep::THREADS, vdn::TokenPrep::SMEM_BYTES, st>>>(
+      tmK, tmQ, a, dev_status(h));
+  prof_mark(h, st, 0, "token_prep");
+  vdn::token_chain_kernel<<<(unsigned)(t.S * t.H), vdn::TokenChain::THREADS, vdn::TokenChain::SMEM_BYTES, st>>>(
+      tmK, tmQ, tmV, a, dev_status(h));
+  prof_mark(h, st, 1, "token_chain");
+  h->launches = 2;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
 template <typename Tio, int D>
 void launch_rotary(const vdn::RotaryArgs& a, bool half, unsigned grid, size_t smem, cudaStream_t st) {
   if (half) vdn::rotary_kernel<Tio, D, true><<<grid, vdn::Rotary::THREADS, smem, st>>>(a);
@@ -1271,9 +1341,8 @@ void launch_rotary(const vdn::RotaryArgs& a, bool half, unsigned grid, size_t sm
 extern "C" {
 
 size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
-  (void)n_tokens;
-  if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params)) return 0;
-  return 0;
+  if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->n_seqs <= 0 || n_tokens < 0) return 0;
+  return token_on_tensor_cores(h, n_tokens, p->n_seqs) ? make_token_layout(n_tokens, p->n_seqs, p->heads).total : 0;
 }
 
 vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1287,7 +1356,11 @@ vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const v
   if (!p->cu_seqlens && p->n_seqs != 1) return fail(h, VDN_ERR_INVALID_ARG, "more than one sequence needs cu_seqlens");
   if (p->index || p->n_slots) return fail(h, VDN_ERR_INVALID_ARG, "index and n_slots belong to vdn_vda_token_step");
   if (out && (out == p->s0 || out == p->state)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias a state");
-  (void)workspace; (void)workspace_bytes;
+  const size_t need = vdn_vda_token_scan_workspace_bytes(h, n_tokens, p);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(h, VDN_ERR_WORKSPACE, "workspace missing or smaller than vdn_vda_token_scan_workspace_bytes");
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
   a.cu_seqlens = p->cu_seqlens;
   a.S = p->n_seqs;
   a.per = (int)n_tokens;
@@ -1296,7 +1369,8 @@ vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const v
   a.state_out = p->state;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
-  return launch_token_rule(h, a, static_cast<cudaStream_t>(cuda_stream));
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  return need ? launch_token_tc(h, a, static_cast<unsigned char*>(workspace), st) : launch_token_rule(h, a, st);
 }
 
 vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
