@@ -74,6 +74,14 @@ __device__ __forceinline__ void bulk_store(void* dst, uint32_t src, uint32_t byt
                : "memory");
 }
 
+// 32 lanes x 8 consecutive columns.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* r) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+               : "memory");
+}
+
 // D[tmem] (+)= A[tmem] * B[smem]: A has its rows in the lanes and two K elements to a 32-bit column.
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                             uint32_t accumulate) {
@@ -85,63 +93,42 @@ __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, ui
       : "memory");
 }
 
-// Two floats at once (the packed fp32 pipe).
-__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void f2_unpack(uint64_t r, float& a, float& b) {
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r));
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-
-// x = hi + lo + rest, |rest| <= 2^-16 |x|, both parts rounded to nearest, two neighbours packed.  The high part comes from
-// Dekker's splitting (c = (2^16 + 1) x, hi = c - (c - x)), which keeps NaN a NaN (rounding the bit pattern by an
-// integer addition would turn the pattern 0x7FFFFFFF into -0); |x| must stay below 2^110.
-__device__ __forceinline__ void split2_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
-  const uint64_t minus = f2_pack(-1.f, -1.f);
-  const uint64_t c = mul2(x, f2_pack(65537.f, 65537.f));
-  const uint64_t t = fma2(x, minus, c);
-  const uint64_t h = fma2(t, minus, c);
-  const uint64_t r = fma2(h, minus, x);
-  float h0, h1, r0, r1;
-  f2_unpack(h, h0, h1);
-  f2_unpack(r, r0, r1);
-  hi = __byte_perm(__float_as_uint(h0), __float_as_uint(h1), 0x7632);
-  lo = __byte_perm(__float_as_uint(r0) + 0x8000u, __float_as_uint(r1) + 0x8000u, 0x7632);
+// x = hi + lo + rest, |rest| <= 2^-16 |x|, both parts rounded to nearest, two neighbours packed.  The packed conversion takes
+// two cycles a warp and keeps NaN (rounding the bit pattern by an integer addition would turn 0x7FFFFFFF into -0):
+// 7 cycles a pair in all, against 12 for Dekker's splitting in packed fp32 arithmetic.
+__device__ __forceinline__ void split2_pair(float x0, float x1, uint32_t& hi, uint32_t& lo) {
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(x1), "f"(x0));
+  const float r0 = x0 - __uint_as_float(hi << 16), r1 = x1 - __uint_as_float(hi & 0xFFFF0000u);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(r1), "f"(r0));
 }
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<const uint32_t*>(&v);
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+  return r;
 }
 
 }  // namespace tc
 
 // ---------------------------------------------------------------------------------------------- chunk operators
 // One CTA (four warps) per (place, head).  [K; Q] K^T is one MMA chain with the keys in rows 0..63 and the queries in rows
-// 64..127 of one operand, so that lane i of tensor memory holds row i of K K^T and lane 64 + i row i of Q K^T.  The inverse
-// of the unit lower triangular I + L is a forward substitution in fp32, a thread to a column: its 64 rows stay in
-// registers, and the rows of L are broadcast from shared memory.  A thread's column is a row of the (K-major) B operand
-// of the two last products, so no transpose is needed.
+// 64..127 of one operand, so that lane i of tensor memory holds row i of K K^T and lane 64 + i row i of Q K^T.
+// The inverse of the unit lower triangular I + L is formed in fp32 in shared memory, block by block: the four 16 x 16 blocks on
+// the diagonal by forward substitution (a warp to a block, a lane to a column, 16 rows in registers), then pairs of
+// blocks are merged, [T11 0; -T22 L21 T11, T22], to 32 and to 64 rows, all threads at once.  A thread to a column over all 64
+// rows needs no products, but 2016 steps in straight line: 6.9 us a CTA-slot instead of FIXME, most of it waiting for
+// instructions.  Everything that could be a long straight line is a loop over 16 columns for the same reason.
 struct TokenPrep {
   static constexpr int THREADS = 128;
   static constexpr int OFF_KQ = 0;                    // [K; Q]: two 64-channel boxes of 128 rows; later the parts of E
   static constexpr int OFF_T = 32768;                 // inverse times factors: high, low; inverse times beta; (first: L)
   static constexpr int OFF_M = OFF_T + 3 * 8192;      // scale M
-  static constexpr int OFF_F = OFF_M + 8192;          // G high, G low, beta, r, weight [64] each, then the factors
-  static constexpr int OFF_BAR = OFF_F + 5 * 256 + 640;
+  static constexpr int OFF_F = OFF_M + 8192;          // G high, G low, beta, r, weight [64] each
+  static constexpr int OFF_BAR = OFF_F + 5 * 256;
   static constexpr int SMEM_BYTES = OFF_BAR + 64 + 1024;
   static constexpr int L_PITCH = 68;                  // floats: 16-byte rows, lanes' rows four banks apart
+  static constexpr int OFF_W = OFF_T + 64 * L_PITCH * 4;   // products on the way to a merge, 32 rows of W_PITCH
+  static constexpr int W_PITCH = 36;
+  static_assert(OFF_W + 32 * W_PITCH * 4 <= OFF_M, "the inverse and its scratch lie where the operands go later");
 };
 
 __global__ void __launch_bounds__(TokenPrep::THREADS, 3)
@@ -176,7 +163,6 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   float* beta = g_hi + 128;
   float* rk = g_hi + 192;
   float* wgt = g_hi + 256;
-  float* fac = g_hi + 320;
 
   if (tid == 0) {
     mbar_init(bar_load, 1);
@@ -214,7 +200,6 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   } else if (warp >= 2) {
     const int j = tid - 64;
     beta[j] = j < n ? t.beta[(row0 + j) * t.H + h] : 0.f;
-    rk[j] = 1.f;
   } else {
     __syncwarp();
     tmem_alloc(smem_u32(tmem_slot), 128);
@@ -246,12 +231,12 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     const bool is_q = warp >= 2;
     const int i = tid & 63;                           // token of this thread's row
-    float rq = 1.f;
-    if (is_q && t.l2_eps > 0.f) {
+    float norm = 1.f;                                 // r of the row's key or query
+    if (t.l2_eps > 0.f) {
       float ss = 0.f;
 #pragma unroll 4
       for (int c = 0; c < 16; ++c) {
-        const uint4 w = *reinterpret_cast<const uint4*>(bp + (c >> 3) * 16384 + (64 + i) * 128 + (((c & 7) ^ (i & 7)) << 4));
+        const uint4 w = *reinterpret_cast<const uint4*>(bp + (c >> 3) * 16384 + tid * 128 + (((c & 7) ^ (i & 7)) << 4));
         const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -259,100 +244,156 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           ss = fmaf(lo, lo, fmaf(hi, hi, ss));
         }
       }
-      rq = rsqrtf(ss + t.l2_eps);
+      norm = rsqrtf(ss + t.l2_eps);
     }
+    if (!is_q) rk[i] = norm;
     ok = mbar_wait(bar_mma, 0, wc);
     if (!__syncthreads_or(!ok)) {
       tc_fence_after_sync();
-      float x[64];
-      tmem_ld32(lanes, *reinterpret_cast<float(*)[32]>(x));
-      tmem_ld32(lanes + 32, *reinterpret_cast<float(*)[32]>(x + 32));
-      tmem_wait_ld();
-      if (t.l2_eps > 0.f) {                           // a key's squared norm is the diagonal of K K^T
-        if (!is_q) {
-          float kk = 0.f;
-#pragma unroll
-          for (int j = 0; j < 64; ++j) kk = j == i ? x[j] : kk;
-          rk[i] = rsqrtf(kk + t.l2_eps);
-        }
-        __syncthreads();
-      }
       const float gi_hi = g_hi[i], gi_lo = g_lo[i];
-      const float row = is_q ? t.scale * rq : beta[i] * rk[i];
+      const float row = is_q ? t.scale * norm : beta[i] * norm;
       const int last = is_q ? i : i - 1;              // L is strictly lower, M has its diagonal
-#pragma unroll
-      for (int j = 0; j < 64; j += 4) {
-        const float4 gh = *reinterpret_cast<const float4*>(g_hi + j), gl = *reinterpret_cast<const float4*>(g_lo + j);
-        const float4 rr = *reinterpret_cast<const float4*>(rk + j);
-        x[j] = j <= last ? row * rr.x * __expf((gi_hi - gh.x) + (gi_lo - gl.x)) * x[j] : 0.f;
-        x[j + 1] = j + 1 <= last ? row * rr.y * __expf((gi_hi - gh.y) + (gi_lo - gl.y)) * x[j + 1] : 0.f;
-        x[j + 2] = j + 2 <= last ? row * rr.z * __expf((gi_hi - gh.z) + (gi_lo - gl.z)) * x[j + 2] : 0.f;
-        x[j + 3] = j + 3 <= last ? row * rr.w * __expf((gi_hi - gh.w) + (gi_lo - gl.w)) * x[j + 3] : 0.f;
-      }
       float* L = reinterpret_cast<float*>(bp + S::OFF_T);
-      if (!is_q) {
+#pragma unroll 1
+      for (int jb = 0; jb < 64; jb += 16) {
+        if (jb > (i | 31)) {                          // nothing of this warp's rows is this far right
+          if (is_q) {
 #pragma unroll
-        for (int j = 0; j < 64; j += 4)
-          *reinterpret_cast<float4*>(L + i * S::L_PITCH + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+            for (int c = 0; c < 2; ++c)
+              *reinterpret_cast<uint4*>(bp + S::OFF_M + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+          }
+          continue;
+        }
+        float x[16];
+        tmem_ld16(lanes + jb, x);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const float4 gh = *reinterpret_cast<const float4*>(g_hi + jb + j), gl = *reinterpret_cast<const float4*>(g_lo + jb + j);
+          const float4 rr = *reinterpret_cast<const float4*>(rk + jb + j);
+          const float h4[4] = {gh.x, gh.y, gh.z, gh.w}, l4[4] = {gl.x, gl.y, gl.z, gl.w}, r4[4] = {rr.x, rr.y, rr.z, rr.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            x[j + e] = jb + j + e <= last ? row * r4[e] * __expf((gi_hi - h4[e]) + (gi_lo - l4[e])) * x[j + e] : 0.f;
+          if (!is_q) *reinterpret_cast<float4*>(L + i * S::L_PITCH + jb + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+        }
+        if (is_q) {
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            *reinterpret_cast<uint4*>(bp + S::OFF_M + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) =
+                make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
+                           bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
+        }
+      }
+      const long long unit = place * t.H + h;
+      {
         const float eg = __expf(gi_hi + gi_lo);
-        wgt[i] = rk[i] * __expf((g_hi[63] - gi_hi) + (g_lo[63] - gi_lo));
-        fac[i] = eg * rk[i];
-        if (i == 0) fac[128] = __expf(g_hi[63] + g_lo[63]);
-      } else {
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-          *reinterpret_cast<uint4*>(bp + S::OFF_M + i * 128 + ((c ^ (i & 7)) << 4)) =
-              make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
-                         bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
-        fac[64 + i] = t.scale * rq * __expf(gi_hi + gi_lo);
+        float* f = reinterpret_cast<float*>(a.f + (size_t)unit * TokenTc::F_BYTES);
+        if (!is_q) wgt[i] = norm * __expf((g_hi[63] - gi_hi) + (g_lo[63] - gi_lo));
+        f[tid] = eg * (is_q ? t.scale * norm : norm); // keys' factors, then the queries'
+        if (tid == 0) f[128] = __expf(g_hi[63] + g_lo[63]);
       }
       __syncthreads();
-      const long long unit = place * t.H + h;
-      if (!is_q) {
-        // forward substitution: column i of (I + L)^-1;  columns from 32 on have nothing above row 32
-        float y[64];
+      // ---- inverse: the blocks on the diagonal, in place
+      {
+        float* Lb = L + warp * 16 * (S::L_PITCH + 1);
+        const int c = lane & 15;
+        float y[16];
 #pragma unroll
-        for (int r = 0; r < 64; ++r) y[r] = 0.f;
-        auto solve = [&](auto first) {
-          constexpr int R0 = decltype(first)::value;
+        for (int r = 0; r < 16; ++r) y[r] = 0.f;
 #pragma unroll
-          for (int r = R0; r < 64; ++r) {
-            float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+        for (int r = 0; r < 16; ++r) {
+          float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-            for (int j = R0; j < r; j += 4) {
-              const float4 l = *reinterpret_cast<const float4*>(L + r * S::L_PITCH + j);
-              s0 = fmaf(l.x, y[j], s0);
-              s1 = fmaf(l.y, y[j + 1], s1);
-              s2 = fmaf(l.z, y[j + 2], s2);
-              s3 = fmaf(l.w, y[j + 3], s3);
-            }
-            y[r] = (r == i ? 1.f : 0.f) - ((s0 + s1) + (s2 + s3));
+          for (int j = 0; j < r; j += 4) {
+            const float4 l = *reinterpret_cast<const float4*>(Lb + r * S::L_PITCH + j);
+            s0 = fmaf(l.x, y[j], s0);
+            s1 = fmaf(l.y, y[j + 1], s1);
+            s0 = fmaf(l.z, y[j + 2], s0);
+            s1 = fmaf(l.w, y[j + 3], s1);
           }
-        };
-        if (warp == 0) solve(std::integral_constant<int, 0>{});
-        else solve(std::integral_constant<int, 32>{});
-        named_barrier_sync(1, 64);                    // L is read, its place is taken by the operands
-        const float b = beta[i];
+          y[r] = (r == c ? 1.f : 0.f) - (s0 + s1);
+        }
+        __syncwarp();
+        if (lane < 16) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
+          for (int r = 0; r < 16; ++r) Lb[r * S::L_PITCH + c] = y[r];
+        }
+      }
+      __syncthreads();
+      float* W = reinterpret_cast<float*>(bp + S::OFF_W);
+      {
+        // ---- pairs of 16: W = L21 T11, then T21 = -T22 W;  64 threads a pair, four neighbouring columns each
+        float* A = L + (tid >> 6) * 32 * (S::L_PITCH + 1);
+        float* Wp = W + (tid >> 6) * 16 * S::W_PITCH;
+        const int r = (tid & 63) >> 2, c = (tid & 3) * 4;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < 16; ++k) {
+          const float l = A[(16 + r) * S::L_PITCH + k];
+          const float4 b = *reinterpret_cast<const float4*>(A + k * S::L_PITCH + c);
+          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y); acc.z = fmaf(l, b.z, acc.z); acc.w = fmaf(l, b.w, acc.w);
+        }
+        *reinterpret_cast<float4*>(Wp + r * S::W_PITCH + c) = acc;
+        __syncthreads();
+        acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int k = 0; k < 16; ++k) {
+          const float l = -A[(16 + r) * S::L_PITCH + 16 + k];
+          const float4 b = *reinterpret_cast<const float4*>(Wp + k * S::W_PITCH + c);
+          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y); acc.z = fmaf(l, b.z, acc.z); acc.w = fmaf(l, b.w, acc.w);
+        }
+        *reinterpret_cast<float4*>(A + (16 + r) * S::L_PITCH + c) = acc;
+      }
+      __syncthreads();
+      {
+        // ---- the pair of 32: two rows and four columns a thread
+        const int r = (tid >> 3) * 2, c = (tid & 7) * 4;
+        auto product = [&](const float* l0, const float* b0, int bp_, int kn, float sign, float* dst, int dp) {
+          float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          for (int k = 0; k < kn; k += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(l0 + k), v = *reinterpret_cast<const float4*>(l0 + S::L_PITCH + k);
+            const float u4[4] = {u.x, u.y, u.z, u.w}, v4[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float4 b = *reinterpret_cast<const float4*>(b0 + (k + e) * bp_ + c);
+              const float b4[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+              for (int o = 0; o < 4; ++o) { a0[o] = fmaf(u4[e], b4[o], a0[o]); a1[o] = fmaf(v4[e], b4[o], a1[o]); }
+            }
+          }
+          *reinterpret_cast<float4*>(dst + c) = make_float4(sign * a0[0], sign * a0[1], sign * a0[2], sign * a0[3]);
+          *reinterpret_cast<float4*>(dst + dp + c) = make_float4(sign * a1[0], sign * a1[1], sign * a1[2], sign * a1[3]);
+        };
+        const float* l21 = L + (32 + r) * S::L_PITCH;
+        product(l21, L, S::L_PITCH, 32, 1.f, W + r * S::W_PITCH, S::W_PITCH);
+        __syncthreads();
+        product(l21 + 32, W, S::W_PITCH, 8 * (warp + 1), -1.f, L + (32 + r) * S::L_PITCH, S::L_PITCH);   // T22 is lower triangular
+      }
+      __syncthreads();
+      {
+        // ---- operands: column i of the inverse times beta (and the weights of E), half of its rows a thread
+        const int half = tid >> 6;
+        float y[32];
+#pragma unroll
+        for (int r = 0; r < 32; ++r) y[r] = warp == 1 ? 0.f : beta[i] * L[(half * 32 + r) * S::L_PITCH + i];   // warp 1: above the diagonal
+        __syncthreads();                              // the inverse is read, the operands take its place
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
           uint32_t hi[4], lo[4], one[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 8 * c + 2 * e;
-            const float u0 = y[r] * b, u1 = y[r + 1] * b;
-            split2_pair(f2_pack(wgt[r] * u0, wgt[r + 1] * u1), hi[e], lo[e]);
-            one[e] = bf16_pair(u0, u1);
+            const float2 w = *reinterpret_cast<const float2*>(wgt + half * 32 + r);
+            split2_pair(w.x * y[r], w.y * y[r + 1], hi[e], lo[e]);
+            one[e] = bf16_pair(y[r], y[r + 1]);
           }
-          unsigned char* at = bp + S::OFF_T + i * 128 + ((c ^ (i & 7)) << 4);
+          unsigned char* at = bp + S::OFF_T + i * 128 + (((half * 4 + c) ^ (i & 7)) << 4);
           *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(at + 8192) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           *reinterpret_cast<uint4*>(at + 16384) = make_uint4(one[0], one[1], one[2], one[3]);
         }
-      } else {
-        float* f = reinterpret_cast<float*>(a.f + (size_t)unit * TokenTc::F_BYTES);
-        f[i] = fac[i];
-        f[64 + i] = fac[64 + i];
-        if (i == 0) f[128] = fac[128];
       }
       fence_proxy_async_smem();
       tc_fence_before_sync();
@@ -378,27 +419,29 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       ok = mbar_wait(bar_mma, 1, wc);
       if (!__syncthreads_or(!ok)) {
         tc_fence_after_sync();
-        tmem_ld32(lanes + 64, *reinterpret_cast<float(*)[32]>(x));
-        tmem_ld32(lanes + 96, *reinterpret_cast<float(*)[32]>(x + 32));
-        tmem_wait_ld();
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {                 // row tid of E: channel tid
-          uint32_t hi[4], lo[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) split2_pair(f2_pack(x[8 * c + 2 * e], x[8 * c + 2 * e + 1]), hi[e], lo[e]);
-          unsigned char* at = bp + S::OFF_KQ + tid * 128 + ((c ^ (tid & 7)) << 4);
-          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(at + TokenTc::E_PART) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        }
-        if (is_q) {
-          tmem_ld32(lanes, *reinterpret_cast<float(*)[32]>(x));
-          tmem_ld32(lanes + 32, *reinterpret_cast<float(*)[32]>(x + 32));
+#pragma unroll 1
+        for (int jb = 0; jb < 64; jb += 16) {         // row tid of E: channel tid
+          float x[16];
+          tmem_ld16(lanes + 64 + jb, x);
           tmem_wait_ld();
 #pragma unroll
-          for (int c = 0; c < 8; ++c)
-            *reinterpret_cast<uint4*>(bp + S::OFF_T + i * 128 + ((c ^ (i & 7)) << 4)) =
-                make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
-                           bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
+          for (int c = 0; c < 2; ++c) {
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) split2_pair(x[8 * c + 2 * e], x[8 * c + 2 * e + 1], hi[e], lo[e]);
+            unsigned char* at = bp + S::OFF_KQ + tid * 128 + (((jb / 8 + c) ^ (tid & 7)) << 4);
+            *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+            *reinterpret_cast<uint4*>(at + TokenTc::E_PART) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          }
+          if (is_q) {
+            tmem_ld16(lanes + jb, x);
+            tmem_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+              *reinterpret_cast<uint4*>(bp + S::OFF_T + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) =
+                  make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
+                             bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
+          }
         }
         fence_proxy_async_smem();
         __syncthreads();
@@ -426,13 +469,14 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // and O keep one row per thread and both factors a product needs from the previous one (the parts of S, the parts of X)
 // are written by the threads that own the rows, as A operands in tensor memory: nothing of the recurrence passes
 // through shared memory.  Roles: one thread feeds the loads (two stages, three groups of operands with their own
-// barriers), one issues the MMAs, eight warps own the state (two threads a row: 64 key channels each), four write out.
+// barriers), one issues the MMAs, sixteen warps own the state (four threads a row: 32 key channels each), four write out.
 struct TokenChain {
-  static constexpr int STATE_WARPS = 8, OUT_WARPS = 4;
+  static constexpr int STATE_WARPS = 16, OUT_WARPS = 4;
   static constexpr int THREADS = 64 + 32 * (STATE_WARPS + OUT_WARPS);
   static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 90112;
   static constexpr int STAGE = 91136;
-  static constexpr int OFF_BAR = 2 * STAGE;
+  static constexpr int OFF_O = 2 * STAGE;             // two tiles of results
+  static constexpr int OFF_BAR = OFF_O + 2 * 16384;
   static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
   // tensor memory columns
   static constexpr uint32_t S_HI = 0, S_LO = 64, DS = 128, D_K = 256, X_HI = 320, X_LO = 352, D_Q = 384, D_O = 448;
@@ -461,8 +505,8 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   enum { KQ = 0, V = 1, E = 2 };
   auto FULL = [&](int g, int st) { return bar0 + 8u * (g * 4 + st); };
   auto FREE = [&](int g, int st) { return bar0 + 8u * (g * 4 + 2 + st); };
-  const uint32_t S_READY = bar0 + 96, DK_FULL = bar0 + 104, DQ_FULL = bar0 + 112, X_READY = bar0 + 120, DS_FULL = bar0 + 128,
-                 DO_FULL = bar0 + 136, O_FREE = bar0 + 144;
+  const uint32_t S_READY = bar0 + 96, DK_FULL = bar0 + 104, X_READY = bar0 + 112, DS_FULL = bar0 + 120, DO_FULL = bar0 + 128,
+                 O_FREE = bar0 + 136;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 160);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 168);
   const WaitCtx wc(abort_flag, ds);
@@ -479,7 +523,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     mbar_init(S_READY, S::STATE_WARPS);
     mbar_init(X_READY, S::STATE_WARPS);
     mbar_init(O_FREE, S::OUT_WARPS);
-    mbar_init(DK_FULL, 1); mbar_init(DQ_FULL, 1); mbar_init(DS_FULL, 1); mbar_init(DO_FULL, 1);
+    mbar_init(DK_FULL, 1); mbar_init(DS_FULL, 1); mbar_init(DO_FULL, 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmV);
@@ -528,18 +572,23 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     // ------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
       constexpr uint32_t id64 = make_idesc_bf16(128, 64, false, false), id128 = make_idesc_bf16(128, 128, false, false);
+      // descriptors of the first stage; one step along K is 32 bytes, the other 64 channels a box further on
+      const uint64_t dk0 = make_smem_desc(base + S::OFF_K, 16, 1024), dq0 = make_smem_desc(base + S::OFF_Q, 16, 1024);
+      const uint64_t de0 = make_smem_desc(base + S::OFF_E, 16, 1024), dp0 = make_smem_desc(base + S::OFF_P, 16, 1024);
       for (int s = 0; s < steps; ++s) {
         const int st = s & 1;
-        const uint32_t at = base + st * S::STAGE, par = (s >> 1) & 1;
+        const uint32_t par = (s >> 1) & 1;
+        const uint64_t off = st ? S::STAGE >> 4 : 0;
+        const uint64_t dk = dk0 + off, dq = dq0 + off, de = de0 + off, dp = dp0 + off;
         if (!mbar_wait(FULL(KQ, st), par, wc) || !mbar_wait(S_READY, s & 1, wc)) break;
         tc_fence_after_sync();
         // S K^T, small part first
 #pragma unroll
-        for (int part = 1; part >= 0; --part)
+        for (int k = 0; k < 8; ++k)
+          mma_bf16_ts(tmem + S::D_K, tmem + S::S_LO + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            mma_bf16_ts(tmem + S::D_K, tmem + (part ? S::S_LO : S::S_HI) + k * 8,
-                        make_smem_desc(at + S::OFF_K + (k >> 2) * 8192 + (k & 3) * 32, 16, 1024), id64, part == 1 && k == 0 ? 0u : 1u);
+        for (int k = 0; k < 8; ++k)
+          mma_bf16_ts(tmem + S::D_K, tmem + S::S_HI + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
         mma_commit(DK_FULL);
         if (s > 0) {
           if (!mbar_wait(O_FREE, (s - 1) & 1, wc)) break;
@@ -547,57 +596,50 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8,
-                      make_smem_desc(at + S::OFF_Q + (k >> 2) * 8192 + (k & 3) * 32, 16, 1024), id64, k ? 1u : 0u);
-        mma_commit(DQ_FULL);
+          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
         mma_commit(FREE(KQ, st));
         if (!mbar_wait(FULL(E, st), par, wc) || !mbar_wait(X_READY, s & 1, wc)) break;
         tc_fence_after_sync();
         // X^T E^T: low X high E, high X low E, high X high E
 #pragma unroll
-        for (int term = 0; term < 3; ++term)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_bf16_ts(tmem + S::DS, tmem + (term == 0 ? S::X_LO : S::X_HI) + k * 8,
-                        make_smem_desc(at + S::OFF_E + (term == 1 ? TokenTc::E_PART : 0) + k * 32, 16, 1024), id128,
-                        term || k ? 1u : 0u);
-        mma_commit(DS_FULL);
+        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::DS, tmem + S::X_LO + k * 8, de + k * 2, id128, k ? 1u : 0u);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, make_smem_desc(at + S::OFF_P + k * 32, 16, 1024), id64, k ? 1u : 0u);
+          mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + ((TokenTc::E_PART >> 4) + k * 2), id128, 1u);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + k * 2, id128, 1u);
+        mma_commit(DS_FULL);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp + k * 2, id64, k ? 1u : 0u);
         mma_commit(DO_FULL);
         mma_commit(FREE(E, st));
       }
     }
   } else if (warp < 2 + S::STATE_WARPS) {
     // ------------------------------------------------------------------ state
-    const int qd = warp & 3, half = (warp - 2) >> 2;
+    const int qd = warp & 3, sl = (warp - 2) >> 2;    // lane quarter; quarter of the key channels and of the chunk's tokens
     const int row = qd * 32 + lane;                   // value channel
     const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
-    uint64_t sv[32];                                  // S[row][64 half ..], two to a register pair
+    float sv[32];                                     // S[row][32 sl ..]
     {
-      const float* src = t.state_in ? t.state_in + (((size_t)seq * t.H + h) * D + row) * D + half * 64 : nullptr;
+      const float* src = t.state_in ? t.state_in + (((size_t)seq * t.H + h) * D + row) * D + sl * 32 : nullptr;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float4 x = src ? *reinterpret_cast<const float4*>(src + 4 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
-        sv[2 * e] = f2_pack(x.x, x.y);
-        sv[2 * e + 1] = f2_pack(x.z, x.w);
+      for (int e = 0; e < 32; e += 4) {
+        const float4 x = src ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        sv[e] = x.x; sv[e + 1] = x.y; sv[e + 2] = x.z; sv[e + 3] = x.w;
       }
     }
     auto publish = [&]() {
+      float hi[16], lo[16];
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {          // 32 key channels at a time: fewer live registers
-        float hi[16], lo[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          uint32_t u, v;
-          split2_pair(sv[part * 16 + e], u, v);
-          hi[e] = __uint_as_float(u);
-          lo[e] = __uint_as_float(v);
-        }
-        tmem_st16(tl + S::S_HI + half * 32 + part * 16, hi);
-        tmem_st16(tl + S::S_LO + half * 32 + part * 16, lo);
+      for (int e = 0; e < 16; ++e) {
+        uint32_t u, v;
+        split2_pair(sv[2 * e], sv[2 * e + 1], u, v);
+        hi[e] = __uint_as_float(u);
+        lo[e] = __uint_as_float(v);
       }
+      tmem_st16(tl + S::S_HI + sl * 16, hi);
+      tmem_st16(tl + S::S_LO + sl * 16, lo);
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive_warp(S_READY);
@@ -605,100 +647,108 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     if (steps > 0) publish();
     for (int s = 0; s < steps; ++s) {
       const int st = s & 1;
-      const int n = min(C, len - s * C) - half * 32;  // tokens of this half that exist
-      const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(bp + st * S::STAGE + S::OFF_V) + half * 32 * D + row;
-      const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F);
+      const int n = min(C, len - s * C) - sl * 16;    // tokens of this quarter that exist
+      // what does not depend on the products is fetched while they run: V (two tokens to a register) and the factors
       if (!warp_wait(FULL(V, st), (s >> 1) & 1)) break;
+      const unsigned short* v = reinterpret_cast<const unsigned short*>(bp + st * S::STAGE + S::OFF_V) + sl * 16 * D + row;
+      const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F);
+      uint32_t vv[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vv[j] = (uint32_t)v[2 * j * D] | ((uint32_t)v[(2 * j + 1) * D] << 16);
       const float whole = f[128];
       if (!warp_wait(DK_FULL, s & 1)) break;
       tc_fence_after_sync();
-      float x[32];
-      tmem_ld32(tl + S::D_K + half * 32, x);
+      float x[16];
+      tmem_ld16(tl + S::D_K + sl * 16, x);
       tmem_wait_ld();
-      float hi[16], lo[16];
 #pragma unroll
-      for (int j = 0; j < 32; j += 4) {
-        const float4 fj = *reinterpret_cast<const float4*>(f + half * 32 + j);
-        const float e[4] = {fj.x, fj.y, fj.z, fj.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[j + i] = fmaf(-e[i], x[j + i], __bfloat162float(v[(j + i) * D]));
-        if (n < C / 2) {                              // rows behind the sequence: whatever they hold, X is zero there
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (j + i >= n) x[j + i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-          uint32_t p, q;
-          split2_pair(f2_pack(x[j + i], x[j + i + 1]), p, q);
-          hi[(j + i) / 2] = __uint_as_float(p);
-          lo[(j + i) / 2] = __uint_as_float(q);
-        }
+      for (int j = 0; j < 16; j += 4) {
+        const float4 fj = *reinterpret_cast<const float4*>(f + sl * 16 + j);
+        x[j] = fmaf(-fj.x, x[j], __uint_as_float(vv[j / 2] << 16));
+        x[j + 1] = fmaf(-fj.y, x[j + 1], __uint_as_float(vv[j / 2] & 0xFFFF0000u));
+        x[j + 2] = fmaf(-fj.z, x[j + 2], __uint_as_float(vv[j / 2 + 1] << 16));
+        x[j + 3] = fmaf(-fj.w, x[j + 3], __uint_as_float(vv[j / 2 + 1] & 0xFFFF0000u));
       }
-      tmem_st16(tl + S::X_HI + half * 16, hi);
-      tmem_st16(tl + S::X_LO + half * 16, lo);
+      if (n < 16) {                                   // rows behind the sequence: whatever they hold, X is zero there
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (j >= n) x[j] = 0.f;
+      }
+      {
+        float hl[16];                                 // high words, then low words
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          uint32_t u, w;
+          split2_pair(x[2 * j], x[2 * j + 1], u, w);
+          hl[j] = __uint_as_float(u);
+          hl[8 + j] = __uint_as_float(w);
+        }
+        tmem_st8(tl + S::X_HI + sl * 8, hl);
+        tmem_st8(tl + S::X_LO + sl * 8, hl + 8);
+      }
       tmem_wait_st();
       tc_fence_before_sync();
       mbar_arrive_warp(X_READY);
       mbar_arrive_warp(FREE(V, st));
       if (!warp_wait(DS_FULL, s & 1)) break;
       tc_fence_after_sync();
-      const uint64_t w2 = f2_pack(whole, whole);
+      float d[32];
+      tmem_ld32(tl + S::DS + sl * 32, d);
+      tmem_wait_ld();
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        tmem_ld32(tl + S::DS + half * 64 + part * 32, x);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 16; ++e) sv[part * 16 + e] = fma2(w2, sv[part * 16 + e], f2_pack(x[2 * e], x[2 * e + 1]));
-      }
+      for (int e = 0; e < 32; ++e) sv[e] = fmaf(whole, sv[e], d[e]);
       if (s + 1 < steps) publish();
     }
     if (t.state_out) {
-      float* dst = t.state_out + (((size_t)seq * t.H + h) * D + row) * D + half * 64;
+      float* dst = t.state_out + (((size_t)seq * t.H + h) * D + row) * D + sl * 32;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        float4 x;
-        f2_unpack(sv[2 * e], x.x, x.y);
-        f2_unpack(sv[2 * e + 1], x.z, x.w);
-        *reinterpret_cast<float4*>(dst + 4 * e) = x;
-      }
+      for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(sv[e], sv[e + 1], sv[e + 2], sv[e + 3]);
     }
   } else {
-    // ------------------------------------------------------------------ output: lanes are value channels, 64 bytes a warp and token
-    const int qd = warp & 3;
+    // ------------------------------------------------------------------ output
+    // Lanes are value channels: the tile is turned round in shared memory and leaves as whole rows of 256 bytes.
+    // (Stored from here, 64 bytes a warp and token, it took 3300 cycles a chunk and held up the MMAs.)
+    const int qd = warp & 3, tid = (warp - 2 - S::STATE_WARPS) * 32 + lane;
     const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(t.out) + start * t.out_stride + h * D + qd * 32 + lane;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(t.out) + (start + (tid >> 4)) * t.out_stride + h * D + (tid & 15) * 8;
     for (int s = 0; s < steps; ++s) {
       const int st = s & 1;
       const int n = min(C, len - s * C);
       const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F) + 64;
-      if (!warp_wait(FULL(V, st), (s >> 1) & 1) || !warp_wait(DQ_FULL, s & 1)) break;
-      tc_fence_after_sync();
-      float o[64];
-      tmem_ld32(tl + S::D_Q, *reinterpret_cast<float(*)[32]>(o));
-      tmem_ld32(tl + S::D_Q + 32, *reinterpret_cast<float(*)[32]>(o + 32));
-      tmem_wait_ld();
+      unsigned char* tile = bp + S::OFF_O + st * 16384;
+      // (the MMAs of S Q^T come before those of X^T P^T, one barrier says that both are there)
+      const bool ok = warp_wait(FULL(V, st), (s >> 1) & 1) && warp_wait(DO_FULL, s & 1);
+      if (ok) {
+        tc_fence_after_sync();
+        unsigned short* col = reinterpret_cast<unsigned short*>(tile) + qd * 32 + lane;
+#pragma unroll 1
+        for (int jb = 0; jb < 64; jb += 16) {
+          float x[16], y[16];
+          tmem_ld16(tl + S::D_Q + jb, x);
+          tmem_ld16(tl + S::D_O + jb, y);
+          tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 64; j += 4) {
-        const float4 e = *reinterpret_cast<const float4*>(f + j);
-        o[j] *= e.x; o[j + 1] *= e.y; o[j + 2] *= e.z; o[j + 3] *= e.w;
+          for (int j = 0; j < 16; j += 4) {
+            const float4 e = *reinterpret_cast<const float4*>(f + jb + j);
+            const uint32_t p = bf16_pair(fmaf(e.x, x[j], y[j]), fmaf(e.y, x[j + 1], y[j + 1]));
+            const uint32_t q = bf16_pair(fmaf(e.z, x[j + 2], y[j + 2]), fmaf(e.w, x[j + 3], y[j + 3]));
+            col[(jb + j) * D] = (unsigned short)p;
+            col[(jb + j + 1) * D] = (unsigned short)(p >> 16);
+            col[(jb + j + 2) * D] = (unsigned short)q;
+            col[(jb + j + 3) * D] = (unsigned short)(q >> 16);
+          }
+        }
+        tc_fence_before_sync();
+        mbar_arrive_warp(O_FREE);
+        mbar_arrive_warp(FREE(V, st));
       }
-      mbar_arrive_warp(FREE(V, st));
-      if (!warp_wait(DO_FULL, s & 1)) break;
-      tc_fence_after_sync();
+      if (named_barrier_or(2, 32 * S::OUT_WARPS, !ok)) break;
+      // two tiles in turn: the next barrier comes after these reads, the next write to this tile after that
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        float x[32];
-        tmem_ld32(tl + S::D_O + part * 32, x);
-        tmem_wait_ld();
-#pragma unroll
-        for (int j = 0; j < 32; ++j) o[part * 32 + j] += x[j];
+      for (int r = 0; r < 8; ++r) {
+        const int j = (tid >> 4) + 8 * r;
+        if (j < n) *reinterpret_cast<uint4*>(out + 8 * r * t.out_stride) = *reinterpret_cast<const uint4*>(tile + j * 256 + (tid & 15) * 16);
       }
-      tc_fence_before_sync();
-      mbar_arrive_warp(O_FREE);
-#pragma unroll
-      for (int j = 0; j < 64; ++j)
-        if (j < n) out[j * t.out_stride] = __float2bfloat16_rn(o[j]);
       out += C * t.out_stride;
     }
   }
