@@ -47,16 +47,25 @@ struct TokenTcArgs {
   long long places;
 };
 
-// The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.
+// The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.  A whole
+// warp looks at 32 offsets at a time: a round trip to memory for 32 sequences, two for a thousand.
 __device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int unit) {
-  int lo = 0, hi = t.S - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    long long start;
-    int len;
-    token_range(t.cu_seqlens, mid, t.per, t.n_tokens, start, len);
-    if (start / unit + mid <= x) lo = mid;
-    else hi = mid - 1;
+  int lo = 0, n = t.S;                                // the answer lies in [lo, lo + n), and sequence lo qualifies
+  const int lane = threadIdx.x & 31;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int s = lo + lane * step;
+    bool fits = false;
+    if (s < lo + n) {
+      long long start;
+      int len;
+      token_range(t.cu_seqlens, s, t.per, t.n_tokens, start, len);
+      fits = start / unit + s <= x;
+    }
+    const unsigned m = __ballot_sync(0xFFFFFFFFu, fits) | 1u;
+    const int k = 31 - __clz(m);
+    n = min(step, lo + n - (lo + k * step));
+    lo += k * step;
   }
   return lo;
 }
@@ -110,28 +119,38 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 }  // namespace tc
 
 // ---------------------------------------------------------------------------------------------- chunk operators
-// One CTA (four warps) per (place, head).  [K; Q] K^T is one MMA chain with the keys in rows 0..63 and the queries in rows
+// One CTA (eight warps) per (place, head).  [K; Q] K^T is one MMA chain with the keys in rows 0..63 and the queries in rows
 // 64..127 of one operand, so that lane i of tensor memory holds row i of K K^T and lane 64 + i row i of Q K^T.
 // The inverse of the unit lower triangular I + L is formed in fp32 in shared memory, block by block: the four 16 x 16 blocks on
 // the diagonal by forward substitution (a warp to a block, a lane to a column, 16 rows in registers), then pairs of
 // blocks are merged, [T11 0; -T22 L21 T11, T22], to 32 and to 64 rows, all threads at once.  A thread to a column over all 64
-// rows needs no products, but 2016 steps in straight line: 6.9 us a CTA-slot instead of FIXME, most of it waiting for
+// rows needs no products, but 2016 steps in straight line: half as fast again, most of it waiting for
 // instructions.  Everything that could be a long straight line is a loop over 16 columns for the same reason.
 struct TokenPrep {
-  static constexpr int THREADS = 128;
-  static constexpr int OFF_KQ = 0;                    // [K; Q]: two 64-channel boxes of 128 rows; later the parts of E
-  static constexpr int OFF_T = 32768;                 // inverse times factors: high, low; inverse times beta; (first: L)
-  static constexpr int OFF_M = OFF_T + 3 * 8192;      // scale M
-  static constexpr int OFF_F = OFF_M + 8192;          // G high, G low, beta, r, weight [64] each
-  static constexpr int OFF_BAR = OFF_F + 5 * 256;
+  static constexpr int THREADS = 256, CTAS = 4;       // a CTA's phases are short and end at barriers: four of them side by side
+  // [K; Q]: two 64-channel boxes of 128 rows, the queries in their lower halves.  Once the queries' product is formed, M
+  // and the inverse times beta take the queries' places (the products W on the way to the inverse before the latter); in the
+  // end the two parts of E take all of it.
+  static constexpr int OFF_KQ = 0, OFF_M = 8192, OFF_ONE = 24576, OFF_W = OFF_ONE;
+  static constexpr int OFF_T = 32768;                 // L and its inverse; then the inverse times factors, high and low; then P
+  static constexpr int L_PITCH = 68, W_PITCH = 36;    // floats: 16-byte rows, lanes' rows four banks apart
+  static constexpr int OFF_F = OFF_T + 64 * L_PITCH * 4;
+  // per token, exponents in units of ln 2: from the start of its 16 tokens (and its negative), to their end, to the chunk's end, from
+  // the chunk's start; beta; r of keys and queries; column factor; then the distances between blocks
+  static constexpr int F_UP = 0, F_DOWN = 64, F_END = 128, F_LAST = 192, F_ALL = 256, F_BETA = 320, F_R = 384, F_COL = 512,
+                       F_DIST = 576, F_FLOATS = 592;
+  static constexpr int OFF_BAR = OFF_F + F_FLOATS * 4;
   static constexpr int SMEM_BYTES = OFF_BAR + 64 + 1024;
-  static constexpr int L_PITCH = 68;                  // floats: 16-byte rows, lanes' rows four banks apart
-  static constexpr int OFF_W = OFF_T + 64 * L_PITCH * 4;   // products on the way to a merge, 32 rows of W_PITCH
-  static constexpr int W_PITCH = 36;
-  static_assert(OFF_W + 32 * W_PITCH * 4 <= OFF_M, "the inverse and its scratch lie where the operands go later");
 };
 
-__global__ void __launch_bounds__(TokenPrep::THREADS, 3)
+// 2^x.  Its argument is at most a little above zero here, and below -126 the result does not matter.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__global__ void __launch_bounds__(TokenPrep::THREADS, TokenPrep::CTAS)
 token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const TokenTcArgs a,
                   tc::DevStatus ds) {
   using namespace tc;
@@ -142,50 +161,53 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   unsigned char* bp = smem_dyn + (base - smem_u32(smem_dyn));
   const TokenArgs& t = a.t;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int h = (int)(blockIdx.x % t.H);
-  const long long place = blockIdx.x / t.H;
-
-  const int seq = token_seq_of(t, place, C);
-  long long start;
-  int len;
-  token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
-  const long long chunk = place - (start / C + seq);
-  if (chunk < 0 || chunk * C >= len) return;          // a place that no chunk has
-  const long long row0 = start + chunk * C;
-  const int n = min(C, len - (int)(chunk * C));
+  const int h = (int)(blockIdx.x % (unsigned)t.H);
+  const int place = (int)(blockIdx.x / (unsigned)t.H);
 
   const uint32_t bar_load = base + S::OFF_BAR, bar_mma = bar_load + 8;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 16);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 24);
+  int* where = reinterpret_cast<int*>(bp + S::OFF_BAR + 32);      // first row, tokens (0: no chunk has this place)
   const WaitCtx wc(abort_flag, ds);
-  float* g_hi = reinterpret_cast<float*>(bp + S::OFF_F);
-  float* g_lo = g_hi + 64;
-  float* beta = g_hi + 128;
-  float* rk = g_hi + 192;
-  float* wgt = g_hi + 256;
+  float* fs = reinterpret_cast<float*>(bp + S::OFF_F);
 
-  if (tid == 0) {
-    mbar_init(bar_load, 1);
-    mbar_init(bar_mma, 1);
-    *abort_flag = 0;
-    mbar_fence_init();
-    const int hk = h / (t.H / t.Hk);
-    mbar_arrive_expect_tx(bar_load, 32768);
-    tma_load_2d(base, &tmK, bar_load, hk * 128, (int)row0);
-    tma_load_2d(base + 16384, &tmK, bar_load, hk * 128 + 64, (int)row0);
-    tma_load_2d(base + 8192, &tmQ, bar_load, hk * 128, (int)row0);
-    tma_load_2d(base + 24576, &tmQ, bar_load, hk * 128 + 64, (int)row0);
+  if (warp == 0) {
+    const int seq = token_seq_of(t, place, C);
+    if (lane == 0) {
+      long long start;
+      int len;
+      token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
+      const long long chunk = place - (start / C + seq), row0 = start + chunk * C;
+      const int n = chunk < 0 || chunk * C >= len ? 0 : min(C, len - (int)(chunk * C));
+      where[0] = (int)row0;
+      where[1] = n;
+      mbar_init(bar_load, 1);
+      mbar_init(bar_mma, 1);
+      *abort_flag = 0;
+      mbar_fence_init();
+      if (n > 0) {
+        const int ch = h / (t.H / t.Hk) * 128;
+        mbar_arrive_expect_tx(bar_load, 32768);
+        tma_load_2d(base, &tmK, bar_load, ch, (int)row0);
+        tma_load_2d(base + 16384, &tmK, bar_load, ch + 64, (int)row0);
+        tma_load_2d(base + 8192, &tmQ, bar_load, ch, (int)row0);
+        tma_load_2d(base + 24576, &tmQ, bar_load, ch + 64, (int)row0);
+      }
+    }
   }
+  __syncthreads();
+  const int row0 = where[0], n = where[1];
+  if (n == 0) return;
   if (warp == 1) {
-    // running sum of the decay in 64 bits, kept as two floats: a difference of two of them is then good to fp32's
-    // rounding however far the sum has run.  A token's log decay counts down to -104 (e^-104 is 0 in fp32), so that -infinity
-    // leaves the differences finite.
+    // Running sum of the decay, in 64 bits and units of ln 2.  What is kept are differences, each rounded once: within 16
+    // tokens, to the end of the 16, between blocks, to the ends of the chunk.  A token's log decay counts down to -104 (e^-104
+    // is 0 in fp32), so that -infinity leaves the differences finite.
     double x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int j = 2 * lane + i;
-      float g = j < n && t.log_alpha ? t.log_alpha[(row0 + j) * t.H + h] : 0.f;
-      x[i] = g < -104.f ? -104.0 : (double)g;
+      const float g = j < n && t.log_alpha ? t.log_alpha[(size_t)(row0 + j) * t.H + h] : 0.f;
+      x[i] = (g < -104.f ? -104.0 : (double)g) * 1.4426950408889634074;
     }
     double sum = x[0] + x[1];
     const double own = sum;
@@ -194,22 +216,33 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const double y = __shfl_up_sync(0xFFFFFFFFu, sum, m);
       if (lane >= m) sum += y;
     }
-    const double g0 = sum - own + x[0], g1 = sum;
-    g_hi[2 * lane] = (float)g0;     g_lo[2 * lane] = (float)(g0 - (double)(float)g0);
-    g_hi[2 * lane + 1] = (float)g1; g_lo[2 * lane + 1] = (float)(g1 - (double)(float)g1);
-  } else if (warp >= 2) {
+    const double end = __shfl_sync(0xFFFFFFFFu, sum, lane | 7);          // of the lane's 16 tokens
+    double from = __shfl_sync(0xFFFFFFFFu, sum, (lane & 24) - 1);        // of those before
+    if (lane < 8) from = 0.0;
+    const double all = __shfl_sync(0xFFFFFFFFu, sum, 31);
+    const double g[2] = {sum - own + x[0], sum};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int j = 2 * lane + i;
+      fs[S::F_UP + j] = (float)(g[i] - from);
+      fs[S::F_DOWN + j] = (float)(from - g[i]);
+      fs[S::F_END + j] = (float)(end - g[i]);
+      fs[S::F_LAST + j] = (float)(all - g[i]);
+      fs[S::F_ALL + j] = (float)g[i];
+    }
+    const double e = __shfl_sync(0xFFFFFFFFu, sum, (lane & 3) * 8 + 7);  // end of block J = lane & 3
+    const double b = __shfl_sync(0xFFFFFFFFu, sum, max(((lane >> 2) & 3) * 8 - 1, 0));   // end of the block before I = lane / 4
+    if (lane < 16) fs[S::F_DIST + lane] = (float)(b - e);                // used for J < I
+  } else if (warp == 2 || warp == 3) {
     const int j = tid - 64;
-    beta[j] = j < n ? t.beta[(row0 + j) * t.H + h] : 0.f;
-  } else {
-    __syncwarp();
+    fs[S::F_BETA + j] = j < n ? t.beta[(size_t)(row0 + j) * t.H + h] : 0.f;
+  } else if (warp == 0) {
     tmem_alloc(smem_u32(tmem_slot), 128);
     tmem_relinquish();
   }
-  tc_fence_before_sync();
-  __syncthreads();
-  tc_fence_after_sync();
-  const uint32_t tmem = *tmem_slot;
-  const uint32_t lanes = tmem + ((uint32_t)(warp * 32) << 16);
+  // two warps share a quarter of the lanes and divide the columns between them
+  const int qd = warp & 3, part = warp >> 2;
+  const int rowid = qd * 32 + lane;                   // lane of tensor memory: a key, or 64 + a query, or a channel
   bool ok = mbar_wait(bar_load, 0, wc);
   if (n < C && ok) {
     // keys behind the sequence are the next one's (or nothing's): they must not enter a sum, not even times zero
@@ -219,24 +252,28 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     }
     fence_proxy_async_smem();
   }
+  tc_fence_before_sync();
   if (!__syncthreads_or(!ok)) {
+    tc_fence_after_sync();
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t lanes = tmem + ((uint32_t)(qd * 32) << 16);
     if (tid == 0) {
       constexpr uint32_t idesc = make_idesc_bf16(128, 64, false, false);
+      const uint64_t d = make_smem_desc(base, 16, 1024);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const uint32_t at = base + (k >> 2) * 16384 + (k & 3) * 32;
-        mma_bf16_ss(tmem, make_smem_desc(at, 16, 1024), make_smem_desc(at, 16, 1024), idesc, k ? 1u : 0u);
+        const uint64_t dk = d + ((k >> 2) * (16384 >> 4) + (k & 3) * 2);
+        mma_bf16_ss(tmem, dk, dk, idesc, k ? 1u : 0u);
       }
       mma_commit(bar_mma);
     }
-    const bool is_q = warp >= 2;
-    const int i = tid & 63;                           // token of this thread's row
-    float norm = 1.f;                                 // r of the row's key or query
-    if (t.l2_eps > 0.f) {
-      float ss = 0.f;
-#pragma unroll 4
-      for (int c = 0; c < 16; ++c) {
-        const uint4 w = *reinterpret_cast<const uint4*>(bp + (c >> 3) * 16384 + tid * 128 + (((c & 7) ^ (i & 7)) << 4));
+    float ss = 1.f;
+    if (t.l2_eps > 0.f) {                             // two lanes a row, 64 channels each
+      const int r = tid >> 1;
+      ss = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const uint4 w = *reinterpret_cast<const uint4*>(bp + (tid & 1) * 16384 + r * 128 + ((c ^ (r & 7)) << 4));
         const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -244,58 +281,73 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           ss = fmaf(lo, lo, fmaf(hi, hi, ss));
         }
       }
-      norm = rsqrtf(ss + t.l2_eps);
+      ss += __shfl_xor_sync(0xFFFFFFFFu, ss, 1);
+      ss = rsqrtf(ss + t.l2_eps);
     }
-    if (!is_q) rk[i] = norm;
+    if (!(tid & 1)) {
+      const int r = tid >> 1;
+      fs[S::F_R + r] = ss;
+      if (r < 64) fs[S::F_COL + r] = ss * exp2_fast(fs[S::F_END + r]);
+    }
     ok = mbar_wait(bar_mma, 0, wc);
     if (!__syncthreads_or(!ok)) {
       tc_fence_after_sync();
-      const float gi_hi = g_hi[i], gi_lo = g_lo[i];
-      const float row = is_q ? t.scale * norm : beta[i] * norm;
+      const bool is_q = qd >= 2;
+      const int i = rowid & 63;                       // token of this thread's row
+      const float norm = fs[S::F_R + rowid], up = fs[S::F_UP + i];
+      const float row = is_q ? t.scale * norm : fs[S::F_BETA + i] * norm;
       const int last = is_q ? i : i - 1;              // L is strictly lower, M has its diagonal
       float* L = reinterpret_cast<float*>(bp + S::OFF_T);
 #pragma unroll 1
-      for (int jb = 0; jb < 64; jb += 16) {
+      for (int jb = part * 16; jb < 64; jb += 32) {
+        unsigned char* m0 = bp + S::OFF_M + i * 128 + (((jb / 8) ^ (i & 7)) << 4);
+        unsigned char* m1 = bp + S::OFF_M + i * 128 + (((jb / 8 + 1) ^ (i & 7)) << 4);
         if (jb > (i | 31)) {                          // nothing of this warp's rows is this far right
-          if (is_q) {
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              *reinterpret_cast<uint4*>(bp + S::OFF_M + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) = make_uint4(0, 0, 0, 0);
-          }
+          if (is_q) *reinterpret_cast<uint4*>(m0) = *reinterpret_cast<uint4*>(m1) = make_uint4(0, 0, 0, 0);
           continue;
         }
         float x[16];
         tmem_ld16(lanes + jb, x);
         tmem_wait_ld();
+        if (jb + 16 <= (i & 32)) {
+          // the warp's rows all lie behind these 16 columns: e^{G_i - G_j} is a factor of the row, from the columns' end on, times
+          // a factor of the column, up to their end, both at most 1
+          const float f = row * exp2_fast(up + fs[S::F_DIST + (i >> 4) * 4 + (jb >> 4)]);
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          const float4 gh = *reinterpret_cast<const float4*>(g_hi + jb + j), gl = *reinterpret_cast<const float4*>(g_lo + jb + j);
-          const float4 rr = *reinterpret_cast<const float4*>(rk + jb + j);
-          const float h4[4] = {gh.x, gh.y, gh.z, gh.w}, l4[4] = {gl.x, gl.y, gl.z, gl.w}, r4[4] = {rr.x, rr.y, rr.z, rr.w};
+          for (int j = 0; j < 16; j += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(fs + S::F_COL + jb + j);
+            x[j] *= f * c.x; x[j + 1] *= f * c.y; x[j + 2] *= f * c.z; x[j + 3] *= f * c.w;
+          }
+        } else {
+          // the row's own 16 columns (exponents from their start), or the 16 before them (the columns' end is the rows' start)
+          const float* col = fs + ((i >> 4) == (jb >> 4) ? S::F_DOWN : S::F_END) + jb;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            x[j + e] = jb + j + e <= last ? row * r4[e] * __expf((gi_hi - h4[e]) + (gi_lo - l4[e])) * x[j + e] : 0.f;
-          if (!is_q) *reinterpret_cast<float4*>(L + i * S::L_PITCH + jb + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+          for (int j = 0; j < 16; j += 4) {
+            const float4 c = *reinterpret_cast<const float4*>(col + j), r = *reinterpret_cast<const float4*>(fs + S::F_R + jb + j);
+            const float c4[4] = {c.x, c.y, c.z, c.w}, r4[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              x[j + e] = jb + j + e <= last ? row * r4[e] * exp2_fast(up + c4[e]) * x[j + e] : 0.f;
+          }
         }
         if (is_q) {
+          *reinterpret_cast<uint4*>(m0) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+          *reinterpret_cast<uint4*>(m1) = make_uint4(bf16_pair(x[8], x[9]), bf16_pair(x[10], x[11]), bf16_pair(x[12], x[13]), bf16_pair(x[14], x[15]));
+        } else {
 #pragma unroll
-          for (int c = 0; c < 2; ++c)
-            *reinterpret_cast<uint4*>(bp + S::OFF_M + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) =
-                make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
-                           bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
+          for (int j = 0; j < 16; j += 4)
+            *reinterpret_cast<float4*>(L + i * S::L_PITCH + jb + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
         }
       }
-      const long long unit = place * t.H + h;
-      {
-        const float eg = __expf(gi_hi + gi_lo);
-        float* f = reinterpret_cast<float*>(a.f + (size_t)unit * TokenTc::F_BYTES);
-        if (!is_q) wgt[i] = norm * __expf((g_hi[63] - gi_hi) + (g_lo[63] - gi_lo));
-        f[tid] = eg * (is_q ? t.scale * norm : norm); // keys' factors, then the queries'
-        if (tid == 0) f[128] = __expf(g_hi[63] + g_lo[63]);
+      const size_t unit = (size_t)place * t.H + h;
+      if (part == 0) {
+        float* f = reinterpret_cast<float*>(a.f + unit * TokenTc::F_BYTES);
+        f[rowid] = exp2_fast(fs[S::F_ALL + i]) * (is_q ? t.scale * norm : norm);   // keys' factors, then the queries'
+        if (tid == 0) f[128] = exp2_fast(fs[S::F_ALL + 63]);
       }
       __syncthreads();
       // ---- inverse: the blocks on the diagonal, in place
-      {
+      if (warp < 4) {
         float* Lb = L + warp * 16 * (S::L_PITCH + 1);
         const int c = lane & 15;
         float y[16];
@@ -323,76 +375,81 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       __syncthreads();
       float* W = reinterpret_cast<float*>(bp + S::OFF_W);
       {
-        // ---- pairs of 16: W = L21 T11, then T21 = -T22 W;  64 threads a pair, four neighbouring columns each
-        float* A = L + (tid >> 6) * 32 * (S::L_PITCH + 1);
-        float* Wp = W + (tid >> 6) * 16 * S::W_PITCH;
-        const int r = (tid & 63) >> 2, c = (tid & 3) * 4;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+        // ---- pairs of 16: W = L21 T11, then T21 = -T22 W;  128 threads a pair, two neighbouring columns each
+        float* A = L + (tid >> 7) * 32 * (S::L_PITCH + 1);
+        float* Wp = W + (tid >> 7) * 16 * S::W_PITCH;
+        const int r = (tid & 127) >> 3, c = (tid & 7) * 2;
+        float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float l = A[(16 + r) * S::L_PITCH + k];
-          const float4 b = *reinterpret_cast<const float4*>(A + k * S::L_PITCH + c);
-          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y); acc.z = fmaf(l, b.z, acc.z); acc.w = fmaf(l, b.w, acc.w);
+          const float2 b = *reinterpret_cast<const float2*>(A + k * S::L_PITCH + c);
+          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y);
         }
-        *reinterpret_cast<float4*>(Wp + r * S::W_PITCH + c) = acc;
+        *reinterpret_cast<float2*>(Wp + r * S::W_PITCH + c) = acc;
         __syncthreads();
-        acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+        acc = make_float2(0.f, 0.f);
+#pragma unroll
         for (int k = 0; k < 16; ++k) {
           const float l = -A[(16 + r) * S::L_PITCH + 16 + k];
-          const float4 b = *reinterpret_cast<const float4*>(Wp + k * S::W_PITCH + c);
-          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y); acc.z = fmaf(l, b.z, acc.z); acc.w = fmaf(l, b.w, acc.w);
+          const float2 b = *reinterpret_cast<const float2*>(Wp + k * S::W_PITCH + c);
+          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y);
         }
-        *reinterpret_cast<float4*>(A + (16 + r) * S::L_PITCH + c) = acc;
+        *reinterpret_cast<float2*>(A + (16 + r) * S::L_PITCH + c) = acc;
       }
       __syncthreads();
       {
-        // ---- the pair of 32: two rows and four columns a thread
-        const int r = (tid >> 3) * 2, c = (tid & 7) * 4;
-        auto product = [&](const float* l0, const float* b0, int bp_, int kn, float sign, float* dst, int dp) {
-          float a0[4] = {0.f, 0.f, 0.f, 0.f}, a1[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
+        // ---- the pair of 32: four neighbouring columns a thread
+        const int r = tid >> 3, c = (tid & 7) * 4;
+        auto product = [&](const float* l, const float* b0, int pitch, int kn, float sign, float* dst) {
+          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
           for (int k = 0; k < kn; k += 4) {
-            const float4 u = *reinterpret_cast<const float4*>(l0 + k), v = *reinterpret_cast<const float4*>(l0 + S::L_PITCH + k);
-            const float u4[4] = {u.x, u.y, u.z, u.w}, v4[4] = {v.x, v.y, v.z, v.w};
+            const float4 u = *reinterpret_cast<const float4*>(l + k);
+            const float u4[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float4 b = *reinterpret_cast<const float4*>(b0 + (k + e) * bp_ + c);
-              const float b4[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-              for (int o = 0; o < 4; ++o) { a0[o] = fmaf(u4[e], b4[o], a0[o]); a1[o] = fmaf(v4[e], b4[o], a1[o]); }
+              const float4 b = *reinterpret_cast<const float4*>(b0 + (k + e) * pitch + c);
+              acc[0] = fmaf(u4[e], b.x, acc[0]); acc[1] = fmaf(u4[e], b.y, acc[1]);
+              acc[2] = fmaf(u4[e], b.z, acc[2]); acc[3] = fmaf(u4[e], b.w, acc[3]);
             }
           }
-          *reinterpret_cast<float4*>(dst + c) = make_float4(sign * a0[0], sign * a0[1], sign * a0[2], sign * a0[3]);
-          *reinterpret_cast<float4*>(dst + dp + c) = make_float4(sign * a1[0], sign * a1[1], sign * a1[2], sign * a1[3]);
+          *reinterpret_cast<float4*>(dst + c) = make_float4(sign * acc[0], sign * acc[1], sign * acc[2], sign * acc[3]);
         };
-        const float* l21 = L + (32 + r) * S::L_PITCH;
-        product(l21, L, S::L_PITCH, 32, 1.f, W + r * S::W_PITCH, S::W_PITCH);
+        float* l21 = L + (32 + r) * S::L_PITCH;
+        product(l21, L, S::L_PITCH, 32, 1.f, W + r * S::W_PITCH);
         __syncthreads();
-        product(l21 + 32, W, S::W_PITCH, 8 * (warp + 1), -1.f, L + (32 + r) * S::L_PITCH, S::L_PITCH);   // T22 is lower triangular
+        product(l21 + 32, W, S::W_PITCH, 4 * (warp + 1), -1.f, l21);   // T22 is lower triangular: rows 4 warp .. 4 warp + 3
       }
       __syncthreads();
       {
-        // ---- operands: column i of the inverse times beta (and the weights of E), half of its rows a thread
-        const int half = tid >> 6;
-        float y[32];
+        // ---- operands: column c of the inverse times beta (and the weights of E), 16 of its rows a thread
+        const int c = tid & 63, r0 = (tid >> 6) * 16;
+        const bool zero = r0 < 32 && c >= 32;         // above the diagonal blocks: never written
+        float y[16];
 #pragma unroll
-        for (int r = 0; r < 32; ++r) y[r] = warp == 1 ? 0.f : beta[i] * L[(half * 32 + r) * S::L_PITCH + i];   // warp 1: above the diagonal
+        for (int r = 0; r < 16; ++r) y[r] = zero ? 0.f : fs[S::F_BETA + c] * L[(r0 + r) * S::L_PITCH + c];
+        float wgt[16];                                // e^{G_C - G} r of the rows
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const float4 g = *reinterpret_cast<const float4*>(fs + S::F_LAST + r0 + r), k = *reinterpret_cast<const float4*>(fs + S::F_R + r0 + r);
+          wgt[r] = k.x * exp2_fast(g.x); wgt[r + 1] = k.y * exp2_fast(g.y); wgt[r + 2] = k.z * exp2_fast(g.z); wgt[r + 3] = k.w * exp2_fast(g.w);
+        }
         __syncthreads();                              // the inverse is read, the operands take its place
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int q = 0; q < 2; ++q) {
           uint32_t hi[4], lo[4], one[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int r = 8 * c + 2 * e;
-            const float2 w = *reinterpret_cast<const float2*>(wgt + half * 32 + r);
-            split2_pair(w.x * y[r], w.y * y[r + 1], hi[e], lo[e]);
+            const int r = 8 * q + 2 * e;
+            const float w0 = wgt[r], w1 = wgt[r + 1];
+            split2_pair(w0 * y[r], w1 * y[r + 1], hi[e], lo[e]);
             one[e] = bf16_pair(y[r], y[r + 1]);
           }
-          unsigned char* at = bp + S::OFF_T + i * 128 + (((half * 4 + c) ^ (i & 7)) << 4);
+          unsigned char* at = bp + S::OFF_T + c * 128 + (((r0 / 8 + q) ^ (c & 7)) << 4);
           *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
           *reinterpret_cast<uint4*>(at + 8192) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          *reinterpret_cast<uint4*>(at + 16384) = make_uint4(one[0], one[1], one[2], one[3]);
+          *reinterpret_cast<uint4*>(at - S::OFF_T + S::OFF_ONE) = make_uint4(one[0], one[1], one[2], one[3]);
         }
       }
       fence_proxy_async_smem();
@@ -402,25 +459,22 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (tid == 0) {
         // E [128 x 64] = K^T (M rows = channels, read MN-major) times the two parts
         constexpr uint32_t ide = make_idesc_bf16(128, 64, true, false);
+        const uint64_t dk = make_smem_desc(base, 16384, 1024), dt = make_smem_desc(base + S::OFF_T, 16, 1024);
 #pragma unroll
-        for (int part = 0; part < 2; ++part)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            mma_bf16_ss(tmem + 64, make_smem_desc(base + k * 2048, 16384, 1024),
-                        make_smem_desc(base + S::OFF_T + part * 8192 + k * 32, 16, 1024), ide, part || k ? 1u : 0u);
-        // P: rows 64..127 of the A operand are scale M, the rows before it are of no interest
+        for (int k = 0; k < 8; ++k)
+          mma_bf16_ss(tmem + 64, dk + (k & 3) * (2048 >> 4), dt + ((k >> 2) * (8192 >> 4) + (k & 3) * 2), ide, k ? 1u : 0u);
+        // P: rows 64..127 of the A operand are scale M, the rows before it (keys) are of no interest
         constexpr uint32_t idp = make_idesc_bf16(128, 64, false, false);
+        const uint64_t dm = make_smem_desc(base + S::OFF_M - 8192, 16, 1024), d1 = make_smem_desc(base + S::OFF_ONE, 16, 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ss(tmem, make_smem_desc(base + S::OFF_M - 8192 + k * 32, 16, 1024),
-                      make_smem_desc(base + S::OFF_T + 16384 + k * 32, 16, 1024), idp, k ? 1u : 0u);
+        for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem, dm + k * 2, d1 + k * 2, idp, k ? 1u : 0u);
         mma_commit(bar_mma);
       }
       ok = mbar_wait(bar_mma, 1, wc);
       if (!__syncthreads_or(!ok)) {
         tc_fence_after_sync();
 #pragma unroll 1
-        for (int jb = 0; jb < 64; jb += 16) {         // row tid of E: channel tid
+        for (int jb = part * 32; jb < part * 32 + 32; jb += 16) {   // a row of E: a channel
           float x[16];
           tmem_ld16(lanes + 64 + jb, x);
           tmem_wait_ld();
@@ -429,7 +483,7 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) split2_pair(x[8 * c + 2 * e], x[8 * c + 2 * e + 1], hi[e], lo[e]);
-            unsigned char* at = bp + S::OFF_KQ + tid * 128 + (((jb / 8 + c) ^ (tid & 7)) << 4);
+            unsigned char* at = bp + S::OFF_KQ + rowid * 128 + (((jb / 8 + c) ^ (rowid & 7)) << 4);
             *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
             *reinterpret_cast<uint4*>(at + TokenTc::E_PART) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
           }
@@ -446,8 +500,8 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         fence_proxy_async_smem();
         __syncthreads();
         if (tid == 0) {
-          bulk_store(a.e + (size_t)unit * TokenTc::E_BYTES, base + S::OFF_KQ, TokenTc::E_BYTES);
-          bulk_store(a.p + (size_t)unit * TokenTc::P_BYTES, base + S::OFF_T, TokenTc::P_BYTES);
+          bulk_store(a.e + unit * TokenTc::E_BYTES, base + S::OFF_KQ, TokenTc::E_BYTES);
+          bulk_store(a.p + unit * TokenTc::P_BYTES, base + S::OFF_T, TokenTc::P_BYTES);
           tma_store_commit();
           tma_store_wait_all<0>();
         }
@@ -460,7 +514,7 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   __syncthreads();
   if (warp == 0) {
     tc_fence_after_sync();
-    tmem_dealloc(tmem, 128);
+    tmem_dealloc(*tmem_slot, 128);
   }
 }
 
