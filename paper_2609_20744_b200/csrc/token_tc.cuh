@@ -135,13 +135,54 @@ struct TokenPrep {
   static constexpr int OFF_T = 32768;                 // L and its inverse; then the inverse times factors, high and low; then P
   static constexpr int L_PITCH = 68, W_PITCH = 36;    // floats: 16-byte rows, lanes' rows four banks apart
   static constexpr int OFF_F = OFF_T + 64 * L_PITCH * 4;
-  // per token, exponents in units of ln 2: from the start of its 16 tokens (and its negative), to their end, to the chunk's end, from
-  // the chunk's start; beta; r of keys and queries; column factor; then the distances between blocks
+  // per token, exponents in units of ln 2: from the start of its 16 tokens; back to it; to their end; to the chunk's end (later
+  // the weight r e^{G_C - G}); from the chunk's start.  beta; r of keys and queries; factor of a column as a whole; distances
+  // between blocks of 16
   static constexpr int F_UP = 0, F_DOWN = 64, F_END = 128, F_LAST = 192, F_ALL = 256, F_BETA = 320, F_R = 384, F_COL = 512,
                        F_DIST = 576, F_FLOATS = 592;
   static constexpr int OFF_BAR = OFF_F + F_FLOATS * 4;
   static constexpr int SMEM_BYTES = OFF_BAR + 64 + 1024;
 };
+
+// c += A B for one 16 x 8 tile of small fp32 matrices in shared memory (row-major, pitches in floats), 8 `ksteps` deep, on the
+// warp-level tensor instruction: each factor as two tf32 parts (the instruction looks at the upper 19 bits), low times low left
+// out: 2^-20 of a product.  A 32-row merge is 14 of these steps; with one multiply-add a thread and LDS.128 for two
+// operands it kept the shared-memory pipe 80 % busy.
+__device__ __forceinline__ void tile_product(float (&c)[4], const float* A, int pa, const float* B, int pb, int ksteps) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  const float* ar = A + g * pa + t;
+  const float* br = B + t * pb + g;
+#pragma unroll 2
+  for (int k = 0; k < ksteps; ++k) {
+    const float av[4] = {ar[0], ar[8 * pa], ar[4], ar[8 * pa + 4]}, bv[2] = {br[0], br[4 * pb]};
+    uint32_t ah[4], al[4], bh[2], bl[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      ah[i] = __float_as_uint(av[i]) & 0xFFFFE000u;
+      al[i] = __float_as_uint(av[i] - __uint_as_float(ah[i]));
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      bh[i] = __float_as_uint(bv[i]) & 0xFFFFE000u;
+      bl[i] = __float_as_uint(bv[i] - __uint_as_float(bh[i]));
+    }
+    auto mma = [&](const uint32_t (&x)[4], const uint32_t (&y)[2]) {
+      asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                   : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                   : "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(y[0]), "r"(y[1]));
+    };
+    mma(al, bh);
+    mma(ah, bl);
+    mma(ah, bh);
+    ar += 8;
+    br += 8 * pb;
+  }
+}
+__device__ __forceinline__ void tile_store(float* D, int pd, float sign, const float (&c)[4]) {
+  const int g = (threadIdx.x & 31) >> 2, t = threadIdx.x & 3;
+  *reinterpret_cast<float2*>(D + g * pd + 2 * t) = make_float2(sign * c[0], sign * c[1]);
+  *reinterpret_cast<float2*>(D + (g + 8) * pd + 2 * t) = make_float2(sign * c[2], sign * c[3]);
+}
 
 // 2^x.  Its argument is at most a little above zero here, and below -126 the result does not matter.
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -273,7 +314,7 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       ss = 0.f;
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
-        const uint4 w = *reinterpret_cast<const uint4*>(bp + (tid & 1) * 16384 + r * 128 + ((c ^ (r & 7)) << 4));
+        const uint4 w = *reinterpret_cast<const uint4*>(bp + (tid & 1) * 16384 + r * 128 + ((c ^ (r & 7) ^ ((tid & 1) << 2)) << 4));
         const uint32_t v[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -287,7 +328,13 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     if (!(tid & 1)) {
       const int r = tid >> 1;
       fs[S::F_R + r] = ss;
-      if (r < 64) fs[S::F_COL + r] = ss * exp2_fast(fs[S::F_END + r]);
+      if (r < 64) {                                   // a key's r goes with its column's exponents
+        const float lg = __log2f(ss), end = fs[S::F_END + r] + lg;
+        fs[S::F_DOWN + r] += lg;
+        fs[S::F_END + r] = end;
+        fs[S::F_COL + r] = exp2_fast(end);
+        fs[S::F_LAST + r] = ss * exp2_fast(fs[S::F_LAST + r]);
+      }
     }
     ok = mbar_wait(bar_mma, 0, wc);
     if (!__syncthreads_or(!ok)) {
@@ -323,11 +370,10 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           const float* col = fs + ((i >> 4) == (jb >> 4) ? S::F_DOWN : S::F_END) + jb;
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(col + j), r = *reinterpret_cast<const float4*>(fs + S::F_R + jb + j);
-            const float c4[4] = {c.x, c.y, c.z, c.w}, r4[4] = {r.x, r.y, r.z, r.w};
+            const float4 c = *reinterpret_cast<const float4*>(col + j);
+            const float c4[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              x[j + e] = jb + j + e <= last ? row * r4[e] * exp2_fast(up + c4[e]) * x[j + e] : 0.f;
+            for (int e = 0; e < 4; ++e) x[j + e] = jb + j + e <= last ? row * exp2_fast(up + c4[e]) * x[j + e] : 0.f;
           }
         }
         if (is_q) {
@@ -345,10 +391,10 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         f[rowid] = exp2_fast(fs[S::F_ALL + i]) * (is_q ? t.scale * norm : norm);   // keys' factors, then the queries'
         if (tid == 0) f[128] = exp2_fast(fs[S::F_ALL + 63]);
       }
-      __syncthreads();
-      // ---- inverse: the blocks on the diagonal, in place
-      if (warp < 4) {
-        float* Lb = L + warp * 16 * (S::L_PITCH + 1);
+      // ---- inverse: the blocks on the diagonal, in place, by the four warps that formed L (the other four form M meanwhile)
+      if (!is_q) {
+        named_barrier_sync(1, 128);
+        float* Lb = L + ((warp & 1) + 2 * part) * 16 * (S::L_PITCH + 1);
         const int c = lane & 15;
         float y[16];
 #pragma unroll
@@ -374,52 +420,32 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       }
       __syncthreads();
       float* W = reinterpret_cast<float*>(bp + S::OFF_W);
-      {
-        // ---- pairs of 16: W = L21 T11, then T21 = -T22 W;  128 threads a pair, two neighbouring columns each
-        float* A = L + (tid >> 7) * 32 * (S::L_PITCH + 1);
-        float* Wp = W + (tid >> 7) * 16 * S::W_PITCH;
-        const int r = (tid & 127) >> 3, c = (tid & 7) * 2;
-        float2 acc = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float l = A[(16 + r) * S::L_PITCH + k];
-          const float2 b = *reinterpret_cast<const float2*>(A + k * S::L_PITCH + c);
-          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y);
-        }
-        *reinterpret_cast<float2*>(Wp + r * S::W_PITCH + c) = acc;
-        __syncthreads();
-        acc = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float l = -A[(16 + r) * S::L_PITCH + 16 + k];
-          const float2 b = *reinterpret_cast<const float2*>(Wp + k * S::W_PITCH + c);
-          acc.x = fmaf(l, b.x, acc.x); acc.y = fmaf(l, b.y, acc.y);
-        }
-        *reinterpret_cast<float2*>(A + (16 + r) * S::L_PITCH + c) = acc;
+      if (warp < 4) {
+        // ---- pairs of 16: W = L21 T11, then T21 = -T22 W;  a warp to eight columns of a pair, which need nobody else's W
+        float* A = L + (warp >> 1) * 32 * (S::L_PITCH + 1);
+        float* Wp = W + warp * 16 * 8;
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        tile_product(c, A + 16 * S::L_PITCH, S::L_PITCH, A + (warp & 1) * 8, S::L_PITCH, 2);
+        tile_store(Wp, 8, 1.f, c);
+        __syncwarp();
+        c[0] = c[1] = c[2] = c[3] = 0.f;
+        tile_product(c, A + 16 * S::L_PITCH + 16, S::L_PITCH, Wp, 8, 2);
+        // (the other warp of the pair still reads these rows of L: wait for it)
+        named_barrier_sync(2, 128);
+        tile_store(A + 16 * S::L_PITCH + (warp & 1) * 8, S::L_PITCH, -1.f, c);
       }
       __syncthreads();
       {
-        // ---- the pair of 32: four neighbouring columns a thread
-        const int r = tid >> 3, c = (tid & 7) * 4;
-        auto product = [&](const float* l, const float* b0, int pitch, int kn, float sign, float* dst) {
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-          for (int k = 0; k < kn; k += 4) {
-            const float4 u = *reinterpret_cast<const float4*>(l + k);
-            const float u4[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float4 b = *reinterpret_cast<const float4*>(b0 + (k + e) * pitch + c);
-              acc[0] = fmaf(u4[e], b.x, acc[0]); acc[1] = fmaf(u4[e], b.y, acc[1]);
-              acc[2] = fmaf(u4[e], b.z, acc[2]); acc[3] = fmaf(u4[e], b.w, acc[3]);
-            }
-          }
-          *reinterpret_cast<float4*>(dst + c) = make_float4(sign * acc[0], sign * acc[1], sign * acc[2], sign * acc[3]);
-        };
-        float* l21 = L + (32 + r) * S::L_PITCH;
-        product(l21, L, S::L_PITCH, 32, 1.f, W + r * S::W_PITCH);
+        // ---- the pair of 32: a warp to 16 rows and 8 columns
+        const int m = (warp & 1) * 16, c0 = (warp >> 1) * 8;
+        float* A = L + 32 * S::L_PITCH;
+        float c[4] = {0.f, 0.f, 0.f, 0.f};
+        tile_product(c, A + m * S::L_PITCH, S::L_PITCH, L + c0, S::L_PITCH, 4);
+        tile_store(W + m * S::W_PITCH + c0, S::W_PITCH, 1.f, c);
         __syncthreads();
-        product(l21 + 32, W, S::W_PITCH, 4 * (warp + 1), -1.f, l21);   // T22 is lower triangular: rows 4 warp .. 4 warp + 3
+        c[0] = c[1] = c[2] = c[3] = 0.f;
+        tile_product(c, A + m * S::L_PITCH + 32, S::L_PITCH, W + c0, S::W_PITCH, m ? 4 : 2);   // T22 is lower triangular
+        tile_store(A + m * S::L_PITCH + c0, S::L_PITCH, -1.f, c);
       }
       __syncthreads();
       {
@@ -429,12 +455,6 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         float y[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) y[r] = zero ? 0.f : fs[S::F_BETA + c] * L[(r0 + r) * S::L_PITCH + c];
-        float wgt[16];                                // e^{G_C - G} r of the rows
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const float4 g = *reinterpret_cast<const float4*>(fs + S::F_LAST + r0 + r), k = *reinterpret_cast<const float4*>(fs + S::F_R + r0 + r);
-          wgt[r] = k.x * exp2_fast(g.x); wgt[r + 1] = k.y * exp2_fast(g.y); wgt[r + 2] = k.z * exp2_fast(g.z); wgt[r + 3] = k.w * exp2_fast(g.w);
-        }
         __syncthreads();                              // the inverse is read, the operands take its place
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -442,8 +462,8 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int r = 8 * q + 2 * e;
-            const float w0 = wgt[r], w1 = wgt[r + 1];
-            split2_pair(w0 * y[r], w1 * y[r + 1], hi[e], lo[e]);
+            const float2 w = *reinterpret_cast<const float2*>(fs + S::F_LAST + r0 + r);
+            split2_pair(w.x * y[r], w.y * y[r + 1], hi[e], lo[e]);
             one[e] = bf16_pair(y[r], y[r + 1]);
           }
           unsigned char* at = bp + S::OFF_T + c * 128 + (((r0 / 8 + q) ^ (c & 7)) << 4);
