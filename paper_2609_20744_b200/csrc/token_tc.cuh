@@ -44,8 +44,18 @@ struct TokenTcArgs {
   unsigned char* e;          // [places * H] E_BYTES
   unsigned char* p;          // ... P_BYTES
   unsigned char* f;          // ... F_BYTES
-  long long places;
+  // long sequences in parts of `part` rows (0: whole); part x of head h has, at (x * H + h) d d,
+  int part;
+  float* enter;              // the state it starts from
+  float* comp_j;             // what it writes on its own: its last state from zero (the first part: from the sequence's first state)
+  float* comp_m;             // what it makes of an entering state: S -> S M
 };
+
+// Parts a sequence of `len` rows is cut into.  Two would gain nothing: composing the first and then running both takes as long as
+// one after the other.
+__host__ __device__ inline int token_parts(int len, int part) {
+  return part > 0 && len > 2 * part ? (len + part - 1) / part : 1;
+}
 
 // The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.  A whole
 // warp looks at 32 offsets at a time: a round trip to memory for 32 sequences, two for a thousand.
@@ -539,14 +549,24 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 }
 
 // ---------------------------------------------------------------------------------------------- chunk after chunk
-// One CTA per (sequence, head).  Everything is transposed: value channels are the rows (lanes) of tensor memory, so S, X
-// and O keep one row per thread and both factors a product needs from the previous one (the parts of S, the parts of X)
-// are written by the threads that own the rows, as A operands in tensor memory: nothing of the recurrence passes
-// through shared memory.  Roles: one thread feeds the loads (two stages, three groups of operands with their own
-// barriers), one issues the MMAs, sixteen warps own the state (four threads a row: 32 key channels each), four write out.
+// One CTA per (sequence, head), or per part of a long sequence.  Everything is transposed: value channels are the rows
+// (lanes) of tensor memory, so S, X and O keep one row per thread and both factors a product needs from the previous one
+// (the parts of S, the parts of X) are written by the threads that own the rows, as A operands in tensor memory: nothing of the
+// recurrence passes through shared memory.  Roles: one thread feeds the loads (two stages, three groups of operands with
+// their own barriers), one issues the MMAs, sixteen warps own the state (four threads a row: 32 key channels each), four
+// write out.
+//
+// Few long sequences would leave most SMs idle.  The rule is linear in the state, S_out = S_in M + J over any stretch, and the rows
+// of S go their own ways, so M is what the same recurrence makes of the rows of the identity when nothing is written
+// (V = 0).  A sequence is then cut into parts: TOKEN_COMPOSE runs all parts but the last side by side, from zero (J) and
+// from the identity (M); token_join_kernel passes the state along the parts; TOKEN_FULL runs all parts from the states they
+// enter with.  About three times the arithmetic, for a chain as short as the SMs allow.
+enum { TOKEN_FULL = 0, TOKEN_COMPOSE = 1 };
+
 struct TokenChain {
   static constexpr int STATE_WARPS = 16, OUT_WARPS = 4;
   static constexpr int THREADS = 64 + 32 * (STATE_WARPS + OUT_WARPS);
+  static constexpr int threads(int mode) { return mode == 0 ? THREADS : 64 + 32 * STATE_WARPS; }
   static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 90112;
   static constexpr int STAGE = 91136;
   static constexpr int OFF_O = 2 * STAGE;             // two tiles of results
@@ -556,6 +576,7 @@ struct TokenChain {
   static constexpr uint32_t S_HI = 0, S_LO = 64, DS = 128, D_K = 256, X_HI = 320, X_LO = 352, D_Q = 384, D_O = 448;
 };
 
+template <int MODE>
 __global__ void __launch_bounds__(TokenChain::THREADS, 1)
 token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ,
                    const __grid_constant__ CUtensorMap tmV, const TokenTcArgs a, tc::DevStatus ds) {
@@ -567,13 +588,36 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   unsigned char* bp = smem_dyn + (base - smem_u32(smem_dyn));
   const TokenArgs& t = a.t;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int h = (int)(blockIdx.x % t.H), seq = (int)(blockIdx.x / t.H);
-
+  constexpr bool WRITE = MODE == TOKEN_FULL;          // results are wanted
+  // this CTA's rows, first state and what becomes of its last one
+  int bid = (int)blockIdx.x;
+  bool from_identity = false;                         // TOKEN_COMPOSE: the half that makes M
+  if constexpr (MODE == TOKEN_COMPOSE) { from_identity = bid & 1; bid >>= 1; }
+  const int h = bid % t.H, x = bid / t.H;
+  const int seq = a.part > 0 ? token_seq_of(t, x, a.part) : x;
   long long start;
   int len;
   token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
+  const int parts = token_parts(len, a.part);
+  const int pos = a.part > 0 ? x - ((int)(start / a.part) + seq) : 0;
+  if (pos < 0 || pos >= parts) return;                // a place that no part has
+  const float* first = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) : nullptr;
+  float* last = nullptr;
+  const size_t comp = ((size_t)x * t.H + h) * (D * D);
+  if constexpr (MODE == TOKEN_COMPOSE) {
+    if (pos + 1 == parts || (from_identity && pos == 0)) return;   // nobody asks for these
+    if (pos > 0) first = nullptr;
+    last = (from_identity ? a.comp_m : a.comp_j) + comp;
+  } else {
+    if (parts > 1) first = a.enter + comp;
+    if (pos + 1 == parts && t.state_out) last = t.state_out + ((size_t)seq * t.H + h) * (D * D);
+  }
+  const long long place0 = start / C + seq + (long long)pos * (a.part / C);
+  if (parts > 1) {
+    start += (long long)pos * a.part;
+    len = min(a.part, len - pos * a.part);
+  }
   const int steps = (len + C - 1) / C;
-  const long long place0 = start / C + seq;
 
   const uint32_t bar0 = base + S::OFF_BAR;
   enum { KQ = 0, V = 1, E = 2 };
@@ -591,7 +635,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (int st = 0; st < 2; ++st) {
       for (int g = 0; g < 3; ++g) {
         mbar_init(FULL(g, st), 1);
-        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + S::OUT_WARPS : 1);
+        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + (WRITE ? S::OUT_WARPS : 0) : 1);
       }
     }
     mbar_init(S_READY, S::STATE_WARPS);
@@ -622,21 +666,23 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint32_t at = base + st * S::STAGE, par = ((s >> 1) & 1) ^ 1;
         const size_t unit = (size_t)(place0 + s) * t.H + h;
         if (s >= 2 && !(ok = mbar_wait(FREE(KQ, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(KQ, st), 32768);
+        mbar_arrive_expect_tx(FULL(KQ, st), WRITE ? 32768 : 16384);
         tma_load_2d(at + S::OFF_K, &tmK, FULL(KQ, st), hk * 128, row);
         tma_load_2d(at + S::OFF_K + 8192, &tmK, FULL(KQ, st), hk * 128 + 64, row);
-        tma_load_2d(at + S::OFF_Q, &tmQ, FULL(KQ, st), hk * 128, row);
-        tma_load_2d(at + S::OFF_Q + 8192, &tmQ, FULL(KQ, st), hk * 128 + 64, row);
+        if constexpr (WRITE) {
+          tma_load_2d(at + S::OFF_Q, &tmQ, FULL(KQ, st), hk * 128, row);
+          tma_load_2d(at + S::OFF_Q + 8192, &tmQ, FULL(KQ, st), hk * 128 + 64, row);
+        }
         issued[KQ] = s + 1;
         if (s >= 2 && !(ok = mbar_wait(FREE(V, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(V, st), 16384 + TokenTc::F_BYTES);
-        tma_load_2d(at + S::OFF_V, &tmV, FULL(V, st), h * 128, row);
+        mbar_arrive_expect_tx(FULL(V, st), (from_identity ? 0 : 16384) + TokenTc::F_BYTES);
+        if (!from_identity) tma_load_2d(at + S::OFF_V, &tmV, FULL(V, st), h * 128, row);
         bulk_load(at + S::OFF_F, a.f + unit * TokenTc::F_BYTES, TokenTc::F_BYTES, FULL(V, st));
         issued[V] = s + 1;
         if (s >= 2 && !(ok = mbar_wait(FREE(E, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(E, st), TokenTc::E_BYTES + TokenTc::P_BYTES);
+        mbar_arrive_expect_tx(FULL(E, st), TokenTc::E_BYTES + (WRITE ? TokenTc::P_BYTES : 0));
         bulk_load(at + S::OFF_E, a.e + unit * TokenTc::E_BYTES, TokenTc::E_BYTES, FULL(E, st));
-        bulk_load(at + S::OFF_P, a.p + unit * TokenTc::P_BYTES, TokenTc::P_BYTES, FULL(E, st));
+        if constexpr (WRITE) bulk_load(at + S::OFF_P, a.p + unit * TokenTc::P_BYTES, TokenTc::P_BYTES, FULL(E, st));
         issued[E] = s + 1;
       }
       // Whoever gives up, and when: copies in flight get a bounded chance to land before the CTA retires.
@@ -664,13 +710,15 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int k = 0; k < 8; ++k)
           mma_bf16_ts(tmem + S::D_K, tmem + S::S_HI + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
         mma_commit(DK_FULL);
-        if (s > 0) {
-          if (!mbar_wait(O_FREE, (s - 1) & 1, wc)) break;
-          tc_fence_after_sync();
-        }
+        if constexpr (WRITE) {
+          if (s > 0) {
+            if (!mbar_wait(O_FREE, (s - 1) & 1, wc)) break;
+            tc_fence_after_sync();
+          }
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+          for (int k = 0; k < 8; ++k)
+            mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+        }
         mma_commit(FREE(KQ, st));
         if (!mbar_wait(FULL(E, st), par, wc) || !mbar_wait(X_READY, s & 1, wc)) break;
         tc_fence_after_sync();
@@ -683,9 +731,11 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
         for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + k * 2, id128, 1u);
         mma_commit(DS_FULL);
+        if constexpr (WRITE) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp + k * 2, id64, k ? 1u : 0u);
-        mma_commit(DO_FULL);
+          for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp + k * 2, id64, k ? 1u : 0u);
+          mma_commit(DO_FULL);
+        }
         mma_commit(FREE(E, st));
       }
     }
@@ -696,11 +746,15 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
     float sv[32];                                     // S[row][32 sl ..]
     {
-      const float* src = t.state_in ? t.state_in + (((size_t)seq * t.H + h) * D + row) * D + sl * 32 : nullptr;
+      const float* src = first ? first + (size_t)row * D + sl * 32 : nullptr;
 #pragma unroll
       for (int e = 0; e < 32; e += 4) {
         const float4 x = src ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
         sv[e] = x.x; sv[e + 1] = x.y; sv[e + 2] = x.z; sv[e + 3] = x.w;
+      }
+      if (from_identity) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sv[e] = sl * 32 + e == row ? 1.f : 0.f;
       }
     }
     auto publish = [&]() {
@@ -728,7 +782,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F);
       uint32_t vv[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vv[j] = (uint32_t)v[2 * j * D] | ((uint32_t)v[(2 * j + 1) * D] << 16);
+      for (int j = 0; j < 8; ++j) vv[j] = from_identity ? 0u : (uint32_t)v[2 * j * D] | ((uint32_t)v[(2 * j + 1) * D] << 16);
       const float whole = f[128];
       if (!warp_wait(DK_FULL, s & 1)) break;
       tc_fence_after_sync();
@@ -773,12 +827,12 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       for (int e = 0; e < 32; ++e) sv[e] = fmaf(whole, sv[e], d[e]);
       if (s + 1 < steps) publish();
     }
-    if (t.state_out) {
-      float* dst = t.state_out + (((size_t)seq * t.H + h) * D + row) * D + sl * 32;
+    if (last) {
+      float* dst = last + (size_t)row * D + sl * 32;
 #pragma unroll
       for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(sv[e], sv[e + 1], sv[e + 2], sv[e + 3]);
     }
-  } else {
+  } else if constexpr (WRITE) {
     // ------------------------------------------------------------------ output
     // Lanes are value channels: the tile is turned round in shared memory and leaves as whole rows of 256 bytes.
     // (Stored from here, 64 bytes a warp and token, it took 3300 cycles a chunk and held up the MMAs.)
@@ -834,6 +888,54 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   if (warp == 1) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- part after part
+// The states the parts of a cut sequence enter with: enter_0 the first one, enter_1 = J_0, enter_{i+1} = enter_i M_i + J_i.  Rows
+// go their own ways: a CTA has 16 of a (sequence, head), four neighbouring columns of two rows a thread, plain fp32.
+struct TokenJoin {
+  static constexpr int THREADS = 256, ROWS = 16;
+};
+__global__ void __launch_bounds__(TokenJoin::THREADS) token_join_kernel(const TokenTcArgs a) {
+  constexpr int D = TokenTc::D, ROWS = TokenJoin::ROWS, GROUPS = D / ROWS;
+  __shared__ float sm[2][ROWS][D];
+  const TokenArgs& t = a.t;
+  const int r0 = (int)(blockIdx.x % GROUPS) * ROWS, h = (int)(blockIdx.x / GROUPS) % t.H, seq = (int)(blockIdx.x / GROUPS) / t.H;
+  long long start;
+  int len;
+  token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
+  const int parts = token_parts(len, a.part);
+  if (parts == 1) return;
+  const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D;
+  const int r = (int)(threadIdx.x >> 5) * 2, c = (int)(threadIdx.x & 31) * 4;
+  const size_t at = (x0 * t.H + h) * (D * D) + (size_t)(r0 + r) * D + c;
+  for (int i = 0; i < 2; ++i) {
+    const float* s0 = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) + (size_t)(r0 + r + i) * D + c : nullptr;
+    *reinterpret_cast<float4*>(a.enter + at + i * D) = s0 ? *reinterpret_cast<const float4*>(s0) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 j = *reinterpret_cast<const float4*>(a.comp_j + at + i * D);
+    *reinterpret_cast<float4*>(a.enter + at + step + i * D) = j;
+    *reinterpret_cast<float4*>(&sm[1][r + i][c]) = j;
+  }
+  for (int p = 1; p + 1 < parts; ++p) {
+    __syncthreads();
+    const float* m = a.comp_m + (x0 * t.H + h) * (D * D) + p * step + c;
+    float4 acc[2];
+    for (int i = 0; i < 2; ++i) acc[i] = *reinterpret_cast<const float4*>(a.comp_j + at + p * step + i * D);
+#pragma unroll 8
+    for (int k = 0; k < D; ++k) {
+      const float4 b = *reinterpret_cast<const float4*>(m + (size_t)k * D);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float s = sm[p & 1][r + i][k];
+        acc[i].x = fmaf(s, b.x, acc[i].x); acc[i].y = fmaf(s, b.y, acc[i].y);
+        acc[i].z = fmaf(s, b.z, acc[i].z); acc[i].w = fmaf(s, b.w, acc[i].w);
+      }
+    }
+    for (int i = 0; i < 2; ++i) {
+      *reinterpret_cast<float4*>(a.enter + at + (p + 1) * step + i * D) = acc[i];
+      *reinterpret_cast<float4*>(&sm[(p + 1) & 1][r + i][c]) = acc[i];
+    }
   }
 }
 

@@ -1262,19 +1262,38 @@ vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t 
   return VDN_OK;
 }
 
-// Workspace of the chunked rule: per (place, head) the chunk's two operators and its factors.
+// Workspace of the chunked rule: per (place, head) the chunk's two operators and its factors; per (part, head) of cut
+// sequences the state it enters with and its composite.
 struct TokenLayout {
-  long long places;
-  size_t e, p, f, total;
+  long long places, parts;
+  int part;                 // rows of a part; 0: no sequence is cut
+  size_t e, p, f, enter, comp_j, comp_m, total;
 };
-TokenLayout make_token_layout(long long n_tokens, int n_seqs, int heads) {
+TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs, int heads) {
+  constexpr int C = vdn::TokenTc::C;
   TokenLayout L;
-  L.places = n_tokens / vdn::TokenTc::C + n_seqs;
-  const size_t units = (size_t)L.places * heads;
+  L.places = n_tokens / C + n_seqs;
+  // A chain is a (sequence, head); fewer than a third of the SMs' number of chains, and cutting them pays: composing costs two
+  // more passes, side by side.  Parts as long as let all of them run at once, but not so short that passing the states along
+  // (about one step a part) weighs.  32760 tokens x 8 heads: FIXME whole, FIXME in 18 parts.
+  L.part = 0;
+  L.parts = n_seqs;
+  const long long per_head = h->sm_count / heads;
+  if (per_head - n_seqs >= 2) {
+    const long long rows = (n_tokens + C * (per_head - n_seqs) - 1) / (C * (per_head - n_seqs)) * C;
+    L.part = (int)(rows < 8 * C ? 8 * C : rows);
+    if (n_tokens <= 2LL * L.part) L.part = 0;
+    else L.parts = n_tokens / L.part + n_seqs;
+  }
+  const size_t units = (size_t)L.places * heads, state = (size_t)128 * 128 * sizeof(float);
   size_t off = 0;
   L.e = off; off += align_up(units * vdn::TokenTc::E_BYTES);
   L.p = off; off += align_up(units * vdn::TokenTc::P_BYTES);
   L.f = off; off += align_up(units * vdn::TokenTc::F_BYTES);
+  const size_t states = L.part ? (size_t)L.parts * heads * state : 0;
+  L.enter = off; off += states;
+  L.comp_j = off; off += states;
+  L.comp_m = off; off += states;
   L.total = off;
   return L;
 }
@@ -1302,11 +1321,14 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (!h->token_attrs_set) {
     VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_prep_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vdn::TokenPrep::SMEM_BYTES));
-    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vdn::TokenChain::SMEM_BYTES));
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel<vdn::TOKEN_FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     vdn::TokenChain::SMEM_BYTES));
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel<vdn::TOKEN_COMPOSE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     vdn::TokenChain::SMEM_BYTES));
     h->token_attrs_set = true;
   }
-  const TokenLayout L = make_token_layout(t.n_tokens, t.S, t.H);
-  if (L.places * t.H > 0x7fffffffLL || (long long)t.S * t.H > 0x7fffffffLL)
+  const TokenLayout L = make_token_layout(h, t.n_tokens, t.S, t.H);
+  if (L.places * t.H > 0x7fffffffLL || (long long)t.S * t.H * 8 > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (chunk, head) pairs for one call");
   CUtensorMap tmK, tmQ, tmV;
   const long long wk = (long long)t.Hk * 128, wv = (long long)t.H * 128;
@@ -1317,15 +1339,27 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   vdn::TokenTcArgs a;
   a.t = t;
   a.e = ws + L.e; a.p = ws + L.p; a.f = ws + L.f;
-  a.places = L.places;
+  a.part = L.part;
+  a.enter = reinterpret_cast<float*>(ws + L.enter);
+  a.comp_j = reinterpret_cast<float*>(ws + L.comp_j);
+  a.comp_m = reinterpret_cast<float*>(ws + L.comp_m);
+  using TC = vdn::TokenChain;
+  int nk = 0;
   prof_begin(h, st);
   vdn::token_prep_kernel<<<(unsigned)(L.places * t.H), vdn::TokenPrep::THREADS, vdn::TokenPrep::SMEM_BYTES, st>>>(
       tmK, tmQ, a, dev_status(h));
-  prof_mark(h, st, 0, "token_prep");
-  vdn::token_chain_kernel<<<(unsigned)(t.S * t.H), vdn::TokenChain::THREADS, vdn::TokenChain::SMEM_BYTES, st>>>(
+  prof_mark(h, st, nk++, "token_prep");
+  if (L.part) {
+    vdn::token_chain_kernel<vdn::TOKEN_COMPOSE><<<(unsigned)(2 * L.parts * t.H), TC::threads(vdn::TOKEN_COMPOSE), TC::SMEM_BYTES, st>>>(
+        tmK, tmQ, tmV, a, dev_status(h));
+    prof_mark(h, st, nk++, "token_compose");
+    vdn::token_join_kernel<<<(unsigned)(t.S * t.H * (128 / vdn::TokenJoin::ROWS)), vdn::TokenJoin::THREADS, 0, st>>>(a);
+    prof_mark(h, st, nk++, "token_join");
+  }
+  vdn::token_chain_kernel<vdn::TOKEN_FULL><<<(unsigned)(L.parts * t.H), TC::threads(vdn::TOKEN_FULL), TC::SMEM_BYTES, st>>>(
       tmK, tmQ, tmV, a, dev_status(h));
-  prof_mark(h, st, 1, "token_chain");
-  h->launches = 2;
+  prof_mark(h, st, nk++, "token_chain");
+  h->launches = nk;
   VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
 }
@@ -1342,7 +1376,7 @@ extern "C" {
 
 size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
   if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->n_seqs <= 0 || n_tokens < 0) return 0;
-  return token_on_tensor_cores(h, n_tokens, p->n_seqs) ? make_token_layout(n_tokens, p->n_seqs, p->heads).total : 0;
+  return token_on_tensor_cores(h, n_tokens, p->n_seqs) ? make_token_layout(h, n_tokens, p->n_seqs, p->heads).total : 0;
 }
 
 vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
