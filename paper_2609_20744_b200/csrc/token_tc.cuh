@@ -101,6 +101,20 @@ __device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* r) {
                : "memory");
 }
 
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const float* r) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(r);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
+               ::"r"(taddr), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3])
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float* r) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(r);
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7])
+               : "r"(taddr)
+               : "memory");
+}
+
 // D[tmem] (+)= A[tmem] * B[smem]: A has its rows in the lanes and two K elements to a 32-bit column.
 __device__ __forceinline__ void mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
                                             uint32_t accumulate) {
@@ -623,10 +637,11 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   enum { KQ = 0, V = 1, E = 2 };
   auto FULL = [&](int g, int st) { return bar0 + 8u * (g * 4 + st); };
   auto FREE = [&](int g, int st) { return bar0 + 8u * (g * 4 + 2 + st); };
-  const uint32_t S_READY = bar0 + 96, DK_FULL = bar0 + 104, X_READY = bar0 + 112, DS_FULL = bar0 + 120, DO_FULL = bar0 + 128,
-                 O_FREE = bar0 + 136;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 160);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 168);
+  // the parts of S and of X are handed over in two halves each: the MMAs on the first run while the second is formed
+  const uint32_t S_READY = bar0 + 96, X_READY = bar0 + 112, DK_FULL = bar0 + 128, DS_FULL = bar0 + 136, DO_FULL = bar0 + 144,
+                 O_FREE = bar0 + 152;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 168);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 176);
   const WaitCtx wc(abort_flag, ds);
   // a whole warp waits, and goes on or gives up together (tensor memory is accessed by whole warps)
   auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, wc)) != 0; };
@@ -638,8 +653,10 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + (WRITE ? S::OUT_WARPS : 0) : 1);
       }
     }
-    mbar_init(S_READY, S::STATE_WARPS);
-    mbar_init(X_READY, S::STATE_WARPS);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(S_READY + 8 * i, S::STATE_WARPS);
+      mbar_init(X_READY + 8 * i, S::STATE_WARPS);
+    }
     mbar_init(O_FREE, S::OUT_WARPS);
     mbar_init(DK_FULL, 1); mbar_init(DS_FULL, 1); mbar_init(DO_FULL, 1);
     *abort_flag = 0;
@@ -700,15 +717,20 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint32_t par = (s >> 1) & 1;
         const uint64_t off = st ? S::STAGE >> 4 : 0;
         const uint64_t dk = dk0 + off, dq = dq0 + off, de = de0 + off, dp = dp0 + off;
-        if (!mbar_wait(FULL(KQ, st), par, wc) || !mbar_wait(S_READY, s & 1, wc)) break;
-        tc_fence_after_sync();
-        // S K^T, small part first
+        if (!mbar_wait(FULL(KQ, st), par, wc)) break;
+        // S K^T: even steps of 16 key channels (the first half that the state warps hand over), then odd ones
+        bool ok = true;
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_bf16_ts(tmem + S::D_K, tmem + S::S_LO + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+        for (int half = 0; half < 2; ++half) {
+          if (!(ok = mbar_wait(S_READY + 8 * half, s & 1, wc))) break;
+          tc_fence_after_sync();
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_bf16_ts(tmem + S::D_K, tmem + S::S_HI + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
+          for (int k = half; k < 8; k += 2) {
+            mma_bf16_ts(tmem + S::D_K, tmem + S::S_LO + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+            mma_bf16_ts(tmem + S::D_K, tmem + S::S_HI + k * 8, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
+          }
+        }
+        if (!ok) break;
         mma_commit(DK_FULL);
         if constexpr (WRITE) {
           if (s > 0) {
@@ -720,16 +742,20 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
             mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
         }
         mma_commit(FREE(KQ, st));
-        if (!mbar_wait(FULL(E, st), par, wc) || !mbar_wait(X_READY, s & 1, wc)) break;
-        tc_fence_after_sync();
-        // X^T E^T: low X high E, high X low E, high X high E
+        if (!mbar_wait(FULL(E, st), par, wc)) break;
+        // X^T E^T, 32 tokens at a time: low X high E, high X low E, high X high E
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::DS, tmem + S::X_LO + k * 8, de + k * 2, id128, k ? 1u : 0u);
+        for (int half = 0; half < 2; ++half) {
+          if (!(ok = mbar_wait(X_READY + 8 * half, s & 1, wc))) break;
+          tc_fence_after_sync();
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + ((TokenTc::E_PART >> 4) + k * 2), id128, 1u);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + k * 2, id128, 1u);
+          for (int k = 2 * half; k < 2 * half + 2; ++k) {
+            mma_bf16_ts(tmem + S::DS, tmem + S::X_LO + k * 8, de + k * 2, id128, k ? 1u : 0u);
+            mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + ((TokenTc::E_PART >> 4) + k * 2), id128, 1u);
+            mma_bf16_ts(tmem + S::DS, tmem + S::X_HI + k * 8, de + k * 2, id128, 1u);
+          }
+        }
+        if (!ok) break;
         mma_commit(DS_FULL);
         if constexpr (WRITE) {
 #pragma unroll
@@ -757,80 +783,101 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         for (int e = 0; e < 32; ++e) sv[e] = sl * 32 + e == row ? 1.f : 0.f;
       }
     }
-    auto publish = [&]() {
-      float hi[16], lo[16];
+    // columns 16 half .. of the thread's 32: one K step of the product
+    auto publish = [&](int half) {
+      float hl[16];                                   // high words, then low words
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = 0; e < 8; ++e) {
         uint32_t u, v;
-        split2_pair(sv[2 * e], sv[2 * e + 1], u, v);
-        hi[e] = __uint_as_float(u);
-        lo[e] = __uint_as_float(v);
+        split2_pair(sv[16 * half + 2 * e], sv[16 * half + 2 * e + 1], u, v);
+        hl[e] = __uint_as_float(u);
+        hl[8 + e] = __uint_as_float(v);
       }
-      tmem_st16(tl + S::S_HI + sl * 16, hi);
-      tmem_st16(tl + S::S_LO + sl * 16, lo);
+      tmem_st8(tl + S::S_HI + sl * 16 + half * 8, hl);
+      tmem_st8(tl + S::S_LO + sl * 16 + half * 8, hl + 8);
       tmem_wait_st();
       tc_fence_before_sync();
-      mbar_arrive_warp(S_READY);
+      mbar_arrive_warp(S_READY + 8 * half);
     };
-    if (steps > 0) publish();
+    if (steps > 0) { publish(0); publish(1); }
     for (int s = 0; s < steps; ++s) {
       const int st = s & 1;
-      const int n = min(C, len - s * C) - sl * 16;    // tokens of this quarter that exist
-      // what does not depend on the products is fetched while they run: V (two tokens to a register) and the factors
+      const int n = min(C, len - s * C) - sl * 8;     // tokens from this warp's first on; it has 8 there and 8 half a chunk further on
+      // what does not depend on the products is fetched while they run: V, two tokens to a register
       if (!warp_wait(FULL(V, st), (s >> 1) & 1)) break;
-      const unsigned short* v = reinterpret_cast<const unsigned short*>(bp + st * S::STAGE + S::OFF_V) + sl * 16 * D + row;
+      const unsigned short* v = reinterpret_cast<const unsigned short*>(bp + st * S::STAGE + S::OFF_V) + sl * 8 * D + row;
       const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F);
       uint32_t vv[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vv[j] = from_identity ? 0u : (uint32_t)v[2 * j * D] | ((uint32_t)v[(2 * j + 1) * D] << 16);
+      for (int j = 0; j < 8; ++j) {
+        const int at = (j >> 2) * 32 + (j & 3) * 2;
+        vv[j] = from_identity ? 0u : (uint32_t)v[at * D] | ((uint32_t)v[(at + 1) * D] << 16);
+      }
       const float whole = f[128];
       if (!warp_wait(DK_FULL, s & 1)) break;
       tc_fence_after_sync();
       float x[16];
-      tmem_ld16(tl + S::D_K + sl * 16, x);
+      tmem_ld8(tl + S::D_K + sl * 8, x);
+      tmem_ld8(tl + S::D_K + 32 + sl * 8, x + 8);
       tmem_wait_ld();
 #pragma unroll
-      for (int j = 0; j < 16; j += 4) {
-        const float4 fj = *reinterpret_cast<const float4*>(f + sl * 16 + j);
-        x[j] = fmaf(-fj.x, x[j], __uint_as_float(vv[j / 2] << 16));
-        x[j + 1] = fmaf(-fj.y, x[j + 1], __uint_as_float(vv[j / 2] & 0xFFFF0000u));
-        x[j + 2] = fmaf(-fj.z, x[j + 2], __uint_as_float(vv[j / 2 + 1] << 16));
-        x[j + 3] = fmaf(-fj.w, x[j + 3], __uint_as_float(vv[j / 2 + 1] & 0xFFFF0000u));
-      }
-      if (n < 16) {                                   // rows behind the sequence: whatever they hold, X is zero there
+      for (int half = 0; half < 2; ++half) {
+        float hl[8];                                  // high words, then low words
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (j >= n) x[j] = 0.f;
-      }
-      {
-        float hl[16];                                 // high words, then low words
+        for (int j = 0; j < 8; j += 4) {
+          const float4 fj = *reinterpret_cast<const float4*>(f + half * 32 + sl * 8 + j);
+          float* y = x + half * 8 + j;
+          const uint32_t v01 = vv[half * 4 + j / 2], v23 = vv[half * 4 + j / 2 + 1];
+          y[0] = fmaf(-fj.x, y[0], __uint_as_float(v01 << 16));
+          y[1] = fmaf(-fj.y, y[1], __uint_as_float(v01 & 0xFFFF0000u));
+          y[2] = fmaf(-fj.z, y[2], __uint_as_float(v23 << 16));
+          y[3] = fmaf(-fj.w, y[3], __uint_as_float(v23 & 0xFFFF0000u));
+          if (n < 40) {                               // rows behind the sequence: whatever they hold, X is zero there
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          uint32_t u, w;
-          split2_pair(x[2 * j], x[2 * j + 1], u, w);
-          hl[j] = __uint_as_float(u);
-          hl[8 + j] = __uint_as_float(w);
+            for (int i = 0; i < 4; ++i)
+              if (half * 32 + j + i >= n) y[i] = 0.f;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            uint32_t u, w;
+            split2_pair(y[i], y[i + 1], u, w);
+            hl[(j + i) / 2] = __uint_as_float(u);
+            hl[4 + (j + i) / 2] = __uint_as_float(w);
+          }
         }
-        tmem_st8(tl + S::X_HI + sl * 8, hl);
-        tmem_st8(tl + S::X_LO + sl * 8, hl + 8);
+        tmem_st4(tl + S::X_HI + half * 16 + sl * 4, hl);
+        tmem_st4(tl + S::X_LO + half * 16 + sl * 4, hl + 4);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive_warp(X_READY + 8 * half);
       }
-      tmem_wait_st();
-      tc_fence_before_sync();
-      mbar_arrive_warp(X_READY);
       mbar_arrive_warp(FREE(V, st));
       if (!warp_wait(DS_FULL, s & 1)) break;
       tc_fence_after_sync();
-      float d[32];
-      tmem_ld32(tl + S::DS + sl * 32, d);
-      tmem_wait_ld();
 #pragma unroll
-      for (int e = 0; e < 32; ++e) sv[e] = fmaf(whole, sv[e], d[e]);
-      if (s + 1 < steps) publish();
+      for (int half = 0; half < 2; ++half) {
+        float d[16];
+        tmem_ld16(tl + S::DS + sl * 32 + half * 16, d);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sv[half * 16 + e] = fmaf(whole, sv[half * 16 + e], d[e]);
+        if (s + 1 < steps) publish(half);
+      }
     }
     if (last) {
-      float* dst = last + (size_t)row * D + sl * 32;
+      // rows leave whole: through shared memory (the loads of all steps have been used), 16-byte pieces in an order that keeps the
+      // banks apart.  Stored from the threads that own the rows, 512 bytes apart, it took 3 us.
 #pragma unroll
-      for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + e) = make_float4(sv[e], sv[e + 1], sv[e + 2], sv[e + 3]);
+      for (int e = 0; e < 8; ++e)
+        *reinterpret_cast<float4*>(bp + row * 512 + (((sl * 8 + e) ^ lane) << 4)) =
+            make_float4(sv[4 * e], sv[4 * e + 1], sv[4 * e + 2], sv[4 * e + 3]);
+      named_barrier_sync(1, 32 * S::STATE_WARPS);
+      const int tid = (warp - 2) * 32 + lane;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int r = (tid >> 5) + 16 * e;
+        *reinterpret_cast<float4*>(last + (size_t)r * D + lane * 4) = *reinterpret_cast<const float4*>(bp + r * 512 + ((lane ^ (r & 31)) << 4));
+      }
     }
   } else if constexpr (WRITE) {
     // ------------------------------------------------------------------ output
@@ -850,13 +897,13 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         tc_fence_after_sync();
         unsigned short* col = reinterpret_cast<unsigned short*>(tile) + qd * 32 + lane;
 #pragma unroll 1
-        for (int jb = 0; jb < 64; jb += 16) {
-          float x[16], y[16];
-          tmem_ld16(tl + S::D_Q + jb, x);
-          tmem_ld16(tl + S::D_O + jb, y);
+        for (int jb = 0; jb < 64; jb += 32) {
+          float x[32], y[32];
+          tmem_ld32(tl + S::D_Q + jb, x);
+          tmem_ld32(tl + S::D_O + jb, y);
           tmem_wait_ld();
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) {
+          for (int j = 0; j < 32; j += 4) {
             const float4 e = *reinterpret_cast<const float4*>(f + jb + j);
             const uint32_t p = bf16_pair(fmaf(e.x, x[j], y[j]), fmaf(e.y, x[j + 1], y[j + 1]));
             const uint32_t q = bf16_pair(fmaf(e.z, x[j + 2], y[j + 2]), fmaf(e.w, x[j + 3], y[j + 3]));
@@ -893,13 +940,16 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 
 // ---------------------------------------------------------------------------------------------- part after part
 // The states the parts of a cut sequence enter with: enter_0 the first one, enter_1 = J_0, enter_{i+1} = enter_i M_i + J_i.  Rows
-// go their own ways: a CTA has 16 of a (sequence, head), four neighbouring columns of two rows a thread, plain fp32.
+// go their own ways: a CTA has 8 of a (sequence, head).  Its eight warps divide M's rows, 16 each, so that each element of M is
+// fetched once, into registers and a part ahead of its use; their partial products are added through shared memory.  Plain
+// fp32.  Bound by the chain of parts.
 struct TokenJoin {
-  static constexpr int THREADS = 256, ROWS = 16;
+  static constexpr int THREADS = 256, ROWS = 8;
 };
 __global__ void __launch_bounds__(TokenJoin::THREADS) token_join_kernel(const TokenTcArgs a) {
   constexpr int D = TokenTc::D, ROWS = TokenJoin::ROWS, GROUPS = D / ROWS;
-  __shared__ float sm[2][ROWS][D];
+  __shared__ float sm[ROWS][D];                       // the state's rows
+  __shared__ float4 partial[8][ROWS][32];
   const TokenArgs& t = a.t;
   const int r0 = (int)(blockIdx.x % GROUPS) * ROWS, h = (int)(blockIdx.x / GROUPS) % t.H, seq = (int)(blockIdx.x / GROUPS) / t.H;
   long long start;
@@ -907,35 +957,54 @@ __global__ void __launch_bounds__(TokenJoin::THREADS) token_join_kernel(const To
   token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
   const int parts = token_parts(len, a.part);
   if (parts == 1) return;
-  const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D;
-  const int r = (int)(threadIdx.x >> 5) * 2, c = (int)(threadIdx.x & 31) * 4;
-  const size_t at = (x0 * t.H + h) * (D * D) + (size_t)(r0 + r) * D + c;
-  for (int i = 0; i < 2; ++i) {
-    const float* s0 = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) + (size_t)(r0 + r + i) * D + c : nullptr;
-    *reinterpret_cast<float4*>(a.enter + at + i * D) = s0 ? *reinterpret_cast<const float4*>(s0) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 j = *reinterpret_cast<const float4*>(a.comp_j + at + i * D);
-    *reinterpret_cast<float4*>(a.enter + at + step + i * D) = j;
-    *reinterpret_cast<float4*>(&sm[1][r + i][c]) = j;
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D, base = (x0 * t.H + h) * (D * D);
+  // the thread's own four elements of the state: row r0 + warp, columns 4 lane ..
+  const size_t own = base + (size_t)(r0 + warp) * D + lane * 4;
+  const float* mp = a.comp_m + base + (size_t)(warp * 16) * D + lane * 4;
+  {
+    const float* s0 = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) + (size_t)(r0 + warp) * D + lane * 4 : nullptr;
+    *reinterpret_cast<float4*>(a.enter + own) = s0 ? *reinterpret_cast<const float4*>(s0) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 j = *reinterpret_cast<const float4*>(a.comp_j + own);
+    *reinterpret_cast<float4*>(a.enter + own + step) = j;
+    *reinterpret_cast<float4*>(&sm[warp][lane * 4]) = j;
   }
-  for (int p = 1; p + 1 < parts; ++p) {
-    __syncthreads();
-    const float* m = a.comp_m + (x0 * t.H + h) * (D * D) + p * step + c;
-    float4 acc[2];
-    for (int i = 0; i < 2; ++i) acc[i] = *reinterpret_cast<const float4*>(a.comp_j + at + p * step + i * D);
-#pragma unroll 8
-    for (int k = 0; k < D; ++k) {
-      const float4 b = *reinterpret_cast<const float4*>(m + (size_t)k * D);
+  float4 m[16], next[16], j = make_float4(0.f, 0.f, 0.f, 0.f), jn = j;
+  auto fetch = [&](int p) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float s = sm[p & 1][r + i][k];
-        acc[i].x = fmaf(s, b.x, acc[i].x); acc[i].y = fmaf(s, b.y, acc[i].y);
-        acc[i].z = fmaf(s, b.z, acc[i].z); acc[i].w = fmaf(s, b.w, acc[i].w);
+    for (int k = 0; k < 16; ++k) next[k] = __ldg(reinterpret_cast<const float4*>(mp + p * step + (size_t)k * D));
+    jn = __ldg(reinterpret_cast<const float4*>(a.comp_j + own + p * step));
+  };
+  if (parts > 2) fetch(1);
+  for (int p = 1; p + 1 < parts; ++p) {
+#pragma unroll
+    for (int k = 0; k < 16; ++k) m[k] = next[k];
+    j = jn;
+    if (p + 2 < parts) fetch(p + 1);
+    __syncthreads();                                  // the state is there
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 16; k += 4) {
+        const float4 s = *reinterpret_cast<const float4*>(&sm[r][warp * 16 + k]);
+        const float s4[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc.x = fmaf(s4[e], m[k + e].x, acc.x); acc.y = fmaf(s4[e], m[k + e].y, acc.y);
+          acc.z = fmaf(s4[e], m[k + e].z, acc.z); acc.w = fmaf(s4[e], m[k + e].w, acc.w);
+        }
       }
+      partial[warp][r][lane] = acc;
     }
-    for (int i = 0; i < 2; ++i) {
-      *reinterpret_cast<float4*>(a.enter + at + (p + 1) * step + i * D) = acc[i];
-      *reinterpret_cast<float4*>(&sm[(p + 1) & 1][r + i][c]) = acc[i];
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float4 q = partial[w][warp][lane];
+      j.x += q.x; j.y += q.y; j.z += q.z; j.w += q.w;
     }
+    *reinterpret_cast<float4*>(a.enter + own + (p + 1) * step) = j;
+    *reinterpret_cast<float4*>(&sm[warp][lane * 4]) = j;
   }
 }
 
