@@ -567,8 +567,8 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // (lanes) of tensor memory, so S, X and O keep one row per thread and both factors a product needs from the previous one
 // (the parts of S, the parts of X) are written by the threads that own the rows, as A operands in tensor memory: nothing of the
 // recurrence passes through shared memory.  Roles: one thread feeds the loads (two stages, three groups of operands with
-// their own barriers), one issues the MMAs, sixteen warps own the state (four threads a row: 32 key channels each), four
-// write out.
+// their own barriers), one issues the MMAs of the recurrence and one those of the results, sixteen warps own the state (four
+// threads a row: 32 key channels each), four write out.
 //
 // Few long sequences would leave most SMs idle.  The rule is linear in the state, S_out = S_in M + J over any stretch, and the rows
 // of S go their own ways, so M is what the same recurrence makes of the rows of the identity when nothing is written
@@ -579,7 +579,8 @@ enum { TOKEN_FULL = 0, TOKEN_COMPOSE = 1 };
 
 struct TokenChain {
   static constexpr int STATE_WARPS = 16, OUT_WARPS = 4;
-  static constexpr int THREADS = 64 + 32 * (STATE_WARPS + OUT_WARPS);
+  static constexpr int RESULT_WARP = 2 + STATE_WARPS + OUT_WARPS;
+  static constexpr int THREADS = 32 * (RESULT_WARP + 1);
   static constexpr int threads(int mode) { return mode == 0 ? THREADS : 64 + 32 * STATE_WARPS; }
   static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 90112;
   static constexpr int STAGE = 91136;
@@ -639,7 +640,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   auto FREE = [&](int g, int st) { return bar0 + 8u * (g * 4 + 2 + st); };
   // the parts of S and of X are handed over in two halves each: the MMAs on the first run while the second is formed
   const uint32_t S_READY = bar0 + 96, X_READY = bar0 + 112, DK_FULL = bar0 + 128, DS_FULL = bar0 + 136, DO_FULL = bar0 + 144,
-                 O_FREE = bar0 + 152;
+                 O_FREE = bar0 + 152, S_FREE = bar0 + 160;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 168);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 176);
   const WaitCtx wc(abort_flag, ds);
@@ -650,7 +651,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (int st = 0; st < 2; ++st) {
       for (int g = 0; g < 3; ++g) {
         mbar_init(FULL(g, st), 1);
-        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + (WRITE ? S::OUT_WARPS : 0) : 1);
+        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + (WRITE ? S::OUT_WARPS : 0) : g == E && WRITE ? 2 : 1);
       }
     }
     for (int i = 0; i < 2; ++i) {
@@ -658,7 +659,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       mbar_init(X_READY + 8 * i, S::STATE_WARPS);
     }
     mbar_init(O_FREE, S::OUT_WARPS);
-    mbar_init(DK_FULL, 1); mbar_init(DS_FULL, 1); mbar_init(DO_FULL, 1);
+    mbar_init(S_FREE, 1); mbar_init(DK_FULL, 1); mbar_init(DS_FULL, 1); mbar_init(DO_FULL, 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmQ); tma_prefetch_desc(&tmV);
@@ -706,17 +707,16 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       for (int g = 0; g < 3; ++g) mbar_drain_ring(FULL(g, 0), 2, issued[g]);
     }
   } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMA issuer
+    // ------------------------------------------------------------------ MMAs of the recurrence
     if (lane == 0) {
       constexpr uint32_t id64 = make_idesc_bf16(128, 64, false, false), id128 = make_idesc_bf16(128, 128, false, false);
       // descriptors of the first stage; one step along K is 32 bytes, the other 64 channels a box further on
-      const uint64_t dk0 = make_smem_desc(base + S::OFF_K, 16, 1024), dq0 = make_smem_desc(base + S::OFF_Q, 16, 1024);
-      const uint64_t de0 = make_smem_desc(base + S::OFF_E, 16, 1024), dp0 = make_smem_desc(base + S::OFF_P, 16, 1024);
+      const uint64_t dk0 = make_smem_desc(base + S::OFF_K, 16, 1024), de0 = make_smem_desc(base + S::OFF_E, 16, 1024);
       for (int s = 0; s < steps; ++s) {
         const int st = s & 1;
         const uint32_t par = (s >> 1) & 1;
         const uint64_t off = st ? S::STAGE >> 4 : 0;
-        const uint64_t dk = dk0 + off, dq = dq0 + off, de = de0 + off, dp = dp0 + off;
+        const uint64_t dk = dk0 + off, de = de0 + off;
         if (!mbar_wait(FULL(KQ, st), par, wc)) break;
         // S K^T: even steps of 16 key channels (the first half that the state warps hand over), then odd ones
         bool ok = true;
@@ -732,16 +732,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         }
         if (!ok) break;
         mma_commit(DK_FULL);
-        if constexpr (WRITE) {
-          if (s > 0) {
-            if (!mbar_wait(O_FREE, (s - 1) & 1, wc)) break;
-            tc_fence_after_sync();
-          }
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
-        }
-        mma_commit(FREE(KQ, st));
+        if constexpr (!WRITE) mma_commit(FREE(KQ, st));
         if (!mbar_wait(FULL(E, st), par, wc)) break;
         // X^T E^T, 32 tokens at a time: low X high E, high X low E, high X high E
 #pragma unroll
@@ -757,11 +748,6 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         }
         if (!ok) break;
         mma_commit(DS_FULL);
-        if constexpr (WRITE) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp + k * 2, id64, k ? 1u : 0u);
-          mma_commit(DO_FULL);
-        }
         mma_commit(FREE(E, st));
       }
     }
@@ -854,6 +840,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       mbar_arrive_warp(FREE(V, st));
       if (!warp_wait(DS_FULL, s & 1)) break;
       tc_fence_after_sync();
+      bool ok = true;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         float d[16];
@@ -861,12 +848,17 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         tmem_wait_ld();
 #pragma unroll
         for (int e = 0; e < 16; ++e) sv[half * 16 + e] = fmaf(whole, sv[half * 16 + e], d[e]);
+        if (WRITE && half == 0) {                     // S Q^T is done with the old parts of S (and, at the end, with Q's memory)
+          if (!(ok = warp_wait(S_FREE, s & 1))) break;
+          tc_fence_after_sync();
+        }
         if (s + 1 < steps) publish(half);
       }
+      if (!ok) break;
     }
     if (last) {
-      // rows leave whole: through shared memory (the loads of all steps have been used), 16-byte pieces in an order that keeps the
-      // banks apart.  Stored from the threads that own the rows, 512 bytes apart, it took 3 us.
+      // rows leave whole: through shared memory (the first stage's keys, queries, values and part of E, which no product reads
+      // any more), 16-byte pieces in an order that keeps the banks apart.  Stored from the threads that own the rows, 512 bytes apart, it took 3 us.
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         *reinterpret_cast<float4*>(bp + row * 512 + (((sl * 8 + e) ^ lane) << 4)) =
@@ -879,23 +871,50 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         *reinterpret_cast<float4*>(last + (size_t)r * D + lane * 4) = *reinterpret_cast<const float4*>(bp + r * 512 + ((lane ^ (r & 31)) << 4));
       }
     }
+  } else if (WRITE && warp == S::RESULT_WARP) {
+    // ------------------------------------------------------------------ MMAs of the results
+    // Their own issuer: in the gaps that the recurrence leaves, and what they wait for (the accumulators being read) does not
+    // hold the recurrence up.
+    if (lane == 0) {
+      constexpr uint32_t id64 = make_idesc_bf16(128, 64, false, false);
+      const uint64_t dq0 = make_smem_desc(base + S::OFF_Q, 16, 1024), dp0 = make_smem_desc(base + S::OFF_P, 16, 1024);
+      for (int s = 0; s < steps; ++s) {
+        const int st = s & 1;
+        const uint64_t off = st ? S::STAGE >> 4 : 0;
+        // (DK_FULL: the keys, the queries and the parts of S are there, and the keys have been used)
+        if (!mbar_wait(DK_FULL, s & 1, wc) || (s > 0 && !mbar_wait(O_FREE, (s - 1) & 1, wc))) break;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq0 + off + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+        mma_commit(S_FREE);
+        mma_commit(FREE(KQ, st));
+        if (!mbar_wait(FULL(E, st), (s >> 1) & 1, wc) || !mbar_wait(X_READY, s & 1, wc) || !mbar_wait(X_READY + 8, s & 1, wc)) break;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp0 + off + k * 2, id64, k ? 1u : 0u);
+        mma_commit(DO_FULL);
+        mma_commit(FREE(E, st));
+      }
+    }
   } else if constexpr (WRITE) {
     // ------------------------------------------------------------------ output
     // Lanes are value channels: the tile is turned round in shared memory and leaves as whole rows of 256 bytes.
     // (Stored from here, 64 bytes a warp and token, it took 3300 cycles a chunk and held up the MMAs.)
     const int qd = warp & 3, tid = (warp - 2 - S::STATE_WARPS) * 32 + lane;
     const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
-    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(t.out) + (start + (tid >> 4)) * t.out_stride + h * D + (tid & 15) * 8;
+    __nv_bfloat16* out = static_cast<__nv_bfloat16*>(t.out) + (start + 2 * (tid >> 4)) * t.out_stride + h * D + (tid & 15) * 8;
     for (int s = 0; s < steps; ++s) {
       const int st = s & 1;
       const int n = min(C, len - s * C);
       const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F) + 64;
       unsigned char* tile = bp + S::OFF_O + st * 16384;
-      // (the MMAs of S Q^T come before those of X^T P^T, one barrier says that both are there)
+      // (one thread issues S Q^T, then X^T P^T: one barrier says that both are there)
       const bool ok = warp_wait(FULL(V, st), (s >> 1) & 1) && warp_wait(DO_FULL, s & 1);
       if (ok) {
         tc_fence_after_sync();
-        unsigned short* col = reinterpret_cast<unsigned short*>(tile) + qd * 32 + lane;
+        // two tokens to a word: [token / 2][channel]
+        uint32_t* col = reinterpret_cast<uint32_t*>(tile) + qd * 32 + lane;
 #pragma unroll 1
         for (int jb = 0; jb < 64; jb += 32) {
           float x[32], y[32];
@@ -905,12 +924,8 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
           for (int j = 0; j < 32; j += 4) {
             const float4 e = *reinterpret_cast<const float4*>(f + jb + j);
-            const uint32_t p = bf16_pair(fmaf(e.x, x[j], y[j]), fmaf(e.y, x[j + 1], y[j + 1]));
-            const uint32_t q = bf16_pair(fmaf(e.z, x[j + 2], y[j + 2]), fmaf(e.w, x[j + 3], y[j + 3]));
-            col[(jb + j) * D] = (unsigned short)p;
-            col[(jb + j + 1) * D] = (unsigned short)(p >> 16);
-            col[(jb + j + 2) * D] = (unsigned short)q;
-            col[(jb + j + 3) * D] = (unsigned short)(q >> 16);
+            col[(jb + j) / 2 * D] = bf16_pair(fmaf(e.x, x[j], y[j]), fmaf(e.y, x[j + 1], y[j + 1]));
+            col[((jb + j) / 2 + 1) * D] = bf16_pair(fmaf(e.z, x[j + 2], y[j + 2]), fmaf(e.w, x[j + 3], y[j + 3]));
           }
         }
         tc_fence_before_sync();
@@ -920,9 +935,17 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       if (named_barrier_or(2, 32 * S::OUT_WARPS, !ok)) break;
       // two tiles in turn: the next barrier comes after these reads, the next write to this tile after that
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const int j = (tid >> 4) + 8 * r;
-        if (j < n) *reinterpret_cast<uint4*>(out + 8 * r * t.out_stride) = *reinterpret_cast<const uint4*>(tile + j * 256 + (tid & 15) * 16);
+      for (int r = 0; r < 4; ++r) {
+        const int pair = (tid >> 4) + 8 * r;
+        const uint4* w = reinterpret_cast<const uint4*>(tile + pair * 512 + (tid & 15) * 32);
+        const uint4 u = w[0], v = w[1];
+        __nv_bfloat16* dst = out + 16 * r * t.out_stride;
+        if (2 * pair < n)
+          *reinterpret_cast<uint4*>(dst) = make_uint4(__byte_perm(u.x, u.y, 0x5410), __byte_perm(u.z, u.w, 0x5410),
+                                                      __byte_perm(v.x, v.y, 0x5410), __byte_perm(v.z, v.w, 0x5410));
+        if (2 * pair + 1 < n)
+          *reinterpret_cast<uint4*>(dst + t.out_stride) = make_uint4(__byte_perm(u.x, u.y, 0x7632), __byte_perm(u.z, u.w, 0x7632),
+                                                                     __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x7632));
       }
       out += C * t.out_stride;
     }
