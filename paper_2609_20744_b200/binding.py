@@ -75,6 +75,9 @@ class VdnRotaryParams(ctypes.Structure):
                 ("k_out_stride", ctypes.c_int64)]
 
 
+_TOKEN_PARAMS_SIZE, _ROTARY_PARAMS_SIZE = ctypes.sizeof(VdnTokenParams), ctypes.sizeof(VdnRotaryParams)
+
+
 class VdnError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"{STATUS_NAMES.get(status, status)}: {msg}")
@@ -273,6 +276,18 @@ def _require_rows(name, x, lead, heads, d, dtype, on_cuda, device_index):
     return step
 
 
+def _rows(name, x, shape, dtype, device, on_cuda, device_index):
+    """_require_rows for a tensor that in all likelihood is dense and right: one glance, the words only if it is not."""
+    if x is not None and x.shape == shape and x.dtype is dtype and x.device == device and x.is_contiguous():
+        return shape[-2] * shape[-1]
+    return _require_rows(name, x, shape[:-2], shape[-2], shape[-1], dtype, on_cuda, device_index)
+
+
+def _dense(name, x, shape, dtype, device, on_cuda, device_index):
+    if x is None or x.shape != shape or x.dtype is not dtype or x.device != device or not x.is_contiguous():
+        _require(name, x, shape, dtype, on_cuda, device_index)
+
+
 def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=None, log_alpha=None, on_cuda=True):
     """Checks the token tensors of token_scan / token_step: q, k [..., Hk, d], v, out [..., H, d], beta, log_alpha [..., H].
     Returns (leading shape, H, Hk, strides of q, k, v, out)."""
@@ -281,17 +296,19 @@ def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=Non
         raise ValueError("v must have shape [tokens, heads, d]")
     if q is None or q.dim() != v.dim():
         raise ValueError("q must have as many dimensions as v")
-    lead, H, Hk, d = tuple(int(n) for n in v.shape[:-2]), int(v.shape[-2]), int(q.shape[-2]), int(v.shape[-1])
+    vs = tuple(v.shape)
+    lead, H, Hk, d = vs[:-2], vs[-2], q.shape[-2], vs[-1]
     if d != d_handle:
         raise ValueError(f"v must have head dimension {d_handle}, got {d}")
     if H == 0 or Hk == 0 or H % Hk:
         raise ValueError(f"q must have a number of heads that divides the {H} of v, got {Hk}")
-    strides = [_require_rows(n, x, lead, c, d, io_dtype, on_cuda, device_index)
-               for n, x, c in (("q", q, Hk), ("k", k, Hk), ("v", v, H))]
-    _require("beta", beta, (*lead, H), torch.float32, on_cuda, device_index)
+    dev = torch.device("cuda", device_index) if on_cuda else v.device
+    ks, f32, rest = (*lead, Hk, d), torch.float32, (dev, on_cuda, device_index)
+    strides = [_rows("q", q, ks, io_dtype, *rest), _rows("k", k, ks, io_dtype, *rest), _rows("v", v, vs, io_dtype, *rest),
+               H * d if out is None else _rows("out", out, vs, io_dtype, *rest)]
+    _dense("beta", beta, (*lead, H), f32, *rest)
     if log_alpha is not None:
-        _require("log_alpha", log_alpha, (*lead, H), torch.float32, on_cuda, device_index)
-    strides.append(H * d if out is None else _require_rows("out", out, lead, H, d, io_dtype, on_cuda, device_index))
+        _dense("log_alpha", log_alpha, (*lead, H), f32, *rest)
     return lead, H, Hk, strides
 
 
@@ -434,16 +451,22 @@ class Vda:
         return qo, ko, vo
 
     # -- token-wise rule, rotary positions ----------------------------------------------------
-    def _new(self, stream, make):
-        """Memory made for a call that runs on `stream`: taken on that stream, so that the allocator does not hand it on
-        while the call still runs; what the caller gets back is also marked as in use on the current stream."""
+    def _streams(self, stream):
+        """(current stream, stream of the call, its handle)."""
+        here = self._torch.cuda.current_stream(self.device)
+        on = here if stream is None else stream
+        return here, on, on.cuda_stream
+
+    def _new(self, streams, *shape, dtype):
+        """Memory made for a call: taken on the call's stream, so that the allocator does not hand it on while the call still
+        runs; where that is not the current stream, what the caller gets back is marked as in use there too."""
         torch = self._torch
-        here = torch.cuda.current_stream(self.device)
-        if stream is None or stream == here:
-            with torch.cuda.device(self.device):
-                return make()
-        with torch.cuda.stream(stream):
-            x = make()
+        here, on, raw = streams
+        dev = torch.device("cuda", self.device)
+        if raw == here.cuda_stream:
+            return torch.empty(shape, dtype=dtype, device=dev)
+        with torch.cuda.stream(on):
+            x = torch.empty(shape, dtype=dtype, device=dev)
         x.record_stream(here)
         return x
 
@@ -460,27 +483,32 @@ class Vda:
         lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
         if len(lead) != 1:
             raise ValueError("v must have shape [tokens, heads, d]")
-        n, d, S = lead[0], self.d, 1
+        n, d, S, dev = lead[0], self.d, 1, v.device
         if cu_seqlens is not None:
             if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
                 raise ValueError("cu_seqlens must have shape [sequences + 1]")
-            S = int(cu_seqlens.numel()) - 1
-            _require("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, True, self.device)
-        for name, x in (("s0", s0), ("state", state)):
-            if x is not None:
-                _require(name, x, (S, H, d, d), torch.float32, True, self.device)
-        dev = v.device
+            S = cu_seqlens.numel() - 1
+            _dense("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, dev, True, self.device)
+        shape = (S, H, d, d)
+        if s0 is not None:
+            _dense("s0", s0, shape, torch.float32, dev, True, self.device)
+        streams = self._streams(stream)
         if out is None:
-            out = self._new(stream, lambda: torch.empty(n, H, d, dtype=self.torch_dtype, device=dev))
+            out = self._new(streams, n, H, d, dtype=self.torch_dtype)
         if state is None:
-            state = self._new(stream, lambda: torch.empty(S, H, d, d, dtype=torch.float32, device=dev))
+            state = self._new(streams, *shape, dtype=torch.float32)
+        else:
+            _dense("state", state, shape, torch.float32, dev, True, self.device)
         p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnTokenParams(ctypes.sizeof(VdnTokenParams), H, Hk, S, scale, l2_eps, p(cu_seqlens), None, p(log_alpha),
-                             p(s0), p(state), 0, *st)
-        need = int(self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, ctypes.byref(prm)))
-        ws = self._new(stream, lambda: torch.empty(need, dtype=torch.uint8, device=dev)) if need else None
-        self._check(self.lib.vdn_vda_token_scan(self.h, p(q), p(k), p(v), p(beta), p(out), n, ctypes.byref(prm), p(ws), need,
-                                                self._stream(stream)))
+        prm = VdnTokenParams(_TOKEN_PARAMS_SIZE, H, Hk, S, scale, l2_eps, p(cu_seqlens), None, p(log_alpha),
+                             p(s0), state.data_ptr(), 0, *st)
+        ref = ctypes.byref(prm)
+        need = self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, ref)
+        ws = self._new(streams, need, dtype=torch.uint8) if need else None
+        r = self.lib.vdn_vda_token_scan(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), n, ref,
+                                        p(ws), need, streams[2])
+        if r:
+            self._check(r)
         return out, state
 
     def token_step(self, q, k, v, beta, state, log_alpha=None, index=None, out=None, scale=1.0, l2_eps=0.0, stream=None):
@@ -494,19 +522,23 @@ class Vda:
         lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
         if len(lead) > 2 or (len(lead) == 2 and lead[1] == 0):
             raise ValueError("v must have shape [requests, heads, d] or [requests, tokens, heads, d]")
-        R, per, d = lead[0], lead[1] if len(lead) == 2 else 1, self.d
+        R, per, d, dev = lead[0], lead[1] if len(lead) == 2 else 1, self.d, v.device
         if state is None or state.dim() != 4:
             raise ValueError("state must have shape [slots, heads, d, d]")
-        _require("state", state, (state.shape[0], H, d, d), torch.float32, True, self.device)
+        slots = state.shape[0]
+        _dense("state", state, (slots, H, d, d), torch.float32, dev, True, self.device)
         if index is not None:
-            _require("index", index, (R,), torch.int32, True, self.device)
+            _dense("index", index, (R,), torch.int32, dev, True, self.device)
+        streams = self._streams(stream)
         if out is None:
-            out = self._new(stream, lambda: torch.empty(*lead, H, d, dtype=self.torch_dtype, device=v.device))
+            out = self._new(streams, *lead, H, d, dtype=self.torch_dtype)
         p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnTokenParams(ctypes.sizeof(VdnTokenParams), H, Hk, 0, scale, l2_eps, None, p(index), p(log_alpha), None,
-                             p(state), state.shape[0], *st)
-        self._check(self.lib.vdn_vda_token_step(self.h, p(q), p(k), p(v), p(beta), p(out), R, per, ctypes.byref(prm),
-                                                self._stream(stream)))
+        prm = VdnTokenParams(_TOKEN_PARAMS_SIZE, H, Hk, 0, scale, l2_eps, None, p(index), p(log_alpha), None,
+                             state.data_ptr(), slots, *st)
+        r = self.lib.vdn_vda_token_step(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), R, per,
+                                        ctypes.byref(prm), streams[2])
+        if r:
+            self._check(r)
         return out
 
     def rotate(self, q, k, freq, axis, Y=None, X=None, t0=0, positions=None, half=False, inverse=False, q_weight=None,
@@ -521,42 +553,51 @@ class Vda:
         torch = self._torch
         if q is None or q.dim() != 5:
             raise ValueError("q must have shape [B, T, F, H, d]")
-        B, T, F, H, d = (int(n) for n in q.shape)
-        lead = (B, T, F)
-        rows = lambda n, x, c: _require_rows(n, x, lead, c, d, self.torch_dtype, True, self.device)
-        qs, ks, Hk = rows("q", q, H), 0, 0
+        shape = tuple(q.shape)
+        B, T, F, H, d = shape
+        io, rest = self.torch_dtype, (torch.device("cuda", self.device), True, self.device)
+        qs, ks, Hk = _rows("q", q, shape, io, *rest), 0, 0
+        kshape = None
         if k is not None:
             if k.dim() != 5:
                 raise ValueError("k must have shape [B, T, F, Hk, d]")
-            Hk = int(k.shape[3])
-            ks = rows("k", k, Hk)
+            Hk = k.shape[3]
+            kshape = (B, T, F, Hk, d)
+            ks = _rows("k", k, kshape, io, *rest)
         if freq is None or freq.dim() != 1:
             raise ValueError("freq must have shape [pairs]")
-        n = int(freq.numel())
-        _require("freq", freq, (n,), torch.float64, True, self.device)
-        _require("axis", axis, (n,), torch.int32, True, self.device)
+        n = freq.shape[0]
+        _dense("freq", freq, (n,), torch.float64, *rest)
+        _dense("axis", axis, (n,), torch.int32, *rest)
         if positions is not None:
-            _require("positions", positions, (3, B * T * F), torch.int32, True, self.device)
+            _dense("positions", positions, (3, B * T * F), torch.int32, *rest)
         elif Y is None or X is None:
             raise ValueError("either Y and X or positions are needed")
-        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-            if w is not None:
-                _require(name, w, (d,), torch.float32, True, self.device)
+        if q_weight is not None:
+            _dense("q_weight", q_weight, (d,), torch.float32, *rest)
+        if k_weight is not None:
+            _dense("k_weight", k_weight, (d,), torch.float32, *rest)
         qo, ko = out if out is not None else (None, None)
+        streams = self._streams(stream)
         if qo is None:
-            qo = self._new(stream, lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device))
+            qo, qos = self._new(streams, *shape, dtype=io), H * d
+        else:
+            qos = _rows("q_out", qo, shape, io, *rest)
+        kos = Hk * d
         if k is None:
             if ko is not None:
                 raise ValueError("out has keys, but there are none to rotate")
         elif ko is None:
-            ko = self._new(stream, lambda: torch.empty(k.shape, dtype=k.dtype, device=k.device))
-        qos, kos = rows("q_out", qo, H), rows("k_out", ko, Hk) if k is not None else 0
+            ko = self._new(streams, *kshape, dtype=io)
+        else:
+            kos = _rows("k_out", ko, kshape, io, *rest)
         p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnRotaryParams(ctypes.sizeof(VdnRotaryParams),
-                              (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0), n, Hk, Y or 0, X or 0,
-                              t0, norm_eps, p(freq), p(axis), p(positions), p(q_weight), p(k_weight), qs, ks, qos, kos)
-        self._check(self.lib.vdn_vda_rotate(self.h, p(q), p(k), p(qo), p(ko), B, T, F, H, d, ctypes.byref(prm),
-                                            self._stream(stream)))
+        prm = VdnRotaryParams(_ROTARY_PARAMS_SIZE, (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0),
+                              n, Hk, Y or 0, X or 0, t0, norm_eps, freq.data_ptr(), axis.data_ptr(), p(positions), p(q_weight),
+                              p(k_weight), qs, ks, qos, kos)
+        r = self.lib.vdn_vda_rotate(self.h, q.data_ptr(), p(k), qo.data_ptr(), p(ko), B, T, F, H, d, ctypes.byref(prm), streams[2])
+        if r:
+            self._check(r)
         return qo, ko
 
     def forward_host(self, q, k, v, beta, gate, out, stream=None, alpha=None, s0=None, chunk=1, radius=0,

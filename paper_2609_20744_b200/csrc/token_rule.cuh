@@ -6,10 +6,12 @@
 // taken with the state as it was before the token, so that one pass over the state serves a token:
 //        S k and S q reduced together,   o = scale (alpha (S q) + u (k.q)).
 //
-// Rows of S (value channels) evolve independently.  A CTA owns 32 rows of one (sequence, head) state; eight lanes share a
-// row and hold d/8 columns each, as 16-byte pieces 128 bytes apart, so that a warp's loads and stores cover whole 128-byte
-// lines and a row's two dot products need three shuffle steps.  For one token a request the kernel is a copy of the states
-// through registers and bound by HBM; for longer sequences it is bound by the latency of a token's step.
+// Rows of S (value channels) evolve independently.  Eight lanes share a row and hold d/8 columns each, as 16-byte pieces 128
+// bytes apart, so that a warp's loads and stores of the state cover whole 128-byte lines and a row's two dot products need
+// three shuffle steps.  Two kernels:
+//   token_few_kernel   a few tokens a sequence (one above all): a copy of the states through registers, bound by HBM.
+//   token_walk_kernel  longer sequences: tokens are fetched in batches ahead of their use, what does not depend on the state is
+//                      formed once a batch, and what is left is bound by the latency of a token's step.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -50,77 +52,63 @@ __device__ __forceinline__ void token_range(const int* cu, int s, int per, long 
   len = (int)(b - a);
 }
 
+// The state of sequence s: its slot, or -1 for an entry that is skipped.  `x` runs over all threads of the block, which come here
+// together.
+__device__ __forceinline__ long long token_slot(const TokenArgs& a, int s, int x, int threads) {
+  const long long slot = a.index ? (long long)a.index[s] : s;
+  if (slot < 0 || slot >= a.slots) return -1;            // a padding entry of the batch: nothing is read or written
+  if (a.index) {
+    // two requests for one state cannot both have it: the first in the batch does, later ones are skipped and reported
+    int twice = 0;
+    for (int j = x; j < s; j += threads) twice |= a.index[j] == (int)slot;
+    if (__syncthreads_or(twice)) {
+      if (x == 0) atomicExch(a.status, kStatusInvalidArg);
+      return -1;
+    }
+  }
+  return slot;
+}
+
+// One CTA to 32 rows of a (sequence, head).
 template <typename Tio, int D>
-__global__ void __launch_bounds__(256) token_rule_kernel(const TokenArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 5 : 3) token_few_kernel(const TokenArgs a) {
   constexpr int ROWS = 32, GROUPS = D / ROWS, NE = D / 8, NV = NE / 4;
   const int tid = threadIdx.x, lane8 = tid & 7;
   const int row = (int)(blockIdx.x % GROUPS) * ROWS + (tid >> 3);
   const int h = (int)(blockIdx.x / GROUPS) % a.H, s = (int)(blockIdx.x / GROUPS) / a.H;
-  const long long slot = a.index ? (long long)a.index[s] : s;
-  if (slot < 0 || slot >= a.slots) return;               // a padding entry of the batch: nothing is read or written
-
-  const size_t soff = (((size_t)slot * a.H + h) * D + row) * D + lane8 * 4;
-  float st[NE];
-  if (a.state_in) {
+  const long long at = a.index ? (long long)a.index[s] : s;
+  const size_t soff = (((size_t)at * a.H + h) * D + row) * D + lane8 * 4;
+  float4 st[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const float4 x = *reinterpret_cast<const float4*>(a.state_in + soff + i * 32);
-      st[4 * i] = x.x; st[4 * i + 1] = x.y; st[4 * i + 2] = x.z; st[4 * i + 3] = x.w;
-    }
-  } else {
+  for (int i = 0; i < NV; ++i) st[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.state_in && at >= 0 && at < a.slots) {           // on its way while the slot is being checked
 #pragma unroll
-    for (int i = 0; i < NE; ++i) st[i] = 0.f;
+    for (int i = 0; i < NV; ++i) st[i] = *reinterpret_cast<const float4*>(a.state_in + soff + i * 32);
   }
-  if (a.index) {
-    // two requests for one state cannot both have it: the first in the batch does, later ones are skipped and reported
-    int twice = 0;
-    for (int j = tid; j < s; j += 256) twice |= a.index[j] == (int)slot;
-    if (__syncthreads_or(twice)) {
-      if (tid == 0) atomicExch(a.status, kStatusInvalidArg);
-      return;
-    }
-  }
+  if (token_slot(a, s, tid, 256) < 0) return;
   long long start;
   int len;
   token_range(a.cu_seqlens, s, a.per, a.n_tokens, start, len);
-
   const int hk = h / (a.H / a.Hk);
   const Tio* qp = static_cast<const Tio*>(a.q) + start * a.q_stride + hk * D + lane8 * 4;
   const Tio* kp = static_cast<const Tio*>(a.k) + start * a.k_stride + hk * D + lane8 * 4;
   const Tio* vp = static_cast<const Tio*>(a.v) + start * a.v_stride + h * D + row;
   Tio* op = static_cast<Tio*>(a.out) + start * a.out_stride + h * D + row;
-  const float* bp = a.beta + start * a.H + h;
-  const float* gp = a.log_alpha ? a.log_alpha + start * a.H + h : nullptr;
-
-  float4 kn[NV], qn[NV];
-  float vn = 0.f, bn = 0.f, gn = 0.f;
-  auto fetch = [&]() {                                   // the next token, one step ahead of its use
-#pragma unroll
-    for (int i = 0; i < NV; ++i) { kn[i] = load4(kp + i * 32); qn[i] = load4(qp + i * 32); }
-    vn = to_float(*vp);
-    bn = *bp;
-    gn = gp ? *gp : 0.f;
-    kp += a.k_stride; qp += a.q_stride; vp += a.v_stride; bp += a.H;
-    if (gp) gp += a.H;
-  };
-  if (len > 0) fetch();
   for (int t = 0; t < len; ++t) {
-    float k[NE], q[NE];
+    float4 k[NV], q[NV];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      k[4 * i] = kn[i].x; k[4 * i + 1] = kn[i].y; k[4 * i + 2] = kn[i].z; k[4 * i + 3] = kn[i].w;
-      q[4 * i] = qn[i].x; q[4 * i + 1] = qn[i].y; q[4 * i + 2] = qn[i].z; q[4 * i + 3] = qn[i].w;
-    }
-    const float v = vn, beta = bn, alpha = expf(gn);
-    if (t + 1 < len) fetch();
+    for (int i = 0; i < NV; ++i) { k[i] = load4(kp + i * 32); q[i] = load4(qp + i * 32); }
+    const float v = to_float(*vp), beta = a.beta[(start + t) * a.H + h];
+    const float alpha = a.log_alpha ? expf(a.log_alpha[(start + t) * a.H + h]) : 1.f;
     float sk = 0.f, sq = 0.f, kq = 0.f, kk = 0.f, qq = 0.f;
+    auto add = [](float& s, const float4& x, const float4& y) {
+      s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s); s = fmaf(x.z, y.z, s); s = fmaf(x.w, y.w, s);
+    };
 #pragma unroll
-    for (int i = 0; i < NE; ++i) {
-      sk = fmaf(st[i], k[i], sk);
-      sq = fmaf(st[i], q[i], sq);
-      kq = fmaf(k[i], q[i], kq);
-      kk = fmaf(k[i], k[i], kk);
-      qq = fmaf(q[i], q[i], qq);
+    for (int i = 0; i < NV; ++i) { add(sk, st[i], k[i]); add(sq, st[i], q[i]); add(kq, k[i], q[i]); }
+    if (a.l2_eps > 0.f) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) { add(kk, k[i], k[i]); add(qq, q[i], q[i]); }
     }
 #pragma unroll
     for (int m = 1; m < 8; m <<= 1) {
@@ -134,17 +122,160 @@ __global__ void __launch_bounds__(256) token_rule_kernel(const TokenArgs a) {
     }
     const float rk = a.l2_eps > 0.f ? rsqrtf(kk + a.l2_eps) : 1.f;
     const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
-    const float u = beta * (v - alpha * rk * sk), uk = u * rk;
+    const float uk = beta * (v - alpha * rk * sk) * rk;
     if (lane8 == 0) *op = from_float<Tio>(a.scale * rq * fmaf(uk, kq, alpha * sq));
-    op += a.out_stride;
 #pragma unroll
-    for (int i = 0; i < NE; ++i) st[i] = fmaf(uk, k[i], alpha * st[i]);
+    for (int i = 0; i < NV; ++i) {
+      st[i].x = fmaf(uk, k[i].x, alpha * st[i].x); st[i].y = fmaf(uk, k[i].y, alpha * st[i].y);
+      st[i].z = fmaf(uk, k[i].z, alpha * st[i].z); st[i].w = fmaf(uk, k[i].w, alpha * st[i].w);
+    }
+    qp += a.q_stride; kp += a.k_stride; vp += a.v_stride; op += a.out_stride;
+  }
+  if (a.state_out) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) *reinterpret_cast<float4*>(a.state_out + soff + i * 32) = st[i];
+  }
+}
+
+// One CTA (four warps) to 16 rows of a (sequence, head): a warp to a scheduler, and as many CTAs as rows allow, since a token's
+// step is a chain of latencies.
+template <typename Tio, int D>
+struct TokenWalk {
+  static constexpr int THREADS = 128, ROWS = 16, BATCH = 16;
+  static constexpr int PIECE = 16 / (int)sizeof(Tio);            // elements of a 16-byte copy
+  struct Stage {
+    Tio k[BATCH][D], q[BATCH][D], v[BATCH][ROWS];
+    float beta[BATCH], log_alpha[BATCH];
+  };
+  struct Smem {
+    Stage st[2];
+    float4 f[BATCH];        // alpha, alpha r_k, beta, r_k
+    float2 g[BATCH];        // of the read-out: scale r_q alpha, scale r_q r_k (k.q)
+  };
+};
+
+template <typename Tio, int D>
+__global__ void __launch_bounds__(128) token_walk_kernel(const TokenArgs a) {
+  using W = TokenWalk<Tio, D>;
+  constexpr int ROWS = W::ROWS, GROUPS = D / ROWS, NE = D / 8, NV = NE / 4, B = W::BATCH, PIECE = W::PIECE;
+  __shared__ __align__(16) typename W::Smem sm;
+  const int tid = threadIdx.x, lane8 = tid & 7, r = tid >> 3;
+  const int row0 = (int)(blockIdx.x % GROUPS) * ROWS;
+  const int h = (int)(blockIdx.x / GROUPS) % a.H, s = (int)(blockIdx.x / GROUPS) / a.H;
+  const long long slot = token_slot(a, s, tid, W::THREADS);
+  if (slot < 0) return;
+  long long start;
+  int len;
+  token_range(a.cu_seqlens, s, a.per, a.n_tokens, start, len);
+  const int hk = h / (a.H / a.Hk);
+  const Tio* qp = static_cast<const Tio*>(a.q) + start * a.q_stride + hk * D;
+  const Tio* kp = static_cast<const Tio*>(a.k) + start * a.k_stride + hk * D;
+  const Tio* vp = static_cast<const Tio*>(a.v) + start * a.v_stride + h * D + row0;
+  const size_t gate0 = (size_t)start * a.H + h;
+  Tio* op = static_cast<Tio*>(a.out) + start * a.out_stride + h * D + row0 + r;
+
+  auto fetch = [&](int t0, typename W::Stage& st) {      // tokens t0 .. of the sequence, those that exist
+    const int n = min(B, len - t0);
+    for (int e = tid; e < n * (D / PIECE); e += W::THREADS) {
+      const int j = e / (D / PIECE), c = e % (D / PIECE) * PIECE;
+      cp_async16(&st.k[j][c], kp + (size_t)(t0 + j) * a.k_stride + c);
+      cp_async16(&st.q[j][c], qp + (size_t)(t0 + j) * a.q_stride + c);
+    }
+    for (int e = tid; e < n * (ROWS / PIECE); e += W::THREADS) {
+      const int j = e / (ROWS / PIECE), c = e % (ROWS / PIECE) * PIECE;
+      cp_async16(&st.v[j][c], vp + (size_t)(t0 + j) * a.v_stride + c);
+    }
+    if (tid < n) {
+      cp_async4(&st.beta[tid], a.beta + gate0 + (size_t)(t0 + tid) * a.H);
+      if (a.log_alpha) cp_async4(&st.log_alpha[tid], a.log_alpha + gate0 + (size_t)(t0 + tid) * a.H);
+      else st.log_alpha[tid] = 0.f;
+    }
+    cp_async_commit();
+  };
+
+  if (len > 0) fetch(0, sm.st[0]);
+  const size_t soff = (((size_t)slot * a.H + h) * D + row0 + r) * D + lane8 * 4;
+  float x[NE];                                           // the state
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const float4 y = a.state_in ? *reinterpret_cast<const float4*>(a.state_in + soff + i * 32) : make_float4(0.f, 0.f, 0.f, 0.f);
+    x[4 * i] = y.x; x[4 * i + 1] = y.y; x[4 * i + 2] = y.z; x[4 * i + 3] = y.w;
+  }
+  auto columns = [&](const Tio* p, float (&y)[NE]) {     // this lane's columns of a token's row in shared memory
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const float4 z = load4(p + lane8 * 4 + i * 32);
+      y[4 * i] = z.x; y[4 * i + 1] = z.y; y[4 * i + 2] = z.z; y[4 * i + 3] = z.w;
+    }
+  };
+  for (int t0 = 0, b = 0; t0 < len; t0 += B, b ^= 1) {
+    const typename W::Stage& st = sm.st[b];
+    const int n = min(B, len - t0);
+    if (t0 + B < len) { fetch(t0 + B, sm.st[b ^ 1]); cp_async_wait<1>(); }
+    else cp_async_wait<0>();
+    __syncthreads();
+    {
+      // what does not depend on the state: eight lanes a token
+      float k[NE], q[NE], kq = 0.f, kk = 0.f, qq = 0.f;
+      columns(st.k[r], k);                               // (rows of tokens that do not exist hold anything: their factors are not used)
+      columns(st.q[r], q);
+#pragma unroll
+      for (int i = 0; i < NE; ++i) { kq = fmaf(k[i], q[i], kq); kk = fmaf(k[i], k[i], kk); qq = fmaf(q[i], q[i], qq); }
+#pragma unroll
+      for (int m = 1; m < 8; m <<= 1) {
+        kq += __shfl_xor_sync(0xFFFFFFFFu, kq, m);
+        kk += __shfl_xor_sync(0xFFFFFFFFu, kk, m);
+        qq += __shfl_xor_sync(0xFFFFFFFFu, qq, m);
+      }
+      if (lane8 == 0) {
+        const float rk = a.l2_eps > 0.f ? rsqrtf(kk + a.l2_eps) : 1.f;
+        const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
+        const float alpha = expf(st.log_alpha[r]);
+        sm.f[r] = make_float4(alpha, alpha * rk, st.beta[r], rk);
+        sm.g[r] = make_float2(a.scale * rq * alpha, a.scale * rq * rk * kq);
+      }
+    }
+    __syncthreads();
+    float k[NE], q[NE];
+    columns(st.k[0], k);
+    columns(st.q[0], q);
+    float v = to_float(st.v[0][r]);
+    float4 f = sm.f[0];
+#pragma unroll 2
+    for (int j = 0; j < n; ++j) {
+      float sk[4] = {0.f, 0.f, 0.f, 0.f}, sq[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < NE; ++i) {
+        sk[i & 3] = fmaf(x[i], k[i], sk[i & 3]);
+        sq[i & 1] = fmaf(x[i], q[i], sq[i & 1]);
+      }
+      float dk = (sk[0] + sk[1]) + (sk[2] + sk[3]), dq = sq[0] + sq[1];
+#pragma unroll
+      for (int m = 1; m < 8; m <<= 1) {
+        dk += __shfl_xor_sync(0xFFFFFFFFu, dk, m);
+        dq += __shfl_xor_sync(0xFFFFFFFFu, dq, m);
+      }
+      const float u = f.z * (v - f.y * dk), uk = u * f.w;
+#pragma unroll
+      for (int i = 0; i < NE; ++i) x[i] = fmaf(uk, k[i], f.x * x[i]);
+      if (lane8 == 0) {
+        const float2 g = sm.g[j];
+        *op = from_float<Tio>(fmaf(g.y, u, g.x * dq));
+      }
+      op += a.out_stride;
+      if (j + 1 < n) {                                   // the next token, under the latencies of this one
+        columns(st.k[j + 1], k);
+        columns(st.q[j + 1], q);
+        v = to_float(st.v[j + 1][r]);
+        f = sm.f[j + 1];
+      }
+    }
+    __syncthreads();                                     // the stage and the factors may be replaced
   }
   if (a.state_out) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-      *reinterpret_cast<float4*>(a.state_out + soff + i * 32) =
-          make_float4(st[4 * i], st[4 * i + 1], st[4 * i + 2], st[4 * i + 3]);
+      *reinterpret_cast<float4*>(a.state_out + soff + i * 32) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
   }
 }
 

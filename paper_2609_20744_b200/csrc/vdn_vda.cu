@@ -1243,20 +1243,29 @@ vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, 
   return VDN_OK;
 }
 
+// Up to so many tokens a sequence on the kernel that fetches each token when it needs it; beyond, batches pay.
+constexpr int kFewTokens = 4;
+
+template <typename Tio, int D>
+void launch_token_plain(const vdn::TokenArgs& a, bool few, cudaStream_t st) {
+  if (few) vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
+  else vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 16)), 128, 0, st>>>(a);
+}
+
 vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t st) {
   const int d = h->cfg.d;
-  const long long ctas = (long long)a.S * a.H * (d / 32);
-  if (ctas > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
+  if ((long long)a.S * a.H * (d / 16) > 0x7fffffffLL)
+    return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
+  const bool few = (a.cu_seqlens ? a.n_tokens / a.S : a.per) <= kFewTokens;
   prof_begin(h, st);
-  const unsigned grid = (unsigned)ctas;
   if (h->cfg.io_dtype == VDN_F32) {
-    if (d == 64) vdn::token_rule_kernel<float, 64><<<grid, 256, 0, st>>>(a);
-    else vdn::token_rule_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+    if (d == 64) launch_token_plain<float, 64>(a, few, st);
+    else launch_token_plain<float, 128>(a, few, st);
   } else {
-    if (d == 64) vdn::token_rule_kernel<__nv_bfloat16, 64><<<grid, 256, 0, st>>>(a);
-    else vdn::token_rule_kernel<__nv_bfloat16, 128><<<grid, 256, 0, st>>>(a);
+    if (d == 64) launch_token_plain<__nv_bfloat16, 64>(a, few, st);
+    else launch_token_plain<__nv_bfloat16, 128>(a, few, st);
   }
-  prof_mark(h, st, 0, "token_rule");
+  prof_mark(h, st, 0, few ? "token_few" : "token_walk");
   h->launches = 1;
   VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
