@@ -312,6 +312,12 @@ def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=Non
     return lead, H, Hk, strides
 
 
+def _current_raw_stream(torch, device):
+    """Handle of the current stream, without the Stream object around it where torch offers that."""
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device) if get is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 def rotary_tables(sections, theta=10000.0, shared_ladder=False):
     """(freq, axis) of rotate() for pairs that are `sections` = (time, height, width) pairs, one axis behind another (host
     tensors).  Each axis has its own ladder theta^(-i / n) over its n pairs; with shared_ladder pair p of all n pairs has
@@ -338,6 +344,7 @@ class Vda:
         self.dtype = dtype
         self.torch_dtype = torch.float32 if dtype == "f32" else torch.bfloat16
         self.device = device
+        self._dev = torch.device("cuda", device)
         cfg = VdnConfig(ctypes.sizeof(VdnConfig), VDN_F32 if dtype == "f32" else VDN_BF16, d, rms_eps, flags, device)
         self.h = ctypes.c_void_p()
         st = self.lib.vdn_vda_create(ctypes.byref(cfg), ctypes.byref(self.h))
@@ -452,22 +459,22 @@ class Vda:
 
     # -- token-wise rule, rotary positions ----------------------------------------------------
     def _streams(self, stream):
-        """(current stream, stream of the call, its handle)."""
-        here = self._torch.cuda.current_stream(self.device)
-        on = here if stream is None else stream
-        return here, on, on.cuda_stream
+        """(handle of the call's stream, the stream where it is not the current one)."""
+        torch = self._torch
+        here = _current_raw_stream(torch, self.device)
+        if stream is None or stream.cuda_stream == here:
+            return here, None
+        return stream.cuda_stream, stream
 
-    def _new(self, streams, *shape, dtype):
+    def _new(self, streams, shape, dtype):
         """Memory made for a call: taken on the call's stream, so that the allocator does not hand it on while the call still
         runs; where that is not the current stream, what the caller gets back is marked as in use there too."""
         torch = self._torch
-        here, on, raw = streams
-        dev = torch.device("cuda", self.device)
-        if raw == here.cuda_stream:
-            return torch.empty(shape, dtype=dtype, device=dev)
-        with torch.cuda.stream(on):
-            x = torch.empty(shape, dtype=dtype, device=dev)
-        x.record_stream(here)
+        if streams[1] is None:
+            return torch.empty(shape, dtype=dtype, device=self._dev)
+        with torch.cuda.stream(streams[1]):
+            x = torch.empty(shape, dtype=dtype, device=self._dev)
+        x.record_stream(torch.cuda.current_stream(self.device))
         return x
 
     def token_scan(self, q, k, v, beta, log_alpha=None, cu_seqlens=None, s0=None, out=None, state=None, scale=1.0,
@@ -483,7 +490,7 @@ class Vda:
         lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
         if len(lead) != 1:
             raise ValueError("v must have shape [tokens, heads, d]")
-        n, d, S, dev = lead[0], self.d, 1, v.device
+        n, d, S, dev = lead[0], self.d, 1, self._dev
         if cu_seqlens is not None:
             if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
                 raise ValueError("cu_seqlens must have shape [sequences + 1]")
@@ -494,9 +501,9 @@ class Vda:
             _dense("s0", s0, shape, torch.float32, dev, True, self.device)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, n, H, d, dtype=self.torch_dtype)
+            out = self._new(streams, (n, H, d), self.torch_dtype)
         if state is None:
-            state = self._new(streams, *shape, dtype=torch.float32)
+            state = self._new(streams, shape, torch.float32)
         else:
             _dense("state", state, shape, torch.float32, dev, True, self.device)
         p = lambda x: x.data_ptr() if x is not None else None
@@ -504,9 +511,9 @@ class Vda:
                              p(s0), state.data_ptr(), 0, *st)
         ref = ctypes.byref(prm)
         need = self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, ref)
-        ws = self._new(streams, need, dtype=torch.uint8) if need else None
+        ws = self._new(streams, (need,), torch.uint8) if need else None
         r = self.lib.vdn_vda_token_scan(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), n, ref,
-                                        p(ws), need, streams[2])
+                                        p(ws), need, streams[0])
         if r:
             self._check(r)
         return out, state
@@ -522,7 +529,7 @@ class Vda:
         lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
         if len(lead) > 2 or (len(lead) == 2 and lead[1] == 0):
             raise ValueError("v must have shape [requests, heads, d] or [requests, tokens, heads, d]")
-        R, per, d, dev = lead[0], lead[1] if len(lead) == 2 else 1, self.d, v.device
+        R, per, d, dev = lead[0], lead[1] if len(lead) == 2 else 1, self.d, self._dev
         if state is None or state.dim() != 4:
             raise ValueError("state must have shape [slots, heads, d, d]")
         slots = state.shape[0]
@@ -531,12 +538,12 @@ class Vda:
             _dense("index", index, (R,), torch.int32, dev, True, self.device)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, *lead, H, d, dtype=self.torch_dtype)
+            out = self._new(streams, (*lead, H, d), self.torch_dtype)
         p = lambda x: x.data_ptr() if x is not None else None
         prm = VdnTokenParams(_TOKEN_PARAMS_SIZE, H, Hk, 0, scale, l2_eps, None, p(index), p(log_alpha), None,
                              state.data_ptr(), slots, *st)
         r = self.lib.vdn_vda_token_step(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), R, per,
-                                        ctypes.byref(prm), streams[2])
+                                        ctypes.byref(prm), streams[0])
         if r:
             self._check(r)
         return out
@@ -555,7 +562,7 @@ class Vda:
             raise ValueError("q must have shape [B, T, F, H, d]")
         shape = tuple(q.shape)
         B, T, F, H, d = shape
-        io, rest = self.torch_dtype, (torch.device("cuda", self.device), True, self.device)
+        io, rest = self.torch_dtype, (self._dev, True, self.device)
         qs, ks, Hk = _rows("q", q, shape, io, *rest), 0, 0
         kshape = None
         if k is not None:
@@ -580,7 +587,7 @@ class Vda:
         qo, ko = out if out is not None else (None, None)
         streams = self._streams(stream)
         if qo is None:
-            qo, qos = self._new(streams, *shape, dtype=io), H * d
+            qo, qos = self._new(streams, shape, io), H * d
         else:
             qos = _rows("q_out", qo, shape, io, *rest)
         kos = Hk * d
@@ -588,14 +595,14 @@ class Vda:
             if ko is not None:
                 raise ValueError("out has keys, but there are none to rotate")
         elif ko is None:
-            ko = self._new(streams, *kshape, dtype=io)
+            ko = self._new(streams, kshape, io)
         else:
             kos = _rows("k_out", ko, kshape, io, *rest)
         p = lambda x: x.data_ptr() if x is not None else None
         prm = VdnRotaryParams(_ROTARY_PARAMS_SIZE, (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0),
                               n, Hk, Y or 0, X or 0, t0, norm_eps, freq.data_ptr(), axis.data_ptr(), p(positions), p(q_weight),
                               p(k_weight), qs, ks, qos, kos)
-        r = self.lib.vdn_vda_rotate(self.h, q.data_ptr(), p(k), qo.data_ptr(), p(ko), B, T, F, H, d, ctypes.byref(prm), streams[2])
+        r = self.lib.vdn_vda_rotate(self.h, q.data_ptr(), p(k), qo.data_ptr(), p(ko), B, T, F, H, d, ctypes.byref(prm), streams[0])
         if r:
             self._check(r)
         return qo, ko

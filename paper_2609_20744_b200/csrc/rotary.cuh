@@ -60,87 +60,98 @@ __device__ __forceinline__ uint4 pack16(const float (&x)[8], const __nv_bfloat16
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <typename Tio, int D, bool HALF>
-__global__ void __launch_bounds__(Rotary::THREADS) rotary_kernel(const RotaryArgs a) {
+template <typename Tio, int D, bool HALF, bool NORM>
+__global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const RotaryArgs a) {
   constexpr int VEC = 16 / (int)sizeof(Tio);       // channels of a 16-byte piece
   constexpr int LPH = D / (2 * VEC);               // lanes of a head
   constexpr int NP = VEC;                          // pairs of a lane
   constexpr int P4 = NP / 2;                       // float4's (two pairs each) of a lane's cosines and sines
+  constexpr int STEP = Rotary::THREADS / LPH;      // head rows side by side
+  constexpr int U = Rotary::UNROLL;
   // [token][pair / 2 mod P4][lane][cos, sin, cos, sin]: the lanes of a head read 16-byte pieces side by side
   extern __shared__ float4 table[];
+  __shared__ float weight[NORM ? 2 : 1][NORM ? D : 1];
   const long long n0 = (long long)blockIdx.x * a.tile;
   const int nt = (int)min((long long)a.tile, a.n_tokens - n0);
 
-  // ---- cosines and sines
-  for (int e = threadIdx.x; e < nt * (D / 2); e += Rotary::THREADS) {
-    const int j = e / (D / 2), lp = e % (D / 2);   // token of the tile; lane * NP + pair of the lane
-    const int l = lp / NP, i = lp % NP;
-    // the pair that slot lp stands for; HALF: lanes past the rotated channels pass theirs through
-    const int p = HALF ? (l * VEC < a.pairs ? lp : a.pairs) : lp;
-    float c = 1.f, s = 0.f;
-    if (p < a.pairs) {
-      const int ax = a.axis[p];
+  // heads: task = (token of the tile, head row of queries then keys, lane)
+  const int rows = a.heads[0] + a.heads[1];
+  const int tasks = nt * rows;
+  const int l = threadIdx.x % LPH, first = (int)threadIdx.x / LPH;
+  // first channel of the lane's two pieces
+  int c0 = 2 * l * VEC, c1 = c0 + VEC;
+  if (HALF && l * VEC < a.pairs) { c0 = l * VEC; c1 = c0 + a.pairs; }
+  uint4 x0[U], x1[U];
+  auto fetch = [&](int t0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * STEP;
+      if (t < tasks) {
+        const int j = t / rows, r = t - j * rows, w = r >= a.heads[0];
+        const Tio* src = static_cast<const Tio*>(a.in[w]) + (size_t)(n0 + j) * a.in_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
+        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
+        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
+      }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < U; ++u) x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+  fetch(first);                                    // on their way while the angles are formed
+
+  // ---- cosines and sines: a thread has one place lp = lane * NP + pair of the lane, and every (256 / places)-th token
+  {
+    constexpr int PLACES = D / 2, TOKENS = Rotary::THREADS / PLACES;
+    const int lp = threadIdx.x % PLACES, tl = lp / NP, ti = lp % NP;
+    // the pair that the place stands for; HALF: lanes past the rotated channels pass theirs through
+    const int p = HALF ? (tl * VEC < a.pairs ? lp : a.pairs) : lp;
+    const int ax = p < a.pairs ? a.axis[p] : -1;
+    const double turn = ax >= 0 && ax <= 2 ? a.freq[p] * 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
+    for (int j = (int)threadIdx.x / PLACES; j < nt; j += TOKENS) {
+      float c = 1.f, s = 0.f;
       if (ax >= 0 && ax <= 2) {
         const long long n = n0 + j;
         int pos;
         if (a.positions) {
           pos = a.positions[(size_t)ax * a.n_tokens + n];
         } else {
-          const int u = (int)(n % a.F);
-          pos = ax == 0 ? a.t0 + (int)((n / a.F) % a.T) : ax == 1 ? u / a.X : u % a.X;
+          const unsigned fr = (unsigned)n / (unsigned)a.F, u = (unsigned)n - fr * (unsigned)a.F;
+          pos = ax == 0 ? a.t0 + (int)(fr % (unsigned)a.T) : ax == 1 ? (int)(u / (unsigned)a.X) : (int)(u % (unsigned)a.X);
         }
-        const double turns = (double)pos * (a.freq[p] * 0.15915494309189533577);   // 1 / (2 pi)
+        const double turns = (double)pos * turn;
         sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
         s *= a.sign;
       }
+      float* t = reinterpret_cast<float*>(&table[(j * P4 + ti / 2) * LPH + tl]);
+      *reinterpret_cast<float2*>(t + (ti & 1) * 2) = make_float2(c, s);
     }
-    float* t = reinterpret_cast<float*>(&table[(j * P4 + i / 2) * LPH + l]);
-    t[(i & 1) * 2] = c;
-    t[(i & 1) * 2 + 1] = s;
+  }
+  if constexpr (NORM) {
+    for (int e = threadIdx.x; e < 2 * D; e += Rotary::THREADS) weight[e / D][e % D] = a.weight[e / D] ? a.weight[e / D][e % D] : 1.f;
   }
   __syncthreads();
 
-  // ---- heads: task = (token of the tile, head row of queries then keys, lane)
-  const int rows = a.heads[0] + a.heads[1];
-  const int tasks = nt * rows;
-  const int l = threadIdx.x % LPH;
-  constexpr int STEP = Rotary::THREADS / LPH;      // tasks side by side
-  // first channel of the lane's two pieces
-  int c0 = 2 * l * VEC, c1 = c0 + VEC;
-  if (HALF && l * VEC < a.pairs) { c0 = l * VEC; c1 = c0 + a.pairs; }
-  for (int t0 = 0; t0 < tasks; t0 += STEP * Rotary::UNROLL) {
-    uint4 x0[Rotary::UNROLL], x1[Rotary::UNROLL];
+  for (int base = 0; base < tasks; base += STEP * U) {
+    if (base) fetch(base + first);
 #pragma unroll
-    for (int u = 0; u < Rotary::UNROLL; ++u) {
-      const int t = t0 + u * STEP + (int)threadIdx.x / LPH;
-      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
-      if (t < tasks) {
-        const int j = t / rows, r = t % rows, w = r >= a.heads[0];
-        const Tio* src = static_cast<const Tio*>(a.in[w]) + (size_t)(n0 + j) * a.in_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
-        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
-        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < Rotary::UNROLL; ++u) {
-      const int t = t0 + u * STEP + (int)threadIdx.x / LPH;
+    for (int u = 0; u < U; ++u) {
+      const int t = base + first + u * STEP;
       const bool live = t < tasks;
-      const int j = live ? t / rows : 0, r = live ? t % rows : 0, w = r >= a.heads[0];
+      const int j = live ? t / rows : 0, r = live ? t - j * rows : 0, w = r >= a.heads[0];
       float y0[VEC], y1[VEC];
       unpack16(x0[u], y0, static_cast<const Tio*>(nullptr));
       unpack16(x1[u], y1, static_cast<const Tio*>(nullptr));
-      if (a.norm_eps > 0.f) {
+      if constexpr (NORM) {
         float ss = 0.f;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) ss += y0[i] * y0[i] + y1[i] * y1[i];
 #pragma unroll
         for (int m = 1; m < LPH; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
         const float rn = rsqrtf(ss * (1.f / D) + a.norm_eps);
-        const float* wt = a.weight[w];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          y0[i] *= wt ? rn * wt[c0 + i] : rn;
-          y1[i] *= wt ? rn * wt[c1 + i] : rn;
+        for (int i = 0; i < VEC; i += 4) {
+          const float4 g = *reinterpret_cast<const float4*>(&weight[w][c0 + i]), k = *reinterpret_cast<const float4*>(&weight[w][c1 + i]);
+          y0[i] *= rn * g.x; y0[i + 1] *= rn * g.y; y0[i + 2] *= rn * g.z; y0[i + 3] *= rn * g.w;
+          y1[i] *= rn * k.x; y1[i + 1] *= rn * k.y; y1[i + 2] *= rn * k.z; y1[i + 3] *= rn * k.w;
         }
       }
 #pragma unroll

@@ -1247,9 +1247,19 @@ vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, 
 constexpr int kFewTokens = 4;
 
 template <typename Tio, int D>
-void launch_token_plain(const vdn::TokenArgs& a, bool few, cudaStream_t st) {
-  if (few) vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
-  else vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 16)), 128, 0, st>>>(a);
+cudaError_t launch_token_plain(const vdn::TokenArgs& a, bool few, cudaStream_t st) {
+  if (few) {
+    vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
+    return cudaGetLastError();
+  }
+  using W = vdn::TokenWalk<Tio, D>;
+  if (sizeof(typename W::Smem) > 48 * 1024) {
+    const cudaError_t e = cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               (int)sizeof(typename W::Smem));
+    if (e != cudaSuccess) return e;
+  }
+  vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, sizeof(typename W::Smem), st>>>(a);
+  return cudaGetLastError();
 }
 
 vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t st) {
@@ -1258,16 +1268,14 @@ vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t 
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
   const bool few = (a.cu_seqlens ? a.n_tokens / a.S : a.per) <= kFewTokens;
   prof_begin(h, st);
-  if (h->cfg.io_dtype == VDN_F32) {
-    if (d == 64) launch_token_plain<float, 64>(a, few, st);
-    else launch_token_plain<float, 128>(a, few, st);
-  } else {
-    if (d == 64) launch_token_plain<__nv_bfloat16, 64>(a, few, st);
-    else launch_token_plain<__nv_bfloat16, 128>(a, few, st);
-  }
+  cudaError_t e;
+  if (h->cfg.io_dtype == VDN_F32)
+    e = d == 64 ? launch_token_plain<float, 64>(a, few, st) : launch_token_plain<float, 128>(a, few, st);
+  else
+    e = d == 64 ? launch_token_plain<__nv_bfloat16, 64>(a, few, st) : launch_token_plain<__nv_bfloat16, 128>(a, few, st);
+  VDN_CUDA(h, e);
   prof_mark(h, st, 0, few ? "token_few" : "token_walk");
   h->launches = 1;
-  VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
 }
 
@@ -1375,8 +1383,14 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
 
 template <typename Tio, int D>
 void launch_rotary(const vdn::RotaryArgs& a, bool half, unsigned grid, size_t smem, cudaStream_t st) {
-  if (half) vdn::rotary_kernel<Tio, D, true><<<grid, vdn::Rotary::THREADS, smem, st>>>(a);
-  else vdn::rotary_kernel<Tio, D, false><<<grid, vdn::Rotary::THREADS, smem, st>>>(a);
+  constexpr int NT = vdn::Rotary::THREADS;
+  if (a.norm_eps > 0.f) {
+    if (half) vdn::rotary_kernel<Tio, D, true, true><<<grid, NT, smem, st>>>(a);
+    else vdn::rotary_kernel<Tio, D, false, true><<<grid, NT, smem, st>>>(a);
+  } else {
+    if (half) vdn::rotary_kernel<Tio, D, true, false><<<grid, NT, smem, st>>>(a);
+    else vdn::rotary_kernel<Tio, D, false, false><<<grid, NT, smem, st>>>(a);
+  }
 }
 
 }  // namespace
