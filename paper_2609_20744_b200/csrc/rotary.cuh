@@ -32,7 +32,7 @@ struct RotaryArgs {
 struct Rotary {
   static constexpr int THREADS = 256;
   static constexpr int MAX_TILE = 32;      // tokens a CTA covers
-  static constexpr int UNROLL = 4;         // head rows a lane has in flight
+  static constexpr int UNROLL = 2;         // head rows a lane has in flight
 };
 
 // 16 bytes of a head's channels as floats, and back
@@ -61,7 +61,7 @@ __device__ __forceinline__ uint4 pack16(const float (&x)[8], const __nv_bfloat16
 }
 
 template <typename Tio, int D, bool HALF, bool NORM>
-__global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const RotaryArgs a) {
+__global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const RotaryArgs a) {
   constexpr int VEC = 16 / (int)sizeof(Tio);       // channels of a 16-byte piece
   constexpr int LPH = D / (2 * VEC);               // lanes of a head
   constexpr int NP = VEC;                          // pairs of a lane
@@ -70,7 +70,8 @@ __global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const Rotary
   constexpr int U = Rotary::UNROLL;
   // [token][pair / 2 mod P4][lane][cos, sin, cos, sin]: the lanes of a head read 16-byte pieces side by side
   extern __shared__ float4 table[];
-  __shared__ float weight[NORM ? 2 : 1][NORM ? D : 1];
+  // of queries and keys, in the order the lanes take them: [4 channels of the first piece .. of the second][lane]
+  __shared__ float4 weight[NORM ? 2 : 1][NORM ? VEC / 2 : 1][LPH];
   const long long n0 = (long long)blockIdx.x * a.tile;
   const int nt = (int)min((long long)a.tile, a.n_tokens - n0);
 
@@ -86,6 +87,7 @@ __global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const Rotary
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = t0 + u * STEP;
+      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
       if (t < tasks) {
         const int j = t / rows, r = t - j * rows, w = r >= a.heads[0];
         const Tio* src = static_cast<const Tio*>(a.in[w]) + (size_t)(n0 + j) * a.in_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
@@ -94,9 +96,6 @@ __global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const Rotary
       }
     }
   };
-#pragma unroll
-  for (int u = 0; u < U; ++u) x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
-  fetch(first);                                    // on their way while the angles are formed
 
   // ---- cosines and sines: a thread has one place lp = lane * NP + pair of the lane, and every (256 / places)-th token
   {
@@ -126,12 +125,17 @@ __global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const Rotary
     }
   }
   if constexpr (NORM) {
-    for (int e = threadIdx.x; e < 2 * D; e += Rotary::THREADS) weight[e / D][e % D] = a.weight[e / D] ? a.weight[e / D][e % D] : 1.f;
+    if (threadIdx.x < 2 * (VEC / 2) * LPH) {
+      const int w = (int)threadIdx.x / (VEC / 2 * LPH), k = (int)threadIdx.x / LPH % (VEC / 2);   // l is the thread's own lane
+      const int c = k < VEC / 4 ? c0 + 4 * k : c1 + 4 * (k - VEC / 4);
+      const float* g = a.weight[w];
+      weight[w][k][l] = g ? make_float4(g[c], g[c + 1], g[c + 2], g[c + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
+    }
   }
   __syncthreads();
 
   for (int base = 0; base < tasks; base += STEP * U) {
-    if (base) fetch(base + first);
+    fetch(base + first);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int t = base + first + u * STEP;
@@ -149,7 +153,7 @@ __global__ void __launch_bounds__(Rotary::THREADS, 3) rotary_kernel(const Rotary
         const float rn = rsqrtf(ss * (1.f / D) + a.norm_eps);
 #pragma unroll
         for (int i = 0; i < VEC; i += 4) {
-          const float4 g = *reinterpret_cast<const float4*>(&weight[w][c0 + i]), k = *reinterpret_cast<const float4*>(&weight[w][c1 + i]);
+          const float4 g = weight[w][i / 4][l], k = weight[w][VEC / 4 + i / 4][l];
           y0[i] *= rn * g.x; y0[i + 1] *= rn * g.y; y0[i + 2] *= rn * g.z; y0[i + 3] *= rn * g.w;
           y1[i] *= rn * k.x; y1[i + 1] *= rn * k.y; y1[i + 2] *= rn * k.z; y1[i + 3] *= rn * k.w;
         }

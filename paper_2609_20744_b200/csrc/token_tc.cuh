@@ -57,6 +57,12 @@ __host__ __device__ inline int token_parts(int len, int part) {
   return part > 0 && len > 2 * part ? (len + part - 1) / part : 1;
 }
 
+// The kernels of one call overlap at their edges: each lets the next one start early, and each first gets ready and then waits
+// for the one before to be done.  Every thread waits, also of a CTA that has nothing to do: a kernel that did not wait could be
+// done before its predecessor, and its successor would then read unfinished results.
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.  A whole
 // warp looks at 32 offsets at a time: a round trip to memory for 32 sequences, two for a thousand.
 __device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int unit) {
@@ -235,6 +241,7 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   int* where = reinterpret_cast<int*>(bp + S::OFF_BAR + 32);      // first row, tokens (0: no chunk has this place)
   const WaitCtx wc(abort_flag, ds);
   float* fs = reinterpret_cast<float*>(bp + S::OFF_F);
+  let_next_kernel_start();
 
   if (warp == 0) {
     const int seq = token_seq_of(t, place, C);
@@ -603,6 +610,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   unsigned char* bp = smem_dyn + (base - smem_u32(smem_dyn));
   const TokenArgs& t = a.t;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_kernel_start();
   constexpr bool WRITE = MODE == TOKEN_FULL;          // results are wanted
   // this CTA's rows, first state and what becomes of its last one
   int bid = (int)blockIdx.x;
@@ -615,12 +623,12 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
   const int parts = token_parts(len, a.part);
   const int pos = a.part > 0 ? x - ((int)(start / a.part) + seq) : 0;
-  if (pos < 0 || pos >= parts) return;                // a place that no part has
+  if (pos < 0 || pos >= parts) { wait_for_kernel_before(); return; }   // a place that no part has
   const float* first = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) : nullptr;
   float* last = nullptr;
   const size_t comp = ((size_t)x * t.H + h) * (D * D);
   if constexpr (MODE == TOKEN_COMPOSE) {
-    if (pos + 1 == parts || (from_identity && pos == 0)) return;   // nobody asks for these
+    if (pos + 1 == parts || (from_identity && pos == 0)) { wait_for_kernel_before(); return; }   // nobody asks for these
     if (pos > 0) first = nullptr;
     last = (from_identity ? a.comp_m : a.comp_j) + comp;
   } else {
@@ -671,6 +679,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   tc_fence_before_sync();
   __syncthreads();
   tc_fence_after_sync();
+  wait_for_kernel_before();
   const uint32_t tmem = *tmem_slot;
 
   if (warp == 0) {
@@ -802,6 +811,11 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
       const float whole = f[128];
       if (!warp_wait(DK_FULL, s & 1)) break;
       tc_fence_after_sync();
+      // (X^T P^T of the step before, which another thread issues, must be done with the old parts of X)
+      if (WRITE && s > 0) {
+        if (!warp_wait(DO_FULL, (s - 1) & 1)) break;
+        tc_fence_after_sync();
+      }
       float x[16];
       tmem_ld8(tl + S::D_K + sl * 8, x);
       tmem_ld8(tl + S::D_K + 32 + sl * 8, x + 8);
@@ -979,6 +993,8 @@ __global__ void __launch_bounds__(TokenJoin::THREADS) token_join_kernel(const To
   int len;
   token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
   const int parts = token_parts(len, a.part);
+  let_next_kernel_start();
+  wait_for_kernel_before();
   if (parts == 1) return;
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D, base = (x0 * t.H + h) * (D * D);

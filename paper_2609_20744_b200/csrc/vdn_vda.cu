@@ -13,6 +13,7 @@
 #include <cstring>
 #include <new>
 #include <string>
+#include <utility>
 
 #include "common.cuh"
 #include "gram_simt.cuh"
@@ -1279,6 +1280,9 @@ vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t 
   return VDN_OK;
 }
 
+// The lengths stay on the device.  Where a choice depends on the longest sequence: four times the average, if there are so many.
+long long longest_guess(long long n_tokens, int n_seqs) { return n_seqs > 4 ? 4 * (n_tokens / n_seqs) : n_tokens; }
+
 // Workspace of the chunked rule: per (place, head) the chunk's two operators and its factors; per (part, head) of cut
 // sequences the state it enters with and its composite.
 struct TokenLayout {
@@ -1296,10 +1300,11 @@ TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs
   L.part = 0;
   L.parts = n_seqs;
   const long long per_head = h->sm_count / heads;
+  const long long longest = longest_guess(n_tokens, n_seqs);
   if (per_head - n_seqs >= 2) {
     const long long rows = (n_tokens + C * (per_head - n_seqs) - 1) / (C * (per_head - n_seqs)) * C;
     L.part = (int)(rows < 8 * C ? 8 * C : rows);
-    if (n_tokens <= 2LL * L.part) L.part = 0;
+    if (longest <= 2LL * L.part) L.part = 0;
     else L.parts = n_tokens / L.part + n_seqs;
   }
   const size_t units = (size_t)L.places * heads, state = (size_t)128 * 128 * sizeof(float);
@@ -1315,9 +1320,16 @@ TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs
   return L;
 }
 
-bool token_on_tensor_cores(const vdn_vda_s* h, long long n_tokens, int n_seqs) {
-  (void)n_seqs;
-  return use_tensor_cores(h, h->cfg.d) && n_tokens > 0;
+// Chunks on the tensor cores, or token by token in plain fp32 (bf16, d = 128: both can).  Costs in microseconds, fitted to
+// graph replays of 1 .. 64 sequences of 1 .. 1024 tokens and 2, 8 and 32 heads: the plain kernel starts faster and pays 0.17 for a
+// token of the longest sequence and 0.006 for each token and head; the two chunked kernels start at 18 and pay 2.3 for a chunk of the longest and 0.07 for each chunk and
+// head.  One sequence, 8 heads: 64 tokens 14.6 plain, 18.5 chunked; 128 tokens 26.8 and 20.5; 1024 tokens 191 and 55.
+bool token_on_tensor_cores(const vdn_vda_s* h, long long n_tokens, int n_seqs, int heads) {
+  if (!use_tensor_cores(h, h->cfg.d) || n_tokens == 0) return false;
+  const double n = (double)n_tokens, longest = (double)longest_guess(n_tokens, n_seqs);
+  const double plain = 4.0 + 0.17 * longest + 0.006 * n * heads;
+  const double chunked = 18.0 + 2.3 * longest / vdn::TokenTc::C + 0.07 * (n / vdn::TokenTc::C + n_seqs) * heads;
+  return chunked < plain;
 }
 
 // Rows of `width` bf16 elements, `stride` elements apart, as a 2-D map with a (box, 64) box.
@@ -1332,6 +1344,22 @@ vdn_status make_rows_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, long long
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (token rows) failed: " + std::to_string((int)r));
   return VDN_OK;
+}
+
+// A kernel that may start while its predecessor on the stream is still running (and waits for it itself).
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, int smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3((unsigned)threads);
+  c.dynamicSmemBytes = (size_t)smem;
+  c.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
 }
 
 vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* ws, cudaStream_t st) {
@@ -1366,15 +1394,17 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   vdn::token_prep_kernel<<<(unsigned)(L.places * t.H), vdn::TokenPrep::THREADS, vdn::TokenPrep::SMEM_BYTES, st>>>(
       tmK, tmQ, a, dev_status(h));
   prof_mark(h, st, nk++, "token_prep");
+  const vdn::tc::DevStatus ds = dev_status(h);
   if (L.part) {
-    vdn::token_chain_kernel<vdn::TOKEN_COMPOSE><<<(unsigned)(2 * L.parts * t.H), TC::threads(vdn::TOKEN_COMPOSE), TC::SMEM_BYTES, st>>>(
-        tmK, tmQ, tmV, a, dev_status(h));
+    VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel<vdn::TOKEN_COMPOSE>, (unsigned)(2 * L.parts * t.H),
+                                  TC::threads(vdn::TOKEN_COMPOSE), TC::SMEM_BYTES, st, tmK, tmQ, tmV, a, ds));
     prof_mark(h, st, nk++, "token_compose");
-    vdn::token_join_kernel<<<(unsigned)(t.S * t.H * (128 / vdn::TokenJoin::ROWS)), vdn::TokenJoin::THREADS, 0, st>>>(a);
+    VDN_CUDA(h, launch_overlapped(vdn::token_join_kernel, (unsigned)(t.S * t.H * (128 / vdn::TokenJoin::ROWS)),
+                                  vdn::TokenJoin::THREADS, 0, st, a));
     prof_mark(h, st, nk++, "token_join");
   }
-  vdn::token_chain_kernel<vdn::TOKEN_FULL><<<(unsigned)(L.parts * t.H), TC::threads(vdn::TOKEN_FULL), TC::SMEM_BYTES, st>>>(
-      tmK, tmQ, tmV, a, dev_status(h));
+  VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel<vdn::TOKEN_FULL>, (unsigned)(L.parts * t.H), TC::threads(vdn::TOKEN_FULL),
+                                TC::SMEM_BYTES, st, tmK, tmQ, tmV, a, ds));
   prof_mark(h, st, nk++, "token_chain");
   h->launches = nk;
   VDN_CUDA(h, cudaGetLastError());
@@ -1399,7 +1429,7 @@ extern "C" {
 
 size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
   if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->n_seqs <= 0 || n_tokens < 0) return 0;
-  return token_on_tensor_cores(h, n_tokens, p->n_seqs) ? make_token_layout(h, n_tokens, p->n_seqs, p->heads).total : 0;
+  return token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads) ? make_token_layout(h, n_tokens, p->n_seqs, p->heads).total : 0;
 }
 
 vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1506,7 +1536,7 @@ vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void*
   // Tokens a CTA covers: enough that its lanes have two full turns of unrolled loads (fewer heads, more tokens), but no
   // more than leave every SM several CTAs.
   const int lanes = d * (int)es / 32, rows = a.heads[0] + a.heads[1];
-  long long tile = (2LL * vdn::Rotary::UNROLL * vdn::Rotary::THREADS / lanes + rows - 1) / rows;
+  long long tile = (4LL * vdn::Rotary::UNROLL * vdn::Rotary::THREADS / lanes + rows - 1) / rows;
   const long long spread = a.n_tokens / (4LL * h->sm_count);
   if (tile > spread) tile = spread;
   a.tile = (int)(tile < 1 ? 1 : tile > vdn::Rotary::MAX_TILE ? vdn::Rotary::MAX_TILE : tile);

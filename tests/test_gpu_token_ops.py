@@ -93,7 +93,8 @@ def check_scan(vda, x, lens, dtype, d, tc, s0=None, scale=1.0, l2_eps=0.0, out=N
     return out, state
 
 
-LENS = [[1], [2], [63], [64], [65], [128], [300], [5, 0, 64, 1, 130, 0, 63], [0], [700]]
+# (the last three, and [128] and [300], are long enough on the whole that bf16 with d = 128 goes in chunks)
+LENS = [[1], [2], [63], [64], [65], [128], [300], [5, 0, 64, 1, 130, 0, 63], [0], [1, 400, 0, 64, 65, 63, 2], [129, 0, 1, 191], [700]]
 
 
 @pytest.mark.parametrize("lens", LENS, ids=str)
@@ -227,14 +228,34 @@ def test_scan_long_sequence_on_the_tensor_cores_agrees_with_the_plain_kernel(tok
     assert rel(s1, np64(s2)) <= 2 * state and rel(o1, np64(o2)) <= 2 * (io + terms)
 
 
-def test_scan_same_call_same_bits():
-    d, h = 128, 5
-    x = draw(1000, h, h, d, "bf16", seed=9)
+@pytest.mark.parametrize("lens,h,hk", [([1000], 5, 5), ([700, 1300, 64, 1, 900] * 6, 32, 16), ([9000], 8, 8)], ids=str)
+def test_scan_same_call_same_bits(lens, h, hk):
+    """Over and over, calls right behind one another, on every SM: what a missing wait between two roles of a kernel would break."""
+    d, n = 128, sum(lens)
+    x = draw(n, h, hk, d, "bf16", seed=9)
+    cu = torch.tensor([0] + lens).cumsum(0).to(torch.int32).to(DEV)
     vda = binding.Vda(d, "bf16")
-    o1, s1 = vda.token_scan(**x)
-    for _ in range(3):
-        o2, s2 = vda.token_scan(**x)
-        assert torch.equal(o1, o2) and torch.equal(s1, s2)
+    o1, s1 = vda.token_scan(**x, cu_seqlens=cu)
+    for _ in range(5):
+        many = [vda.token_scan(**x, cu_seqlens=cu) for _ in range(4)]
+        assert all(torch.equal(o, o1) and torch.equal(s, s1) for o, s in many)
+    io, terms, state = tolerances("bf16", d, max(lens), True)
+    o2, s2 = binding.Vda(d, "bf16", flags=binding.VDN_FLAG_FORCE_SIMT).token_scan(**x, cu_seqlens=cu)
+    # token by token of each head: the largest difference of a row counts, not the mean over all
+    off = (o1.double() - o2.double()).norm(dim=-1) / o2.double().norm(dim=(0, 2))[None] * n ** 0.5
+    assert float(off.max()) <= 8 * (io + terms)          # rows are up to a few times the mean row
+    assert rel(s1, np64(s2)) <= 2 * state
+
+
+def test_scan_takes_the_kernels_its_sizes_call_for():
+    """Short sequences token by token, longer ones in chunks, few long ones in parts."""
+    d, h = 128, 2
+    vda, plain = binding.Vda(d, "bf16"), binding.Vda(d, "bf16", flags=binding.VDN_FLAG_FORCE_SIMT)
+    for n, launches in ((2, 1), (20, 1), (300, 2), (3000, 4)):
+        x = draw(n, h, h, d, "bf16")
+        vda.token_scan(**x)
+        plain.token_scan(**x)
+        assert vda.launch_count() == launches and plain.launch_count() == 1
 
 
 def test_scan_of_no_tokens():
