@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -75,7 +76,9 @@ class VdnRotaryParams(ctypes.Structure):
                 ("k_out_stride", ctypes.c_int64)]
 
 
-_TOKEN_PARAMS_SIZE, _ROTARY_PARAMS_SIZE = ctypes.sizeof(VdnTokenParams), ctypes.sizeof(VdnRotaryParams)
+# the same two structs as packed bytes (the header's layout, no padding anywhere): a third of the time of filling a Structure
+_TOKEN_PARAMS = struct.Struct("=IiiiffQQQQQqqqqq")
+_ROTARY_PARAMS = struct.Struct("=IIiiiiifQQQQQqqqq")
 
 
 class VdnError(RuntimeError):
@@ -120,14 +123,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.vdn_vda_workspace_bytes_opt.restype = sz
     lib.vdn_vda_prepare.argtypes = [vp, vp, vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnPrepParams), vp]
     lib.vdn_vda_prepare.restype = ci
-    tok, i64 = ctypes.POINTER(VdnTokenParams), ctypes.c_longlong
+    tok, i64 = vp, ctypes.c_longlong        # parameter structs: packed bytes, or byref of the Structure
     lib.vdn_vda_token_scan_workspace_bytes.argtypes = [vp, i64, tok]
     lib.vdn_vda_token_scan_workspace_bytes.restype = sz
     lib.vdn_vda_token_scan.argtypes = [vp, vp, vp, vp, vp, vp, i64, tok, vp, sz, vp]
     lib.vdn_vda_token_scan.restype = ci
     lib.vdn_vda_token_step.argtypes = [vp, vp, vp, vp, vp, vp, ci, ci, tok, vp]
     lib.vdn_vda_token_step.restype = ci
-    lib.vdn_vda_rotate.argtypes = [vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnRotaryParams), vp]
+    lib.vdn_vda_rotate.argtypes = [vp, vp, vp, vp, vp, *shape, vp, vp]
     lib.vdn_vda_rotate.restype = ci
     lib.vdn_vda_forward_host.argtypes = fwd_args
     lib.vdn_vda_forward_host.restype = ci
@@ -276,22 +279,23 @@ def _require_rows(name, x, lead, heads, d, dtype, on_cuda, device_index):
     return step
 
 
-def _rows(name, x, shape, dtype, device, on_cuda, device_index):
+def _rows(name, x, shape, dtype, on_cuda, device_index):
     """_require_rows for a tensor that in all likelihood is dense and right: one glance, the words only if it is not."""
-    if x is not None and x.shape == shape and x.dtype is dtype and x.device == device and x.is_contiguous():
+    if x is not None and x.shape == shape and x.dtype is dtype and x.get_device() == (device_index if on_cuda else -1) \
+            and x.is_contiguous():
         return shape[-2] * shape[-1]
     return _require_rows(name, x, shape[:-2], shape[-2], shape[-1], dtype, on_cuda, device_index)
 
 
-def _dense(name, x, shape, dtype, device, on_cuda, device_index):
-    if x is None or x.shape != shape or x.dtype is not dtype or x.device != device or not x.is_contiguous():
+def _dense(name, x, shape, dtype, on_cuda, device_index):
+    if x is None or x.shape != shape or x.dtype is not dtype or x.get_device() != (device_index if on_cuda else -1) \
+            or not x.is_contiguous():
         _require(name, x, shape, dtype, on_cuda, device_index)
 
 
 def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=None, log_alpha=None, on_cuda=True):
     """Checks the token tensors of token_scan / token_step: q, k [..., Hk, d], v, out [..., H, d], beta, log_alpha [..., H].
     Returns (leading shape, H, Hk, strides of q, k, v, out)."""
-    import torch
     if v is None or v.dim() < 3:
         raise ValueError("v must have shape [tokens, heads, d]")
     if q is None or q.dim() != v.dim():
@@ -302,14 +306,24 @@ def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=Non
         raise ValueError(f"v must have head dimension {d_handle}, got {d}")
     if H == 0 or Hk == 0 or H % Hk:
         raise ValueError(f"q must have a number of heads that divides the {H} of v, got {Hk}")
-    dev = torch.device("cuda", device_index) if on_cuda else v.device
-    ks, f32, rest = (*lead, Hk, d), torch.float32, (dev, on_cuda, device_index)
-    strides = [_rows("q", q, ks, io_dtype, *rest), _rows("k", k, ks, io_dtype, *rest), _rows("v", v, vs, io_dtype, *rest),
-               H * d if out is None else _rows("out", out, vs, io_dtype, *rest)]
-    _dense("beta", beta, (*lead, H), f32, *rest)
+    ks, gates = (*lead, Hk, d), (*lead, H)
+    strides = (_rows("q", q, ks, io_dtype, on_cuda, device_index), _rows("k", k, ks, io_dtype, on_cuda, device_index),
+               _rows("v", v, vs, io_dtype, on_cuda, device_index),
+               H * d if out is None else _rows("out", out, vs, io_dtype, on_cuda, device_index))
+    f32 = _float32()
+    _dense("beta", beta, gates, f32, on_cuda, device_index)
     if log_alpha is not None:
-        _dense("log_alpha", log_alpha, (*lead, H), f32, *rest)
+        _dense("log_alpha", log_alpha, gates, f32, on_cuda, device_index)
     return lead, H, Hk, strides
+
+
+def _float32():
+    import torch
+    return torch.float32
+
+
+def _ptr(x):
+    return x.data_ptr() if x is not None else 0
 
 
 def _current_raw_stream(torch, device):
@@ -486,34 +500,32 @@ class Vda:
         and that of forward(s0=...); `state` may be s0 itself.  Rows behind the last sequence are not written: a fresh `out`
         holds whatever was there.
         """
-        torch = self._torch
-        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
+        torch, dev = self._torch, self.device
+        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, dev, q, k, v, beta, out, log_alpha)
         if len(lead) != 1:
             raise ValueError("v must have shape [tokens, heads, d]")
-        n, d, S, dev = lead[0], self.d, 1, self._dev
+        n, d, S = lead[0], self.d, 1
         if cu_seqlens is not None:
             if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 2:
                 raise ValueError("cu_seqlens must have shape [sequences + 1]")
             S = cu_seqlens.numel() - 1
-            _dense("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, dev, True, self.device)
+            _dense("cu_seqlens", cu_seqlens, (S + 1,), torch.int32, True, dev)
         shape = (S, H, d, d)
         if s0 is not None:
-            _dense("s0", s0, shape, torch.float32, dev, True, self.device)
+            _dense("s0", s0, shape, torch.float32, True, dev)
         streams = self._streams(stream)
         if out is None:
             out = self._new(streams, (n, H, d), self.torch_dtype)
         if state is None:
             state = self._new(streams, shape, torch.float32)
         else:
-            _dense("state", state, shape, torch.float32, dev, True, self.device)
-        p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnTokenParams(_TOKEN_PARAMS_SIZE, H, Hk, S, scale, l2_eps, p(cu_seqlens), None, p(log_alpha),
-                             p(s0), state.data_ptr(), 0, *st)
-        ref = ctypes.byref(prm)
-        need = self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, ref)
+            _dense("state", state, shape, torch.float32, True, dev)
+        prm = _TOKEN_PARAMS.pack(_TOKEN_PARAMS.size, H, Hk, S, scale, l2_eps, _ptr(cu_seqlens), 0, _ptr(log_alpha), _ptr(s0),
+                                 state.data_ptr(), 0, *st)
+        need = self.lib.vdn_vda_token_scan_workspace_bytes(self.h, n, prm)
         ws = self._new(streams, (need,), torch.uint8) if need else None
-        r = self.lib.vdn_vda_token_scan(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), n, ref,
-                                        p(ws), need, streams[0])
+        r = self.lib.vdn_vda_token_scan(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), n, prm,
+                                        _ptr(ws), need, streams[0])
         if r:
             self._check(r)
         return out, state
@@ -525,25 +537,24 @@ class Vda:
         (float); index int32 [R] (CUDA): each request's slot, None: request r has slot r.  Requests with an index outside
         the pool are padding: their rows of `out` are not written.
         """
-        torch = self._torch
-        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, self.device, q, k, v, beta, out, log_alpha)
+        torch, dev = self._torch, self.device
+        lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, dev, q, k, v, beta, out, log_alpha)
         if len(lead) > 2 or (len(lead) == 2 and lead[1] == 0):
             raise ValueError("v must have shape [requests, heads, d] or [requests, tokens, heads, d]")
-        R, per, d, dev = lead[0], lead[1] if len(lead) == 2 else 1, self.d, self._dev
+        R, per, d = lead[0], lead[1] if len(lead) == 2 else 1, self.d
         if state is None or state.dim() != 4:
             raise ValueError("state must have shape [slots, heads, d, d]")
         slots = state.shape[0]
-        _dense("state", state, (slots, H, d, d), torch.float32, dev, True, self.device)
+        _dense("state", state, (slots, H, d, d), torch.float32, True, dev)
         if index is not None:
-            _dense("index", index, (R,), torch.int32, dev, True, self.device)
+            _dense("index", index, (R,), torch.int32, True, dev)
         streams = self._streams(stream)
         if out is None:
             out = self._new(streams, (*lead, H, d), self.torch_dtype)
-        p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnTokenParams(_TOKEN_PARAMS_SIZE, H, Hk, 0, scale, l2_eps, None, p(index), p(log_alpha), None,
-                             state.data_ptr(), slots, *st)
+        prm = _TOKEN_PARAMS.pack(_TOKEN_PARAMS.size, H, Hk, 0, scale, l2_eps, 0, _ptr(index), _ptr(log_alpha), 0, state.data_ptr(),
+                                 slots, *st)
         r = self.lib.vdn_vda_token_step(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), R, per,
-                                        ctypes.byref(prm), streams[0])
+                                        prm, streams[0])
         if r:
             self._check(r)
         return out
@@ -557,39 +568,38 @@ class Vda:
         norm_eps > 0 each head is RMS-normalised first (weights [d], float).  `out` = optional (q_out, k_out); each may be
         its input.  Returns (q', k').
         """
-        torch = self._torch
+        torch, dev, io = self._torch, self.device, self.torch_dtype
         if q is None or q.dim() != 5:
             raise ValueError("q must have shape [B, T, F, H, d]")
         shape = tuple(q.shape)
         B, T, F, H, d = shape
-        io, rest = self.torch_dtype, (self._dev, True, self.device)
-        qs, ks, Hk = _rows("q", q, shape, io, *rest), 0, 0
+        qs, ks, Hk = _rows("q", q, shape, io, True, dev), 0, 0
         kshape = None
         if k is not None:
             if k.dim() != 5:
                 raise ValueError("k must have shape [B, T, F, Hk, d]")
             Hk = k.shape[3]
             kshape = (B, T, F, Hk, d)
-            ks = _rows("k", k, kshape, io, *rest)
+            ks = _rows("k", k, kshape, io, True, dev)
         if freq is None or freq.dim() != 1:
             raise ValueError("freq must have shape [pairs]")
         n = freq.shape[0]
-        _dense("freq", freq, (n,), torch.float64, *rest)
-        _dense("axis", axis, (n,), torch.int32, *rest)
+        _dense("freq", freq, (n,), torch.float64, True, dev)
+        _dense("axis", axis, (n,), torch.int32, True, dev)
         if positions is not None:
-            _dense("positions", positions, (3, B * T * F), torch.int32, *rest)
+            _dense("positions", positions, (3, B * T * F), torch.int32, True, dev)
         elif Y is None or X is None:
             raise ValueError("either Y and X or positions are needed")
         if q_weight is not None:
-            _dense("q_weight", q_weight, (d,), torch.float32, *rest)
+            _dense("q_weight", q_weight, (d,), torch.float32, True, dev)
         if k_weight is not None:
-            _dense("k_weight", k_weight, (d,), torch.float32, *rest)
+            _dense("k_weight", k_weight, (d,), torch.float32, True, dev)
         qo, ko = out if out is not None else (None, None)
         streams = self._streams(stream)
         if qo is None:
             qo, qos = self._new(streams, shape, io), H * d
         else:
-            qos = _rows("q_out", qo, shape, io, *rest)
+            qos = _rows("q_out", qo, shape, io, True, dev)
         kos = Hk * d
         if k is None:
             if ko is not None:
@@ -597,12 +607,11 @@ class Vda:
         elif ko is None:
             ko = self._new(streams, kshape, io)
         else:
-            kos = _rows("k_out", ko, kshape, io, *rest)
-        p = lambda x: x.data_ptr() if x is not None else None
-        prm = VdnRotaryParams(_ROTARY_PARAMS_SIZE, (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0),
-                              n, Hk, Y or 0, X or 0, t0, norm_eps, freq.data_ptr(), axis.data_ptr(), p(positions), p(q_weight),
-                              p(k_weight), qs, ks, qos, kos)
-        r = self.lib.vdn_vda_rotate(self.h, q.data_ptr(), p(k), qo.data_ptr(), p(ko), B, T, F, H, d, ctypes.byref(prm), streams[0])
+            kos = _rows("k_out", ko, kshape, io, True, dev)
+        prm = _ROTARY_PARAMS.pack(_ROTARY_PARAMS.size, (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0),
+                                  n, Hk, Y or 0, X or 0, t0, norm_eps, freq.data_ptr(), axis.data_ptr(), _ptr(positions),
+                                  _ptr(q_weight), _ptr(k_weight), qs, ks, qos, kos)
+        r = self.lib.vdn_vda_rotate(self.h, q.data_ptr(), _ptr(k), qo.data_ptr(), _ptr(ko), B, T, F, H, d, prm, streams[0])
         if r:
             self._check(r)
         return qo, ko

@@ -22,18 +22,18 @@ def check(x, **kw):
 
 
 def test_matching_tensors_pass():
-    assert check(good()) == ((N,), H, HK, [HK * D, HK * D, H * D, H * D])
+    assert check(good()) == ((N,), H, HK, (HK * D, HK * D, H * D, H * D))
     assert check(good((3, 2)))[0] == (3, 2)
     x = good()
     x["out"] = x["log_alpha"] = None
-    assert check(x)[3] == [HK * D, HK * D, H * D, H * D]
+    assert check(x)[3] == (HK * D, HK * D, H * D, H * D)
 
 
 def test_slices_of_one_projected_tensor_pass_with_their_stride():
     both = torch.zeros(3, 2, 2 * HK + H, D, dtype=torch.bfloat16)
     x = good((3, 2))
     x["q"], x["k"], x["v"] = both[:, :, :HK], both[:, :, HK:2 * HK], both[:, :, 2 * HK:]
-    assert check(x)[3] == [(2 * HK + H) * D] * 3 + [H * D]
+    assert check(x)[3] == ((2 * HK + H) * D,) * 3 + (H * D,)
     x["q"] = both[:, :1, :HK].expand(3, 2, HK, D)                # one token for two: not evenly spaced
     with pytest.raises(ValueError, match="q"):
         check(x)
@@ -93,3 +93,11 @@ def test_struct_sizes_match_the_header(tmp_path):
     subprocess.run(["gcc", "-std=c99", f"-I{root}/include", str(src), "-o", str(tmp_path / "s")], check=True)
     got = subprocess.run([str(tmp_path / "s")], capture_output=True, text=True, check=True).stdout.split()
     assert [int(x) for x in got] == [ctypes.sizeof(binding.VdnTokenParams), ctypes.sizeof(binding.VdnRotaryParams)]
+    assert [int(x) for x in got] == [binding._TOKEN_PARAMS.size, binding._ROTARY_PARAMS.size]
+
+
+def test_packed_structs_have_the_fields_of_the_structures():
+    for cls, packed in ((binding.VdnTokenParams, binding._TOKEN_PARAMS), (binding.VdnRotaryParams, binding._ROTARY_PARAMS)):
+        values = [1.5 if t is ctypes.c_float else i + 1 for i, (_, t) in enumerate(cls._fields_)]
+        x = cls.from_buffer_copy(packed.pack(*values))
+        assert [getattr(x, n) for n, _ in cls._fields_] == values
