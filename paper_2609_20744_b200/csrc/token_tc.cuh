@@ -577,18 +577,10 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // their own barriers), one issues the MMAs of the recurrence and one those of the results, sixteen warps own the state (four
 // threads a row: 32 key channels each), four write out.
 //
-// Few long sequences would leave most SMs idle.  The rule is linear in the state, S_out = S_in M + J over any stretch, and the rows
-// of S go their own ways, so M is what the same recurrence makes of the rows of the identity when nothing is written
-// (V = 0).  A sequence is then cut into parts: TOKEN_COMPOSE runs all parts but the last side by side, from zero (J) and
-// from the identity (M); token_join_kernel passes the state along the parts; TOKEN_FULL runs all parts from the states they
-// enter with.  About three times the arithmetic, for a chain as short as the SMs allow.
-enum { TOKEN_FULL = 0, TOKEN_COMPOSE = 1 };
-
 struct TokenChain {
   static constexpr int STATE_WARPS = 16, OUT_WARPS = 4;
   static constexpr int RESULT_WARP = 2 + STATE_WARPS + OUT_WARPS;
   static constexpr int THREADS = 32 * (RESULT_WARP + 1);
-  static constexpr int threads(int mode) { return mode == 0 ? THREADS : 64 + 32 * STATE_WARPS; }
   static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 90112;
   static constexpr int STAGE = 91136;
   static constexpr int OFF_O = 2 * STAGE;             // two tiles of results
@@ -598,7 +590,6 @@ struct TokenChain {
   static constexpr uint32_t S_HI = 0, S_LO = 64, DS = 128, D_K = 256, X_HI = 320, X_LO = 352, D_Q = 384, D_O = 448;
 };
 
-template <int MODE>
 __global__ void __launch_bounds__(TokenChain::THREADS, 1)
 token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ,
                    const __grid_constant__ CUtensorMap tmV, const TokenTcArgs a, tc::DevStatus ds) {
@@ -611,12 +602,8 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const TokenArgs& t = a.t;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   let_next_kernel_start();
-  constexpr bool WRITE = MODE == TOKEN_FULL;          // results are wanted
   // this CTA's rows, first state and what becomes of its last one
-  int bid = (int)blockIdx.x;
-  bool from_identity = false;                         // TOKEN_COMPOSE: the half that makes M
-  if constexpr (MODE == TOKEN_COMPOSE) { from_identity = bid & 1; bid >>= 1; }
-  const int h = bid % t.H, x = bid / t.H;
+  const int h = (int)blockIdx.x % t.H, x = (int)blockIdx.x / t.H;
   const int seq = a.part > 0 ? token_seq_of(t, x, a.part) : x;
   long long start;
   int len;
@@ -624,17 +611,9 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   const int parts = token_parts(len, a.part);
   const int pos = a.part > 0 ? x - ((int)(start / a.part) + seq) : 0;
   if (pos < 0 || pos >= parts) { wait_for_kernel_before(); return; }   // a place that no part has
-  const float* first = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) : nullptr;
-  float* last = nullptr;
-  const size_t comp = ((size_t)x * t.H + h) * (D * D);
-  if constexpr (MODE == TOKEN_COMPOSE) {
-    if (pos + 1 == parts || (from_identity && pos == 0)) { wait_for_kernel_before(); return; }   // nobody asks for these
-    if (pos > 0) first = nullptr;
-    last = (from_identity ? a.comp_m : a.comp_j) + comp;
-  } else {
-    if (parts > 1) first = a.enter + comp;
-    if (pos + 1 == parts && t.state_out) last = t.state_out + ((size_t)seq * t.H + h) * (D * D);
-  }
+  const float* first = parts > 1 ? a.enter + ((size_t)x * t.H + h) * (D * D)
+                                 : t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) : nullptr;
+  float* last = pos + 1 == parts && t.state_out ? t.state_out + ((size_t)seq * t.H + h) * (D * D) : nullptr;
   const long long place0 = start / C + seq + (long long)pos * (a.part / C);
   if (parts > 1) {
     start += (long long)pos * a.part;
@@ -659,7 +638,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
     for (int st = 0; st < 2; ++st) {
       for (int g = 0; g < 3; ++g) {
         mbar_init(FULL(g, st), 1);
-        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + (WRITE ? S::OUT_WARPS : 0) : g == E && WRITE ? 2 : 1);
+        mbar_init(FREE(g, st), g == V ? S::STATE_WARPS + S::OUT_WARPS : g == E ? 2 : 1);
       }
     }
     for (int i = 0; i < 2; ++i) {
@@ -693,23 +672,21 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const uint32_t at = base + st * S::STAGE, par = ((s >> 1) & 1) ^ 1;
         const size_t unit = (size_t)(place0 + s) * t.H + h;
         if (s >= 2 && !(ok = mbar_wait(FREE(KQ, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(KQ, st), WRITE ? 32768 : 16384);
+        mbar_arrive_expect_tx(FULL(KQ, st), 32768);
         tma_load_2d(at + S::OFF_K, &tmK, FULL(KQ, st), hk * 128, row);
         tma_load_2d(at + S::OFF_K + 8192, &tmK, FULL(KQ, st), hk * 128 + 64, row);
-        if constexpr (WRITE) {
-          tma_load_2d(at + S::OFF_Q, &tmQ, FULL(KQ, st), hk * 128, row);
-          tma_load_2d(at + S::OFF_Q + 8192, &tmQ, FULL(KQ, st), hk * 128 + 64, row);
-        }
+        tma_load_2d(at + S::OFF_Q, &tmQ, FULL(KQ, st), hk * 128, row);
+        tma_load_2d(at + S::OFF_Q + 8192, &tmQ, FULL(KQ, st), hk * 128 + 64, row);
         issued[KQ] = s + 1;
         if (s >= 2 && !(ok = mbar_wait(FREE(V, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(V, st), (from_identity ? 0 : 16384) + TokenTc::F_BYTES);
-        if (!from_identity) tma_load_2d(at + S::OFF_V, &tmV, FULL(V, st), h * 128, row);
+        mbar_arrive_expect_tx(FULL(V, st), 16384 + TokenTc::F_BYTES);
+        tma_load_2d(at + S::OFF_V, &tmV, FULL(V, st), h * 128, row);
         bulk_load(at + S::OFF_F, a.f + unit * TokenTc::F_BYTES, TokenTc::F_BYTES, FULL(V, st));
         issued[V] = s + 1;
         if (s >= 2 && !(ok = mbar_wait(FREE(E, st), par, wc))) break;
-        mbar_arrive_expect_tx(FULL(E, st), TokenTc::E_BYTES + (WRITE ? TokenTc::P_BYTES : 0));
+        mbar_arrive_expect_tx(FULL(E, st), TokenTc::E_BYTES + TokenTc::P_BYTES);
         bulk_load(at + S::OFF_E, a.e + unit * TokenTc::E_BYTES, TokenTc::E_BYTES, FULL(E, st));
-        if constexpr (WRITE) bulk_load(at + S::OFF_P, a.p + unit * TokenTc::P_BYTES, TokenTc::P_BYTES, FULL(E, st));
+        bulk_load(at + S::OFF_P, a.p + unit * TokenTc::P_BYTES, TokenTc::P_BYTES, FULL(E, st));
         issued[E] = s + 1;
       }
       // Whoever gives up, and when: copies in flight get a bounded chance to land before the CTA retires.
@@ -741,7 +718,6 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         }
         if (!ok) break;
         mma_commit(DK_FULL);
-        if constexpr (!WRITE) mma_commit(FREE(KQ, st));
         if (!mbar_wait(FULL(E, st), par, wc)) break;
         // X^T E^T, 32 tokens at a time: low X high E, high X low E, high X high E
 #pragma unroll
@@ -773,10 +749,6 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         const float4 x = src ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
         sv[e] = x.x; sv[e + 1] = x.y; sv[e + 2] = x.z; sv[e + 3] = x.w;
       }
-      if (from_identity) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) sv[e] = sl * 32 + e == row ? 1.f : 0.f;
-      }
     }
     // columns 16 half .. of the thread's 32: one K step of the product
     auto publish = [&](int half) {
@@ -806,13 +778,13 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int at = (j >> 2) * 32 + (j & 3) * 2;
-        vv[j] = from_identity ? 0u : (uint32_t)v[at * D] | ((uint32_t)v[(at + 1) * D] << 16);
+        vv[j] = (uint32_t)v[at * D] | ((uint32_t)v[(at + 1) * D] << 16);
       }
       const float whole = f[128];
       if (!warp_wait(DK_FULL, s & 1)) break;
       tc_fence_after_sync();
       // (X^T P^T of the step before, which another thread issues, must be done with the old parts of X)
-      if (WRITE && s > 0) {
+      if (s > 0) {
         if (!warp_wait(DO_FULL, (s - 1) & 1)) break;
         tc_fence_after_sync();
       }
@@ -862,7 +834,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         tmem_wait_ld();
 #pragma unroll
         for (int e = 0; e < 16; ++e) sv[half * 16 + e] = fmaf(whole, sv[half * 16 + e], d[e]);
-        if (WRITE && half == 0) {                     // S Q^T is done with the old parts of S (and, at the end, with Q's memory)
+        if (half == 0) {                     // S Q^T is done with the old parts of S (and, at the end, with Q's memory)
           if (!(ok = warp_wait(S_FREE, s & 1))) break;
           tc_fence_after_sync();
         }
@@ -885,7 +857,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         *reinterpret_cast<float4*>(last + (size_t)r * D + lane * 4) = *reinterpret_cast<const float4*>(bp + r * 512 + ((lane ^ (r & 31)) << 4));
       }
     }
-  } else if (WRITE && warp == S::RESULT_WARP) {
+  } else if (warp == S::RESULT_WARP) {
     // ------------------------------------------------------------------ MMAs of the results
     // Their own issuer: in the gaps that the recurrence leaves, and what they wait for (the accumulators being read) does not
     // hold the recurrence up.
@@ -911,7 +883,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         mma_commit(FREE(E, st));
       }
     }
-  } else if constexpr (WRITE) {
+  } else {
     // ------------------------------------------------------------------ output
     // Lanes are value channels: the tile is turned round in shared memory and leaves as whole rows of 256 bytes.
     // (Stored from here, 64 bytes a warp and token, it took 3300 cycles a chunk and held up the MMAs.)
@@ -962,6 +934,273 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
                                                                      __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x7632));
       }
       out += C * t.out_stride;
+    }
+  }
+
+  // ------------------------------------------------------------------ teardown
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- parts of a sequence
+// Few long sequences would leave most SMs idle.  The rule is linear in the state, S_out = S_in M + J over any stretch, and the rows
+// of S go their own ways, so M is what the same recurrence makes of the rows of the identity when nothing is written
+// (V = 0).  A sequence is then cut into parts: token_compose_kernel runs all parts but the last side by side, from zero (J; the
+// first part from the sequence's first state) and from the identity (M); token_join_kernel passes the state along the parts;
+// token_chain_kernel runs all parts from the states they enter with.
+//
+// J and M of a part share a CTA: the same keys and operators, and two independent chains, so that the MMAs of one run
+// while the state warps work on the other -- S K^T of J, of M, X^T E^T of J, of M, and under each the state warps' turn
+// that it does not depend on.  Measured: FIXME.  Tensor memory holds both because each chain has two
+// regions only: the parts of S, which X^T E^T overwrites (they are used up by then) and whose place the thread that owns a piece of
+// the new state fills again, and S K^T, which the parts of X replace in the same way.
+struct TokenCompose {
+  static constexpr int STATE_WARPS = 16, THREADS = 64 + 32 * STATE_WARPS, STAGES = 3;
+  static constexpr int OFF_K = 0, OFF_V = 16384, OFF_E = 32768, OFF_F = 65536, STAGE = 66560;
+  static constexpr int OFF_BAR = STAGES * STAGE;
+  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  // columns of a chain: 128 of S or X^T E^T (32 for each quarter of the key channels: 16 high words, 16 low ones), 64 of S K^T
+  // or X (16 for each 16 tokens: 8 high words, 8 low ones)
+  static constexpr uint32_t CHAIN = 192, D_K = 128;
+};
+
+__global__ void __launch_bounds__(TokenCompose::THREADS, 1)
+token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const TokenTcArgs a,
+                     tc::DevStatus ds) {
+  using namespace tc;
+  using S = TokenCompose;
+  constexpr int C = TokenTc::C, D = TokenTc::D;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* bp = smem_dyn + (base - smem_u32(smem_dyn));
+  const TokenArgs& t = a.t;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  let_next_kernel_start();
+  const int h = (int)blockIdx.x % t.H, x = (int)blockIdx.x / t.H;
+  const int seq = token_seq_of(t, x, a.part);
+  long long start;
+  int len;
+  token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
+  const int parts = token_parts(len, a.part);
+  const int pos = x - ((int)(start / a.part) + seq);
+  if (pos < 0 || pos + 1 >= parts) { wait_for_kernel_before(); return; }   // no part, or one that nobody follows
+  const float* first = pos == 0 && t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) : nullptr;
+  const size_t comp = ((size_t)x * t.H + h) * (D * D);
+  const long long place0 = start / C + seq + (long long)pos * (a.part / C);
+  start += (long long)pos * a.part;
+  const int steps = a.part / C;                       // all parts but the last are whole
+
+  const uint32_t bar0 = base + S::OFF_BAR;
+  auto FULL = [&](int st) { return bar0 + 8u * st; };
+  auto FREE = [&](int st) { return bar0 + 8u * (S::STAGES + st); };
+  // of chain c (0: J, 1: M)
+  auto S_READY = [&](int c) { return bar0 + 64u + 8u * c; };
+  auto DK_FULL = [&](int c) { return bar0 + 80u + 8u * c; };
+  auto X_READY = [&](int c) { return bar0 + 96u + 8u * c; };
+  auto DS_FULL = [&](int c) { return bar0 + 112u + 8u * c; };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bp + S::OFF_BAR + 128);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + S::OFF_BAR + 136);
+  const WaitCtx wc(abort_flag, ds);
+  auto warp_wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, wc)) != 0; };
+
+  if (threadIdx.x == 0) {
+    for (int st = 0; st < S::STAGES; ++st) { mbar_init(FULL(st), 1); mbar_init(FREE(st), 1 + S::STATE_WARPS); }
+    for (int c = 0; c < 2; ++c) {
+      mbar_init(S_READY(c), S::STATE_WARPS);
+      mbar_init(X_READY(c), S::STATE_WARPS);
+      mbar_init(DK_FULL(c), 1);
+      mbar_init(DS_FULL(c), 1);
+    }
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tmK); tma_prefetch_desc(&tmV);
+  }
+  if (warp == 1) {
+    tmem_alloc(smem_u32(tmem_slot), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  wait_for_kernel_before();
+  const uint32_t tmem = *tmem_slot;
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ loads
+    if (lane == 0) {
+      const int ch = h / (t.H / t.Hk) * 128;
+      uint32_t issued = 0;
+      for (int s = 0; s < steps; ++s) {
+        const int st = s % S::STAGES, row = (int)(start + (long long)s * C);
+        if (s >= S::STAGES && !mbar_wait(FREE(st), ((s / S::STAGES) & 1) ^ 1, wc)) break;
+        const uint32_t at = base + st * S::STAGE;
+        const size_t unit = (size_t)(place0 + s) * t.H + h;
+        mbar_arrive_expect_tx(FULL(st), 32768 + TokenTc::E_BYTES + TokenTc::F_BYTES);
+        tma_load_2d(at + S::OFF_K, &tmK, FULL(st), ch, row);
+        tma_load_2d(at + S::OFF_K + 8192, &tmK, FULL(st), ch + 64, row);
+        tma_load_2d(at + S::OFF_V, &tmV, FULL(st), h * 128, row);
+        bulk_load(at + S::OFF_E, a.e + unit * TokenTc::E_BYTES, TokenTc::E_BYTES, FULL(st));
+        bulk_load(at + S::OFF_F, a.f + unit * TokenTc::F_BYTES, TokenTc::F_BYTES, FULL(st));
+        issued = s + 1;
+      }
+      mbar_drain_ring(FULL(0), S::STAGES, issued);    // copies in flight get a bounded chance to land before the CTA retires
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMAs
+    if (lane == 0) {
+      constexpr uint32_t id64 = make_idesc_bf16(128, 64, false, false), id128 = make_idesc_bf16(128, 128, false, false);
+      const uint64_t dk0 = make_smem_desc(base + S::OFF_K, 16, 1024), de0 = make_smem_desc(base + S::OFF_E, 16, 1024);
+      bool ok = true;
+      for (int s = 0; s < steps && ok; ++s) {
+        const int st = s % S::STAGES;
+        const uint64_t off = (uint64_t)(st * (S::STAGE >> 4)), dk = dk0 + off, de = de0 + off;
+        if (!mbar_wait(FULL(st), (s / S::STAGES) & 1, wc)) break;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (!(ok = ok && mbar_wait(S_READY(c), s & 1, wc))) break;
+          tc_fence_after_sync();
+          const uint32_t tc0 = tmem + c * S::CHAIN;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const uint32_t sp = tc0 + (k >> 1) * 32 + (k & 1) * 8;
+            mma_bf16_ts(tc0 + S::D_K, sp + 16, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+            mma_bf16_ts(tc0 + S::D_K, sp, dk + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
+          }
+          mma_commit(DK_FULL(c));
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (!(ok = ok && mbar_wait(X_READY(c), s & 1, wc))) break;
+          tc_fence_after_sync();
+          const uint32_t tc0 = tmem + c * S::CHAIN, xp = tc0 + S::D_K;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            mma_bf16_ts(tc0, xp + k * 16 + 8, de + k * 2, id128, k ? 1u : 0u);
+            mma_bf16_ts(tc0, xp + k * 16, de + ((TokenTc::E_PART >> 4) + k * 2), id128, 1u);
+            mma_bf16_ts(tc0, xp + k * 16, de + k * 2, id128, 1u);
+          }
+          mma_commit(DS_FULL(c));
+        }
+        if (ok) mma_commit(FREE(st));
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------ state
+    const int qd = warp & 3, sl = (warp - 2) >> 2;    // lane quarter; quarter of the key channels and of the chunk's tokens
+    const int row = qd * 32 + lane;                   // value channel
+    const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
+    float sv[2][32];                                  // of both chains: S[row][32 sl ..]
+    {
+      const float* src = first ? first + (size_t)row * D + sl * 32 : nullptr;
+#pragma unroll
+      for (int e = 0; e < 32; e += 4) {
+        const float4 y = src ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        sv[0][e] = y.x; sv[0][e + 1] = y.y; sv[0][e + 2] = y.z; sv[0][e + 3] = y.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 32; ++e) sv[1][e] = sl * 32 + e == row ? 1.f : 0.f;
+    }
+    auto publish = [&](int c) {
+      const uint32_t at = tl + c * S::CHAIN + sl * 32;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        float hl[16];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t u, v;
+          split2_pair(sv[c][16 * half + 2 * e], sv[c][16 * half + 2 * e + 1], u, v);
+          hl[e] = __uint_as_float(u);
+          hl[8 + e] = __uint_as_float(v);
+        }
+        tmem_st8(at + half * 8, hl);
+        tmem_st8(at + 16 + half * 8, hl + 8);
+      }
+      tmem_wait_st();
+      tc_fence_before_sync();
+      mbar_arrive_warp(S_READY(c));
+    };
+    publish(0);
+    publish(1);
+    bool ok = true;
+    for (int s = 0; s < steps && ok; ++s) {
+      const int st = s % S::STAGES;
+      if (!warp_wait(FULL(st), (s / S::STAGES) & 1)) break;
+      const unsigned short* v = reinterpret_cast<const unsigned short*>(bp + st * S::STAGE + S::OFF_V) + sl * 16 * D + row;
+      const float* f = reinterpret_cast<const float*>(bp + st * S::STAGE + S::OFF_F);
+      const float whole = f[128];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t vv[8];
+        if (c == 0) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) vv[j] = (uint32_t)v[2 * j * D] | ((uint32_t)v[(2 * j + 1) * D] << 16);
+        }
+        if (!(ok = ok && warp_wait(DK_FULL(c), s & 1))) break;
+        tc_fence_after_sync();
+        float y[16], hl[16];
+        const uint32_t at = tl + c * S::CHAIN + S::D_K + sl * 16;
+        tmem_ld16(at, y);
+        tmem_wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+          const float4 fj = *reinterpret_cast<const float4*>(f + sl * 16 + j);
+          const float f4[4] = {fj.x, fj.y, fj.z, fj.w};
+#pragma unroll
+          for (int i = 0; i < 4; i += 2) {
+            const uint32_t w = c == 0 ? vv[(j + i) / 2] : 0u;
+            uint32_t u, l;
+            split2_pair(fmaf(-f4[i], y[j + i], __uint_as_float(w << 16)), fmaf(-f4[i + 1], y[j + i + 1], __uint_as_float(w & 0xFFFF0000u)), u, l);
+            hl[(j + i) / 2] = __uint_as_float(u);
+            hl[8 + (j + i) / 2] = __uint_as_float(l);
+          }
+        }
+        tmem_st16(at, hl);
+        tmem_wait_st();
+        tc_fence_before_sync();
+        mbar_arrive_warp(X_READY(c));
+      }
+      if (!ok) break;
+      mbar_arrive_warp(FREE(st));
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        if (!(ok = ok && warp_wait(DS_FULL(c), s & 1))) break;
+        tc_fence_after_sync();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float d[16];
+          tmem_ld16(tl + c * S::CHAIN + sl * 32 + half * 16, d);
+          tmem_wait_ld();
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sv[c][half * 16 + e] = fmaf(whole, sv[c][half * 16 + e], d[e]);
+        }
+        if (s + 1 < steps) publish(c);
+      }
+    }
+    // whole rows leave through shared memory (the loads of all steps have been used; the first part's M is not wanted)
+    const int tid = (warp - 2) * 32 + lane;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        *reinterpret_cast<float4*>(bp + c * 65536 + row * 512 + (((sl * 8 + e) ^ lane) << 4)) =
+            make_float4(sv[c][4 * e], sv[c][4 * e + 1], sv[c][4 * e + 2], sv[c][4 * e + 3]);
+    }
+    named_barrier_sync(1, 32 * S::STATE_WARPS);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      float* dst = (c == 0 ? a.comp_j : a.comp_m) + comp;
+      if (c == 1 && pos == 0) break;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int r = (tid >> 5) + 16 * e;
+        *reinterpret_cast<float4*>(dst + (size_t)r * D + lane * 4) =
+            *reinterpret_cast<const float4*>(bp + c * 65536 + r * 512 + ((lane ^ (r & 31)) << 4));
+      }
     }
   }
 

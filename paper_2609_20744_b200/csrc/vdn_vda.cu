@@ -1366,10 +1366,10 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (!h->token_attrs_set) {
     VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_prep_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, vdn::TokenPrep::SMEM_BYTES));
-    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel<vdn::TOKEN_FULL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                      vdn::TokenChain::SMEM_BYTES));
-    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_chain_kernel<vdn::TOKEN_COMPOSE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                     vdn::TokenChain::SMEM_BYTES));
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_compose_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                     vdn::TokenCompose::SMEM_BYTES));
     h->token_attrs_set = true;
   }
   const TokenLayout L = make_token_layout(h, t.n_tokens, t.S, t.H);
@@ -1396,15 +1396,15 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   prof_mark(h, st, nk++, "token_prep");
   const vdn::tc::DevStatus ds = dev_status(h);
   if (L.part) {
-    VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel<vdn::TOKEN_COMPOSE>, (unsigned)(2 * L.parts * t.H),
-                                  TC::threads(vdn::TOKEN_COMPOSE), TC::SMEM_BYTES, st, tmK, tmQ, tmV, a, ds));
+    VDN_CUDA(h, launch_overlapped(vdn::token_compose_kernel, (unsigned)(L.parts * t.H), vdn::TokenCompose::THREADS,
+                                  vdn::TokenCompose::SMEM_BYTES, st, tmK, tmV, a, ds));
     prof_mark(h, st, nk++, "token_compose");
     VDN_CUDA(h, launch_overlapped(vdn::token_join_kernel, (unsigned)(t.S * t.H * (128 / vdn::TokenJoin::ROWS)),
                                   vdn::TokenJoin::THREADS, 0, st, a));
     prof_mark(h, st, nk++, "token_join");
   }
-  VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel<vdn::TOKEN_FULL>, (unsigned)(L.parts * t.H), TC::threads(vdn::TOKEN_FULL),
-                                TC::SMEM_BYTES, st, tmK, tmQ, tmV, a, ds));
+  VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel, (unsigned)(L.parts * t.H), TC::THREADS, TC::SMEM_BYTES, st, tmK, tmQ, tmV,
+                                a, ds));
   prof_mark(h, st, nk++, "token_chain");
   h->launches = nk;
   VDN_CUDA(h, cudaGetLastError());
