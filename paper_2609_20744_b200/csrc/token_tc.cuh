@@ -140,6 +140,25 @@ __device__ __forceinline__ void split2_pair(float x0, float x1, uint32_t& hi, ui
   const float r0 = x0 - __uint_as_float(hi << 16), r1 = x1 - __uint_as_float(hi & 0xFFFF0000u);
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(r1), "f"(r0));
 }
+// Two floats at once on the packed fp32 pipe: no faster, but half as many instructions, and these kernels are short of issue slots.
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ void split2_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
+  float x0, x1, r0, r1;
+  f2_unpack(x, x0, x1);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(x1), "f"(x0));
+  f2_unpack(f2_fma(f2_pack(__uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u)), f2_pack(-1.f, -1.f), x), r0, r1);
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(r1), "f"(r0));
+}
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
@@ -1094,16 +1113,17 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     const int qd = warp & 3, sl = (warp - 2) >> 2;    // lane quarter; quarter of the key channels and of the chunk's tokens
     const int row = qd * 32 + lane;                   // value channel
     const uint32_t tl = tmem + ((uint32_t)(qd * 32) << 16);
-    float sv[2][32];                                  // of both chains: S[row][32 sl ..]
+    uint64_t sv[2][16];                               // of both chains: S[row][32 sl ..], two to a register pair
     {
       const float* src = first ? first + (size_t)row * D + sl * 32 : nullptr;
 #pragma unroll
-      for (int e = 0; e < 32; e += 4) {
-        const float4 y = src ? *reinterpret_cast<const float4*>(src + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-        sv[0][e] = y.x; sv[0][e + 1] = y.y; sv[0][e + 2] = y.z; sv[0][e + 3] = y.w;
+      for (int e = 0; e < 16; e += 2) {
+        const float4 y = src ? *reinterpret_cast<const float4*>(src + 2 * e) : make_float4(0.f, 0.f, 0.f, 0.f);
+        sv[0][e] = f2_pack(y.x, y.y);
+        sv[0][e + 1] = f2_pack(y.z, y.w);
       }
 #pragma unroll
-      for (int e = 0; e < 32; ++e) sv[1][e] = sl * 32 + e == row ? 1.f : 0.f;
+      for (int e = 0; e < 16; ++e) sv[1][e] = f2_pack(sl * 32 + 2 * e == row ? 1.f : 0.f, sl * 32 + 2 * e + 1 == row ? 1.f : 0.f);
     }
     auto publish = [&](int c) {
       const uint32_t at = tl + c * S::CHAIN + sl * 32;
@@ -1113,7 +1133,7 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           uint32_t u, v;
-          split2_pair(sv[c][16 * half + 2 * e], sv[c][16 * half + 2 * e + 1], u, v);
+          split2_pair(sv[c][8 * half + e], u, v);
           hl[e] = __uint_as_float(u);
           hl[8 + e] = __uint_as_float(v);
         }
@@ -1154,7 +1174,8 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
           for (int i = 0; i < 4; i += 2) {
             const uint32_t w = c == 0 ? vv[(j + i) / 2] : 0u;
             uint32_t u, l;
-            split2_pair(fmaf(-f4[i], y[j + i], __uint_as_float(w << 16)), fmaf(-f4[i + 1], y[j + i + 1], __uint_as_float(w & 0xFFFF0000u)), u, l);
+            split2_pair(f2_fma(f2_pack(-f4[i], -f4[i + 1]), f2_pack(y[j + i], y[j + i + 1]),
+                               f2_pack(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u))), u, l);
             hl[(j + i) / 2] = __uint_as_float(u);
             hl[8 + (j + i) / 2] = __uint_as_float(l);
           }
@@ -1170,14 +1191,11 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
       for (int c = 0; c < 2; ++c) {
         if (!(ok = ok && warp_wait(DS_FULL(c), s & 1))) break;
         tc_fence_after_sync();
+        float d[32];
+        tmem_ld32(tl + c * S::CHAIN + sl * 32, d);
+        tmem_wait_ld();
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float d[16];
-          tmem_ld16(tl + c * S::CHAIN + sl * 32 + half * 16, d);
-          tmem_wait_ld();
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sv[c][half * 16 + e] = fmaf(whole, sv[c][half * 16 + e], d[e]);
-        }
+        for (int e = 0; e < 16; ++e) sv[c][e] = f2_fma(f2_pack(whole, whole), sv[c][e], f2_pack(d[2 * e], d[2 * e + 1]));
         if (s + 1 < steps) publish(c);
       }
     }
@@ -1187,8 +1205,8 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
     for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        *reinterpret_cast<float4*>(bp + c * 65536 + row * 512 + (((sl * 8 + e) ^ lane) << 4)) =
-            make_float4(sv[c][4 * e], sv[c][4 * e + 1], sv[c][4 * e + 2], sv[c][4 * e + 3]);
+        *reinterpret_cast<ulonglong2*>(bp + c * 65536 + row * 512 + (((sl * 8 + e) ^ lane) << 4)) =
+            make_ulonglong2(sv[c][2 * e], sv[c][2 * e + 1]);
     }
     named_barrier_sync(1, 32 * S::STATE_WARPS);
 #pragma unroll
