@@ -10,12 +10,13 @@
 // bytes apart, so that a warp's loads and stores of the state cover whole 128-byte lines and a row's two dot products need
 // three shuffle steps.  Two kernels:
 //   token_few_kernel   a few tokens a sequence (one above all): a copy of the states through registers, bound by HBM.
-//   token_walk_kernel  longer sequences: tokens are fetched in batches ahead of their use, what does not depend on the state is
-//                      formed once a batch, and what is left is bound by the latency of a token's step.
+//   token_coef_kernel, token_walk_kernel  longer sequences: what does not depend on the state is formed first, for all tokens;
+//                      what is left is bound by the latency of a step, or by issue slots when all SMs are busy.
 #pragma once
 #include <cuda_bf16.h>
 
 #include "common.cuh"
+#include "tc_common.cuh"
 
 namespace vdn {
 
@@ -137,78 +138,185 @@ __global__ void __launch_bounds__(256, D == 64 ? 5 : 3) token_few_kernel(const T
   }
 }
 
-// One CTA (four warps) to 16 rows of a (sequence, head): a warp to a scheduler, and as many CTAs as rows allow, since a step is a
-// chain of latencies (dot products, shuffles, update).  Four tokens make one step.  With P_i = alpha_1 .. alpha_i and
-// A_ij = alpha_{j+1} .. alpha_i (products, so that nothing is divided), S the state before the four:
+// The kernels of one call overlap at their edges: each lets the next one start early, and each first gets ready and then waits
+// for the one before to be done.  Every thread waits, also of a CTA that has nothing to do: a kernel that did not wait could be
+// done before its predecessor, and its successor would then read unfinished results.
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.  A whole
+// warp looks at 32 offsets at a time: a round trip to memory for 32 sequences, two for a thousand.
+__device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int unit) {
+  int lo = 0, n = t.S;                                // the answer lies in [lo, lo + n), and sequence lo qualifies
+  const int lane = threadIdx.x & 31;
+  while (n > 1) {
+    const int step = (n + 31) / 32;
+    const int s = lo + lane * step;
+    bool fits = false;
+    if (s < lo + n) {
+      long long start;
+      int len;
+      token_range(t.cu_seqlens, s, t.per, t.n_tokens, start, len);
+      fits = start / unit + s <= x;
+    }
+    const unsigned m = __ballot_sync(0xFFFFFFFFu, fits) | 1u;
+    const int k = 31 - __clz(m);
+    n = min(step, lo + n - (lo + k * step));
+    lo += k * step;
+  }
+  return lo;
+}
+
+// Longer sequences: four tokens make one step.  With P_i = alpha_1 .. alpha_i and A_ij = alpha_{j+1} .. alpha_i (products, so that
+// nothing is divided), S the state before the four:
 //        u_i = beta_i (v_i - P_i S k_i - sum_{j<i} A_ij (k_i.k_j) u_j),    o_i = P_i S q_i + sum_{j<=i} A_ij (q_i.k_j) u_j,
 //        S' = P_4 S + sum_j A_4j u_j k_j^T.
-// The coefficients are formed once a batch, a warp to each four tokens.  A row is shared by 16 lanes, which hold two rows each;
-// the sixteen dot products of a step are reduced together, each lane ending with one of them (15 shuffles instead of 64).
-// Measured, d = 128, one sequence: FIXME.
+// The coefficients do not depend on the state: token_coef_kernel forms them for all tokens, twelve numbers each, a warp to four
+// tokens of a head, eight lanes to a token.  (Formed by the walking CTAs, eight of which share a head's tokens at d = 128, they took a
+// fifth of the time.)
+//   [0] beta P r, beta, (i,0), (i,1) of the first sum;  [1] (i,2), A_4i r_i, scale r_q P, P_4;  [2] (i,0) .. (i,3) of the second, times scale
+constexpr int kCoefFloats = 12;
+
+template <typename Tio, int D>
+__global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, float4* coef, long long warps) {
+  const int lane = threadIdx.x & 31, l8 = lane & 7, i4 = lane >> 3;
+  const long long w = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (w >= warps) return;
+  const int h = (int)(w % a.H);
+  const long long place = w / a.H;
+  const int seq = token_seq_of(a, place, 4);
+  long long start;
+  int len;
+  token_range(a.cu_seqlens, seq, a.per, a.n_tokens, start, len);
+  const long long g0 = (place - (start / 4 + seq)) * 4;  // first token of the four, in the sequence
+  if (g0 < 0 || g0 >= len) return;
+  const int n = (int)min(4LL, len - g0);
+  const int hk = h / (a.H / a.Hk);
+  const Tio* kp = static_cast<const Tio*>(a.k) + (start + g0) * a.k_stride + hk * D + l8 * 4;
+  const Tio* qp = static_cast<const Tio*>(a.q) + (start + g0 + i4) * a.q_stride + hk * D + l8 * 4;
+  const bool there = i4 < n;
+  float kk[4] = {0.f, 0.f, 0.f, 0.f}, qk[4] = {0.f, 0.f, 0.f, 0.f}, qq = 0.f;
+  const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto dot = [](float s, const float4& x, const float4& y) { return fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, s)))); };
+#pragma unroll
+  for (int i = 0; i < D / 32; ++i) {
+    const float4 q = there ? load4(qp + i * 32) : none;
+    float4 k[4];
+#pragma unroll
+    for (int o = 0; o < 4; ++o) k[o] = o < n ? load4(kp + o * a.k_stride + i * 32) : none;
+    const float4 own = i4 == 0 ? k[0] : i4 == 1 ? k[1] : i4 == 2 ? k[2] : k[3];
+    qq = dot(qq, q, q);
+#pragma unroll
+    for (int o = 0; o < 4; ++o) { kk[o] = dot(kk[o], own, k[o]); qk[o] = dot(qk[o], q, k[o]); }
+  }
+#pragma unroll
+  for (int m = 1; m < 8; m <<= 1) {
+    qq += __shfl_xor_sync(0xFFFFFFFFu, qq, m);
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+      kk[o] += __shfl_xor_sync(0xFFFFFFFFu, kk[o], m);
+      qk[o] += __shfl_xor_sync(0xFFFFFFFFu, qk[o], m);
+    }
+  }
+  const float own = i4 == 0 ? kk[0] : i4 == 1 ? kk[1] : i4 == 2 ? kk[2] : kk[3];
+  const float rk = a.l2_eps > 0.f ? rsqrtf(own + a.l2_eps) : 1.f;
+  const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
+  const size_t gate = (size_t)(start + g0 + i4) * a.H + h;
+  const float alpha = there && a.log_alpha ? expf(a.log_alpha[gate]) : 1.f, beta = there ? a.beta[gate] : 0.f;
+  float al[4], ro[4];
+#pragma unroll
+  for (int o = 0; o < 4; ++o) {
+    al[o] = __shfl_sync(0xFFFFFFFFu, alpha, o * 8);
+    ro[o] = __shfl_sync(0xFFFFFFFFu, rk, o * 8);
+  }
+  if (l8 == 0 && there) {
+    float first[3], second[4], pi = 1.f, to_end = 1.f;
+#pragma unroll
+    for (int o = 0; o < 4; ++o) {
+      pi *= o <= i4 ? al[o] : 1.f;
+      to_end *= o > i4 ? al[o] : 1.f;
+      float dec = 1.f;                                   // A_{i4, o}
+#pragma unroll
+      for (int m = 0; m < 4; ++m) dec *= m > o && m <= i4 ? al[m] : 1.f;
+      if (o < 3) first[o] = o < i4 ? beta * rk * ro[o] * dec * kk[o] : 0.f;
+      second[o] = o <= i4 ? a.scale * rq * ro[o] * dec * qk[o] : 0.f;
+    }
+    float4* c = coef + gate * (kCoefFloats / 4);
+    c[0] = make_float4(beta * pi * rk, beta, first[0], first[1]);
+    c[1] = make_float4(first[2], to_end * rk, a.scale * rq * pi, pi * to_end);
+    c[2] = make_float4(second[0], second[1], second[2], second[3]);
+  }
+}
+
+// One CTA (four warps, one to a scheduler) to 16 rows of a (sequence, head), as many CTAs as rows allow, since a step is a chain of
+// latencies (dot products, shuffles, update).  A row is shared by 16 lanes, which hold two rows each; the sixteen dot products
+// of a step are reduced together, each lane ending with one of them (15 shuffles instead of 64).  Batches of 16 tokens -- keys,
+// queries, this CTA's values, coefficients -- arrive by four tile copies each, which a fifth warp issues, three batches ahead.
+// Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: FIXME us; a token at a time it took 289.
 template <typename Tio, int D>
 struct TokenWalk {
-  static constexpr int THREADS = 128, ROWS = 16, BATCH = 16;
-  static constexpr int PIECE = 16 / (int)sizeof(Tio);            // elements of a 16-byte copy
-  struct Stage {
+  static constexpr int WALKERS = 128, THREADS = WALKERS + 32, ROWS = 16, BATCH = 16, STAGES = 3;
+  struct alignas(128) Stage {
     Tio k[BATCH][D], q[BATCH][D], v[BATCH][ROWS];
-    float beta[BATCH], log_alpha[BATCH];
+    float4 c[BATCH][kCoefFloats / 4];
   };
-  struct Batch {            // the batch being walked, as the steps want it
-    float k[BATCH][D], q[BATCH][D];
-    float4 a[BATCH];        // beta P r, beta, (i,0), (i,1) of the first sum
-    float4 b[BATCH];        // (i,2); A_4i r_i; scale r_q P; P_4
-    float4 c[BATCH];        // (i,0) .. (i,3) of the second sum, times scale
-    float v[BATCH][ROWS];
-  };
-  struct Smem {
-    Stage st[2];
-    Batch now;
-  };
+  static constexpr int BYTES = BATCH * (2 * D + ROWS) * (int)sizeof(Tio) + BATCH * kCoefFloats * 4;   // of one batch's copies
+  static constexpr int SMEM_BYTES = STAGES * (int)sizeof(Stage) + 64 + 128;
 };
 
 template <typename Tio, int D>
-__global__ void __launch_bounds__(128) token_walk_kernel(const TokenArgs a) {
+__global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ,
+                                                         const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmC,
+                                                         const TokenArgs a, tc::DevStatus ds) {
+  using namespace tc;
   using W = TokenWalk<Tio, D>;
-  constexpr int ROWS = W::ROWS, GROUPS = D / ROWS, B = W::BATCH, PIECE = W::PIECE;
-  constexpr int NE = D / 16, NV = NE / 4;                // columns of a lane, in 16-byte pieces 256 bytes apart
-  extern __shared__ __align__(16) unsigned char walk_smem[];
-  typename W::Smem& sm = *reinterpret_cast<typename W::Smem*>(walk_smem);
+  constexpr int ROWS = W::ROWS, GROUPS = D / ROWS, B = W::BATCH;
+  constexpr int NE = D / 16, NV = NE / 4;                // columns of a lane, in pieces of four, 64 apart
+  extern __shared__ unsigned char walk_smem[];
+  unsigned char* bp = walk_smem + ((128u - (smem_u32(walk_smem) & 127u)) & 127u);
+  typename W::Stage* stages = reinterpret_cast<typename W::Stage*>(bp);
+  const uint32_t bars = smem_u32(bp) + W::STAGES * (uint32_t)sizeof(typename W::Stage);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bp + W::STAGES * sizeof(typename W::Stage) + 16 * W::STAGES);
+  const WaitCtx wc(abort_flag, ds);
   const int tid = threadIdx.x, lane = tid & 31, l16 = lane & 15;
   const int row0 = (int)(blockIdx.x % GROUPS) * ROWS;
-  const int r = (tid >> 4) * 2;                          // this lane's rows: row0 + r, row0 + r + 1
+  const int r = ((tid >> 4) & 7) * 2;                    // a walker's rows: row0 + r, row0 + r + 1
   const int h = (int)(blockIdx.x / GROUPS) % a.H, s = (int)(blockIdx.x / GROUPS) / a.H;
-  const long long slot = token_slot(a, s, tid, W::THREADS);
-  if (slot < 0) return;
   long long start;
   int len;
   token_range(a.cu_seqlens, s, a.per, a.n_tokens, start, len);
-  const int hk = h / (a.H / a.Hk);
-  const Tio* qp = static_cast<const Tio*>(a.q) + start * a.q_stride + hk * D;
-  const Tio* kp = static_cast<const Tio*>(a.k) + start * a.k_stride + hk * D;
-  const Tio* vp = static_cast<const Tio*>(a.v) + start * a.v_stride + h * D + row0;
-  const size_t gate0 = (size_t)start * a.H + h;
-
-  auto fetch = [&](int t0, typename W::Stage& st) {      // tokens t0 .. of the sequence, those that exist
-    const int n = min(B, len - t0);
-    for (int e = tid; e < n * (D / PIECE); e += W::THREADS) {
-      const int j = e / (D / PIECE), c = e % (D / PIECE) * PIECE;
-      cp_async16(&st.k[j][c], kp + (size_t)(t0 + j) * a.k_stride + c);
-      cp_async16(&st.q[j][c], qp + (size_t)(t0 + j) * a.q_stride + c);
+  if (tid == 0) {
+    for (int i = 0; i < W::STAGES; ++i) { mbar_init(bars + 8 * i, 1); mbar_init(bars + 8 * (W::STAGES + i), W::WALKERS / 32); }
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  __syncthreads();
+  const int batches = (len + B - 1) / B;
+  if (tid >= W::WALKERS) {
+    // one thread keeps two batches on their way (issuing the copies takes a walker 600 cycles of a batch's 4500)
+    if (tid == W::WALKERS) {
+      const int kc = h / (a.H / a.Hk) * D;
+      auto fetch = [&](int b) {
+        const int st = b % W::STAGES, row = (int)start + b * B;
+        const uint32_t bar = bars + 8 * st;
+        mbar_arrive_expect_tx(bar, W::BYTES);
+        tma_load_2d(smem_u32(stages[st].k), &tmK, bar, kc, row);
+        tma_load_2d(smem_u32(stages[st].q), &tmQ, bar, kc, row);
+        tma_load_2d(smem_u32(stages[st].v), &tmV, bar, h * D + row0, row);
+        tma_load_2d(smem_u32(stages[st].c), &tmC, bar, h * kCoefFloats, row);
+      };
+      uint32_t issued = 0;
+      for (int b = 0; b < batches; ++b) {
+        // a stage is free once the four walking warps have left it
+        if (b >= W::STAGES && !mbar_wait(bars + 8 * (W::STAGES + b % W::STAGES), ((b / W::STAGES) & 1) ^ 1, wc)) break;
+        fetch(b);
+        issued = b + 1;
+      }
+      mbar_drain_ring(bars, W::STAGES, issued);          // copies in flight get a bounded chance to land before the CTA retires
     }
-    for (int e = tid; e < n * (ROWS / PIECE); e += W::THREADS) {
-      const int j = e / (ROWS / PIECE), c = e % (ROWS / PIECE) * PIECE;
-      cp_async16(&st.v[j][c], vp + (size_t)(t0 + j) * a.v_stride + c);
-    }
-    if (tid < n) {
-      cp_async4(&st.beta[tid], a.beta + gate0 + (size_t)(t0 + tid) * a.H);
-      if (a.log_alpha) cp_async4(&st.log_alpha[tid], a.log_alpha + gate0 + (size_t)(t0 + tid) * a.H);
-      else st.log_alpha[tid] = 0.f;
-    }
-    cp_async_commit();
-  };
-
-  if (len > 0) fetch(0, sm.st[0]);
-  const size_t soff = (((size_t)slot * a.H + h) * D + row0 + r) * D + l16 * 4;
+    return;
+  }
+  const size_t soff = (((size_t)s * a.H + h) * D + row0 + r) * D + l16 * 4;
   float x[2][NE];                                        // the state
 #pragma unroll
   for (int i = 0; i < 2; ++i)
@@ -217,89 +325,42 @@ __global__ void __launch_bounds__(128) token_walk_kernel(const TokenArgs a) {
       const float4 y = a.state_in ? *reinterpret_cast<const float4*>(a.state_in + soff + i * D + c * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
       x[i][4 * c] = y.x; x[i][4 * c + 1] = y.y; x[i][4 * c + 2] = y.z; x[i][4 * c + 3] = y.w;
     }
-  auto columns = [&](const float* p, float (&y)[NE]) {
+  auto columns = [&](const Tio* p, float (&y)[NE]) {
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-      const float4 z = *reinterpret_cast<const float4*>(p + l16 * 4 + c * 64);
+      const float4 z = load4(p + l16 * 4 + c * 64);
       y[4 * c] = z.x; y[4 * c + 1] = z.y; y[4 * c + 2] = z.z; y[4 * c + 3] = z.w;
     }
   };
-  for (int t0 = 0, b = 0; t0 < len; t0 += B, b ^= 1) {
-    const typename W::Stage& st = sm.st[b];
-    const int n = min(B, len - t0);
-    if (t0 + B < len) { fetch(t0 + B, sm.st[b ^ 1]); cp_async_wait<1>(); }
-    else cp_async_wait<0>();
-    __syncthreads();                                     // the stage is there, the batch before has been walked
-    {
-      // ---- coefficients: a warp to four tokens, eight lanes to a token.  Tokens that do not exist count as keys and queries of
-      // zero that are not written and do not decay.
-      constexpr int ME = D / 8;
-      const int j = tid >> 3, l8 = tid & 7, i4 = j & 3, g0 = j & ~3;
-      float kk[4] = {0.f, 0.f, 0.f, 0.f}, qk[4] = {0.f, 0.f, 0.f, 0.f}, qq = 0.f;
-      const float4 none = make_float4(0.f, 0.f, 0.f, 0.f);
-      auto dot = [](float s, const float4& x, const float4& y) { return fmaf(x.w, y.w, fmaf(x.z, y.z, fmaf(x.y, y.y, fmaf(x.x, y.x, s)))); };
-#pragma unroll
-      for (int i = 0; i < ME / 4; ++i) {
-        const int c = l8 * 4 + i * 32;
-        const float4 k = j < n ? load4(&st.k[j][c]) : none, q = j < n ? load4(&st.q[j][c]) : none;
-        *reinterpret_cast<float4*>(&sm.now.k[j][c]) = k;
-        *reinterpret_cast<float4*>(&sm.now.q[j][c]) = q;
-        qq = dot(qq, q, q);
-#pragma unroll
-        for (int o = 0; o < 4; ++o) {
-          const float4 ko = g0 + o < n ? load4(&st.k[g0 + o][c]) : none;
-          kk[o] = dot(kk[o], k, ko);
-          qk[o] = dot(qk[o], q, ko);
-        }
-      }
-#pragma unroll
-      for (int m = 1; m < 8; m <<= 1) {
-        qq += __shfl_xor_sync(0xFFFFFFFFu, qq, m);
-#pragma unroll
-        for (int o = 0; o < 4; ++o) {
-          kk[o] += __shfl_xor_sync(0xFFFFFFFFu, kk[o], m);
-          qk[o] += __shfl_xor_sync(0xFFFFFFFFu, qk[o], m);
-        }
-      }
-      const float own = i4 == 0 ? kk[0] : i4 == 1 ? kk[1] : i4 == 2 ? kk[2] : kk[3];
-      const float rk = a.l2_eps > 0.f ? rsqrtf(own + a.l2_eps) : 1.f;
-      const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
-      const float alpha = j < n ? expf(st.log_alpha[j]) : 1.f, beta = j < n ? st.beta[j] : 0.f;
-      float al[4], ro[4];
-#pragma unroll
-      for (int o = 0; o < 4; ++o) {
-        al[o] = __shfl_sync(0xFFFFFFFFu, alpha, o * 8);
-        ro[o] = __shfl_sync(0xFFFFFFFFu, rk, o * 8);
-      }
-      sm.now.v[j][l8] = j < n ? to_float(st.v[j][l8]) : 0.f;
-      sm.now.v[j][l8 + 8] = j < n ? to_float(st.v[j][l8 + 8]) : 0.f;
-      if (l8 == 0) {
-        float first[3], second[4], pi = 1.f, to_end = 1.f;
-#pragma unroll
-        for (int o = 0; o < 4; ++o) {
-          pi *= o <= i4 ? al[o] : 1.f;
-          to_end *= o > i4 ? al[o] : 1.f;
-          float dec = 1.f;                               // A_{i4, o}
-#pragma unroll
-          for (int m = 0; m < 4; ++m) dec *= m > o && m <= i4 ? al[m] : 1.f;
-          if (o < 3) first[o] = o < i4 ? beta * rk * ro[o] * dec * kk[o] : 0.f;
-          second[o] = o <= i4 ? a.scale * rq * ro[o] * dec * qk[o] : 0.f;
-        }
-        sm.now.a[j] = make_float4(beta * pi * rk, beta, first[0], first[1]);
-        sm.now.b[j] = make_float4(first[2], to_end * rk, a.scale * rq * pi, pi * to_end);
-        sm.now.c[j] = make_float4(second[0], second[1], second[2], second[3]);
-      }
-    }
-    __syncthreads();
+  for (int b = 0; b < batches; ++b) {
+    typename W::Stage& st = stages[b % W::STAGES];
+    const int t0 = b * B, n = min(B, len - t0);
+    // a warp waits, and goes on or gives up together; it needs nothing of the other warps
+    if (!__all_sync(0xFFFFFFFFu, mbar_wait(bars + 8 * (b % W::STAGES), (b / W::STAGES) & 1, wc))) break;
     for (int g = 0; g < n; g += 4) {
+      if (g + 4 > n) {
+        // the end of the sequence: what lies behind it is the next one's.  Tokens that do not exist count as keys and queries
+        // of zero that are not written and do not decay; the state's factor is that of the last one that exists.  (All four
+        // warps write the same; a warp reads what it wrote itself.)
+        if (lane >= n - g && lane < 4) {
+          st.c[g + lane][0] = st.c[g + lane][2] = make_float4(0.f, 0.f, 0.f, 0.f);
+          st.c[g + lane][1] = make_float4(0.f, 0.f, 0.f, st.c[n - 1][1].w);
+        }
+        for (int e = lane; e < (g + 4 - n) * D; e += 32) {
+          st.k[n + e / D][e % D] = from_float<Tio>(0.f);
+          st.q[n + e / D][e % D] = from_float<Tio>(0.f);
+        }
+        for (int e = lane; e < (g + 4 - n) * ROWS; e += 32) st.v[n + e / ROWS][e % ROWS] = from_float<Tio>(0.f);
+        __syncwarp();
+      }
       float k[4][NE];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) columns(sm.now.k[g + i], k[i]);
+      for (int i = 0; i < 4; ++i) columns(st.k[g + i], k[i]);
       float d[16];                                       // [row][S k_1 .. S k_4, S q_1 .. S q_4], this lane's columns
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float q[NE];
-        columns(sm.now.q[g + i], q);
+        columns(st.q[g + i], q);
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           float sk = 0.f, sq = 0.f;
@@ -320,30 +381,30 @@ __global__ void __launch_bounds__(128) token_walk_kernel(const TokenArgs a) {
       const float mine = (b0 ? d[1] : d[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? d[0] : d[1], 1);
       // lane (row, query?, token) has its product; the keys' ones go to all lanes
       float u[2][4];
-      const float4 a0 = sm.now.a[g], a1 = sm.now.a[g + 1], a2 = sm.now.a[g + 2], a3 = sm.now.a[g + 3];
-      const float4 b3v = sm.now.b[g + 3];
+      const float4 a0 = st.c[g][0], a1 = st.c[g + 1][0], a2 = st.c[g + 2][0], a3 = st.c[g + 3][0];
+      const float4 b3v = st.c[g + 3][1];
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         float sk[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) sk[i] = __shfl_sync(0xFFFFFFFFu, mine, (lane & 16) + 8 * w + i);
-        u[w][0] = a0.y * sm.now.v[g][r + w] - a0.x * sk[0];
-        u[w][1] = a1.y * sm.now.v[g + 1][r + w] - a1.x * sk[1] - a1.z * u[w][0];
-        u[w][2] = a2.y * sm.now.v[g + 2][r + w] - a2.x * sk[2] - a2.z * u[w][0] - a2.w * u[w][1];
-        u[w][3] = a3.y * sm.now.v[g + 3][r + w] - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - b3v.x * u[w][2];
+        u[w][0] = a0.y * to_float(st.v[g][r + w]) - a0.x * sk[0];
+        u[w][1] = a1.y * to_float(st.v[g + 1][r + w]) - a1.x * sk[1] - a1.z * u[w][0];
+        u[w][2] = a2.y * to_float(st.v[g + 2][r + w]) - a2.x * sk[2] - a2.z * u[w][0] - a2.w * u[w][1];
+        u[w][3] = a3.y * to_float(st.v[g + 3][r + w]) - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - b3v.x * u[w][2];
       }
       {
         const int i = g + (l16 & 3);
         if (b2 && i < n) {
-          const float4 c = sm.now.c[i];
-          const float o = fmaf(sm.now.b[i].z, mine, fmaf(c.x, b3 ? u[1][0] : u[0][0], fmaf(c.y, b3 ? u[1][1] : u[0][1],
+          const float4 c = st.c[i][2];
+          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, b3 ? u[1][0] : u[0][0], fmaf(c.y, b3 ? u[1][1] : u[0][1],
                           fmaf(c.z, b3 ? u[1][2] : u[0][2], c.w * (b3 ? u[1][3] : u[0][3])))));
           static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (b3 ? 1 : 0)] = from_float<Tio>(o);
         }
       }
       float e4[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) e4[i] = sm.now.b[g + i].y;
+      for (int i = 0; i < 4; ++i) e4[i] = st.c[g + i][1].y;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
 #pragma unroll
@@ -353,6 +414,7 @@ __global__ void __launch_bounds__(128) token_walk_kernel(const TokenArgs a) {
           x[w][e] = fmaf(u[w][3], k[3][e], fmaf(u[w][2], k[2][e], fmaf(u[w][1], k[1][e], fmaf(u[w][0], k[0][e], b3v.w * x[w][e]))));
       }
     }
+    mbar_arrive_warp(bars + 8 * (W::STAGES + b % W::STAGES));
   }
   if (a.state_out) {
 #pragma unroll

@@ -57,35 +57,6 @@ __host__ __device__ inline int token_parts(int len, int part) {
   return part > 0 && len > 2 * part ? (len + part - 1) / part : 1;
 }
 
-// The kernels of one call overlap at their edges: each lets the next one start early, and each first gets ready and then waits
-// for the one before to be done.  Every thread waits, also of a CTA that has nothing to do: a kernel that did not wait could be
-// done before its predecessor, and its successor would then read unfinished results.
-__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void wait_for_kernel_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-// The sequence that owns place x, places being `unit` rows wide: the last one whose first place is not behind x.  A whole
-// warp looks at 32 offsets at a time: a round trip to memory for 32 sequences, two for a thousand.
-__device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int unit) {
-  int lo = 0, n = t.S;                                // the answer lies in [lo, lo + n), and sequence lo qualifies
-  const int lane = threadIdx.x & 31;
-  while (n > 1) {
-    const int step = (n + 31) / 32;
-    const int s = lo + lane * step;
-    bool fits = false;
-    if (s < lo + n) {
-      long long start;
-      int len;
-      token_range(t.cu_seqlens, s, t.per, t.n_tokens, start, len);
-      fits = start / unit + s <= x;
-    }
-    const unsigned m = __ballot_sync(0xFFFFFFFFu, fits) | 1u;
-    const int k = 31 - __clz(m);
-    n = min(step, lo + n - (lo + k * step));
-    lo += k * step;
-  }
-  return lo;
-}
-
 namespace tc {
 
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {

@@ -1244,40 +1244,85 @@ vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, 
   return VDN_OK;
 }
 
-// Up to so many tokens a sequence on the kernel that fetches each token when it needs it; beyond, batches pay.
-constexpr int kFewTokens = 4;
+// Up to so many tokens a sequence on the kernel that fetches each token when it needs it; beyond, coefficients and batches pay.
+constexpr int kFewTokens = 8;
+bool few_tokens(long long n_tokens, int n_seqs) { return n_tokens <= (long long)kFewTokens * n_seqs; }
 
-template <typename Tio, int D>
-cudaError_t launch_token_plain(const vdn::TokenArgs& a, bool few, cudaStream_t st) {
-  if (few) {
-    vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
-    return cudaGetLastError();
-  }
-  using W = vdn::TokenWalk<Tio, D>;
-  if (sizeof(typename W::Smem) > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (int)sizeof(typename W::Smem));
-    if (e != cudaSuccess) return e;
-  }
-  vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, sizeof(typename W::Smem), st>>>(a);
-  return cudaGetLastError();
+// Rows of a token tensor, `stride` elements apart, as a 2-D map with a (box, box_rows) box.
+vdn_status make_rows_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, bool f32, long long rows, long long width, long long stride,
+                         unsigned box_width, unsigned box_rows, CUtensorMapSwizzle swizzle) {
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)stride * (f32 ? 4 : 2)};
+  const cuuint32_t box[2] = {box_width, box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  CUresult r = h->encode(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims,
+                         strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (token rows) failed: " + std::to_string((int)r));
+  return VDN_OK;
 }
 
-vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, cudaStream_t st) {
+// A kernel that may start while its predecessor on the stream is still running (and waits for it itself).
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, int smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(grid);
+  c.blockDim = dim3((unsigned)threads);
+  c.dynamicSmemBytes = (size_t)smem;
+  c.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  c.attrs = at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
+}
+
+// Plain fp32.  `coef`: workspace of the walking kernels, or null: token by token.
+template <typename Tio, int D>
+vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
+  prof_begin(h, st);
+  if (!coef) {
+    vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
+    prof_mark(h, st, 0, "token_few");
+    h->launches = 1;
+    VDN_CUDA(h, cudaGetLastError());
+    return VDN_OK;
+  }
+  using W = vdn::TokenWalk<Tio, D>;
+  constexpr bool F32 = sizeof(Tio) == 4;
+  CUtensorMap tmK, tmQ, tmV, tmC;
+  vdn_status r;
+  const long long wk = (long long)a.Hk * D, wv = (long long)a.H * D, wc = (long long)a.H * vdn::kCoefFloats;
+  constexpr CUtensorMapSwizzle none = CU_TENSOR_MAP_SWIZZLE_NONE;
+  if ((r = make_rows_map(h, &tmK, a.k, F32, a.n_tokens, wk, a.k_stride, D, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmQ, a.q, F32, a.n_tokens, wk, a.q_stride, D, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmV, a.v, F32, a.n_tokens, wv, a.v_stride, W::ROWS, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmC, coef, true, a.n_tokens, wc, wc, vdn::kCoefFloats, W::BATCH, none)) != VDN_OK) return r;
+  if (W::SMEM_BYTES > 48 * 1024)
+    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::SMEM_BYTES));
+  const long long warps = (a.n_tokens / 4 + a.S) * a.H;
+  if (warps / 8 + 1 > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (token, head) pairs for one call");
+  vdn::token_coef_kernel<Tio, D><<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, coef, warps);
+  prof_mark(h, st, 0, "token_coef");
+  // (not overlapped with its predecessor: CTAs placed while that still holds most SMs would share the few free ones, and each of
+  // these has little but latency to offer)
+  vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, W::SMEM_BYTES, st>>>(tmK, tmQ, tmV, tmC, a,
+                                                                                                          dev_status(h));
+  prof_mark(h, st, 1, "token_walk");
+  h->launches = 2;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
+vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
   const int d = h->cfg.d;
   if ((long long)a.S * a.H * (d / 16) > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
-  const bool few = (a.cu_seqlens ? a.n_tokens / a.S : a.per) <= kFewTokens;
-  prof_begin(h, st);
-  cudaError_t e;
+  if (coef && !h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (h->cfg.io_dtype == VDN_F32)
-    e = d == 64 ? launch_token_plain<float, 64>(a, few, st) : launch_token_plain<float, 128>(a, few, st);
-  else
-    e = d == 64 ? launch_token_plain<__nv_bfloat16, 64>(a, few, st) : launch_token_plain<__nv_bfloat16, 128>(a, few, st);
-  VDN_CUDA(h, e);
-  prof_mark(h, st, 0, few ? "token_few" : "token_walk");
-  h->launches = 1;
-  return VDN_OK;
+    return d == 64 ? launch_token_plain<float, 64>(h, a, coef, st) : launch_token_plain<float, 128>(h, a, coef, st);
+  return d == 64 ? launch_token_plain<__nv_bfloat16, 64>(h, a, coef, st) : launch_token_plain<__nv_bfloat16, 128>(h, a, coef, st);
 }
 
 // The lengths stay on the device.  Where a choice depends on the longest sequence: four times the average, if there are so many.
@@ -1332,36 +1377,6 @@ bool token_on_tensor_cores(const vdn_vda_s* h, long long n_tokens, int n_seqs, i
   return chunked < plain;
 }
 
-// Rows of `width` bf16 elements, `stride` elements apart, as a 2-D map with a (box, 64) box.
-vdn_status make_rows_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, long long rows, long long width, long long stride,
-                         unsigned box_width, CUtensorMapSwizzle swizzle) {
-  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
-  const cuuint64_t strides[1] = {(cuuint64_t)stride * 2};
-  const cuuint32_t box[2] = {box_width, 64};
-  const cuuint32_t estr[2] = {1, 1};
-  CUresult r = h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), dims, strides, box, estr,
-                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (token rows) failed: " + std::to_string((int)r));
-  return VDN_OK;
-}
-
-// A kernel that may start while its predecessor on the stream is still running (and waits for it itself).
-template <typename... P, typename... A>
-cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, int smem, cudaStream_t st, A&&... args) {
-  cudaLaunchConfig_t c = {};
-  c.gridDim = dim3(grid);
-  c.blockDim = dim3((unsigned)threads);
-  c.dynamicSmemBytes = (size_t)smem;
-  c.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  c.attrs = at;
-  c.numAttrs = 1;
-  return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
-}
-
 vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* ws, cudaStream_t st) {
   if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (!h->token_attrs_set) {
@@ -1378,9 +1393,9 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   CUtensorMap tmK, tmQ, tmV;
   const long long wk = (long long)t.Hk * 128, wv = (long long)t.H * 128;
   vdn_status r;
-  if ((r = make_rows_map(h, &tmK, t.k, t.n_tokens, wk, t.k_stride, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmQ, t.q, t.n_tokens, wk, t.q_stride, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmV, t.v, t.n_tokens, wv, t.v_stride, 128, CU_TENSOR_MAP_SWIZZLE_NONE)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmK, t.k, false, t.n_tokens, wk, t.k_stride, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmQ, t.q, false, t.n_tokens, wk, t.q_stride, 64, 64, CU_TENSOR_MAP_SWIZZLE_128B)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmV, t.v, false, t.n_tokens, wv, t.v_stride, 128, 64, CU_TENSOR_MAP_SWIZZLE_NONE)) != VDN_OK) return r;
   vdn::TokenTcArgs a;
   a.t = t;
   a.e = ws + L.e; a.p = ws + L.p; a.f = ws + L.f;
@@ -1429,7 +1444,8 @@ extern "C" {
 
 size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
   if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->n_seqs <= 0 || n_tokens < 0) return 0;
-  return token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads) ? make_token_layout(h, n_tokens, p->n_seqs, p->heads).total : 0;
+  if (token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads)) return make_token_layout(h, n_tokens, p->n_seqs, p->heads).total;
+  return few_tokens(n_tokens, p->n_seqs) ? 0 : align_up((size_t)n_tokens * p->heads * vdn::kCoefFloats * sizeof(float));
 }
 
 vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1457,7 +1473,8 @@ vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const v
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  return need ? launch_token_tc(h, a, static_cast<unsigned char*>(workspace), st) : launch_token_rule(h, a, st);
+  if (token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads)) return launch_token_tc(h, a, static_cast<unsigned char*>(workspace), st);
+  return launch_token_rule(h, a, need ? static_cast<float4*>(workspace) : nullptr, st);
 }
 
 vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1482,7 +1499,7 @@ vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const v
   a.state_out = p->state;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
-  return launch_token_rule(h, a, static_cast<cudaStream_t>(cuda_stream));
+  return launch_token_rule(h, a, nullptr, static_cast<cudaStream_t>(cuda_stream));
 }
 
 vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void* q_out, void* k_out, int B, int T, int F,

@@ -250,12 +250,15 @@ def test_scan_same_call_same_bits(lens, h, hk):
 def test_scan_takes_the_kernels_its_sizes_call_for():
     """Short sequences token by token, longer ones in chunks, few long ones in parts."""
     d, h = 128, 2
-    vda, plain = binding.Vda(d, "bf16"), binding.Vda(d, "bf16", flags=binding.VDN_FLAG_FORCE_SIMT)
-    for n, launches in ((2, 1), (20, 1), (300, 2), (3000, 4)):
-        x = draw(n, h, h, d, "bf16")
-        vda.token_scan(**x)
-        plain.token_scan(**x)
-        assert vda.launch_count() == launches and plain.launch_count() == 1
+    few, walk, chunks = ["token_few"], ["token_coef", "token_walk"], ["token_prep", "token_chain"]
+    parts = ["token_prep", "token_compose", "token_join", "token_chain"]
+    for flags, wanted in ((0, {2: few, 20: walk, 300: chunks, 3000: parts}),
+                          (binding.VDN_FLAG_FORCE_SIMT, {2: few, 20: walk, 300: walk, 3000: walk})):
+        for n, names in wanted.items():
+            vda = binding.Vda(d, "bf16", flags=flags)
+            vda.profile(True)
+            vda.token_scan(**draw(n, h, h, d, "bf16"))
+            assert [k[0] for k in vda.kernel_times()] == names and vda.launch_count() == len(names)
 
 
 def test_scan_of_no_tokens():
