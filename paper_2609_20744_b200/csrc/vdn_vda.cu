@@ -1283,7 +1283,9 @@ template <typename Tio, int D>
 vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
   prof_begin(h, st);
   if (!coef) {
-    vdn::token_few_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / 32)), 256, 0, st>>>(a);
+    const long long states = (long long)a.S * a.H;
+    if (states >= 4LL * h->sm_count) vdn::token_few_kernel<Tio, D, D / 32><<<(unsigned)states, 256, 0, st>>>(a);
+    else vdn::token_few_kernel<Tio, D, 1><<<(unsigned)(states * (D / 32)), 256, 0, st>>>(a);
     prof_mark(h, st, 0, "token_few");
     h->launches = 1;
     VDN_CUDA(h, cudaGetLastError());

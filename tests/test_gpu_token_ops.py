@@ -271,7 +271,7 @@ def test_scan_of_no_tokens():
 
 # ---------------------------------------------------------------------------------------------------------------- step
 @pytest.mark.parametrize("dtype,d", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 128)])
-@pytest.mark.parametrize("requests,per,h,hk", [(1, 1, 2, 2), (7, 1, 6, 2), (5, 3, 4, 4), (2, 40, 2, 1)])
+@pytest.mark.parametrize("requests,per,h,hk", [(1, 1, 2, 2), (7, 1, 6, 2), (5, 3, 4, 4), (2, 40, 2, 1), (61, 2, 12, 4)])
 def test_step(dtype, d, requests, per, h, hk):
     slots = requests + 3
     x = draw(requests * per, h, hk, d, dtype, seed=requests, l2=True)
