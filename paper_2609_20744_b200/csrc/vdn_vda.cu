@@ -1335,7 +1335,8 @@ long long longest_guess(long long n_tokens, int n_seqs) { return n_seqs > 4 ? 4 
 struct TokenLayout {
   long long places, parts;
   int part;                 // rows of a part; 0: no sequence is cut
-  size_t e, p, f, enter, comp_j, comp_m, total;
+  bool ordered;             // longest sequence first
+  size_t e, p, f, enter, comp_j, comp_m, order, total;
 };
 TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs, int heads) {
   constexpr int C = vdn::TokenTc::C;
@@ -1363,6 +1364,8 @@ TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs
   L.enter = off; off += states;
   L.comp_j = off; off += states;
   L.comp_m = off; off += states;
+  L.ordered = !L.part && n_seqs > 1 && n_seqs <= vdn::kOrderMax && (long long)n_seqs * heads > h->sm_count;
+  L.order = off; off += L.ordered ? align_up(n_seqs * sizeof(int)) : 0;
   L.total = off;
   return L;
 }
@@ -1390,7 +1393,7 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
     h->token_attrs_set = true;
   }
   const TokenLayout L = make_token_layout(h, t.n_tokens, t.S, t.H);
-  if (L.places * t.H > 0x7fffffffLL || (long long)t.S * t.H * 8 > 0x7fffffffLL)
+  if (L.places * t.H >= 0x7fffffffLL || (long long)t.S * t.H * 8 > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (chunk, head) pairs for one call");
   CUtensorMap tmK, tmQ, tmV;
   const long long wk = (long long)t.Hk * 128, wv = (long long)t.H * 128;
@@ -1402,13 +1405,15 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
   a.t = t;
   a.e = ws + L.e; a.p = ws + L.p; a.f = ws + L.f;
   a.part = L.part;
+  a.places = (int)L.places;
+  a.order = L.ordered ? reinterpret_cast<int*>(ws + L.order) : nullptr;
   a.enter = reinterpret_cast<float*>(ws + L.enter);
   a.comp_j = reinterpret_cast<float*>(ws + L.comp_j);
   a.comp_m = reinterpret_cast<float*>(ws + L.comp_m);
   using TC = vdn::TokenChain;
   int nk = 0;
   prof_begin(h, st);
-  vdn::token_prep_kernel<<<(unsigned)(L.places * t.H), vdn::TokenPrep::THREADS, vdn::TokenPrep::SMEM_BYTES, st>>>(
+  vdn::token_prep_kernel<<<(unsigned)(L.places * t.H + (L.ordered ? 1 : 0)), vdn::TokenPrep::THREADS, vdn::TokenPrep::SMEM_BYTES, st>>>(
       tmK, tmQ, a, dev_status(h));
   prof_mark(h, st, nk++, "token_prep");
   const vdn::tc::DevStatus ds = dev_status(h);
