@@ -25,6 +25,7 @@ struct RotaryArgs {
   const int* positions;      // [3][n_tokens] or null: frame t0 + t, row, column of the token's grid place
   long long n_tokens;
   int pairs, T, F, X, t0, tile;
+  unsigned per_row;          // ceil(2^32 / (all heads of a token)), 0 where a tile is one token: division by multiplication
   float norm_eps;            // > 0: RMSNorm first
   float sign;                // -1: rotate back
 };
@@ -82,21 +83,6 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
   // first channel of the lane's two pieces
   int c0 = 2 * l * VEC, c1 = c0 + VEC;
   if (HALF && l * VEC < a.pairs) { c0 = l * VEC; c1 = c0 + a.pairs; }
-  uint4 x0[U], x1[U];
-  auto fetch = [&](int t0) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + u * STEP;
-      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
-      if (t < tasks) {
-        const int j = t / rows, r = t - j * rows, w = r >= a.heads[0];
-        const Tio* src = static_cast<const Tio*>(a.in[w]) + (size_t)(n0 + j) * a.in_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
-        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
-        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
-      }
-    }
-  };
-
   // ---- cosines and sines: a thread has one place lp = lane * NP + pair of the lane, and every (256 / places)-th token
   {
     constexpr int PLACES = D / 2, TOKENS = Rotary::THREADS / PLACES;
@@ -134,13 +120,30 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
   }
   __syncthreads();
 
-  for (int base = 0; base < tasks; base += STEP * U) {
-    fetch(base + first);
+  for (int base = first; base < tasks + first; base += STEP * U) {   // (all lanes together: the norm shuffles)
+    uint4 x0[U], x1[U];
+    int token[U], head[U];
+    bool key[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int t = base + first + u * STEP;
-      const bool live = t < tasks;
-      const int j = live ? t / rows : 0, r = live ? t - j * rows : 0, w = r >= a.heads[0];
+      const int t = base + u * STEP;
+      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+      token[u] = head[u] = 0;
+      key[u] = false;
+      if (t < tasks) {
+        token[u] = (int)__umulhi((unsigned)t, a.per_row);
+        head[u] = t - token[u] * rows;
+        key[u] = head[u] >= a.heads[0];
+        if (key[u]) head[u] -= a.heads[0];
+        const Tio* src = static_cast<const Tio*>(a.in[key[u]]) + (size_t)(n0 + token[u]) * a.in_stride[key[u]] + head[u] * D;
+        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
+        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool live = base + u * STEP < tasks;
+      const int j = token[u], w = key[u];
       float y0[VEC], y1[VEC];
       unpack16(x0[u], y0, static_cast<const Tio*>(nullptr));
       unpack16(x1[u], y1, static_cast<const Tio*>(nullptr));
@@ -174,7 +177,7 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
         }
       }
       if (live) {
-        Tio* dst = static_cast<Tio*>(a.out[w]) + (size_t)(n0 + j) * a.out_stride[w] + (r - (w ? a.heads[0] : 0)) * D;
+        Tio* dst = static_cast<Tio*>(a.out[w]) + (size_t)(n0 + j) * a.out_stride[w] + head[u] * D;
         *reinterpret_cast<uint4*>(dst + c0) = pack16(y0, static_cast<const Tio*>(nullptr));
         *reinterpret_cast<uint4*>(dst + c1) = pack16(y1, static_cast<const Tio*>(nullptr));
       }
