@@ -1342,9 +1342,9 @@ TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs
   constexpr int C = vdn::TokenTc::C;
   TokenLayout L;
   L.places = n_tokens / C + n_seqs;
-  // A chain is a (sequence, head); fewer than a third of the SMs' number of chains, and cutting them pays: composing costs two
+  // A chain is a (sequence, head).  Fewer of them than a third of the SMs, and cutting long ones pays: composing costs two
   // more passes, side by side.  Parts as long as let all of them run at once, but not so short that passing the states along
-  // (about one step a part) weighs.  32760 tokens x 8 heads: FIXME whole, FIXME in 18 parts.
+  // (about one step a part) weighs.  32760 tokens x 8 heads: 1.27 ms whole, 0.31 ms in 18 parts.
   L.part = 0;
   L.parts = n_seqs;
   const long long per_head = h->sm_count / heads;
@@ -1393,7 +1393,7 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
     h->token_attrs_set = true;
   }
   const TokenLayout L = make_token_layout(h, t.n_tokens, t.S, t.H);
-  if (L.places * t.H >= 0x7fffffffLL || (long long)t.S * t.H * 8 > 0x7fffffffLL)
+  if (L.places * t.H >= 0x7fffffffLL || (long long)t.S * t.H * 16 > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (chunk, head) pairs for one call");
   CUtensorMap tmK, tmQ, tmV;
   const long long wk = (long long)t.Hk * 128, wv = (long long)t.H * 128;
