@@ -271,14 +271,15 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
   }
 }
 
-// One CTA (four warps, one to a scheduler) to 16 rows of a (sequence, head), as many CTAs as rows allow, since a step is a chain of
-// latencies (dot products, shuffles, update).  A row is shared by 16 lanes, which hold two rows each; the sixteen dot products
-// of a step are reduced together, each lane ending with one of them (15 shuffles instead of 64).  Batches of 16 tokens -- keys,
-// queries, this CTA's values, coefficients -- arrive by four tile copies each, which a fifth warp issues, three batches ahead.
-// Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: 150 us, both kernels; a token at a time it took 289.
-template <typename Tio, int D>
+// One CTA (four warps, one to a scheduler) to 8 R rows of a (sequence, head), since a step is a chain of latencies (dot products,
+// shuffles, update).  A row is shared by 16 lanes, which hold R rows each; the 8 R dot products of a step are reduced together,
+// each lane ending with one of them (15 shuffles instead of 64).  R = 2 does the least work; R = 1 shortens a step, with twice the CTAs,
+// where SMs would be left over.  Batches of 16 tokens -- keys, queries, this CTA's values, coefficients -- arrive by four tile
+// copies each, which a fifth warp issues, three batches ahead.
+// Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: 119 us, both kernels (R = 2: 150); a token at a time it took 289.
+template <typename Tio, int D, int R>
 struct TokenWalk {
-  static constexpr int WALKERS = 128, THREADS = WALKERS + 32, ROWS = 16, BATCH = 16, STAGES = 3;
+  static constexpr int WALKERS = 128, THREADS = WALKERS + 32, ROWS = 8 * R, BATCH = 16, STAGES = 3;
   struct alignas(128) Stage {
     Tio k[BATCH][D], q[BATCH][D], v[BATCH][ROWS];
     float4 c[BATCH][kCoefFloats / 4];
@@ -287,12 +288,12 @@ struct TokenWalk {
   static constexpr int SMEM_BYTES = STAGES * (int)sizeof(Stage) + 64 + 128;
 };
 
-template <typename Tio, int D>
+template <typename Tio, int D, int R>
 __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ,
                                                          const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmC,
                                                          const TokenArgs a, tc::DevStatus ds) {
   using namespace tc;
-  using W = TokenWalk<Tio, D>;
+  using W = TokenWalk<Tio, D, R>;
   constexpr int ROWS = W::ROWS, GROUPS = D / ROWS, B = W::BATCH;
   constexpr int NE = D / 16, NV = NE / 4;                // columns of a lane, in pieces of four, 64 apart
   extern __shared__ unsigned char walk_smem[];
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
   const WaitCtx wc(abort_flag, ds);
   const int tid = threadIdx.x, lane = tid & 31, l16 = lane & 15;
   const int row0 = (int)(blockIdx.x % GROUPS) * ROWS;
-  const int r = ((tid >> 4) & 7) * 2;                    // a walker's rows: row0 + r, row0 + r + 1
+  const int r = ((tid >> 4) & 7) * R;                    // a walker's rows: row0 + r ..
   const int h = (int)(blockIdx.x / GROUPS) % a.H, s = (int)(blockIdx.x / GROUPS) / a.H;
   long long start;
   int len;
@@ -340,9 +341,9 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
     return;
   }
   const size_t soff = (((size_t)s * a.H + h) * D + row0 + r) * D + l16 * 4;
-  float x[2][NE];                                        // the state
+  float x[R][NE];                                        // the state
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
       const float4 y = a.state_in ? *reinterpret_cast<const float4*>(a.state_in + soff + i * D + c * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -379,13 +380,13 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
       float k[4][NE];
 #pragma unroll
       for (int i = 0; i < 4; ++i) columns(st.k[g + i], k[i]);
-      float d[16];                                       // [row][S k_1 .. S k_4, S q_1 .. S q_4], this lane's columns
+      float d[8 * R];                                    // [row][S k_1 .. S k_4, S q_1 .. S q_4], this lane's columns
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float q[NE];
         columns(st.q[g + i], q);
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
+        for (int w = 0; w < R; ++w) {
           float sk = 0.f, sq = 0.f;
 #pragma unroll
           for (int e = 0; e < NE; ++e) { sk = fmaf(x[w][e], k[i][e], sk); sq = fmaf(x[w][e], q[e], sq); }
@@ -393,55 +394,60 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
           d[8 * w + 4 + i] = sq;
         }
       }
-      // reduce: at each step a lane keeps the half of its values that its bit names and adds its partner's
-      const bool b3 = l16 & 8, b2 = l16 & 4, b1 = l16 & 2, b0 = l16 & 1;
+      // reduce: at each step a lane keeps the half of its values that its bit names and adds its partner's; with one row the
+      // last step adds two halves of the same
+      int m = 8;                                         // the bit, from the highest
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = (b3 ? d[8 + i] : d[i]) + __shfl_xor_sync(0xFFFFFFFFu, b3 ? d[i] : d[8 + i], 8);
+      for (int half = 4 * R; half > 0; half >>= 1, m >>= 1) {
+        const bool upper = l16 & m;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[i] = (b2 ? d[4 + i] : d[i]) + __shfl_xor_sync(0xFFFFFFFFu, b2 ? d[i] : d[4 + i], 4);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) d[i] = (b1 ? d[2 + i] : d[i]) + __shfl_xor_sync(0xFFFFFFFFu, b1 ? d[i] : d[2 + i], 2);
-      const float mine = (b0 ? d[1] : d[0]) + __shfl_xor_sync(0xFFFFFFFFu, b0 ? d[0] : d[1], 1);
+        for (int i = 0; i < half; ++i) d[i] = (upper ? d[half + i] : d[i]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? d[i] : d[half + i], m);
+      }
+      float mine = d[0];
+      if (R == 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, 1);
+      constexpr int LOW = R == 2 ? 0 : 1;                // bits of the lane below those that say (row, query?, token)
+      const int what = l16 >> LOW;
       // lane (row, query?, token) has its product; the keys' ones go to all lanes
-      float u[2][4];
+      float u[R][4];
       const float4 a0 = st.c[g][0], a1 = st.c[g + 1][0], a2 = st.c[g + 2][0], a3 = st.c[g + 3][0];
-      const float4 b3v = st.c[g + 3][1];
+      const float4 tail = st.c[g + 3][1];
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
+      for (int w = 0; w < R; ++w) {
         float sk[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sk[i] = __shfl_sync(0xFFFFFFFFu, mine, (lane & 16) + 8 * w + i);
+        for (int i = 0; i < 4; ++i) sk[i] = __shfl_sync(0xFFFFFFFFu, mine, (lane & 16) + ((8 * w + i) << LOW));
         u[w][0] = a0.y * to_float(st.v[g][r + w]) - a0.x * sk[0];
         u[w][1] = a1.y * to_float(st.v[g + 1][r + w]) - a1.x * sk[1] - a1.z * u[w][0];
         u[w][2] = a2.y * to_float(st.v[g + 2][r + w]) - a2.x * sk[2] - a2.z * u[w][0] - a2.w * u[w][1];
-        u[w][3] = a3.y * to_float(st.v[g + 3][r + w]) - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - b3v.x * u[w][2];
+        u[w][3] = a3.y * to_float(st.v[g + 3][r + w]) - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - tail.x * u[w][2];
       }
       {
-        const int i = g + (l16 & 3);
-        if (b2 && i < n) {
+        const int i = g + (what & 3);
+        const bool second = R == 2 && (what & 8);        // of the lane's two rows
+        if ((what & 4) && (R == 2 || !(l16 & 1)) && i < n) {
           const float4 c = st.c[i][2];
-          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, b3 ? u[1][0] : u[0][0], fmaf(c.y, b3 ? u[1][1] : u[0][1],
-                          fmaf(c.z, b3 ? u[1][2] : u[0][2], c.w * (b3 ? u[1][3] : u[0][3])))));
-          static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (b3 ? 1 : 0)] = from_float<Tio>(o);
+          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, second ? u[R - 1][0] : u[0][0], fmaf(c.y, second ? u[R - 1][1] : u[0][1],
+                          fmaf(c.z, second ? u[R - 1][2] : u[0][2], c.w * (second ? u[R - 1][3] : u[0][3])))));
+          static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (second ? 1 : 0)] = from_float<Tio>(o);
         }
       }
       float e4[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) e4[i] = st.c[g + i][1].y;
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
+      for (int w = 0; w < R; ++w) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) u[w][i] *= e4[i];
 #pragma unroll
         for (int e = 0; e < NE; ++e)
-          x[w][e] = fmaf(u[w][3], k[3][e], fmaf(u[w][2], k[2][e], fmaf(u[w][1], k[1][e], fmaf(u[w][0], k[0][e], b3v.w * x[w][e]))));
+          x[w][e] = fmaf(u[w][3], k[3][e], fmaf(u[w][2], k[2][e], fmaf(u[w][1], k[1][e], fmaf(u[w][0], k[0][e], tail.w * x[w][e]))));
       }
     }
     mbar_arrive_warp(bars + 8 * (W::STAGES + b % W::STAGES));
   }
   if (a.state_out) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < NV; ++c)
         *reinterpret_cast<float4*>(a.state_out + soff + i * D + c * 64) =

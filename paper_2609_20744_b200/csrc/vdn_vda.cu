@@ -1278,6 +1278,31 @@ cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, 
   return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
 }
 
+template <typename Tio, int D, int R>
+vdn_status launch_walk(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
+  using W = vdn::TokenWalk<Tio, D, R>;
+  constexpr bool F32 = sizeof(Tio) == 4;
+  CUtensorMap tmK, tmQ, tmV, tmC;
+  vdn_status r;
+  const long long wk = (long long)a.Hk * D, wv = (long long)a.H * D, wc = (long long)a.H * vdn::kCoefFloats;
+  constexpr CUtensorMapSwizzle none = CU_TENSOR_MAP_SWIZZLE_NONE;
+  if ((r = make_rows_map(h, &tmK, a.k, F32, a.n_tokens, wk, a.k_stride, D, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmQ, a.q, F32, a.n_tokens, wk, a.q_stride, D, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmV, a.v, F32, a.n_tokens, wv, a.v_stride, W::ROWS, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &tmC, coef, true, a.n_tokens, wc, wc, vdn::kCoefFloats, W::BATCH, none)) != VDN_OK) return r;
+  if (W::SMEM_BYTES > 48 * 1024)
+    VDN_CUDA(h, (cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::SMEM_BYTES)));
+  const long long warps = (a.n_tokens / 4 + a.S) * a.H;
+  if (warps / 8 + 1 > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (token, head) pairs for one call");
+  vdn::token_coef_kernel<Tio, D><<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, coef, warps);
+  prof_mark(h, st, 0, "token_coef");
+  // (not overlapped with its predecessor: CTAs placed while that still holds most SMs would share the few free ones, and each of
+  // these has little but latency to offer)
+  vdn::token_walk_kernel<Tio, D, R><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, W::SMEM_BYTES, st>>>(tmK, tmQ, tmV, tmC, a,
+                                                                                                             dev_status(h));
+  return VDN_OK;
+}
+
 // Plain fp32.  `coef`: workspace of the walking kernels, or null: token by token.
 template <typename Tio, int D>
 vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
@@ -1291,26 +1316,11 @@ vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef
     VDN_CUDA(h, cudaGetLastError());
     return VDN_OK;
   }
-  using W = vdn::TokenWalk<Tio, D>;
-  constexpr bool F32 = sizeof(Tio) == 4;
-  CUtensorMap tmK, tmQ, tmV, tmC;
-  vdn_status r;
-  const long long wk = (long long)a.Hk * D, wv = (long long)a.H * D, wc = (long long)a.H * vdn::kCoefFloats;
-  constexpr CUtensorMapSwizzle none = CU_TENSOR_MAP_SWIZZLE_NONE;
-  if ((r = make_rows_map(h, &tmK, a.k, F32, a.n_tokens, wk, a.k_stride, D, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmQ, a.q, F32, a.n_tokens, wk, a.q_stride, D, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmV, a.v, F32, a.n_tokens, wv, a.v_stride, W::ROWS, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmC, coef, true, a.n_tokens, wc, wc, vdn::kCoefFloats, W::BATCH, none)) != VDN_OK) return r;
-  if (W::SMEM_BYTES > 48 * 1024)
-    VDN_CUDA(h, cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::SMEM_BYTES));
-  const long long warps = (a.n_tokens / 4 + a.S) * a.H;
-  if (warps / 8 + 1 > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (token, head) pairs for one call");
-  vdn::token_coef_kernel<Tio, D><<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, coef, warps);
-  prof_mark(h, st, 0, "token_coef");
-  // (not overlapped with its predecessor: CTAs placed while that still holds most SMs would share the few free ones, and each of
-  // these has little but latency to offer)
-  vdn::token_walk_kernel<Tio, D><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, W::SMEM_BYTES, st>>>(tmK, tmQ, tmV, tmC, a,
-                                                                                                          dev_status(h));
+  // CTAs of eight rows where that leaves at most two on an SM.  1024 tokens, d = 128, bf16: 2 heads (32 CTAs) 119 us instead of
+  // 150, 8 heads (128 CTAs) 121 instead of 191, 8 sequences of 2 heads (256 CTAs) 152 instead of 160.
+  const bool narrow = (long long)a.S * a.H * (D / 8) <= 2LL * h->sm_count;
+  const vdn_status r = narrow ? launch_walk<Tio, D, 1>(h, a, coef, st) : launch_walk<Tio, D, 2>(h, a, coef, st);
+  if (r != VDN_OK) return r;
   prof_mark(h, st, 1, "token_walk");
   h->launches = 2;
   VDN_CUDA(h, cudaGetLastError());
@@ -1319,7 +1329,7 @@ vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef
 
 vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
   const int d = h->cfg.d;
-  if ((long long)a.S * a.H * (d / 16) > 0x7fffffffLL)
+  if ((long long)a.S * a.H * (d / 8) > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
   if (coef && !h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (h->cfg.io_dtype == VDN_F32)
@@ -1371,14 +1381,15 @@ TokenLayout make_token_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs
 }
 
 // Chunks on the tensor cores, or token by token in plain fp32 (bf16, d = 128: both can).  Costs in microseconds, fitted to
-// graph replays of 1 .. 64 sequences of 1 .. 1024 tokens and 2, 8 and 32 heads: the plain kernel starts faster and pays 0.17 for a
-// token of the longest sequence and 0.006 for each token and head; the two chunked kernels start at 18 and pay 2.3 for a chunk of the longest and 0.07 for each chunk and
-// head.  One sequence, 8 heads: 64 tokens 14.6 plain, 18.5 chunked; 128 tokens 26.8 and 20.5; 1024 tokens 191 and 55.
+// graph replays of 1 .. 64 sequences of 1 .. 1024 tokens and 2, 8 and 32 heads: the plain kernels start at 6 and pay 0.12 for a
+// token of the longest sequence and 0.0042 for each token and head; the two chunked kernels start at 14 and pay 2.3 for a chunk of
+// the longest and 0.045 for each chunk and head.  One sequence, 8 heads: 64 tokens 14.4 plain, 16.5 chunked; 128 tokens 20.5 and
+// 18.5; 1024 tokens 121 and 53.
 bool token_on_tensor_cores(const vdn_vda_s* h, long long n_tokens, int n_seqs, int heads) {
   if (!use_tensor_cores(h, h->cfg.d) || n_tokens == 0) return false;
   const double n = (double)n_tokens, longest = (double)longest_guess(n_tokens, n_seqs);
-  const double plain = 4.0 + 0.17 * longest + 0.006 * n * heads;
-  const double chunked = 18.0 + 2.3 * longest / vdn::TokenTc::C + 0.07 * (n / vdn::TokenTc::C + n_seqs) * heads;
+  const double plain = 6.0 + 0.12 * longest + 0.0042 * n * heads;
+  const double chunked = 14.0 + 2.3 * longest / vdn::TokenTc::C + 0.045 * (n / vdn::TokenTc::C + n_seqs) * heads;
   return chunked < plain;
 }
 

@@ -108,6 +108,16 @@ def test_scan(dtype, d, flags, lens):
     check_scan(vda, x, lens, dtype, d, tensor_cores(dtype, d, flags), s0, scale=0.5)
 
 
+@pytest.mark.parametrize("dtype,d,flags", [("f32", 64, 0), ("f32", 128, 0), ("bf16", 64, 0),
+                                           ("bf16", 128, binding.VDN_FLAG_FORCE_SIMT)])
+def test_scan_of_more_rows_than_run_at_once(dtype, d, flags):
+    """The plain kernel gives a CTA more rows where there are many sequences and heads."""
+    lens = [9, 17, 34, 0, 1, 63] * 5
+    x = draw(sum(lens), 4, 2, d, dtype, seed=11)
+    s0 = 0.3 * torch.randn(len(lens), 4, d, d, device=DEV)
+    check_scan(binding.Vda(d, dtype, flags=flags), x, lens, dtype, d, False, s0, scale=0.5)
+
+
 @pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 64), ("bf16", 128)])
 def test_scan_normalises_queries_and_keys(dtype, d):
     x = draw(200, 4, 2, d, dtype, seed=3, l2=True)
