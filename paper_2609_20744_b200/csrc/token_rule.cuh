@@ -38,6 +38,20 @@ struct TokenArgs {
   int* status;
 };
 
+// Long sequences may be cut into parts of `part` rows (0: none is).  Part x of head h has, at (x * H + h) d d,
+struct TokenParts {
+  int part;
+  float* enter;              // the state it starts from
+  float* comp_j;             // what it writes on its own: its last state from zero (the first part: from the sequence's first state)
+  float* comp_m;             // what it makes of an entering state: S -> S M
+};
+
+// Parts a sequence of `len` rows is cut into.  Two would gain nothing: composing the first and then running both takes as long as
+// one after the other.
+__host__ __device__ inline int token_parts(int len, int part) {
+  return part > 0 && len > 2 * part ? (len + part - 1) / part : 1;
+}
+
 constexpr int kStatusInvalidArg = 1;   // mirrors VDN_ERR_INVALID_ARG
 
 // Rows [start, start + len) of sequence s.  The offsets live in device memory, where the host cannot check them: they are
@@ -277,23 +291,26 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
 // where SMs would be left over.  Batches of 16 tokens -- keys, queries, this CTA's values, coefficients -- arrive by four tile
 // copies each, which a fifth warp issues, three batches ahead.
 // Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: 119 us, both kernels (R = 2: 150); a token at a time it took 289.
-template <typename Tio, int D, int R>
+// Long sequences of few (sequence, head)s: with COMPOSE the kernel makes, side by side, of each part what it writes by itself (J) and
+// what it makes of an entering state (M, rows of the identity walked without values); token_join_kernel passes the states along, and
+// the parts are walked from those.  9000 tokens, 1 head, d = 128, f32: 921 us whole, 167 in 33 parts (compose 62, join 58, walk 55).
+template <typename Tio, int D, int R, bool COMPOSE = false>
 struct TokenWalk {
   static constexpr int WALKERS = 128, THREADS = WALKERS + 32, ROWS = 8 * R, BATCH = 16, STAGES = 3;
   struct alignas(128) Stage {
-    Tio k[BATCH][D], q[BATCH][D], v[BATCH][ROWS];
+    Tio k[BATCH][D], v[BATCH][ROWS];
     float4 c[BATCH][kCoefFloats / 4];
+    Tio q[COMPOSE ? 1 : BATCH][D];                       // (composing reads none)
   };
-  static constexpr int BYTES = BATCH * (2 * D + ROWS) * (int)sizeof(Tio) + BATCH * kCoefFloats * 4;   // of one batch's copies
   static constexpr int SMEM_BYTES = STAGES * (int)sizeof(Stage) + 64 + 128;
 };
 
-template <typename Tio, int D, int R>
+template <typename Tio, int D, int R, bool COMPOSE>
 __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ,
                                                          const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmC,
-                                                         const TokenArgs a, tc::DevStatus ds) {
+                                                         const TokenArgs a, const TokenParts cut, tc::DevStatus ds) {
   using namespace tc;
-  using W = TokenWalk<Tio, D, R>;
+  using W = TokenWalk<Tio, D, R, COMPOSE>;
   constexpr int ROWS = W::ROWS, GROUPS = D / ROWS, B = W::BATCH;
   constexpr int NE = D / 16, NV = NE / 4;                // columns of a lane, in pieces of four, 64 apart
   extern __shared__ unsigned char walk_smem[];
@@ -305,10 +322,21 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
   const int tid = threadIdx.x, lane = tid & 31, l16 = lane & 15;
   const int row0 = (int)(blockIdx.x % GROUPS) * ROWS;
   const int r = ((tid >> 4) & 7) * R;                    // a walker's rows: row0 + r ..
-  const int h = (int)(blockIdx.x / GROUPS) % a.H, s = (int)(blockIdx.x / GROUPS) / a.H;
+  const int h = (int)(blockIdx.x / GROUPS) % a.H, y = (int)(blockIdx.x / GROUPS) / a.H;
+  const bool of_m = COMPOSE && (y & 1);                  // M's rows, or J's
+  const int p = COMPOSE ? y >> 1 : y;                    // the part, or the sequence where none is cut
+  const int s = cut.part > 0 ? token_seq_of(a, p, cut.part) : p;
   long long start;
   int len;
   token_range(a.cu_seqlens, s, a.per, a.n_tokens, start, len);
+  const int parts = token_parts(len, cut.part);
+  const int pos = cut.part > 0 ? p - ((int)(start / cut.part) + s) : 0;
+  // not every sequence fills its places; nothing follows the last part, and nothing enters the first
+  if (pos < 0 || pos >= parts || (COMPOSE && (pos + 1 == parts || (of_m && pos == 0)))) return;
+  if (parts > 1) {
+    start += (long long)pos * cut.part;
+    len = min(cut.part, len - pos * cut.part);
+  }
   if (tid == 0) {
     for (int i = 0; i < W::STAGES; ++i) { mbar_init(bars + 8 * i, 1); mbar_init(bars + 8 * (W::STAGES + i), W::WALKERS / 32); }
     *abort_flag = 0;
@@ -319,14 +347,16 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
   if (tid >= W::WALKERS) {
     // one thread keeps two batches on their way (issuing the copies takes a walker 600 cycles of a batch's 4500)
     if (tid == W::WALKERS) {
+      const typename W::Stage& st0 = stages[0];
       const int kc = h / (a.H / a.Hk) * D;
+      const int bytes = (int)(sizeof(st0.k) + sizeof(st0.c) + (COMPOSE ? 0 : sizeof(st0.q)) + (of_m ? 0 : sizeof(st0.v)));
       auto fetch = [&](int b) {
         const int st = b % W::STAGES, row = (int)start + b * B;
         const uint32_t bar = bars + 8 * st;
-        mbar_arrive_expect_tx(bar, W::BYTES);
+        mbar_arrive_expect_tx(bar, bytes);
         tma_load_2d(smem_u32(stages[st].k), &tmK, bar, kc, row);
-        tma_load_2d(smem_u32(stages[st].q), &tmQ, bar, kc, row);
-        tma_load_2d(smem_u32(stages[st].v), &tmV, bar, h * D + row0, row);
+        if (!COMPOSE) tma_load_2d(smem_u32(stages[st].q), &tmQ, bar, kc, row);
+        if (!of_m) tma_load_2d(smem_u32(stages[st].v), &tmV, bar, h * D + row0, row);
         tma_load_2d(smem_u32(stages[st].c), &tmC, bar, h * kCoefFloats, row);
       };
       uint32_t issued = 0;
@@ -340,14 +370,21 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
     }
     return;
   }
-  const size_t soff = (((size_t)s * a.H + h) * D + row0 + r) * D + l16 * 4;
+  const size_t own = (size_t)(row0 + r) * D + l16 * 4;
+  const size_t of_seq = ((size_t)s * a.H + h) * (D * D) + own, of_part = ((size_t)p * a.H + h) * (D * D) + own;
+  const float* first = !COMPOSE && parts > 1 ? cut.enter + of_part : pos == 0 && a.state_in ? a.state_in + of_seq : nullptr;
+  float* last = COMPOSE ? (of_m ? cut.comp_m : cut.comp_j) + of_part : pos + 1 == parts && a.state_out ? a.state_out + of_seq : nullptr;
   float x[R][NE];                                        // the state
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-      const float4 y = a.state_in ? *reinterpret_cast<const float4*>(a.state_in + soff + i * D + c * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 y = first ? *reinterpret_cast<const float4*>(first + i * D + c * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
       x[i][4 * c] = y.x; x[i][4 * c + 1] = y.y; x[i][4 * c + 2] = y.z; x[i][4 * c + 3] = y.w;
+      if (of_m) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i][4 * c + e] = l16 * 4 + c * 64 + e == row0 + r + i ? 1.f : 0.f;
+      }
     }
   auto columns = [&](const Tio* p, float (&y)[NE]) {
 #pragma unroll
@@ -372,7 +409,7 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
         }
         for (int e = lane; e < (g + 4 - n) * D; e += 32) {
           st.k[n + e / D][e % D] = from_float<Tio>(0.f);
-          st.q[n + e / D][e % D] = from_float<Tio>(0.f);
+          if (!COMPOSE) st.q[n + e / D][e % D] = from_float<Tio>(0.f);
         }
         for (int e = lane; e < (g + 4 - n) * ROWS; e += 32) st.v[n + e / ROWS][e % ROWS] = from_float<Tio>(0.f);
         __syncwarp();
@@ -380,48 +417,54 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
       float k[4][NE];
 #pragma unroll
       for (int i = 0; i < 4; ++i) columns(st.k[g + i], k[i]);
-      float d[8 * R];                                    // [row][S k_1 .. S k_4, S q_1 .. S q_4], this lane's columns
+      constexpr int N = COMPOSE ? 4 : 8;
+      float d[N * R];                                    // [row][S k_1 .. S k_4, S q_1 .. S q_4], this lane's columns
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float q[NE];
-        columns(st.q[g + i], q);
+        if (!COMPOSE) columns(st.q[g + i], q);
 #pragma unroll
         for (int w = 0; w < R; ++w) {
           float sk = 0.f, sq = 0.f;
 #pragma unroll
-          for (int e = 0; e < NE; ++e) { sk = fmaf(x[w][e], k[i][e], sk); sq = fmaf(x[w][e], q[e], sq); }
-          d[8 * w + i] = sk;
-          d[8 * w + 4 + i] = sq;
+          for (int e = 0; e < NE; ++e) {
+            sk = fmaf(x[w][e], k[i][e], sk);
+            if (!COMPOSE) sq = fmaf(x[w][e], q[e], sq);
+          }
+          d[N * w + i] = sk;
+          if (!COMPOSE) d[N * w + 4 + i] = sq;
         }
       }
-      // reduce: at each step a lane keeps the half of its values that its bit names and adds its partner's; with one row the
-      // last step adds two halves of the same
+      // reduce: at each step a lane keeps the half of its values that its bit names and adds its partner's; where that
+      // leaves one before the last bits, they are sums of the same
       int m = 8;                                         // the bit, from the highest
 #pragma unroll
-      for (int half = 4 * R; half > 0; half >>= 1, m >>= 1) {
+      for (int half = N * R / 2; half > 0; half >>= 1, m >>= 1) {
         const bool upper = l16 & m;
 #pragma unroll
         for (int i = 0; i < half; ++i) d[i] = (upper ? d[half + i] : d[i]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? d[i] : d[half + i], m);
       }
+      constexpr int LOW = N * R == 16 ? 0 : N * R == 8 ? 1 : 2;   // bits of the lane below those that say (row, query?, token)
       float mine = d[0];
-      if (R == 1) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, 1);
-      constexpr int LOW = R == 2 ? 0 : 1;                // bits of the lane below those that say (row, query?, token)
+#pragma unroll
+      for (int low = LOW - 1; low >= 0; --low) mine += __shfl_xor_sync(0xFFFFFFFFu, mine, 1 << low);
       const int what = l16 >> LOW;
       // lane (row, query?, token) has its product; the keys' ones go to all lanes
       float u[R][4];
       const float4 a0 = st.c[g][0], a1 = st.c[g + 1][0], a2 = st.c[g + 2][0], a3 = st.c[g + 3][0];
       const float4 tail = st.c[g + 3][1];
+      auto value = [&](int i, int w) { return of_m ? 0.f : to_float(st.v[i][r + w]); };
 #pragma unroll
       for (int w = 0; w < R; ++w) {
         float sk[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sk[i] = __shfl_sync(0xFFFFFFFFu, mine, (lane & 16) + ((8 * w + i) << LOW));
-        u[w][0] = a0.y * to_float(st.v[g][r + w]) - a0.x * sk[0];
-        u[w][1] = a1.y * to_float(st.v[g + 1][r + w]) - a1.x * sk[1] - a1.z * u[w][0];
-        u[w][2] = a2.y * to_float(st.v[g + 2][r + w]) - a2.x * sk[2] - a2.z * u[w][0] - a2.w * u[w][1];
-        u[w][3] = a3.y * to_float(st.v[g + 3][r + w]) - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - tail.x * u[w][2];
+        for (int i = 0; i < 4; ++i) sk[i] = __shfl_sync(0xFFFFFFFFu, mine, (lane & 16) + ((N * w + i) << LOW));
+        u[w][0] = a0.y * value(g, w) - a0.x * sk[0];
+        u[w][1] = a1.y * value(g + 1, w) - a1.x * sk[1] - a1.z * u[w][0];
+        u[w][2] = a2.y * value(g + 2, w) - a2.x * sk[2] - a2.z * u[w][0] - a2.w * u[w][1];
+        u[w][3] = a3.y * value(g + 3, w) - a3.x * sk[3] - a3.z * u[w][0] - a3.w * u[w][1] - tail.x * u[w][2];
       }
-      {
+      if (!COMPOSE) {
         const int i = g + (what & 3);
         const bool second = R == 2 && (what & 8);        // of the lane's two rows
         if ((what & 4) && (R == 2 || !(l16 & 1)) && i < n) {
@@ -445,13 +488,86 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
     }
     mbar_arrive_warp(bars + 8 * (W::STAGES + b % W::STAGES));
   }
-  if (a.state_out) {
+  if (last) {
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < NV; ++c)
-        *reinterpret_cast<float4*>(a.state_out + soff + i * D + c * 64) =
+        *reinterpret_cast<float4*>(last + i * D + c * 64) =
             make_float4(x[i][4 * c], x[i][4 * c + 1], x[i][4 * c + 2], x[i][4 * c + 3]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- part after part
+// The states the parts of a cut sequence enter with: enter_0 the first one, enter_1 = J_0, enter_{i+1} = enter_i M_i + J_i.  Rows
+// go their own ways: a CTA has 8 of a (sequence, head).  Eight groups of d/4 threads divide M's rows, d/8 each, so that each element of M is
+// fetched once, into registers and a part ahead of its use; their partial products are added through shared memory.  Plain
+// fp32.  Bound by the chain of parts.
+template <int D>
+struct TokenJoin {
+  static constexpr int THREADS = 2 * D, ROWS = 8;
+};
+template <int D>
+__global__ void __launch_bounds__(TokenJoin<D>::THREADS) token_join_kernel(const TokenArgs t, const TokenParts a) {
+  constexpr int ROWS = TokenJoin<D>::ROWS, GROUPS = D / ROWS, LANES = D / 4, K = D / 8;
+  __shared__ float sm[ROWS][D];                       // the state's rows
+  __shared__ float4 partial[8][ROWS][LANES];
+  const int r0 = (int)(blockIdx.x % GROUPS) * ROWS, h = (int)(blockIdx.x / GROUPS) % t.H, seq = (int)(blockIdx.x / GROUPS) / t.H;
+  long long start;
+  int len;
+  token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
+  const int parts = token_parts(len, a.part);
+  let_next_kernel_start();
+  wait_for_kernel_before();
+  if (parts == 1) return;
+  const int group = (int)threadIdx.x / LANES, lane = (int)threadIdx.x % LANES;
+  const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D, base = (x0 * t.H + h) * (D * D);
+  // the thread's own four elements of the state: row r0 + group, columns 4 lane ..
+  const size_t own = base + (size_t)(r0 + group) * D + lane * 4;
+  const float* mp = a.comp_m + base + (size_t)(group * K) * D + lane * 4;
+  {
+    const float* s0 = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) + (size_t)(r0 + group) * D + lane * 4 : nullptr;
+    *reinterpret_cast<float4*>(a.enter + own) = s0 ? *reinterpret_cast<const float4*>(s0) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float4 j = *reinterpret_cast<const float4*>(a.comp_j + own);
+    *reinterpret_cast<float4*>(a.enter + own + step) = j;
+    *reinterpret_cast<float4*>(&sm[group][lane * 4]) = j;
+  }
+  float4 m[K], next[K], j = make_float4(0.f, 0.f, 0.f, 0.f), jn = j;
+  auto fetch = [&](int p) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) next[k] = __ldg(reinterpret_cast<const float4*>(mp + p * step + (size_t)k * D));
+    jn = __ldg(reinterpret_cast<const float4*>(a.comp_j + own + p * step));
+  };
+  if (parts > 2) fetch(1);
+  for (int p = 1; p + 1 < parts; ++p) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) m[k] = next[k];
+    j = jn;
+    if (p + 2 < parts) fetch(p + 1);
+    __syncthreads();                                  // the state is there
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < K; k += 4) {
+        const float4 s = *reinterpret_cast<const float4*>(&sm[r][group * K + k]);
+        const float s4[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc.x = fmaf(s4[e], m[k + e].x, acc.x); acc.y = fmaf(s4[e], m[k + e].y, acc.y);
+          acc.z = fmaf(s4[e], m[k + e].z, acc.z); acc.w = fmaf(s4[e], m[k + e].w, acc.w);
+        }
+      }
+      partial[group][r][lane] = acc;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const float4 q = partial[w][group][lane];
+      j.x += q.x; j.y += q.y; j.z += q.z; j.w += q.w;
+    }
+    *reinterpret_cast<float4*>(a.enter + own + (p + 1) * step) = j;
+    *reinterpret_cast<float4*>(&sm[group][lane * 4]) = j;
   }
 }
 

@@ -39,17 +39,12 @@ struct TokenTc {
   static constexpr int F_FLOATS = 132, F_BYTES = F_FLOATS * 4;
 };
 
-struct TokenTcArgs {
+struct TokenTcArgs : TokenParts {
   TokenArgs t;
   unsigned char* e;          // [places * H] E_BYTES
   unsigned char* p;          // ... P_BYTES
   unsigned char* f;          // ... F_BYTES
-  // long sequences in parts of `part` rows (0: whole); part x of head h has, at (x * H + h) d d,
-  int part;
   int places;                // of chunks
-  float* enter;              // the state it starts from
-  float* comp_j;             // what it writes on its own: its last state from zero (the first part: from the sequence's first state)
-  float* comp_m;             // what it makes of an entering state: S -> S M
   int* order;                // [S] the sequences, longest first, or null: as they come
 };
 
@@ -68,12 +63,6 @@ __device__ __forceinline__ void token_order(const TokenArgs& t, int* order, int*
     for (int j = 0; j < t.S; ++j) rank += lens[j] > own || (lens[j] == own && j < s);
     order[rank] = s;
   }
-}
-
-// Parts a sequence of `len` rows is cut into.  Two would gain nothing: composing the first and then running both takes as long as
-// one after the other.
-__host__ __device__ inline int token_parts(int len, int part) {
-  return part > 0 && len > 2 * part ? (len + part - 1) / part : 1;
 }
 
 namespace tc {
@@ -1230,78 +1219,6 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   if (warp == 1) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
-  }
-}
-
-// ---------------------------------------------------------------------------------------------- part after part
-// The states the parts of a cut sequence enter with: enter_0 the first one, enter_1 = J_0, enter_{i+1} = enter_i M_i + J_i.  Rows
-// go their own ways: a CTA has 8 of a (sequence, head).  Its eight warps divide M's rows, 16 each, so that each element of M is
-// fetched once, into registers and a part ahead of its use; their partial products are added through shared memory.  Plain
-// fp32.  Bound by the chain of parts.
-struct TokenJoin {
-  static constexpr int THREADS = 256, ROWS = 8;
-};
-__global__ void __launch_bounds__(TokenJoin::THREADS) token_join_kernel(const TokenTcArgs a) {
-  constexpr int D = TokenTc::D, ROWS = TokenJoin::ROWS, GROUPS = D / ROWS;
-  __shared__ float sm[ROWS][D];                       // the state's rows
-  __shared__ float4 partial[8][ROWS][32];
-  const TokenArgs& t = a.t;
-  const int r0 = (int)(blockIdx.x % GROUPS) * ROWS, h = (int)(blockIdx.x / GROUPS) % t.H, seq = (int)(blockIdx.x / GROUPS) / t.H;
-  long long start;
-  int len;
-  token_range(t.cu_seqlens, seq, t.per, t.n_tokens, start, len);
-  const int parts = token_parts(len, a.part);
-  let_next_kernel_start();
-  wait_for_kernel_before();
-  if (parts == 1) return;
-  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-  const size_t x0 = (size_t)(start / a.part + seq), step = (size_t)t.H * D * D, base = (x0 * t.H + h) * (D * D);
-  // the thread's own four elements of the state: row r0 + warp, columns 4 lane ..
-  const size_t own = base + (size_t)(r0 + warp) * D + lane * 4;
-  const float* mp = a.comp_m + base + (size_t)(warp * 16) * D + lane * 4;
-  {
-    const float* s0 = t.state_in ? t.state_in + ((size_t)seq * t.H + h) * (D * D) + (size_t)(r0 + warp) * D + lane * 4 : nullptr;
-    *reinterpret_cast<float4*>(a.enter + own) = s0 ? *reinterpret_cast<const float4*>(s0) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4 j = *reinterpret_cast<const float4*>(a.comp_j + own);
-    *reinterpret_cast<float4*>(a.enter + own + step) = j;
-    *reinterpret_cast<float4*>(&sm[warp][lane * 4]) = j;
-  }
-  float4 m[16], next[16], j = make_float4(0.f, 0.f, 0.f, 0.f), jn = j;
-  auto fetch = [&](int p) {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) next[k] = __ldg(reinterpret_cast<const float4*>(mp + p * step + (size_t)k * D));
-    jn = __ldg(reinterpret_cast<const float4*>(a.comp_j + own + p * step));
-  };
-  if (parts > 2) fetch(1);
-  for (int p = 1; p + 1 < parts; ++p) {
-#pragma unroll
-    for (int k = 0; k < 16; ++k) m[k] = next[k];
-    j = jn;
-    if (p + 2 < parts) fetch(p + 1);
-    __syncthreads();                                  // the state is there
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 16; k += 4) {
-        const float4 s = *reinterpret_cast<const float4*>(&sm[r][warp * 16 + k]);
-        const float s4[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          acc.x = fmaf(s4[e], m[k + e].x, acc.x); acc.y = fmaf(s4[e], m[k + e].y, acc.y);
-          acc.z = fmaf(s4[e], m[k + e].z, acc.z); acc.w = fmaf(s4[e], m[k + e].w, acc.w);
-        }
-      }
-      partial[warp][r][lane] = acc;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float4 q = partial[w][warp][lane];
-      j.x += q.x; j.y += q.y; j.z += q.z; j.w += q.w;
-    }
-    *reinterpret_cast<float4*>(a.enter + own + (p + 1) * step) = j;
-    *reinterpret_cast<float4*>(&sm[warp][lane * 4]) = j;
   }
 }
 

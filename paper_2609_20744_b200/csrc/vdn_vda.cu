@@ -1278,36 +1278,80 @@ cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, 
   return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
 }
 
-template <typename Tio, int D, int R>
-vdn_status launch_walk(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
-  using W = vdn::TokenWalk<Tio, D, R>;
-  constexpr bool F32 = sizeof(Tio) == 4;
-  CUtensorMap tmK, tmQ, tmV, tmC;
+// The lengths stay on the device.  Where a choice depends on the longest sequence: four times the average, if there are so many.
+long long longest_guess(long long n_tokens, int n_seqs) { return n_seqs > 4 ? 4 * (n_tokens / n_seqs) : n_tokens; }
+
+// Workspace of the plain rule: nothing for a few tokens a sequence; else the coefficients, and per (part, head) of cut sequences
+// three states.
+struct TokenPlainLayout {
+  bool few;
+  int part;                 // rows of a part; 0: no sequence is cut
+  long long parts;
+  size_t enter, comp_j, comp_m, total;
+};
+TokenPlainLayout make_plain_layout(const vdn_vda_s* h, long long n_tokens, int n_seqs, int heads) {
+  TokenPlainLayout L = {};
+  L.few = few_tokens(n_tokens, n_seqs);
+  if (L.few) return L;
+  const size_t state = (size_t)h->cfg.d * h->cfg.d * sizeof(float);
+  L.parts = n_seqs;
+  // Cutting costs more than twice the work (parts are composed and walked) and leaves two walks of a part, with the join between them,
+  // where a walk of the whole sequence was.  Microseconds, fitted to graph replays of 1 .. 20 sequences of 256 .. 9000 tokens and
+  // 1 .. 36 heads, d = 64 and 128: 0.1 for a token of a walk, 0.0025 (d = 128) for each token and head besides; cut, 0.01
+  // (d = 128; 0.0037, d = 64) for each token and head, and 1.7 / 0.85 to join a part.  The length of a part balances its walk with the
+  // joins.  9000 tokens, f32: 1 head 921 us whole, 167 cut (d = 64: 834, 91); 12 heads 1311, 1203 (854, 453); 36 heads 1720,
+  // 3434; 256 tokens, 2 heads, d = 64: 31, 23.
+  const double wide = h->cfg.d / 128.0, longest = (double)longest_guess(n_tokens, n_seqs), work = (double)n_tokens * heads;
+  const double rows = std::max(64.0, std::sqrt(8.5 * wide * longest));
+  const double whole = 6.0 + 0.1 * longest + 0.0025 * wide * wide * work;
+  const double parted = 12.0 + 0.2 * rows + 1.7 * wide * longest / rows + 0.01 * std::pow(wide, 1.5) * work;
+  if (longest > 2.0 * rows && parted < whole) {
+    L.part = ((int)rows + 15) / 16 * 16;                // (whole batches of the walk)
+    L.parts = n_tokens / L.part + n_seqs;
+  }
+  size_t off = align_up((size_t)n_tokens * heads * vdn::kCoefFloats * sizeof(float));
+  const size_t states = L.part ? (size_t)L.parts * heads * state : 0;
+  L.enter = off; off += states;
+  L.comp_j = off; off += states;
+  L.comp_m = off; off += states;
+  L.total = off;
+  return L;
+}
+
+struct WalkMaps { CUtensorMap k, q, v, c; };
+
+template <typename Tio, int D, int R, bool COMPOSE>
+vdn_status launch_walk(vdn_vda_t h, const vdn::TokenArgs& a, const vdn::TokenParts& cut, long long units, WalkMaps& m, cudaStream_t st) {
+  using W = vdn::TokenWalk<Tio, D, R, COMPOSE>;
+  const long long wv = (long long)a.H * D;
   vdn_status r;
-  const long long wk = (long long)a.Hk * D, wv = (long long)a.H * D, wc = (long long)a.H * vdn::kCoefFloats;
-  constexpr CUtensorMapSwizzle none = CU_TENSOR_MAP_SWIZZLE_NONE;
-  if ((r = make_rows_map(h, &tmK, a.k, F32, a.n_tokens, wk, a.k_stride, D, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmQ, a.q, F32, a.n_tokens, wk, a.q_stride, D, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmV, a.v, F32, a.n_tokens, wv, a.v_stride, W::ROWS, W::BATCH, none)) != VDN_OK) return r;
-  if ((r = make_rows_map(h, &tmC, coef, true, a.n_tokens, wc, wc, vdn::kCoefFloats, W::BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &m.v, a.v, sizeof(Tio) == 4, a.n_tokens, wv, a.v_stride, W::ROWS, W::BATCH, CU_TENSOR_MAP_SWIZZLE_NONE)) != VDN_OK)
+    return r;
   if (W::SMEM_BYTES > 48 * 1024)
-    VDN_CUDA(h, (cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, W::SMEM_BYTES)));
-  const long long warps = (a.n_tokens / 4 + a.S) * a.H;
-  if (warps / 8 + 1 > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (token, head) pairs for one call");
-  vdn::token_coef_kernel<Tio, D><<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, coef, warps);
-  prof_mark(h, st, 0, "token_coef");
+    VDN_CUDA(h, (cudaFuncSetAttribute(vdn::token_walk_kernel<Tio, D, R, COMPOSE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      W::SMEM_BYTES)));
   // (not overlapped with its predecessor: CTAs placed while that still holds most SMs would share the few free ones, and each of
   // these has little but latency to offer)
-  vdn::token_walk_kernel<Tio, D, R><<<(unsigned)(a.S * a.H * (D / W::ROWS)), W::THREADS, W::SMEM_BYTES, st>>>(tmK, tmQ, tmV, tmC, a,
-                                                                                                             dev_status(h));
+  vdn::token_walk_kernel<Tio, D, R, COMPOSE><<<(unsigned)(units * a.H * (D / W::ROWS)), W::THREADS, W::SMEM_BYTES, st>>>(
+      m.k, m.q, m.v, m.c, a, cut, dev_status(h));
   return VDN_OK;
 }
 
-// Plain fp32.  `coef`: workspace of the walking kernels, or null: token by token.
+// `units`: sequences, or parts, or twice as many where parts are composed.
+template <typename Tio, int D, bool COMPOSE>
+vdn_status launch_walk(vdn_vda_t h, const vdn::TokenArgs& a, const vdn::TokenParts& cut, long long units, WalkMaps& m, cudaStream_t st) {
+  if (units * a.H * (D / 8) > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
+  // CTAs of eight rows where that leaves at most two on an SM.  1024 tokens, d = 128, bf16: 2 heads (32 CTAs) 119 us instead of
+  // 150, 8 heads (128 CTAs) 121 instead of 191, 8 sequences of 2 heads (256 CTAs) 152 instead of 160.
+  if (units * a.H * (D / 8) <= 2LL * h->sm_count) return launch_walk<Tio, D, 1, COMPOSE>(h, a, cut, units, m, st);
+  return launch_walk<Tio, D, 2, COMPOSE>(h, a, cut, units, m, st);
+}
+
+// Plain fp32.
 template <typename Tio, int D>
-vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
+vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, const TokenPlainLayout& L, unsigned char* ws, cudaStream_t st) {
   prof_begin(h, st);
-  if (!coef) {
+  if (L.few) {
     const long long states = (long long)a.S * a.H;
     if (states >= 4LL * h->sm_count) vdn::token_few_kernel<Tio, D, D / 32><<<(unsigned)states, 256, 0, st>>>(a);
     else vdn::token_few_kernel<Tio, D, 1><<<(unsigned)(states * (D / 32)), 256, 0, st>>>(a);
@@ -1316,29 +1360,47 @@ vdn_status launch_token_plain(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef
     VDN_CUDA(h, cudaGetLastError());
     return VDN_OK;
   }
-  // CTAs of eight rows where that leaves at most two on an SM.  1024 tokens, d = 128, bf16: 2 heads (32 CTAs) 119 us instead of
-  // 150, 8 heads (128 CTAs) 121 instead of 191, 8 sequences of 2 heads (256 CTAs) 152 instead of 160.
-  const bool narrow = (long long)a.S * a.H * (D / 8) <= 2LL * h->sm_count;
-  const vdn_status r = narrow ? launch_walk<Tio, D, 1>(h, a, coef, st) : launch_walk<Tio, D, 2>(h, a, coef, st);
-  if (r != VDN_OK) return r;
-  prof_mark(h, st, 1, "token_walk");
-  h->launches = 2;
+  constexpr bool F32 = sizeof(Tio) == 4;
+  constexpr int BATCH = vdn::TokenWalk<Tio, D, 1>::BATCH;
+  constexpr CUtensorMapSwizzle none = CU_TENSOR_MAP_SWIZZLE_NONE;
+  float4* coef = reinterpret_cast<float4*>(ws);
+  const vdn::TokenParts cut = {L.part, reinterpret_cast<float*>(ws + L.enter), reinterpret_cast<float*>(ws + L.comp_j),
+                               reinterpret_cast<float*>(ws + L.comp_m)};
+  const long long wk = (long long)a.Hk * D, wc = (long long)a.H * vdn::kCoefFloats;
+  WalkMaps m;
+  vdn_status r;
+  if ((r = make_rows_map(h, &m.k, a.k, F32, a.n_tokens, wk, a.k_stride, D, BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &m.q, a.q, F32, a.n_tokens, wk, a.q_stride, D, BATCH, none)) != VDN_OK) return r;
+  if ((r = make_rows_map(h, &m.c, coef, true, a.n_tokens, wc, wc, vdn::kCoefFloats, BATCH, none)) != VDN_OK) return r;
+  const long long warps = (a.n_tokens / 4 + a.S) * a.H;
+  if (warps / 8 + 1 > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "too many (token, head) pairs for one call");
+  int nk = 0;
+  vdn::token_coef_kernel<Tio, D><<<(unsigned)((warps + 7) / 8), 256, 0, st>>>(a, coef, warps);
+  prof_mark(h, st, nk++, "token_coef");
+  if (L.part) {
+    if ((r = launch_walk<Tio, D, true>(h, a, cut, 2 * L.parts, m, st)) != VDN_OK) return r;
+    prof_mark(h, st, nk++, "token_walk_compose");
+    using J = vdn::TokenJoin<D>;
+    vdn::token_join_kernel<D><<<(unsigned)(a.S * a.H * (D / J::ROWS)), J::THREADS, 0, st>>>(a, cut);
+    prof_mark(h, st, nk++, "token_join");
+  }
+  if ((r = launch_walk<Tio, D, false>(h, a, cut, L.parts, m, st)) != VDN_OK) return r;
+  prof_mark(h, st, nk++, "token_walk");
+  h->launches = nk;
   VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
 }
 
-vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, float4* coef, cudaStream_t st) {
+// `ws`: workspace of a scan, null for a step.
+vdn_status launch_token_rule(vdn_vda_t h, const vdn::TokenArgs& a, const TokenPlainLayout& L, unsigned char* ws, cudaStream_t st) {
   const int d = h->cfg.d;
   if ((long long)a.S * a.H * (d / 8) > 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (sequence, head) pairs for one call");
-  if (coef && !h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  if (!L.few && !h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
   if (h->cfg.io_dtype == VDN_F32)
-    return d == 64 ? launch_token_plain<float, 64>(h, a, coef, st) : launch_token_plain<float, 128>(h, a, coef, st);
-  return d == 64 ? launch_token_plain<__nv_bfloat16, 64>(h, a, coef, st) : launch_token_plain<__nv_bfloat16, 128>(h, a, coef, st);
+    return d == 64 ? launch_token_plain<float, 64>(h, a, L, ws, st) : launch_token_plain<float, 128>(h, a, L, ws, st);
+  return d == 64 ? launch_token_plain<__nv_bfloat16, 64>(h, a, L, ws, st) : launch_token_plain<__nv_bfloat16, 128>(h, a, L, ws, st);
 }
-
-// The lengths stay on the device.  Where a choice depends on the longest sequence: four times the average, if there are so many.
-long long longest_guess(long long n_tokens, int n_seqs) { return n_seqs > 4 ? 4 * (n_tokens / n_seqs) : n_tokens; }
 
 // Workspace of the chunked rule: per (place, head) the chunk's two operators and its factors; per (part, head) of cut
 // sequences the state it enters with and its composite.
@@ -1432,8 +1494,9 @@ vdn_status launch_token_tc(vdn_vda_t h, const vdn::TokenArgs& t, unsigned char* 
     VDN_CUDA(h, launch_overlapped(vdn::token_compose_kernel, (unsigned)(L.parts * t.H), vdn::TokenCompose::THREADS,
                                   vdn::TokenCompose::SMEM_BYTES, st, tmK, tmV, a, ds));
     prof_mark(h, st, nk++, "token_compose");
-    VDN_CUDA(h, launch_overlapped(vdn::token_join_kernel, (unsigned)(t.S * t.H * (128 / vdn::TokenJoin::ROWS)),
-                                  vdn::TokenJoin::THREADS, 0, st, a));
+    using J = vdn::TokenJoin<128>;
+    const vdn::TokenParts cut = a;
+    VDN_CUDA(h, launch_overlapped(vdn::token_join_kernel<128>, (unsigned)(t.S * t.H * (128 / J::ROWS)), J::THREADS, 0, st, t, cut));
     prof_mark(h, st, nk++, "token_join");
   }
   VDN_CUDA(h, launch_overlapped(vdn::token_chain_kernel, (unsigned)(L.parts * t.H), TC::THREADS, TC::SMEM_BYTES, st, tmK, tmQ, tmV,
@@ -1461,9 +1524,11 @@ void launch_rotary(const vdn::RotaryArgs& a, bool half, unsigned grid, size_t sm
 extern "C" {
 
 size_t vdn_vda_token_scan_workspace_bytes(vdn_vda_t h, long long n_tokens, const vdn_vda_token_params* p) {
-  if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->n_seqs <= 0 || n_tokens < 0) return 0;
+  if (!h || !p || p->struct_size != sizeof(vdn_vda_token_params) || p->heads <= 0 || p->heads > 65535 || p->n_seqs <= 0 ||
+      n_tokens < 0 || n_tokens > 0x7fffffffLL / 2)
+    return 0;
   if (token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads)) return make_token_layout(h, n_tokens, p->n_seqs, p->heads).total;
-  return few_tokens(n_tokens, p->n_seqs) ? 0 : align_up((size_t)n_tokens * p->heads * vdn::kCoefFloats * sizeof(float));
+  return make_plain_layout(h, n_tokens, p->n_seqs, p->heads).total;
 }
 
 vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1492,7 +1557,7 @@ vdn_status vdn_vda_token_scan(vdn_vda_t h, const void* q, const void* k, const v
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (token_on_tensor_cores(h, n_tokens, p->n_seqs, p->heads)) return launch_token_tc(h, a, static_cast<unsigned char*>(workspace), st);
-  return launch_token_rule(h, a, need ? static_cast<float4*>(workspace) : nullptr, st);
+  return launch_token_rule(h, a, make_plain_layout(h, n_tokens, p->n_seqs, p->heads), static_cast<unsigned char*>(workspace), st);
 }
 
 vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const void* v, const float* beta, void* out,
@@ -1517,7 +1582,9 @@ vdn_status vdn_vda_token_step(vdn_vda_t h, const void* q, const void* k, const v
   a.state_out = p->state;
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
-  return launch_token_rule(h, a, nullptr, static_cast<cudaStream_t>(cuda_stream));
+  TokenPlainLayout few = {};
+  few.few = true;
+  return launch_token_rule(h, a, few, nullptr, static_cast<cudaStream_t>(cuda_stream));
 }
 
 vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void* q_out, void* k_out, int B, int T, int F,

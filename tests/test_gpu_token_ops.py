@@ -73,7 +73,7 @@ def rel(got, want):
     return off / np.linalg.norm(want) if np.linalg.norm(want) else off
 
 
-def check_scan(vda, x, lens, dtype, d, tc, s0=None, scale=1.0, l2_eps=0.0, out=None, state=None, **kw):
+def check_scan(vda, x, lens, dtype, d, tc, s0=None, scale=1.0, l2_eps=0.0, out=None, state=None, walks=1, **kw):
     cu = torch.tensor([0] + list(lens)).cumsum(0).to(torch.int32).to(DEV)
     sizes = []
     want_o, want_s = tok.packed(np64(x["q"]), np64(x["k"]), np64(x["v"]), np64(x["beta"]), lens, np64(x["log_alpha"]),
@@ -84,7 +84,7 @@ def check_scan(vda, x, lens, dtype, d, tc, s0=None, scale=1.0, l2_eps=0.0, out=N
     assert vda.status() == binding.VDN_OK
     at = 0
     for i, n in enumerate(lens):
-        tol = tolerances(dtype, d, n, tc)
+        tol = tolerances(dtype, d, walks * n, tc)
         w = slice(at, at + n)
         for h in range(state.shape[1]):
             assert rel(state[i, h], want_s[i, h]) <= tol[2], (i, h, n)
@@ -116,6 +116,21 @@ def test_scan_of_more_rows_than_run_at_once(dtype, d, flags):
     x = draw(sum(lens), 4, 2, d, dtype, seed=11)
     s0 = 0.3 * torch.randn(len(lens), 4, d, d, device=DEV)
     check_scan(binding.Vda(d, dtype, flags=flags), x, lens, dtype, d, False, s0, scale=0.5)
+
+
+@pytest.mark.parametrize("dtype,d,flags", [("f32", 64, 0), ("f32", 128, 0), ("bf16", 64, 0),
+                                           ("bf16", 128, binding.VDN_FLAG_FORCE_SIMT)])
+@pytest.mark.parametrize("lens", [[1000], [131, 0, 1203, 64], [577, 578]], ids=str)
+def test_scan_plain_in_parts(dtype, d, flags, lens):
+    """Few long sequences, cut into parts.  Three walks (what a part writes, what it makes of an entering state, the part itself) each
+    add a rounding a token, the joins one product of d terms a part of 64 tokens or more: fewer than four walks' roundings."""
+    vda = binding.Vda(d, dtype, flags=flags)
+    x = draw(sum(lens), 2, 1, d, dtype, seed=12)
+    x["log_alpha"][200] = -float("inf")
+    s0 = 0.3 * torch.randn(len(lens), 2, d, d, device=DEV)
+    vda.profile(True)
+    check_scan(vda, x, lens, dtype, d, False, s0, scale=0.5, state=s0, walks=4)
+    assert [k[0] for k in vda.kernel_times()] == ["token_coef", "token_walk_compose", "token_join", "token_walk"]
 
 
 @pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 64), ("bf16", 128)])
@@ -262,8 +277,9 @@ def test_scan_takes_the_kernels_its_sizes_call_for():
     d, h = 128, 2
     few, walk, chunks = ["token_few"], ["token_coef", "token_walk"], ["token_prep", "token_chain"]
     parts = ["token_prep", "token_compose", "token_join", "token_chain"]
+    plain_parts = ["token_coef", "token_walk_compose", "token_join", "token_walk"]
     for flags, wanted in ((0, {2: few, 20: walk, 300: chunks, 3000: parts}),
-                          (binding.VDN_FLAG_FORCE_SIMT, {2: few, 20: walk, 300: walk, 3000: walk})):
+                          (binding.VDN_FLAG_FORCE_SIMT, {2: few, 20: walk, 300: walk, 3000: plain_parts})):
         for n, names in wanted.items():
             vda = binding.Vda(d, "bf16", flags=flags)
             vda.profile(True)
