@@ -272,6 +272,22 @@ def test_scan_same_call_same_bits(lens, h, hk):
     assert rel(s1, np64(s2)) <= 2 * state
 
 
+@pytest.mark.parametrize("dtype,d,lens,h", [("f32", 64, [2500], 2), ("f32", 128, [700, 3, 1300], 4), ("bf16", 64, [80] * 40, 8)],
+                         ids=str)
+def test_plain_scan_same_call_same_bits(dtype, d, lens, h):
+    """The plain kernels likewise, in parts and whole, two calls of one handle at once on streams of their own among them."""
+    x = draw(sum(lens), h, h, d, dtype, seed=13)
+    cu = torch.tensor([0] + lens).cumsum(0).to(torch.int32).to(DEV)
+    vda = binding.Vda(d, dtype)
+    o1, s1 = vda.token_scan(**x, cu_seqlens=cu)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        many = [vda.token_scan(**x, cu_seqlens=cu, stream=streams[i % 2]) for i in range(6)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, o1) and torch.equal(s, s1) for o, s in many)
+
+
 def test_scan_takes_the_kernels_its_sizes_call_for():
     """Short sequences token by token, longer ones in chunks, few long ones in parts."""
     d, h = 128, 2
