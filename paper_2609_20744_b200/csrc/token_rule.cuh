@@ -285,6 +285,21 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
   }
 }
 
+// Two fp32 numbers worked on by one instruction: the fp32 pipe is no faster so, but half as many instructions are issued.
+namespace tc {
+__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+}  // namespace tc
+
 // One CTA (four warps, one to a scheduler) to 8 R rows of a (sequence, head), since a step is a chain of latencies (dot products,
 // shuffles, update).  A row is shared by 16 lanes, which hold R rows each; the 8 R dot products of a step are reduced together,
 // each lane ending with one of them (15 shuffles instead of 64).  R = 2 does the least work; R = 1 shortens a step, with twice the CTAs,
@@ -293,7 +308,9 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
 // Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: 119 us, both kernels (R = 2: 150); a token at a time it took 289.
 // Long sequences of few (sequence, head)s: with COMPOSE the kernel makes, side by side, of each part what it writes by itself (J) and
 // what it makes of an entering state (M, rows of the identity walked without values); token_join_kernel passes the states along, and
-// the parts are walked from those.  9000 tokens, 1 head, d = 128, f32: 921 us whole, 167 in 33 parts (compose 62, join 58, walk 55).
+// the parts are walked from those.  9000 tokens, 1 head, d = 128, f32: 921 us whole, 167 in 33 parts (compose 62, join 51, walk 55).
+// Many heads (9000 tokens, 36, d = 128, f32): 1540 us; 1720 with queries fetched one by one and single fp32 instructions, about 60 % of
+// the issue slots and of the shared-memory pipe either way.
 template <typename Tio, int D, int R, bool COMPOSE = false>
 struct TokenWalk {
   static constexpr int WALKERS = 128, THREADS = WALKERS + 32, ROWS = 8 * R, BATCH = 16, STAGES = 3;
@@ -374,23 +391,28 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
   const size_t of_seq = ((size_t)s * a.H + h) * (D * D) + own, of_part = ((size_t)p * a.H + h) * (D * D) + own;
   const float* first = !COMPOSE && parts > 1 ? cut.enter + of_part : pos == 0 && a.state_in ? a.state_in + of_seq : nullptr;
   float* last = COMPOSE ? (of_m ? cut.comp_m : cut.comp_j) + of_part : pos + 1 == parts && a.state_out ? a.state_out + of_seq : nullptr;
-  float x[R][NE];                                        // the state
+  uint64_t x[R][NE / 2];                                 // the state, in pairs
 #pragma unroll
   for (int i = 0; i < R; ++i)
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
       const float4 y = first ? *reinterpret_cast<const float4*>(first + i * D + c * 64) : make_float4(0.f, 0.f, 0.f, 0.f);
-      x[i][4 * c] = y.x; x[i][4 * c + 1] = y.y; x[i][4 * c + 2] = y.z; x[i][4 * c + 3] = y.w;
+      x[i][2 * c] = f2_pack(y.x, y.y);
+      x[i][2 * c + 1] = f2_pack(y.z, y.w);
       if (of_m) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[i][4 * c + e] = l16 * 4 + c * 64 + e == row0 + r + i ? 1.f : 0.f;
+        for (int e = 0; e < 2; ++e) {
+          const int col = l16 * 4 + c * 64 + 2 * e;
+          x[i][2 * c + e] = f2_pack(col == row0 + r + i ? 1.f : 0.f, col + 1 == row0 + r + i ? 1.f : 0.f);
+        }
       }
     }
-  auto columns = [&](const Tio* p, float (&y)[NE]) {
+  auto columns = [&](const Tio* p, uint64_t (&y)[NE / 2]) {
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
       const float4 z = load4(p + l16 * 4 + c * 64);
-      y[4 * c] = z.x; y[4 * c + 1] = z.y; y[4 * c + 2] = z.z; y[4 * c + 3] = z.w;
+      y[2 * c] = f2_pack(z.x, z.y);
+      y[2 * c + 1] = f2_pack(z.z, z.w);
     }
   };
   for (int b = 0; b < batches; ++b) {
@@ -414,7 +436,7 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
         for (int e = lane; e < (g + 4 - n) * ROWS; e += 32) st.v[n + e / ROWS][e % ROWS] = from_float<Tio>(0.f);
         __syncwarp();
       }
-      float k[4][NE], q[4][NE];                          // (all fetched first: 36 heads, f32, d = 128: 5 % faster than one by one)
+      uint64_t k[4][NE / 2], q[4][NE / 2];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         columns(st.k[g + i], k[i]);
@@ -426,14 +448,19 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
       for (int i = 0; i < 4; ++i) {
 #pragma unroll
         for (int w = 0; w < R; ++w) {
-          float sk = 0.f, sq = 0.f;
+          uint64_t sk = 0, sq = 0;
 #pragma unroll
-          for (int e = 0; e < NE; ++e) {
-            sk = fmaf(x[w][e], k[i][e], sk);
-            if (!COMPOSE) sq = fmaf(x[w][e], q[i][e], sq);
+          for (int e = 0; e < NE / 2; ++e) {
+            sk = f2_fma(x[w][e], k[i][e], sk);
+            if (!COMPOSE) sq = f2_fma(x[w][e], q[i][e], sq);
           }
-          d[N * w + i] = sk;
-          if (!COMPOSE) d[N * w + 4 + i] = sq;
+          float lo, hi;
+          f2_unpack(sk, lo, hi);
+          d[N * w + i] = lo + hi;
+          if (!COMPOSE) {
+            f2_unpack(sq, lo, hi);
+            d[N * w + 4 + i] = lo + hi;
+          }
         }
       }
       // reduce: at each step a lane keeps the half of its values that its bit names and adds its partner's; where that
@@ -480,11 +507,13 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
       for (int i = 0; i < 4; ++i) e4[i] = st.c[g + i][1].y;
 #pragma unroll
       for (int w = 0; w < R; ++w) {
+        uint64_t uu[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[w][i] *= e4[i];
+        for (int i = 0; i < 4; ++i) uu[i] = f2_pack(u[w][i] * e4[i], u[w][i] * e4[i]);
 #pragma unroll
-        for (int e = 0; e < NE; ++e)
-          x[w][e] = fmaf(u[w][3], k[3][e], fmaf(u[w][2], k[2][e], fmaf(u[w][1], k[1][e], fmaf(u[w][0], k[0][e], tail.w * x[w][e]))));
+        for (int e = 0; e < NE / 2; ++e)
+          x[w][e] = f2_fma(uu[3], k[3][e], f2_fma(uu[2], k[2][e], f2_fma(uu[1], k[1][e],
+                    f2_fma(uu[0], k[0][e], f2_fma(f2_pack(tail.w, tail.w), x[w][e], 0ull)))));
       }
     }
     mbar_arrive_warp(bars + 8 * (W::STAGES + b % W::STAGES));
@@ -494,8 +523,12 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
     for (int i = 0; i < R; ++i)
 #pragma unroll
       for (int c = 0; c < NV; ++c)
-        *reinterpret_cast<float4*>(last + i * D + c * 64) =
-            make_float4(x[i][4 * c], x[i][4 * c + 1], x[i][4 * c + 2], x[i][4 * c + 3]);
+      {
+        float4 y;
+        f2_unpack(x[i][2 * c], y.x, y.y);
+        f2_unpack(x[i][2 * c + 1], y.z, y.w);
+        *reinterpret_cast<float4*>(last + i * D + c * 64) = y;
+      }
   }
 }
 

@@ -119,18 +119,7 @@ __device__ __forceinline__ void split2_pair(float x0, float x1, uint32_t& hi, ui
   const float r0 = x0 - __uint_as_float(hi << 16), r1 = x1 - __uint_as_float(hi & 0xFFFF0000u);
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(r1), "f"(r0));
 }
-// Two floats at once on the packed fp32 pipe: no faster, but half as many instructions, and these kernels are short of issue slots.
-__device__ __forceinline__ uint64_t f2_pack(float a, float b) {
-  uint64_t r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ void f2_unpack(uint64_t r, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
+// The same in packed fp32 arithmetic: these kernels are short of issue slots.
 __device__ __forceinline__ void split2_pair(uint64_t x, uint32_t& hi, uint32_t& lo) {
   float x0, x1, r0, r1;
   f2_unpack(x, x0, x1);
