@@ -303,6 +303,43 @@ def test_scan_takes_the_kernels_its_sizes_call_for():
             assert [k[0] for k in vda.kernel_times()] == names and vda.launch_count() == len(names)
 
 
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128)])
+def test_offsets_beyond_32_bits(dtype, d):
+    """Slices of one wide buffer whose last rows lie more than 2^31 elements in, a pool of states likewise: the bits of dense tensors."""
+    h, n, width = 2, 2150, 1 << 20
+    if torch.cuda.mem_get_info(DEV)[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    x = draw(n, h, h, d, dtype, seed=14)
+    vda = binding.Vda(d, dtype)
+    wide = torch.empty(n, width, dtype=TYPES[dtype], device=DEV)
+    part = {}
+    for i, name in enumerate(("q", "k", "v", "out")):
+        part[name] = wide[:, i * 1024:i * 1024 + h * d].view(n, h, d)
+        if name != "out":
+            part[name].copy_(x[name])
+    assert (n - 1) * width > 2 ** 31
+    o1, s1 = vda.token_scan(**x)
+    o2, s2 = vda.token_scan(**{**x, **part})
+    assert torch.equal(o2, o1) and torch.equal(s2, s1) and o2.data_ptr() == part["out"].data_ptr()
+    # its last four rows as four requests
+    slots = 2 ** 31 // (h * d * d) + 3
+    pool = torch.empty(slots, h, d, d, device=DEV)
+    index = torch.tensor([slots - 1, 0, slots - 2, 7], dtype=torch.int32, device=DEV)
+    pool[index.long()] = s1
+    few = {name: t[-4:] for name, t in x.items()}
+    small = s1.expand(4, -1, -1, -1).contiguous()
+    o1 = vda.token_step(**few, state=small)
+    vda.token_step(**few, **{name: t[-4:] for name, t in part.items() if name == "out"}, state=pool, index=index)
+    assert torch.equal(part["out"][-4:], o1) and torch.equal(pool[index.long()], small)
+    del pool
+    # one frame of all tokens, in place
+    freq, axis = binding.rotary_tables((8, 8, 8))
+    at = dict(freq=freq.to(DEV), axis=axis.to(DEV), Y=1, X=n)
+    q1, k1 = vda.rotate(x["q"][None, None], x["k"][None, None], **at)
+    q2, k2 = vda.rotate(part["q"][None, None], part["k"][None, None], out=(part["q"][None, None], part["k"][None, None]), **at)
+    assert torch.equal(q2, q1) and torch.equal(k2, k1)
+
+
 def test_scan_of_no_tokens():
     for dtype, d in (("f32", 64), ("bf16", 128)):
         x = draw(0, 2, 2, d, dtype)
