@@ -491,6 +491,12 @@ class Vda:
         x.record_stream(torch.cuda.current_stream(self.device))
         return x
 
+    def _new_like(self, streams, x):
+        """_new for a checked input's shape and type (a microsecond less where that is dense)."""
+        if streams[1] is None and x.is_contiguous():
+            return self._torch.empty_like(x)
+        return self._new(streams, x.shape, x.dtype)
+
     def token_scan(self, q, k, v, beta, log_alpha=None, cu_seqlens=None, s0=None, out=None, state=None, scale=1.0,
                    l2_eps=0.0, stream=None):
         """vdn_vda_token_scan: the gated delta rule over packed sequences.  Returns (out, state).
@@ -515,9 +521,9 @@ class Vda:
             _dense("s0", s0, shape, torch.float32, True, dev)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, (n, H, d), self.torch_dtype)
+            out = self._new_like(streams, v)
         if state is None:
-            state = self._new(streams, shape, torch.float32)
+            state = self._new(streams, shape, torch.float32) if s0 is None else self._new_like(streams, s0)
         else:
             _dense("state", state, shape, torch.float32, True, dev)
         prm = _TOKEN_PARAMS.pack(_TOKEN_PARAMS.size, H, Hk, S, scale, l2_eps, _ptr(cu_seqlens), 0, _ptr(log_alpha), _ptr(s0),
@@ -550,7 +556,7 @@ class Vda:
             _dense("index", index, (R,), torch.int32, True, dev)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, (*lead, H, d), self.torch_dtype)
+            out = self._new_like(streams, v)
         prm = _TOKEN_PARAMS.pack(_TOKEN_PARAMS.size, H, Hk, 0, scale, l2_eps, 0, _ptr(index), _ptr(log_alpha), 0, state.data_ptr(),
                                  slots, *st)
         r = self.lib.vdn_vda_token_step(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), beta.data_ptr(), out.data_ptr(), R, per,
@@ -597,7 +603,7 @@ class Vda:
         qo, ko = out if out is not None else (None, None)
         streams = self._streams(stream)
         if qo is None:
-            qo, qos = self._new(streams, shape, io), H * d
+            qo, qos = self._new_like(streams, q), H * d
         else:
             qos = _rows("q_out", qo, shape, io, True, dev)
         kos = Hk * d
@@ -605,7 +611,7 @@ class Vda:
             if ko is not None:
                 raise ValueError("out has keys, but there are none to rotate")
         elif ko is None:
-            ko = self._new(streams, kshape, io)
+            ko = self._new_like(streams, k)
         else:
             kos = _rows("k_out", ko, kshape, io, True, dev)
         prm = _ROTARY_PARAMS.pack(_ROTARY_PARAMS.size, (VDN_ROTARY_HALF if half else 0) | (VDN_ROTARY_INVERSE if inverse else 0),
