@@ -15,7 +15,9 @@
 // Precision.  K and Q are bf16 as given and enter exactly.  S, X, E and the triangular inverse are fp32 and enter the
 // products that reach the state as two bf16 parts (16 bits; products of the two low parts are left out: 2^-16 of the
 // whole), accumulated in fp32; S itself is carried in fp32 registers.  What only the rounded output sees (S Q^T, X^T P^T)
-// takes the high parts alone.
+// takes the high parts alone; P is formed from two parts of M and of the inverse, because that product cancels where keys
+// are alike and beta is near 1 (one key throughout, beta = 1: the read-out is off by 4.3e-3, with one part of each 2.3e-2;
+// with keys of length 1.2, 5.1e-3 and 1.1e-1).
 #pragma once
 #include <cuda_bf16.h>
 
@@ -143,22 +145,23 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // blocks are merged, [T11 0; -T22 L21 T11, T22], to 32 and to 64 rows, all threads at once.  A thread to a column over all 64
 // rows needs no products, but 2016 steps in straight line: half as fast again, most of it waiting for
 // instructions.  Everything that could be a long straight line is a loop over 16 columns for the same reason.
-// Measured on 65536 tokens x 32 heads (33 000 chunks): 629 us, 3.8 TB/s of the 73 KB a chunk reads and writes; four CTAs an SM use 53 % of
+// Measured on 65536 tokens x 32 heads (33 000 chunks): 689 us, 3.5 TB/s of the 73 KB a chunk reads and writes; four CTAs an SM use 53 % of
 // the issue slots and 68 % of the shared-memory pipe (ncu) and wait at barriers for the rest.
 struct TokenPrep {
   static constexpr int THREADS = 256, CTAS = 4;       // a CTA's phases are short and end at barriers: four of them side by side
-  // [K; Q]: two 64-channel boxes of 128 rows, the queries in their lower halves.  Once the queries' product is formed, M
-  // and the inverse times beta take the queries' places (the products W on the way to the inverse before the latter); in the
-  // end the two parts of E take all of it.
-  static constexpr int OFF_KQ = 0, OFF_M = 8192, OFF_ONE = 24576, OFF_W = OFF_ONE;
-  static constexpr int OFF_T = 32768;                 // L and its inverse; then the inverse times factors, high and low; then P
+  // [K; Q]: two 64-channel boxes of 128 rows, the queries in their lower halves.  Once the queries' product is formed, the
+  // two parts of M take the queries' places; in the end the two parts of E take all of it.
+  static constexpr int OFF_KQ = 0, OFF_M = 8192, OFF_M_LOW = 24576;
+  // L and its inverse; then the inverse times beta, high and low (for P), and the same times factors (for E); then P
+  static constexpr int OFF_T = 32768;
   static constexpr int L_PITCH = 68, W_PITCH = 36;    // floats: 16-byte rows, lanes' rows four banks apart
-  static constexpr int OFF_F = OFF_T + 64 * L_PITCH * 4;
-  // per token, exponents in units of ln 2: from the start of its 16 tokens; back to it; to their end; to the chunk's end (later
-  // the weight r e^{G_C - G}); from the chunk's start.  beta; r of keys and queries; factor of a column as a whole; distances
-  // between blocks of 16
-  static constexpr int F_UP = 0, F_DOWN = 64, F_END = 128, F_LAST = 192, F_ALL = 256, F_BETA = 320, F_R = 384, F_COL = 512,
-                       F_DIST = 576, F_FLOATS = 592;
+  static constexpr int OFF_W = OFF_T + 64 * L_PITCH * 4;   // products on the way to the inverse
+  // per token, exponents in units of ln 2: from the start of its 16 tokens; back to it; to their end; factor of a column as a whole;
+  // distances between blocks of 16 (all these are used up when W grows over them); to the chunk's end (later the weight
+  // r e^{G_C - G}); from the chunk's start; beta; r of keys and queries
+  static constexpr int F_UP = 0, F_DOWN = 64, F_END = 128, F_COL = 192, F_DIST = 256, F_LAST = 272, F_ALL = 336, F_BETA = 400, F_R = 464,
+                       F_FLOATS = 592;
+  static constexpr int OFF_F = OFF_W + 32 * W_PITCH * 4 - F_LAST * 4;
   static constexpr int OFF_BAR = OFF_F + F_FLOATS * 4;
   static constexpr int SMEM_BYTES = OFF_BAR + 64 + 1024;
 };
@@ -369,12 +372,15 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const float row = is_q ? t.scale * norm : fs[S::F_BETA + i] * norm;
       const int last = is_q ? i : i - 1;              // L is strictly lower, M has its diagonal
       float* L = reinterpret_cast<float*>(bp + S::OFF_T);
+      constexpr int LOW = S::OFF_M_LOW - S::OFF_M;
 #pragma unroll 1
       for (int jb = part * 16; jb < 64; jb += 32) {
         unsigned char* m0 = bp + S::OFF_M + i * 128 + (((jb / 8) ^ (i & 7)) << 4);
         unsigned char* m1 = bp + S::OFF_M + i * 128 + (((jb / 8 + 1) ^ (i & 7)) << 4);
         if (jb > (i | 31)) {                          // nothing of this warp's rows is this far right
-          if (is_q) *reinterpret_cast<uint4*>(m0) = *reinterpret_cast<uint4*>(m1) = make_uint4(0, 0, 0, 0);
+          if (is_q)
+            *reinterpret_cast<uint4*>(m0) = *reinterpret_cast<uint4*>(m1) = *reinterpret_cast<uint4*>(m0 + LOW) =
+                *reinterpret_cast<uint4*>(m1 + LOW) = make_uint4(0, 0, 0, 0);
           continue;
         }
         float x[16];
@@ -401,8 +407,13 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
         }
         if (is_q) {
-          *reinterpret_cast<uint4*>(m0) = make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
-          *reinterpret_cast<uint4*>(m1) = make_uint4(bf16_pair(x[8], x[9]), bf16_pair(x[10], x[11]), bf16_pair(x[12], x[13]), bf16_pair(x[14], x[15]));
+          uint32_t hi[8], lo[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) split2_pair(x[2 * e], x[2 * e + 1], hi[e], lo[e]);
+          *reinterpret_cast<uint4*>(m0) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+          *reinterpret_cast<uint4*>(m1) = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+          *reinterpret_cast<uint4*>(m0 + LOW) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          *reinterpret_cast<uint4*>(m1 + LOW) = make_uint4(lo[4], lo[5], lo[6], lo[7]);
         } else {
 #pragma unroll
           for (int j = 0; j < 16; j += 4)
@@ -472,49 +483,63 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         tile_store(A + m * S::L_PITCH + c0, S::L_PITCH, -1.f, c);
       }
       __syncthreads();
+      // ---- operands: column c of the inverse times beta, 16 of its rows a thread; first as it is for P, then with the weights of E
+      const int c = tid & 63, r0 = (tid >> 6) * 16;
+      uint32_t hi[8], lo[8];
+      auto operand = [&]() {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          unsigned char* at = bp + S::OFF_T + c * 128 + (((r0 / 8 + q) ^ (c & 7)) << 4);
+          *reinterpret_cast<uint4*>(at) = make_uint4(hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]);
+          *reinterpret_cast<uint4*>(at + 8192) = make_uint4(lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]);
+        }
+        fence_proxy_async_smem();
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+      };
       {
-        // ---- operands: column c of the inverse times beta (and the weights of E), 16 of its rows a thread
-        const int c = tid & 63, r0 = (tid >> 6) * 16;
         const bool zero = r0 < 32 && c >= 32;         // above the diagonal blocks: never written
         float y[16];
 #pragma unroll
         for (int r = 0; r < 16; ++r) y[r] = zero ? 0.f : fs[S::F_BETA + c] * L[(r0 + r) * S::L_PITCH + c];
-        __syncthreads();                              // the inverse is read, the operands take its place
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t hi[4], lo[4], one[4];
+        for (int e = 0; e < 8; ++e) split2_pair(y[2 * e], y[2 * e + 1], hi[e], lo[e]);
+        __syncthreads();                              // the inverse is read, the operand takes its place
+        operand();
+        if (tid == 0) {
+          // P: rows 64..127 of the A operand are scale M, the rows before it (keys) are of no interest.  low high, high low, high high
+          constexpr uint32_t idp = make_idesc_bf16(128, 64, false, false);
+          const uint64_t dm = make_smem_desc(base + S::OFF_M - 8192, 16, 1024), dl = make_smem_desc(base + S::OFF_M_LOW - 8192, 16, 1024);
+          const uint64_t dt = make_smem_desc(base + S::OFF_T, 16, 1024);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int r = 8 * q + 2 * e;
-            const float2 w = *reinterpret_cast<const float2*>(fs + S::F_LAST + r0 + r);
-            split2_pair(w.x * y[r], w.y * y[r + 1], hi[e], lo[e]);
-            one[e] = bf16_pair(y[r], y[r + 1]);
+          for (int k = 0; k < 4; ++k) {
+            mma_bf16_ss(tmem, dl + k * 2, dt + k * 2, idp, k ? 1u : 0u);
+            mma_bf16_ss(tmem, dm + k * 2, dt + (8192 >> 4) + k * 2, idp, 1u);
+            mma_bf16_ss(tmem, dm + k * 2, dt + k * 2, idp, 1u);
           }
-          unsigned char* at = bp + S::OFF_T + c * 128 + (((r0 / 8 + q) ^ (c & 7)) << 4);
-          *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-          *reinterpret_cast<uint4*>(at + 8192) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-          *reinterpret_cast<uint4*>(at - S::OFF_T + S::OFF_ONE) = make_uint4(one[0], one[1], one[2], one[3]);
+          mma_commit(bar_mma);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float2 w = *reinterpret_cast<const float2*>(fs + S::F_LAST + r0 + 2 * e);
+          split2_pair(w.x * y[2 * e], w.y * y[2 * e + 1], hi[e], lo[e]);
         }
       }
-      fence_proxy_async_smem();
-      tc_fence_before_sync();
-      __syncthreads();
-      tc_fence_after_sync();
-      if (tid == 0) {
-        // E [128 x 64] = K^T (M rows = channels, read MN-major) times the two parts
-        constexpr uint32_t ide = make_idesc_bf16(128, 64, true, false);
-        const uint64_t dk = make_smem_desc(base, 16384, 1024), dt = make_smem_desc(base + S::OFF_T, 16, 1024);
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_bf16_ss(tmem + 64, dk + (k & 3) * (2048 >> 4), dt + ((k >> 2) * (8192 >> 4) + (k & 3) * 2), ide, k ? 1u : 0u);
-        // P: rows 64..127 of the A operand are scale M, the rows before it (keys) are of no interest
-        constexpr uint32_t idp = make_idesc_bf16(128, 64, false, false);
-        const uint64_t dm = make_smem_desc(base + S::OFF_M - 8192, 16, 1024), d1 = make_smem_desc(base + S::OFF_ONE, 16, 1024);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16_ss(tmem, dm + k * 2, d1 + k * 2, idp, k ? 1u : 0u);
-        mma_commit(bar_mma);
-      }
       ok = mbar_wait(bar_mma, 1, wc);
+      if (!__syncthreads_or(!ok)) {
+        operand();
+        if (tid == 0) {
+          // E [128 x 64] = K^T (M rows = channels, read MN-major) times the two parts
+          constexpr uint32_t ide = make_idesc_bf16(128, 64, true, false);
+          const uint64_t dk = make_smem_desc(base, 16384, 1024), dt = make_smem_desc(base + S::OFF_T, 16, 1024);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            mma_bf16_ss(tmem + 64, dk + (k & 3) * (2048 >> 4), dt + ((k >> 2) * (8192 >> 4) + (k & 3) * 2), ide, k ? 1u : 0u);
+          mma_commit(bar_mma);
+        }
+        ok = mbar_wait(bar_mma, 0, wc);
+      }
       if (!__syncthreads_or(!ok)) {
         tc_fence_after_sync();
 #pragma unroll 1
