@@ -306,12 +306,11 @@ vdn_status vdn_vda_prepare(vdn_vda_t h, const void* q_in, const void* k_in, cons
  *           then).  It is an argument and not the handle's, so that calls that may overlap, or captured graphs, can each
  *           have their own; nothing in it outlives the call.
  *   bf16 with d = 128 runs on the tensor cores in chunks of 64 tokens where that is faster (by sizes alone: short sequences go
- *   token by token), a few long sequences in parts side by side.  What reaches the state keeps 16 significant bits or more
- *   of every factor and fp32 sums: the state is within 1e-5 of a 64-bit evaluation, relative to its norm (measured 3e-6 .. 5e-6
- *   for unit keys, a third of them within 0.4 of eight shared directions); the read-out takes its factors in bf16 once more
- *   before it is rounded: 3.5e-3 where a single rounding gives 1.7e-3.  A value that is not finite reaches the other tokens of
- *   its 64, and what follows.  All else, and VDN_FLAG_FORCE_SIMT, runs in plain fp32 (4e-7 with f32 I/O),
- *   a few long sequences in parts as well.
+ *   token by token), a few long sequences in parts side by side.  Every factor keeps 16 significant bits or more, sums are
+ *   fp32: against a 64-bit evaluation the state is off by 3e-6 .. 5e-6 of its norm (measured: unit keys, a third of them within
+ *   0.4 of eight shared directions; 4e-5 with one key throughout and beta = 1), the read-out by 3e-4 at most before its
+ *   rounding.  A value that is not finite reaches the other tokens of its 64, and what follows.  All else, and
+ *   VDN_FLAG_FORCE_SIMT, runs in plain fp32 (4e-7 with f32 I/O), a few long sequences in parts as well.
  * vdn_vda_token_step: request s is rows s * per .. (s + 1) * per - 1 of n_requests * per.
  *   p->state      [n_slots, heads, d, d]: the pool, updated in place.
  *   p->index      int32 [n_requests], DEVICE, or NULL (= s): the request's state.  A negative or too large index marks a

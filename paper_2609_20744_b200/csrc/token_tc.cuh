@@ -12,12 +12,12 @@
 // so that a chunk's step of the sequential kernel (token_chain_kernel) is two dependent products,
 //        X^T = V^T - (S K^T) Diag(e^G r),      S <- e^{G_C} S + X^T E^T,      O^T = (S Q^T) Diag(scale e^G) + X^T P^T.
 //
-// Precision.  K and Q are bf16 as given and enter exactly.  S, X, E and the triangular inverse are fp32 and enter the
-// products that reach the state as two bf16 parts (16 bits; products of the two low parts are left out: 2^-16 of the
-// whole), accumulated in fp32; S itself is carried in fp32 registers.  What only the rounded output sees (S Q^T, X^T P^T)
-// takes the high parts alone; P is formed from two parts of M and of the inverse, because that product cancels where keys
-// are alike and beta is near 1 (one key throughout, beta = 1: the read-out is off by 4.3e-3, with one part of each 2.3e-2;
-// with keys of length 1.2, 5.1e-3 and 1.1e-1).
+// Precision.  K and Q are bf16 as given and enter exactly.  Every other factor -- S, X, E, P, M, the triangular inverse -- is fp32 and
+// enters its product as two bf16 parts (16 bits; products of the two low parts are left out: 2^-16 of the whole),
+// accumulated in fp32; S itself is carried in fp32 registers.  One part would do for what only the rounded output sees where keys
+// differ (read-out off by 3.4e-3, 1.7e-3 of which is its rounding), but not where they are alike and beta is near 1, where
+// M times the inverse cancels: 2.3e-2 with one key throughout, 1.1e-1 with keys of length 1.2; 1.7e-3 everywhere with two.
+// They cost 10 % (65536 tokens x 32 heads: 1.27 -> 1.39 ms).
 #pragma once
 #include <cuda_bf16.h>
 
@@ -36,7 +36,7 @@ struct TokenTc {
   static constexpr int C = 64, D = 128;
   static constexpr int E_PART = D * C * 2;            // one part of E: 128 rows of 128 bytes, as the swizzled operand lies in shared memory
   static constexpr int E_BYTES = 2 * E_PART;
-  static constexpr int P_BYTES = C * C * 2;
+  static constexpr int P_PART = C * C * 2, P_BYTES = 2 * P_PART;
   // per-token factors: e^G r [64], scale r_q e^G [64], e^{G_C}, padding
   static constexpr int F_FLOATS = 132, F_BYTES = F_FLOATS * 4;
 };
@@ -145,8 +145,8 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // blocks are merged, [T11 0; -T22 L21 T11, T22], to 32 and to 64 rows, all threads at once.  A thread to a column over all 64
 // rows needs no products, but 2016 steps in straight line: half as fast again, most of it waiting for
 // instructions.  Everything that could be a long straight line is a loop over 16 columns for the same reason.
-// Measured on 65536 tokens x 32 heads (33 000 chunks): 689 us, 3.5 TB/s of the 73 KB a chunk reads and writes; four CTAs an SM use 53 % of
-// the issue slots and 68 % of the shared-memory pipe (ncu) and wait at barriers for the rest.
+// Measured on 65536 tokens x 32 heads (33 000 chunks): 714 us, 3.8 TB/s of the 81 KB a chunk reads and writes; four CTAs an SM use about half of
+// the issue slots and two thirds of the shared-memory pipe (ncu) and wait at barriers for the rest.
 struct TokenPrep {
   static constexpr int THREADS = 256, CTAS = 4;       // a CTA's phases are short and end at barriers: four of them side by side
   // [K; Q]: two 64-channel boxes of 128 rows, the queries in their lower halves.  Once the queries' product is formed, the
@@ -560,10 +560,14 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             tmem_ld16(lanes + jb, x);
             tmem_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-              *reinterpret_cast<uint4*>(bp + S::OFF_T + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4)) =
-                  make_uint4(bf16_pair(x[8 * c], x[8 * c + 1]), bf16_pair(x[8 * c + 2], x[8 * c + 3]),
-                             bf16_pair(x[8 * c + 4], x[8 * c + 5]), bf16_pair(x[8 * c + 6], x[8 * c + 7]));
+            for (int c = 0; c < 2; ++c) {
+              uint32_t hi[4], lo[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) split2_pair(x[8 * c + 2 * e], x[8 * c + 2 * e + 1], hi[e], lo[e]);
+              unsigned char* at = bp + S::OFF_T + i * 128 + (((jb / 8 + c) ^ (i & 7)) << 4);
+              *reinterpret_cast<uint4*>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+              *reinterpret_cast<uint4*>(at + TokenTc::P_PART) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
           }
         }
         fence_proxy_async_smem();
@@ -596,16 +600,17 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 // threads a row: 32 key channels each), four write out.
 //
 // Measured: 2.3 us a chunk alone (4400 cycles: 830 S K^T, 830 X^T E^T, the rest the state warps' turns and the hand-overs);
-// 65536 tokens x 32 heads, a chain after another on every SM: 640 us, 105 KB a chunk, 5.5 TB/s with what shared keys leave to DRAM.
+// 65536 tokens x 32 heads, a chain after another on every SM: 675 us, 113 KB a chunk, 5.6 TB/s with what shared keys leave to DRAM.
 struct TokenChain {
   static constexpr int STATE_WARPS = 16, OUT_WARPS = 4;
   static constexpr int RESULT_WARP = 2 + STATE_WARPS + OUT_WARPS;
   static constexpr int THREADS = 32 * (RESULT_WARP + 1);
-  static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 90112;
-  static constexpr int STAGE = 91136;
+  static constexpr int OFF_K = 0, OFF_Q = 16384, OFF_V = 32768, OFF_E = 49152, OFF_P = 81920, OFF_F = 98304;
+  static constexpr int STAGE = 99328;
   static constexpr int OFF_O = 2 * STAGE;             // two tiles of results
-  static constexpr int OFF_BAR = OFF_O + 2 * 16384;
-  static constexpr int SMEM_BYTES = OFF_BAR + 256 + 1024;
+  static constexpr int OFF_BAR = STAGE + OFF_F + TokenTc::F_BYTES;   // (where the second stage's last kilobyte is free)
+  static constexpr int SMEM_BYTES = OFF_O + 2 * 16384 + 1024;
+  static_assert(OFF_BAR % 8 == 0 && OFF_BAR + 192 <= OFF_O && SMEM_BYTES <= 227 * 1024, "");
   // tensor memory columns
   static constexpr uint32_t S_HI = 0, S_LO = 64, DS = 128, D_K = 256, X_HI = 320, X_LO = 352, D_Q = 384, D_O = 448;
 };
@@ -892,14 +897,20 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
         if (!mbar_wait(DK_FULL, s & 1, wc) || (s > 0 && !mbar_wait(O_FREE, (s - 1) & 1, wc))) break;
         tc_fence_after_sync();
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq0 + off + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+        for (int k = 0; k < 8; ++k) {
+          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_LO + k * 8, dq0 + off + ((k >> 2) * 512 + (k & 3) * 2), id64, k ? 1u : 0u);
+          mma_bf16_ts(tmem + S::D_Q, tmem + S::S_HI + k * 8, dq0 + off + ((k >> 2) * 512 + (k & 3) * 2), id64, 1u);
+        }
         mma_commit(S_FREE);
         mma_commit(FREE(KQ, st));
         if (!mbar_wait(FULL(E, st), (s >> 1) & 1, wc) || !mbar_wait(X_READY, s & 1, wc) || !mbar_wait(X_READY + 8, s & 1, wc)) break;
         tc_fence_after_sync();
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp0 + off + k * 2, id64, k ? 1u : 0u);
+        for (int k = 0; k < 4; ++k) {
+          mma_bf16_ts(tmem + S::D_O, tmem + S::X_LO + k * 8, dp0 + off + k * 2, id64, k ? 1u : 0u);
+          mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp0 + off + (TokenTc::P_PART >> 4) + k * 2, id64, 1u);
+          mma_bf16_ts(tmem + S::D_O, tmem + S::X_HI + k * 8, dp0 + off + k * 2, id64, 1u);
+        }
         mma_commit(DO_FULL);
         mma_commit(FREE(E, st));
       }

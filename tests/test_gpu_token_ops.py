@@ -7,9 +7,10 @@ Tolerances, all relative in the 2-norm over one (sequence or request, head) slic
   state, tensor cores: the state, the differences X, the operator E and the triangular inverse are each cut to two bf16
      parts, off by at most u16^2 = 2^-16 of the value:  4 * 2^-16, plus the fp32 term above.
   out: one rounding to io_dtype, u16 (u32 for fp32) of the value.  Further errors -- the state's, and on the tensor cores
-     the state, X and the mixing matrix taken as one bf16 part each, 3 u16 -- are roundings of the terms S_ij q_j, which may
+     those of the state, X and the mixing matrix, allowed 3 u16 here -- are roundings of the terms S_ij q_j, which may
      cancel in their sum: independent, they are relative to the root of the terms' summed squares (the oracle's `sizes`),
-     not to the result.  (A rank-one state read by a query at right angles to its key gives next to nothing.)
+     not to the result.  (A rank-one state read by a query at right angles to its key gives next to nothing.)  The tensor
+     cores' two parts of each factor give far less than 3 u16: test_scan_readout_with_keys_alike.
 """
 import numpy as np
 import pytest
@@ -106,6 +107,42 @@ def test_scan(dtype, d, flags, lens):
     x = draw(sum(lens), h, hk, d, dtype, seed=len(lens))
     s0 = 0.3 * torch.randn(len(lens), h, d, d, device=DEV) if len(lens) > 1 or lens[0] % 3 == 0 else None
     check_scan(vda, x, lens, dtype, d, tensor_cores(dtype, d, flags), s0, scale=0.5)
+
+
+@pytest.mark.parametrize("length", [1.0, 1.3])
+@pytest.mark.parametrize("keys", ["same", "two", "near"])
+def test_scan_readout_with_keys_alike(keys, length):
+    """Chunks whose operators cancel: keys alike, beta = 1.  Per chunk of 64, O = e^G S q + P X with P = M T, M the decayed q.k, T the
+    inverse of I + L.  Every factor but q and k has two bf16 parts, off by u16^2 = 2^-16, and the accumulators are fp32: the
+    result is off by u16 of itself, by 2^-16 of each of S, X, M, T and P's terms, taken without their signs, and by what the state
+    is off, at most the state's tolerance of its norm (and of X's, which has it as e^G S k)."""
+    d, h, n, C = 128, 2, 320, 64
+    x = draw(n, h, h, d, "bf16", seed=15)
+    unit = lambda t: t / t.norm(dim=-1, keepdim=True)  # noqa: E731
+    g = torch.Generator().manual_seed(16)
+    shared = unit(torch.randn(4, h, d, generator=g))
+    pick = torch.randint(0, {"same": 1, "two": 2, "near": 4}[keys], (n,), generator=g)
+    k = shared[pick] if keys != "near" else unit(shared[pick] + 0.05 * unit(torch.randn(n, h, d, generator=g)))
+    x["k"] = (length * k).to(torch.bfloat16).to(DEV)
+    x["beta"] = torch.ones(n, h, device=DEV)
+    x["log_alpha"] = -1e-3 * torch.rand(n, h, generator=g).to(DEV)
+    got, state = binding.Vda(d, "bf16").token_scan(**x)
+    q, k, v, beta, ga = (x[name].double().cpu() for name in ("q", "k", "v", "beta", "log_alpha"))
+    for j in range(h):
+        S, want, off = torch.zeros(d, d, dtype=torch.float64), [], []
+        for c in range(0, n, C):
+            Q, K, V, b, G = q[c:c + C, j], k[c:c + C, j], v[c:c + C, j], beta[c:c + C, j], ga[c:c + C, j].cumsum(0)
+            decay = torch.exp(G[:, None] - G[None]).tril()
+            T = torch.linalg.inv(torch.eye(C, dtype=torch.float64) + (b[:, None] * decay * (K @ K.T)).tril(-1)) * b[None]
+            M, X, e = decay * (Q @ K.T), V - torch.exp(G)[:, None] * (K @ S.T), torch.exp(G)[:, None]
+            want.append(e * (Q @ S.T) + M @ T @ X)
+            P = M.abs() @ T.abs()                     # what the parts of M and of T are relative to
+            eps, tol = 2.0 ** -16, 4 * 2.0 ** -16 * length ** 2
+            from_state = tol * float(S.norm()) * (e * Q.norm(dim=1, keepdim=True) + (P @ (e * K.norm(dim=1, keepdim=True))))
+            off.append(eps * (e * (Q.abs() @ S.abs().T) + 4 * (P @ X.abs())) + from_state / d ** 0.5)
+            S = torch.exp(G[-1]) * S + (T @ X).T @ (torch.exp(G[-1] - G)[:, None] * K)
+        want, off = torch.cat(want), torch.cat(off)
+        assert float((got[:, j].double().cpu() - want).norm()) <= U16 * float(want.norm()) + float(off.norm())
 
 
 @pytest.mark.parametrize("dtype,d,flags", [("f32", 64, 0), ("f32", 128, 0), ("bf16", 64, 0),
