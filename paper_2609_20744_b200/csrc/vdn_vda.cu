@@ -1301,7 +1301,10 @@ TokenPlainLayout make_plain_layout(const vdn_vda_s* h, long long n_tokens, int n
   // (d = 128; 0.0037, d = 64) for each token and head, and 1.7 / 0.85 to join a part.  The length of a part balances its walk with the
   // joins.  9000 tokens, f32: 1 head 921 us whole, 167 cut (d = 64: 834, 94); 12 heads 1300, 1190 (854, 442); 36 heads 1540,
   // 3300; 256 tokens, 2 heads, d = 64: 31, 23.
-  const double wide = h->cfg.d / 128.0, longest = (double)longest_guess(n_tokens, n_seqs), work = (double)n_tokens * heads;
+  // (several sequences: the longest is taken to be twice the average.  8 of 512 tokens, 2 heads, d = 128: 82 us whole, 124 cut;
+  // one of them four times the average: 227 whole.)
+  const double longest = n_seqs == 1 ? (double)n_tokens : std::min((double)n_tokens, 2.0 * n_tokens / n_seqs);
+  const double wide = h->cfg.d / 128.0, work = (double)n_tokens * heads;
   const double rows = std::max(64.0, std::sqrt(8.5 * longest));
   const double whole = 6.0 + 0.1 * longest + 0.0025 * wide * wide * work;
   const double parted = 12.0 + 0.2 * rows + 1.7 * wide * longest / rows + 0.01 * std::pow(wide, 1.5) * work;
