@@ -26,7 +26,7 @@ struct RotaryArgs {
   const int* positions;      // [3][n_tokens] or null: frame t0 + t, row, column of the token's grid place
   long long n_tokens;
   int pairs, T, F, X, t0, tile;
-  unsigned per_row;          // ceil(2^32 / (all heads of a token)), 0 where a tile is one token: division by multiplication
+  unsigned per_row;          // rotary_per_row
   float norm_eps;            // > 0: RMSNorm first
   float sign;                // -1: rotate back
 };
@@ -36,6 +36,17 @@ struct Rotary {
   static constexpr int MAX_TILE = 32;      // tokens a CTA covers
   static constexpr int UNROLL = 2;         // head rows a lane has in flight
 };
+
+// A tile's head rows are counted through, `rows` (all heads of queries and keys) to a token: row t belongs to token t / rows.
+// Division by multiplication with ceil(2^32 / rows) = (2^32 + e) / rows, e < rows: right while t * e < 2^32, and a tile of more than
+// one token has fewer than 512 rows to a token and 32 tokens at most.  One row to a token (queries of one head alone) has no such
+// factor in 32 bits, and needs none; nor does a tile of one token, whose rows may be many.
+__host__ __device__ inline unsigned rotary_per_row(int rows, int tile) {
+  return tile > 1 && rows > 1 ? (unsigned)((0x100000000ULL + rows - 1) / rows) : 0u;
+}
+__host__ __device__ inline int rotary_token(int t, int rows, unsigned per_row) {
+  return rows == 1 ? t : (int)(((unsigned long long)(unsigned)t * per_row) >> 32);
+}
 
 // 16 bytes of a head's channels as floats, and back
 __device__ __forceinline__ void unpack16(const uint4& r, float (&x)[4], const float*) {
@@ -132,7 +143,7 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
       token[u] = head[u] = 0;
       key[u] = false;
       if (t < tasks) {
-        token[u] = (int)__umulhi((unsigned)t, a.per_row);
+        token[u] = rotary_token(t, rows, a.per_row);
         head[u] = t - token[u] * rows;
         key[u] = head[u] >= a.heads[0];
         if (key[u]) head[u] -= a.heads[0];

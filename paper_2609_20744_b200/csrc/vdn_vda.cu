@@ -1645,8 +1645,7 @@ vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void*
   const long long spread = a.n_tokens / (4LL * h->sm_count);
   if (tile > spread) tile = spread;
   a.tile = (int)(tile < 1 ? 1 : tile > vdn::Rotary::MAX_TILE ? vdn::Rotary::MAX_TILE : tile);
-  // (exact while task x rows < 2^32: a tile of more than one token has fewer than 512 head rows to a token, and 32 tokens at most)
-  a.per_row = a.tile > 1 ? (unsigned)((0x100000000ULL + rows - 1) / rows) : 0u;
+  a.per_row = vdn::rotary_per_row(rows, a.tile);
   const unsigned grid = (unsigned)((a.n_tokens + a.tile - 1) / a.tile);
   const size_t smem = (size_t)a.tile * (d / 2) * 8;
   DeviceGuard guard(h->cfg.device);
