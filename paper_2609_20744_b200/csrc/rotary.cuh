@@ -11,6 +11,8 @@
 #pragma once
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace vdn {
@@ -81,6 +83,9 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
   constexpr int P4 = NP / 2;                       // float4's (two pairs each) of a lane's cosines and sines
   constexpr int STEP = Rotary::THREADS / LPH;      // head rows side by side
   constexpr int U = Rotary::UNROLL;
+  // 1 for a pair that is turned, in the order the lanes take them; the channels of the others are copied, not computed: times 1 and
+  // 0 an infinite partner would make them NaN
+  __shared__ alignas(8) unsigned char on_axis[D / 2];
   // [token][pair / 2 mod P4][lane][cos, sin, cos, sin]: the lanes of a head read 16-byte pieces side by side
   extern __shared__ float4 table[];
   // of queries and keys, in the order the lanes take them: [4 channels of the first piece .. of the second][lane]
@@ -95,6 +100,7 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
   // first channel of the lane's two pieces
   int c0 = 2 * l * VEC, c1 = c0 + VEC;
   if (HALF && l * VEC < a.pairs) { c0 = l * VEC; c1 = c0 + a.pairs; }
+  bool turned;
   // ---- cosines and sines: a thread has one place lp = lane * NP + pair of the lane, and every (256 / places)-th token
   {
     constexpr int PLACES = D / 2, TOKENS = Rotary::THREADS / PLACES;
@@ -102,10 +108,12 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
     // the pair that the place stands for; HALF: lanes past the rotated channels pass theirs through
     const int p = HALF ? (tl * VEC < a.pairs ? lp : a.pairs) : lp;
     const int ax = p < a.pairs ? a.axis[p] : -1;
-    const double turn = ax >= 0 && ax <= 2 ? a.freq[p] * 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
+    turned = ax >= 0 && ax <= 2;
+    if (threadIdx.x < PLACES) on_axis[lp] = turned;
+    const double turn = turned ? a.freq[p] * 0.15915494309189533577 : 0.0;   // 1 / (2 pi)
     for (int j = (int)threadIdx.x / PLACES; j < nt; j += TOKENS) {
       float c = 1.f, s = 0.f;
-      if (ax >= 0 && ax <= 2) {
+      if (turned) {
         const long long n = n0 + j;
         int pos;
         if (a.positions) {
@@ -130,71 +138,76 @@ __global__ void __launch_bounds__(Rotary::THREADS, 4) rotary_kernel(const Rotary
       weight[w][k][l] = g ? make_float4(g[c], g[c + 1], g[c + 2], g[c + 3]) : make_float4(1.f, 1.f, 1.f, 1.f);
     }
   }
-  __syncthreads();
+  const bool all = __syncthreads_and(turned);
+  const unsigned char* on = on_axis + l * NP;
 
-  for (int base = first; base < tasks + first; base += STEP * U) {   // (all lanes together: the norm shuffles)
-    uint4 x0[U], x1[U];
-    int token[U], head[U];
-    bool key[U];
+  // whole: every pair is turned.  A loop of its own: asked for each head row it cost 2 % (768p) to 5 % (480p, norms); a block with
+  // pairs that are not turned pays 2 to 3 % for copying them (160 000 tokens x 48 heads, 32 of 64 pairs: 594 -> 608 us).
+  auto heads = [&](auto whole) {
+    for (int base = first; base < tasks + first; base += STEP * U) {   // (all lanes together: the norm shuffles)
+      uint4 x0[U], x1[U];
+      int token[U], head[U];
+      bool key[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = base + u * STEP;
-      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
-      token[u] = head[u] = 0;
-      key[u] = false;
-      if (t < tasks) {
-        token[u] = rotary_token(t, rows, a.per_row);
-        head[u] = t - token[u] * rows;
-        key[u] = head[u] >= a.heads[0];
-        if (key[u]) head[u] -= a.heads[0];
-        const Tio* src = static_cast<const Tio*>(a.in[key[u]]) + (size_t)(n0 + token[u]) * a.in_stride[key[u]] + head[u] * D;
-        x0[u] = *reinterpret_cast<const uint4*>(src + c0);
-        x1[u] = *reinterpret_cast<const uint4*>(src + c1);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool live = base + u * STEP < tasks;
-      const int j = token[u], w = key[u];
-      float y0[VEC], y1[VEC];
-      unpack16(x0[u], y0, static_cast<const Tio*>(nullptr));
-      unpack16(x1[u], y1, static_cast<const Tio*>(nullptr));
-      if constexpr (NORM) {
-        float ss = 0.f;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) ss += y0[i] * y0[i] + y1[i] * y1[i];
-#pragma unroll
-        for (int m = 1; m < LPH; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-        const float rn = rsqrtf(ss * (1.f / D) + a.norm_eps);
-#pragma unroll
-        for (int i = 0; i < VEC; i += 4) {
-          const float4 g = weight[w][i / 4][l], k = weight[w][VEC / 4 + i / 4][l];
-          y0[i] *= rn * g.x; y0[i + 1] *= rn * g.y; y0[i + 2] *= rn * g.z; y0[i + 3] *= rn * g.w;
-          y1[i] *= rn * k.x; y1[i + 1] *= rn * k.y; y1[i + 2] *= rn * k.z; y1[i + 3] *= rn * k.w;
+      for (int u = 0; u < U; ++u) {
+        const int t = base + u * STEP;
+        x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+        token[u] = head[u] = 0;
+        key[u] = false;
+        if (t < tasks) {
+          token[u] = rotary_token(t, rows, a.per_row);
+          head[u] = t - token[u] * rows;
+          key[u] = head[u] >= a.heads[0];
+          if (key[u]) head[u] -= a.heads[0];
+          const Tio* src = static_cast<const Tio*>(a.in[key[u]]) + (size_t)(n0 + token[u]) * a.in_stride[key[u]] + head[u] * D;
+          x0[u] = *reinterpret_cast<const uint4*>(src + c0);
+          x1[u] = *reinterpret_cast<const uint4*>(src + c1);
         }
       }
 #pragma unroll
-      for (int i = 0; i < NP; i += 2) {
-        const float4 cs = table[(j * P4 + i / 2) * LPH + l];
-        if (HALF) {
-          const float p0 = y0[i], p1 = y0[i + 1], z0 = y1[i], z1 = y1[i + 1];
-          y0[i] = p0 * cs.x - z0 * cs.y;     y1[i] = p0 * cs.y + z0 * cs.x;
-          y0[i + 1] = p1 * cs.z - z1 * cs.w; y1[i + 1] = p1 * cs.w + z1 * cs.z;
-        } else {
-          // pairs i, i + 1 of the lane are channels 2i .. 2i + 3 of its 2 VEC neighbouring channels
-          float* y = 2 * i < VEC ? &y0[(2 * i) % VEC] : &y1[(2 * i) % VEC];
-          const float p0 = y[0], z0 = y[1], p1 = y[2], z1 = y[3];
-          y[0] = p0 * cs.x - z0 * cs.y; y[1] = p0 * cs.y + z0 * cs.x;
-          y[2] = p1 * cs.z - z1 * cs.w; y[3] = p1 * cs.w + z1 * cs.z;
+      for (int u = 0; u < U; ++u) {
+        const bool live = base + u * STEP < tasks;
+        const int j = token[u], w = key[u];
+        float y0[VEC], y1[VEC];
+        unpack16(x0[u], y0, static_cast<const Tio*>(nullptr));
+        unpack16(x1[u], y1, static_cast<const Tio*>(nullptr));
+        if constexpr (NORM) {
+          float ss = 0.f;
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) ss += y0[i] * y0[i] + y1[i] * y1[i];
+#pragma unroll
+          for (int m = 1; m < LPH; m <<= 1) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
+          const float rn = rsqrtf(ss * (1.f / D) + a.norm_eps);
+#pragma unroll
+          for (int i = 0; i < VEC; i += 4) {
+            const float4 g = weight[w][i / 4][l], k = weight[w][VEC / 4 + i / 4][l];
+            y0[i] *= rn * g.x; y0[i + 1] *= rn * g.y; y0[i + 2] *= rn * g.z; y0[i + 3] *= rn * g.w;
+            y1[i] *= rn * k.x; y1[i + 1] *= rn * k.y; y1[i + 2] *= rn * k.z; y1[i + 3] *= rn * k.w;
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < NP; i += 2) {
+          const float4 cs = table[(j * P4 + i / 2) * LPH + l];
+          // HALF: pair i is channel i of either piece; else pairs i, i + 1 are channels 2i .. 2i + 3 of the 2 VEC neighbouring ones
+          float* y = HALF ? &y0[i] : 2 * i < VEC ? &y0[(2 * i) % VEC] : &y1[(2 * i) % VEC];
+          float& a0 = y[0];
+          float& b0 = HALF ? y1[i] : y[1];
+          float& a1 = HALF ? y[1] : y[2];
+          float& b1 = HALF ? y1[i + 1] : y[3];
+          const float p0 = a0, z0 = b0, p1 = a1, z1 = b1;
+          if (whole || on[i]) { a0 = p0 * cs.x - z0 * cs.y; b0 = p0 * cs.y + z0 * cs.x; }
+          if (whole || on[i + 1]) { a1 = p1 * cs.z - z1 * cs.w; b1 = p1 * cs.w + z1 * cs.z; }
+        }
+        if (live) {
+          Tio* dst = static_cast<Tio*>(a.out[w]) + (size_t)(n0 + j) * a.out_stride[w] + head[u] * D;
+          *reinterpret_cast<uint4*>(dst + c0) = pack16(y0, static_cast<const Tio*>(nullptr));
+          *reinterpret_cast<uint4*>(dst + c1) = pack16(y1, static_cast<const Tio*>(nullptr));
         }
       }
-      if (live) {
-        Tio* dst = static_cast<Tio*>(a.out[w]) + (size_t)(n0 + j) * a.out_stride[w] + head[u] * D;
-        *reinterpret_cast<uint4*>(dst + c0) = pack16(y0, static_cast<const Tio*>(nullptr));
-        *reinterpret_cast<uint4*>(dst + c1) = pack16(y1, static_cast<const Tio*>(nullptr));
-      }
     }
-  }
+  };
+  if (all) heads(std::true_type());
+  else heads(std::false_type());
 }
 
 }  // namespace vdn

@@ -66,3 +66,36 @@ def test_one_head_of_a_wider_tensor():
     ref = tok.rotary(before[..., 1:2, :].double().cpu().numpy().reshape(n, 1, d), tok.grid_positions(1, 1, 50, 100), freq.tolist(),
                      axis.tolist())
     assert (np.abs(want.double().cpu().numpy().reshape(n, 1, d) - ref) <= allowed("bf16", ref)).all()
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("half,pairs", [(False, 21), (False, 32), (True, 24), (True, 32)])
+@pytest.mark.parametrize("frames", [1, 40])
+def test_channels_that_are_not_turned_are_copied(dtype, d, half, pairs, frames):
+    """Channels beyond the pairs and a pair on no axis: infinities, NaN and signed zeros beside one another stay what they are, and
+    the turned channels are what they are without them."""
+    T, F, h = frames, 64, 3
+    g = torch.Generator().manual_seed(d + pairs)
+    freq, axis = binding.rotary_tables((pairs // 4, pairs // 4, pairs - 2 * (pairs // 4)), theta=500.0)
+    off = [3, pairs - 1]
+    axis[3], axis[pairs - 1] = -1, 7
+    turned = torch.zeros(d, dtype=torch.bool)
+    for p in range(pairs):
+        if p not in off:
+            turned[[p, p + pairs] if half else [2 * p, 2 * p + 1]] = True
+    kept = (~turned).nonzero()[:, 0]
+    clean = torch.randn(1, T, F, h, d, generator=g)
+    x = clean.clone()
+    odd = torch.tensor([float("inf"), -0.0, float("nan"), 1.5, -float("inf"), 0.0, 2.5, -0.0])
+    which = torch.randint(0, 8, x[..., kept].shape, generator=g)
+    x[..., kept] = odd[which]
+    x, clean = (t.to(TYPES[dtype]).to(DEV) for t in (x, clean))
+    vda = binding.Vda(d, dtype)
+    at = dict(freq=freq.to(DEV), axis=axis.to(DEV), Y=8, X=8, half=half)
+    got, _ = vda.rotate(x, None, **at)
+    want, _ = vda.rotate(clean, None, **at)
+    assert torch.equal(got[..., turned.to(DEV)], want[..., turned.to(DEV)])
+    got, x = got[..., kept.to(DEV)], x[..., kept.to(DEV)]
+    nan = x.isnan()
+    bits = torch.int32 if dtype == "f32" else torch.int16
+    assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan].view(bits), x[~nan].view(bits))
