@@ -158,9 +158,9 @@ struct TokenPrep {
   static constexpr int OFF_W = OFF_T + 64 * L_PITCH * 4;   // products on the way to the inverse
   // per token, exponents in units of ln 2: from the start of its 16 tokens; back to it; to their end; factor of a column as a whole;
   // distances between blocks of 16 (all these are used up when W grows over them); to the chunk's end (later the weight
-  // r e^{G_C - G}); from the chunk's start; beta; r of keys and queries
-  static constexpr int F_UP = 0, F_DOWN = 64, F_END = 128, F_COL = 192, F_DIST = 256, F_LAST = 272, F_ALL = 336, F_BETA = 400, F_R = 464,
-                       F_FLOATS = 592;
+  // r e^{G_C - G}); from the chunk's start; beta; r of keys and queries.  LOW: what their rounding to fp32 left, plus a key's log2 r
+  static constexpr int F_UP = 0, F_UP_LOW = 64, F_DOWN = 128, F_DOWN_LOW = 192, F_END = 256, F_END_LOW = 320, F_COL = 384, F_DIST = 448,
+                       F_LAST = 464, F_ALL = 528, F_BETA = 592, F_R = 656, F_FLOATS = 784;
   static constexpr int OFF_F = OFF_W + 32 * W_PITCH * 4 - F_LAST * 4;
   static constexpr int OFF_BAR = OFF_F + F_FLOATS * 4;
   static constexpr int SMEM_BYTES = OFF_BAR + 64 + 1024;
@@ -267,9 +267,11 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const int row0 = where[0], n = where[1];
   if (n == 0) return;
   if (warp == 1) {
-    // Running sum of the decay, in 64 bits and units of ln 2.  What is kept are differences, each rounded once: within 16
-    // tokens, to the end of the 16, between blocks, to the ends of the chunk.  A token's log decay counts down to -104 (e^-104
-    // is 0 in fp32), so that -infinity leaves the differences finite.
+    // Running sum of the decay, in 64 bits and units of ln 2.  What is kept are differences, each rounded once: to the end of 16
+    // tokens, between blocks, to the ends of the chunk; and within 16 tokens as two numbers each, because there the distances
+    // of two tokens to the start of the 16 are subtracted: after a few strong decays (a reset counts 150) they are in the hundreds
+    // and the difference that matters is small (14 resets and two ordinary tokens: 1.2e-4 off with one number).  A token's log decay
+    // counts down to -104 (e^-104 is 0 in fp32), so that -infinity leaves the differences finite.
     double x[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -292,8 +294,11 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int j = 2 * lane + i;
-      fs[S::F_UP + j] = (float)(g[i] - from);
-      fs[S::F_DOWN + j] = (float)(from - g[i]);
+      const float up = (float)(g[i] - from), low = (float)(g[i] - from - up);
+      fs[S::F_UP + j] = up;
+      fs[S::F_UP_LOW + j] = low;
+      fs[S::F_DOWN + j] = -up;
+      fs[S::F_DOWN_LOW + j] = -low;
       fs[S::F_END + j] = (float)(end - g[i]);
       fs[S::F_LAST + j] = (float)(all - g[i]);
       fs[S::F_ALL + j] = (float)g[i];
@@ -356,10 +361,10 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const int r = tid >> 1;
       fs[S::F_R + r] = ss;
       if (r < 64) {                                   // a key's r goes with its column's exponents
-        const float lg = __log2f(ss), end = fs[S::F_END + r] + lg;
-        fs[S::F_DOWN + r] += lg;
-        fs[S::F_END + r] = end;
-        fs[S::F_COL + r] = exp2_fast(end);
+        const float lg = __log2f(ss);
+        fs[S::F_DOWN_LOW + r] += lg;
+        fs[S::F_END_LOW + r] = lg;
+        fs[S::F_COL + r] = exp2_fast(fs[S::F_END + r] + lg);
         fs[S::F_LAST + r] = ss * exp2_fast(fs[S::F_LAST + r]);
       }
     }
@@ -368,11 +373,12 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       tc_fence_after_sync();
       const bool is_q = qd >= 2;
       const int i = rowid & 63;                       // token of this thread's row
-      const float norm = fs[S::F_R + rowid], up = fs[S::F_UP + i];
+      const float norm = fs[S::F_R + rowid], up = fs[S::F_UP + i], up_low = fs[S::F_UP_LOW + i];
       const float row = is_q ? t.scale * norm : fs[S::F_BETA + i] * norm;
       const int last = is_q ? i : i - 1;              // L is strictly lower, M has its diagonal
       float* L = reinterpret_cast<float*>(bp + S::OFF_T);
       constexpr int LOW = S::OFF_M_LOW - S::OFF_M;
+      static_assert(S::F_DOWN_LOW - S::F_DOWN == S::F_END_LOW - S::F_END, "");
 #pragma unroll 1
       for (int jb = part * 16; jb < 64; jb += 32) {
         unsigned char* m0 = bp + S::OFF_M + i * 128 + (((jb / 8) ^ (i & 7)) << 4);
@@ -400,10 +406,11 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           const float* col = fs + ((i >> 4) == (jb >> 4) ? S::F_DOWN : S::F_END) + jb;
 #pragma unroll
           for (int j = 0; j < 16; j += 4) {
-            const float4 c = *reinterpret_cast<const float4*>(col + j);
-            const float c4[4] = {c.x, c.y, c.z, c.w};
+            const float4 c = *reinterpret_cast<const float4*>(col + j), r = *reinterpret_cast<const float4*>(col + (S::F_END_LOW - S::F_END) + j);
+            const float c4[4] = {c.x, c.y, c.z, c.w}, r4[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[j + e] = jb + j + e <= last ? row * exp2_fast(up + c4[e]) * x[j + e] : 0.f;
+            for (int e = 0; e < 4; ++e)
+              x[j + e] = jb + j + e <= last ? row * exp2_fast((up + c4[e]) + (up_low + r4[e])) * x[j + e] : 0.f;
           }
         }
         if (is_q) {
