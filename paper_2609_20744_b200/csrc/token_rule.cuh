@@ -497,8 +497,9 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
         const bool second = R == 2 && (what & 8);        // of the lane's two rows
         if ((what & 4) && (R == 2 || !(l16 & 1)) && i < n) {
           const float4 c = st.c[i][2];
-          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, second ? u[R - 1][0] : u[0][0], fmaf(c.y, second ? u[R - 1][1] : u[0][1],
-                          fmaf(c.z, second ? u[R - 1][2] : u[0][2], c.w * (second ? u[R - 1][3] : u[0][3])))));
+          // (what the tokens behind this one write has coefficients of zero, but need not be finite: left out, not multiplied)
+          auto from = [&](int t) { return t > (what & 3) ? 0.f : second ? u[R - 1][t] : u[0][t]; };
+          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, from(0), fmaf(c.y, from(1), fmaf(c.z, from(2), c.w * from(3)))));
           static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (second ? 1 : 0)] = from_float<Tio>(o);
         }
       }

@@ -63,3 +63,60 @@ def test_state_after_strong_decays(pattern, l2):
     limit = tolerances("bf16", d, 16, True)[2]
     worst = max(rel(state[i, j], want[i, j]) for i in range(len(lens)) for j in range(h))
     assert worst <= limit, (worst, limit)
+
+
+def spoil(x, name, t, value):
+    """The inputs with token t of one of them set to `value` (q, k: all heads; v: one channel; gates: one head)."""
+    x = dict(x, **{name: x[name].clone()})
+    if name == "v":
+        x[name][t, :, 5] = value
+    elif name in ("q", "k"):
+        x[name][t] = value
+    else:
+        x[name][t, 0] = value
+    return x
+
+
+@pytest.mark.parametrize("dtype,d,flags", [("f32", 64, 0), ("f32", 128, 0), ("bf16", 64, 0),
+                                           ("bf16", 128, binding.VDN_FLAG_FORCE_SIMT)])
+@pytest.mark.parametrize("n,names", [(7, ["token_few"]), (103, ["token_coef", "token_walk"]),
+                                     (2000, ["token_coef", "token_walk_compose", "token_join", "token_walk"])])
+def test_plain_kernels_keep_what_is_not_finite_from_the_tokens_before(dtype, d, flags, n, names):
+    """Token by token or four at a step, whole or in parts: token t reaches itself and what follows, a value only its own channel."""
+    h = 2
+    x = draw(n, h, h, d, dtype, seed=22)
+    vda = binding.Vda(d, dtype, flags=flags)
+    vda.profile(True)
+    clean, state = vda.token_scan(**x)
+    assert kernels(vda) == names
+    for t in (n - 2, n - 3, n - 4, n - 5, n // 2):
+        for name, value in (("q", float("nan")), ("k", float("inf")), ("v", float("nan")), ("v", float("inf")), ("beta", float("nan")),
+                            ("log_alpha", float("nan"))):
+            out, after = vda.token_scan(**spoil(x, name, t, value))
+            assert torch.equal(out[:t], clean[:t]), (name, t)
+            if name == "q":
+                assert torch.equal(out[t + 1:], clean[t + 1:]) and torch.equal(after, state) and out[t].isnan().all()
+            elif name == "v":
+                other = torch.arange(d, device=DEV) != 5
+                assert torch.equal(out[..., other], clean[..., other]) and torch.equal(after[:, :, other], state[:, :, other])
+                assert not out[t:, :, 5].isfinite().any()
+
+
+def test_chunks_keep_what_is_not_finite_from_the_chunks_before():
+    """In chunks of 64 such a value reaches its whole chunk and what follows, but no chunk before, and a value only its own channel."""
+    d, h = 128, 2
+    for n, t in ((300, 150), (5000, 4100)):
+        x = draw(n, h, h, d, "bf16", seed=23)
+        vda = binding.Vda(d, "bf16")
+        vda.profile(True)
+        clean, state = vda.token_scan(**x)
+        assert kernels(vda) == (CHUNKS if n == 300 else PARTS)
+        first = t // 64 * 64
+        for name in ("q", "k", "v", "beta", "log_alpha"):
+            out, after = vda.token_scan(**spoil(x, name, t, float("nan")))
+            assert torch.equal(out[:first], clean[:first]), name
+            if name == "q":
+                assert torch.equal(out[t + 1:], clean[t + 1:]) and torch.equal(out[first:t], clean[first:t]) and torch.equal(after, state)
+            elif name == "v":
+                other = torch.arange(d, device=DEV) != 5
+                assert torch.equal(out[..., other], clean[..., other]) and torch.equal(after[:, :, other], state[:, :, other])
