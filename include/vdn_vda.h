@@ -456,7 +456,7 @@ vdn_status vdn_vda_scan_static(const float* stats, const float* inv, float* read
 /* Plumbing (no passage of the paper to cite).  Last device-side status recorded by this handle's kernels: VDN_OK,
  * VDN_ERR_TIMEOUT (a wait inside a kernel ran out; that kernel's CTA stopped early and the outputs of the call are
  * incomplete), VDN_ERR_INTERNAL or VDN_ERR_INVALID_ARG (vdn_vda_token_step skipped a request whose state an earlier one of
- * the same call has).  Does not synchronise: call it after synchronising the stream.  The word is
+ * the same call has; it does not take the place of either of the others).  Does not synchronise: call it after synchronising the stream.  The word is
  * sticky: reading it clears nothing, and no forward call clears it, so that an error is not lost between a call
  * and the moment the caller looks.  vdn_vda_clear_status resets it. */
 vdn_status vdn_vda_status(vdn_vda_t h);

@@ -77,7 +77,7 @@ __device__ __forceinline__ long long token_slot(const TokenArgs& a, int s, int x
     int twice = 0;
     for (int j = x; j < s; j += threads) twice |= a.index[j] == (int)slot;
     if (__syncthreads_or(twice)) {
-      if (x == 0) atomicExch(a.status, kStatusInvalidArg);
+      if (x == 0) atomicCAS(a.status, 0, kStatusInvalidArg);   // (a timeout that nobody has read yet says more)
       return -1;
     }
   }

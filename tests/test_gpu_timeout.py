@@ -77,3 +77,18 @@ def test_other_handles_do_not_see_the_timeout():
     torch.cuda.synchronize()
     assert a.status() == binding.VDN_ERR_TIMEOUT and b.status() == binding.VDN_OK
     a.clear_status()
+
+
+def test_a_doubled_state_does_not_hide_a_timeout():
+    d, h = 64, 2
+    vda = binding.Vda(d, "f32")
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    twice = dict(q=z(2, h, d), k=z(2, h, d), v=z(2, h, d), beta=z(2, h), state=z(3, h, d, d),
+                 index=torch.ones(2, dtype=torch.int32, device="cuda"))
+    vda.selftest_wait_expiry(limit_us=200)
+    vda.token_step(**twice)
+    torch.cuda.synchronize()
+    assert vda.clear_status() == binding.VDN_ERR_TIMEOUT
+    vda.token_step(**twice)
+    torch.cuda.synchronize()
+    assert vda.clear_status() == binding.VDN_ERR_INVALID_ARG
