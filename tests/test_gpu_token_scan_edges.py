@@ -120,3 +120,95 @@ def test_chunks_keep_what_is_not_finite_from_the_chunks_before():
             elif name == "v":
                 other = torch.arange(d, device=DEV) != 5
                 assert torch.equal(out[..., other], clean[..., other]) and torch.equal(after[:, :, other], state[:, :, other])
+
+
+def in_chunks(q, k, v, beta, log_alpha, s0, scale, l2_eps, state_tol, C=64):
+    """One sequence in 64 bits, chunk by chunk, and how far the tensor cores may be off.  q, k, v [n, H, d], gates [n, H], s0 [H, d, d];
+    returns read-out [n, H, d], its bound without the last rounding, state.
+
+    O = e^G S q + P X with P = M T, M the decayed q.k, T the inverse of I + L.  Every factor but q and k has two bf16 parts, off by
+    2^-16 (r, e^G: 2^-20), and accumulators are fp32: the result is off by 2^-16 of each of S, X, M, T and P's terms, taken without
+    their signs, and by what the state is off, state_tol of its norm (and of X's, which has it as e^G S k)."""
+    q, k, v, beta = (t.double() for t in (q, k, v, beta))
+    g = log_alpha.double().clamp(min=-104) if log_alpha is not None else torch.zeros_like(beta)
+    if l2_eps > 0:
+        q, k = (t / torch.sqrt((t * t).sum(-1, keepdim=True) + l2_eps) for t in (q, k))
+    n, h, d = v.shape
+    r = h // q.shape[1]
+    q, k = q.repeat_interleave(r, 1), k.repeat_interleave(r, 1)
+    S = s0.double().clone() if s0 is not None else torch.zeros(h, d, d, dtype=torch.float64, device=v.device)
+    want, off = torch.empty_like(v), torch.empty_like(v)
+    for c in range(0, n, C):
+        w = slice(c, min(n, c + C))
+        Q, K, V = (t[w].transpose(0, 1) for t in (q, k, v))                # [H, C, d]
+        b, G = beta[w].T, g[w].T.cumsum(-1)
+        decay = torch.exp((G[:, :, None] - G[:, None]).tril()).tril()
+        eye = torch.eye(G.shape[1], dtype=torch.float64, device=v.device)
+        T = torch.linalg.inv(eye + (b[:, :, None] * decay * (K @ K.mT)).tril(-1)) * b[:, None]
+        M, e = decay * (Q @ K.mT), torch.exp(G)[..., None]
+        X = V - e * (K @ S.mT)
+        P = M.abs() @ T.abs()
+        norm = S.flatten(1).norm(dim=1)[:, None, None] * state_tol / d ** 0.5
+        from_state = norm * (e * Q.norm(dim=2, keepdim=True) + P @ (e * K.norm(dim=2, keepdim=True)))
+        want[w] = (scale * (e * (Q @ S.mT) + M @ T @ X)).transpose(0, 1)
+        off[w] = (abs(scale) * (2.0 ** -16 * (e * (Q.abs() @ S.abs().mT) + 4 * (P @ X.abs())) + from_state)).transpose(0, 1)
+        S = torch.exp(G[:, -1])[:, None, None] * S + (T @ X).mT @ (torch.exp(G[:, -1:] - G)[..., None] * K)
+    return want, off, S
+
+
+def check_chunks(vda, x, lens, names, s0=None, in_place=False, scale=0.5, l2_eps=0.0, walks=1):
+    """token_scan on the tensor cores against in_chunks, sequence by sequence and head by head."""
+    d = 128
+    cu = torch.tensor([0] + list(lens)).cumsum(0).to(torch.int32).to(DEV)
+    first = s0.clone() if s0 is not None else None
+    vda.profile(True)
+    out, state = vda.token_scan(**x, cu_seqlens=cu, s0=s0, state=s0 if in_place else None, scale=scale, l2_eps=l2_eps)
+    torch.cuda.synchronize()
+    assert vda.status() == binding.VDN_OK and kernels(vda) == names
+    at = 0
+    for i, n in enumerate(lens):
+        w = slice(at, at + n)
+        tol = walks * tolerances("bf16", d, n, True)[2]
+        want, off, want_s = in_chunks(*(x[m][w] if x[m] is not None else None for m in ("q", "k", "v", "beta", "log_alpha")),
+                                      first[i] if first is not None else None, scale, l2_eps, tol)
+        for j in range(state.shape[1]):
+            assert float((state[i, j].double() - want_s[j]).norm()) <= tol * float(want_s[j].norm()), (i, j, n)
+            far = float((out[w, j].double() - want[:, j]).norm())
+            assert far <= 2.0 ** -8 * float(want[:, j].norm()) + float(off[:, j].norm()), (i, j, n)
+        at += n
+
+
+@pytest.mark.parametrize("lens,h,hk,l2,decay,first", [
+    ([131, 0, 3003, 64, 2500], 4, 2, 1e-6, True, True), ([1500, 1501], 4, 4, 0.0, False, True), ([1, 5000, 3], 1, 1, 1e-6, True, False),
+    ([2049], 6, 2, 0.0, True, True), ([100, 4000], 9, 3, 1e-6, False, False)], ids=str)
+def test_cut_sequences(lens, h, hk, l2, decay, first):
+    """Sequences in parts that start anywhere, several in a call, with shared key heads, normalised keys, resets inside a part and at its
+    border, states in place.  A part's last state is enter M + J: M, J and the walk itself are each off as a whole sequence's state
+    is, hence three times its tolerance."""
+    d, n = 128, sum(lens)
+    x = draw(n, h, hk, d, "bf16", seed=31, l2=l2 > 0, decay=decay)
+    if decay:
+        at = max(range(len(lens)), key=lambda i: lens[i])
+        start = sum(lens[:at])
+        x["log_alpha"][[start + 700, start + 1024, start + lens[at] - 30]] = -float("inf")
+    g = torch.Generator().manual_seed(32)
+    s0 = 0.3 * torch.randn(len(lens), h, d, d, generator=g).to(DEV) if first else None
+    check_chunks(binding.Vda(d, "bf16"), x, lens, PARTS, s0, first, l2_eps=l2, walks=3)
+
+
+@pytest.mark.parametrize("seqs,h,hk", [(90, 6, 2), (256, 4, 4), (300, 8, 4)])
+def test_many_sequences_in_chunks(seqs, h, hk):
+    """More chains than SMs: the longest first up to 256 sequences, as they come beyond."""
+    d = 128
+    g = torch.Generator().manual_seed(seqs)
+    lens = torch.randint(0, 170, (seqs,), generator=g).tolist()
+    x = draw(sum(lens), h, hk, d, "bf16", seed=33, l2=True)
+    s0 = 0.3 * torch.randn(seqs, h, d, d, generator=g).to(DEV)
+    check_chunks(binding.Vda(d, "bf16"), x, lens, CHUNKS, s0, True, l2_eps=1e-6)
+
+
+def test_uneven_lengths_in_chunks():
+    lens = [5, 0, 64, 1, 130, 0, 63, 700, 2, 129]
+    for h, hk, l2, decay in ((3, 3, 0.0, True), (4, 1, 1e-6, True), (4, 2, 0.0, False)):
+        x = draw(sum(lens), h, hk, 128, "bf16", seed=34, l2=l2 > 0, decay=decay)
+        check_chunks(binding.Vda(128, "bf16"), x, lens, CHUNKS, l2_eps=l2)
