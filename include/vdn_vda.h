@@ -291,7 +291,7 @@ vdn_status vdn_vda_prepare(vdn_vda_t h, const void* q_in, const void* k_in, cons
  *           state.
  *   p->q_stride, k_stride, v_stride, out_stride   elements from one token to the next, 0 = dense (heads of a token are
  *           always dense): q, k, v may be slices of one projected tensor.  Multiples of 16 bytes.
- *   p->l2_eps     0: q and k are used as they are.  > 0: x / sqrt(sum_j x_j^2 + l2_eps) first.
+ *   p->l2_eps     0: q and k are used as they are.  Else (a normal number, up to 1e30): x / sqrt(sum_j x_j^2 + l2_eps) first.
  *   p->scale      factor on the read-out.
  * States are float [.., heads, d_v, d_k], the orientation of s0 above, whatever io_dtype is.
  *

@@ -6,6 +6,7 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <atomic>
@@ -1223,8 +1224,9 @@ vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, 
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(p->s0) || !aligned16(p->state))
     return fail(h, VDN_ERR_INVALID_ARG, "q, k, v, out and the states must be 16-byte aligned");
   if (out && (out == q || out == k || out == v)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias an input");
-  if (!(p->l2_eps >= 0.f) || p->l2_eps > 1e30f || !std::isfinite(p->scale))
-    return fail(h, VDN_ERR_INVALID_ARG, "scale must be finite, l2_eps a finite non-negative number");
+  // (two keys of zero have the factor 1 / l2_eps, which must be finite: times their product, zero, it would be NaN)
+  if (!(p->l2_eps >= 0.f) || p->l2_eps > 1e30f || (p->l2_eps > 0.f && p->l2_eps < FLT_MIN) || !std::isfinite(p->scale))
+    return fail(h, VDN_ERR_INVALID_ARG, "scale must be finite, l2_eps zero or a normal number up to 1e30");
   const long long dk = (long long)p->key_heads * h->cfg.d, dv = (long long)p->heads * h->cfg.d;
   const size_t es = elem_size(h);
   if (!stride_ok(p->q_stride, dk, es) || !stride_ok(p->k_stride, dk, es) || !stride_ok(p->v_stride, dv, es) ||

@@ -212,3 +212,25 @@ def test_uneven_lengths_in_chunks():
     for h, hk, l2, decay in ((3, 3, 0.0, True), (4, 1, 1e-6, True), (4, 2, 0.0, False)):
         x = draw(sum(lens), h, hk, 128, "bf16", seed=34, l2=l2 > 0, decay=decay)
         check_chunks(binding.Vda(128, "bf16"), x, lens, CHUNKS, l2_eps=l2)
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128)])
+@pytest.mark.parametrize("n", [5, 40, 300])
+def test_keys_of_zero_with_the_smallest_eps(dtype, d, n):
+    """1 / l2_eps is the factor between two keys of zero: finite down to the smallest eps that is taken, and nothing is written."""
+    x = draw(n, 2, 2, d, dtype, seed=41)
+    x["k"][n // 3:] = 0
+    x["q"][n // 2:] = 0
+    vda = binding.Vda(d, dtype)
+    out, state = vda.token_scan(**x, l2_eps=1.2e-38)
+    assert out.isfinite().all() and state.isfinite().all() and (out[n // 2:] == 0).all()
+    step = {m: t[-3:] for m, t in x.items()}
+    pool = torch.randn(3, 2, d, d, device=DEV)
+    want = pool * torch.exp(step["log_alpha"])[..., None, None]
+    assert (vda.token_step(**step, state=pool, l2_eps=1.2e-38) == 0).all()
+    assert float((pool - want).norm()) <= 2.0 ** -22 * float(want.norm())
+    for eps in (1e-38, 1e-40, 1e-45):
+        with pytest.raises(binding.VdnError, match="l2_eps"):
+            vda.token_scan(**x, l2_eps=eps)
+        with pytest.raises(binding.VdnError, match="l2_eps"):
+            vda.token_step(**step, state=pool, l2_eps=eps)
