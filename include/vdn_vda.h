@@ -307,10 +307,20 @@ vdn_status vdn_vda_prepare(vdn_vda_t h, const void* q_in, const void* k_in, cons
  *           have their own; nothing in it outlives the call.
  *   bf16 with d = 128 runs on the tensor cores in chunks of 64 tokens where that is faster (by sizes alone: short sequences go
  *   token by token), a few long sequences in parts side by side.  Every factor keeps 16 significant bits or more, sums are
- *   fp32: against a 64-bit evaluation the state is off by 3e-6 .. 5e-6 of its norm (measured: unit keys, a third of them within
- *   0.4 of eight shared directions; 4e-5 with one key throughout and beta = 1), the read-out by 3e-4 at most before its
- *   rounding.  A value that is not finite reaches the other tokens of its 64, and what follows.  All else, and
- *   VDN_FLAG_FORCE_SIMT, runs in plain fp32 (4e-7 with f32 I/O), a few long sequences in parts as well.
+ *   fp32: against a 64-bit evaluation the state is off by 3e-6 .. 8e-6 of its norm (measured: unit keys, a third of them near
+ *   shared directions; 1e-5 where few tokens are left after many resets, 4e-5 with one key throughout and beta = 1), the read-out by
+ *   3e-4 at most before its rounding.  All else, and VDN_FLAG_FORCE_SIMT, runs in plain fp32, a few long sequences in parts as
+ *   well: 1e-7 .. 4e-7, but up to 7e-6 with heads that hardly decay, since each alpha is rounded to fp32 and the roundings of gates
+ *   within 1e-7 of 1 add up.  The choice goes by sizes, so what is packed beside a sequence can change its last bits;
+ *   VDN_FLAG_FORCE_SIMT keeps to plain fp32.
+ *   A value that is not finite reaches its token and those after it, in v only its own channel; on the tensor cores the tokens
+ *   before it in its chunk of 64 too.
+ *   The lengths stay on the device, so every choice is made for an average length, n_tokens / n_seqs.  However uneven they are the
+ *   results are right, but the call may be slow: with 8 tokens a sequence or fewer on average each sequence goes token by token (1400 tokens
+ *   beside 200 single ones, 8 heads: 1700 us; the long one by itself 73, the others 31), and a long sequence beside many short
+ *   ones is not cut (32760 tokens beside 12 of 64, 8 heads: 1400 us, by itself 313).  Give such a sequence a call of its own.
+ *   The workspace grows with the tokens: 48.5 KB for each head and 64 tokens on the tensor cores (4.5 GiB for 262144 tokens of 24
+ *   heads), 48 bytes a token and head otherwise.  A sequence that needs less can be scanned in pieces, state to s0.
  * vdn_vda_token_step: request s is rows s * per .. (s + 1) * per - 1 of n_requests * per.
  *   p->state      [n_slots, heads, d, d]: the pool, updated in place.
  *   p->index      int32 [n_requests], DEVICE, or NULL (= s): the request's state.  A negative or too large index marks a

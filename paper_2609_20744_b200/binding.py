@@ -504,7 +504,8 @@ class Vda:
         q, k [N,Hk,d], v [N,H,d], beta, log_alpha [N,H] (float), cu_seqlens int32 [S+1] (CUDA; None: one sequence of all N
         rows), s0 [S,H,d,d] (float, state before each sequence).  state [S,H,d,d] after each sequence, in s0's orientation
         and that of forward(s0=...); `state` may be s0 itself.  Rows behind the last sequence are not written: a fresh `out`
-        holds whatever was there.
+        holds whatever was there.  Kernels are chosen for the average length: a long sequence among many short ones is faster in a
+        call of its own.
         """
         torch, dev = self._torch, self.device
         lead, H, Hk, st = validate_token_args(self.torch_dtype, self.d, dev, q, k, v, beta, out, log_alpha)

@@ -6,8 +6,9 @@
 // up to 4e-3 radians.  A CTA first writes the cosines and sines of its tokens to shared memory -- they are the same for
 // all heads of the queries and the keys -- and then streams the heads through registers: a lane holds two 16-byte
 // pieces, which are the two halves of its pairs (HALF) or hold whole neighbouring pairs.  Bound by HBM: each tensor is
-// read once and written once.  768p clip, 40 heads of queries and of keys: 2.10 ms, 6.8 TB/s (the measured copy: 6.6); 480p clip,
-// 8 and 2 heads: 37 us without norm, 41 to 45 with it, where a plain copy of as many bytes takes 31.
+// read once and written once.  768p clip, 40 heads of queries and of keys: 2.10 ms on the same tensors again and again, 2.16 ms on others in
+// turn (6.7 TB/s; the measured copy: 6.6); 480p clip, 8 and 2 heads: 37 us without norm, 43 with it, where a plain copy of as many
+// bytes takes 31: with the norm it is short of issue slots (64 % used, DRAM 37 %).
 #pragma once
 #include <cuda_bf16.h>
 

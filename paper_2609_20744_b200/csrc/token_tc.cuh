@@ -17,7 +17,7 @@
 // accumulated in fp32; S itself is carried in fp32 registers.  One part would do for what only the rounded output sees where keys
 // differ (read-out off by 3.4e-3, 1.7e-3 of which is its rounding), but not where they are alike and beta is near 1, where
 // M times the inverse cancels: 2.3e-2 with one key throughout, 1.1e-1 with keys of length 1.2; 1.7e-3 everywhere with two.
-// They cost 10 % (65536 tokens x 32 heads: 1.27 -> 1.39 ms).
+// They cost 10 % (65536 tokens x 32 heads, a call: 1.43 -> 1.59 ms).
 #pragma once
 #include <cuda_bf16.h>
 
@@ -145,7 +145,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
 // blocks are merged, [T11 0; -T22 L21 T11, T22], to 32 and to 64 rows, all threads at once.  A thread to a column over all 64
 // rows needs no products, but 2016 steps in straight line: half as fast again, most of it waiting for
 // instructions.  Everything that could be a long straight line is a loop over 16 columns for the same reason.
-// Measured on 65536 tokens x 32 heads (33 000 chunks): 714 us, 3.8 TB/s of the 81 KB a chunk reads and writes; four CTAs an SM use about half of
+// Measured on 65536 tokens x 32 heads (33 000 chunks): 724 us, 3.7 TB/s of the 81 KB a chunk reads and writes; four CTAs an SM use about half of
 // the issue slots and two thirds of the shared-memory pipe (ncu) and wait at barriers for the rest.
 struct TokenPrep {
   static constexpr int THREADS = 256, CTAS = 4;       // a CTA's phases are short and end at barriers: four of them side by side
@@ -997,7 +997,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
 // while the state warps work on the other -- S K^T of J, of M, X^T E^T of J, of M, and under each the state warps' turn
 // that it does not depend on (262144 tokens x 24 heads in 6 parts: 3.49 ms with a CTA to each, 2.23 ms so; the split into bf16
 // parts on the packed fp32 pipe is a tenth of that; it is bound by issue slots, 12 000 instructions a step of both chains, 44 % of
-// the slots used).  Tensor memory holds both because each chain has two
+// the slots used; 96 registers a thread and 108 bytes of spills).  Tensor memory holds both because each chain has two
 // regions only: the parts of S, which X^T E^T overwrites (they are used up by then) and whose place the thread that owns a piece of
 // the new state fills again, and S K^T, which the parts of X replace in the same way.
 struct TokenCompose {

@@ -1281,6 +1281,8 @@ cudaError_t launch_overlapped(void (*kernel)(P...), unsigned grid, int threads, 
 }
 
 // The lengths stay on the device.  Where a choice depends on the longest sequence: four times the average, if there are so many.
+// (The plain kernels' parts were fitted to twice the average, see there; and whether a few tokens a sequence go one by one hangs
+// on the average alone.  A longer sequence among shorter ones is then slow, not wrong: the header says by how much.)
 long long longest_guess(long long n_tokens, int n_seqs) { return n_seqs > 4 ? 4 * (n_tokens / n_seqs) : n_tokens; }
 
 // Workspace of the plain rule: nothing for a few tokens a sequence; else the coefficients, and per (part, head) of cut sequences
