@@ -84,6 +84,12 @@ __device__ __forceinline__ long long token_slot(const TokenArgs& a, int s, int x
   return slot;
 }
 
+// A factor that every token multiplies the state with must not be off by the same part of a step each time: with a constant gate near
+// 1 (log_alpha = -1e-6, 3000 tokens, d = 128) the state was off by 2.3e-5, without a gate by 4e-7.  So where a gate is above a
+// half the state x becomes x + (alpha - 1) x, or alpha x + (what alpha lost) x; below, it forgets too fast for that to matter,
+// and alpha - 1 would have lost alpha's last bits.
+__device__ __forceinline__ bool slow_decay(float log_alpha) { return fabsf(log_alpha) < 0.69f; }
+
 // One CTA to 32 R rows of a (sequence, head), R of them to a thread.  R = d / 32, a whole state to a CTA, where there are states
 // enough to fill the GPU: more bytes on their way, keys and queries read once.  256 requests x 32 heads of 128 x 128 take 232 us
 // with R = 1, 201 with 2 and 179 with 4 (the bytes alone: 165); 40 states are faster on four CTAs each.
@@ -122,8 +128,9 @@ __global__ void __launch_bounds__(256, R == 4 ? 2 : 3) token_few_kernel(const To
     float v[R];
 #pragma unroll
     for (int w = 0; w < R; ++w) v[w] = to_float(vp[w * 32]);
-    const float beta = a.beta[(start + t) * a.H + h];
-    const float alpha = a.log_alpha ? expf(a.log_alpha[(start + t) * a.H + h]) : 1.f;
+    const float beta = a.beta[(start + t) * a.H + h], ga = a.log_alpha ? a.log_alpha[(start + t) * a.H + h] : 0.f;
+    const bool slow = slow_decay(ga);                    // (the same for all threads)
+    const float less = slow ? expm1f(ga) : 0.f, alpha = slow ? 1.f + less : expf(ga);   // less: alpha - 1
     float sk[R], sq[R], kq = 0.f, kk = 0.f, qq = 0.f;
     auto add = [](float& s, const float4& x, const float4& y) {
       s = fmaf(x.x, y.x, s); s = fmaf(x.y, y.y, s); s = fmaf(x.z, y.z, s); s = fmaf(x.w, y.w, s);
@@ -155,15 +162,30 @@ __global__ void __launch_bounds__(256, R == 4 ? 2 : 3) token_few_kernel(const To
     }
     const float rk = a.l2_eps > 0.f ? rsqrtf(kk + a.l2_eps) : 1.f;
     const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
+    float uk[R];
 #pragma unroll
     for (int w = 0; w < R; ++w) {
-      const float uk = beta * (v[w] - alpha * rk * sk[w]) * rk;
-      if (lane8 == 0) op[w * 32] = from_float<Tio>(a.scale * rq * fmaf(uk, kq, alpha * sq[w]));
+      uk[w] = beta * (v[w] - alpha * rk * sk[w]) * rk;
+      if (lane8 == 0) op[w * 32] = from_float<Tio>(a.scale * rq * fmaf(uk[w], kq, alpha * sq[w]));
+    }
+    if (slow) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        st[w][i].x = fmaf(uk, k[i].x, alpha * st[w][i].x); st[w][i].y = fmaf(uk, k[i].y, alpha * st[w][i].y);
-        st[w][i].z = fmaf(uk, k[i].z, alpha * st[w][i].z); st[w][i].w = fmaf(uk, k[i].w, alpha * st[w][i].w);
-      }
+      for (int w = 0; w < R; ++w)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float4& y = st[w][i];
+          y.x = fmaf(uk[w], k[i].x, fmaf(less, y.x, y.x)); y.y = fmaf(uk[w], k[i].y, fmaf(less, y.y, y.y));
+          y.z = fmaf(uk[w], k[i].z, fmaf(less, y.z, y.z)); y.w = fmaf(uk[w], k[i].w, fmaf(less, y.w, y.w));
+        }
+    } else {
+#pragma unroll
+      for (int w = 0; w < R; ++w)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          float4& y = st[w][i];
+          y.x = fmaf(uk[w], k[i].x, alpha * y.x); y.y = fmaf(uk[w], k[i].y, alpha * y.y);
+          y.z = fmaf(uk[w], k[i].z, alpha * y.z); y.w = fmaf(uk[w], k[i].w, alpha * y.w);
+        }
     }
     qp += a.q_stride; kp += a.k_stride; vp += a.v_stride; op += a.out_stride;
   }
@@ -212,6 +234,8 @@ __device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int
 // tokens of a head, eight lanes to a token.  (Formed by the walking CTAs, eight of which share a head's tokens at d = 128, they took a
 // fifth of the time.)
 //   [0] beta P r, beta, (i,0), (i,1) of the first sum;  [1] (i,2), A_4i r_i, scale r_q P, P_4;  [2] (i,0) .. (i,3) of the second, times scale
+// The first of the four has no (i,2): there stands what P_4 lost when it was rounded (slow_decay).  (A branch on the size, as below, is
+// slower here: 9000 tokens, 36 heads, f32, d = 128 1.94 ms instead of 1.86.)
 constexpr int kCoefFloats = 12;
 
 template <typename Tio, int D>
@@ -259,8 +283,10 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
   const float rk = a.l2_eps > 0.f ? rsqrtf(own + a.l2_eps) : 1.f;
   const float rq = a.l2_eps > 0.f ? rsqrtf(qq + a.l2_eps) : 1.f;
   const size_t gate = (size_t)(start + g0 + i4) * a.H + h;
-  const float alpha = there && a.log_alpha ? expf(a.log_alpha[gate]) : 1.f, beta = there ? a.beta[gate] : 0.f;
-  float al[4], ro[4];
+  const float ga = there && a.log_alpha ? a.log_alpha[gate] : 0.f, alpha = expf(ga), beta = there ? a.beta[gate] : 0.f;
+  float al[4], ro[4], four = ga;
+  four += __shfl_xor_sync(0xFFFFFFFFu, four, 8);
+  four += __shfl_xor_sync(0xFFFFFFFFu, four, 16);
 #pragma unroll
   for (int o = 0; o < 4; ++o) {
     al[o] = __shfl_sync(0xFFFFFFFFu, alpha, o * 8);
@@ -278,9 +304,15 @@ __global__ void __launch_bounds__(256) token_coef_kernel(const TokenArgs a, floa
       if (o < 3) first[o] = o < i4 ? beta * rk * ro[o] * dec * kk[o] : 0.f;
       second[o] = o <= i4 ? a.scale * rq * ro[o] * dec * qk[o] : 0.f;
     }
+    float p4 = pi * to_end, rest = 0.f;
+    if (slow_decay(four)) {
+      const float less = expm1f(four);
+      p4 = 1.f + less;
+      rest = less - (p4 - 1.f);                          // exact
+    }
     float4* c = coef + gate * (kCoefFloats / 4);
     c[0] = make_float4(beta * pi * rk, beta, first[0], first[1]);
-    c[1] = make_float4(first[2], to_end * rk, a.scale * rq * pi, pi * to_end);
+    c[1] = make_float4(i4 > 0 ? first[2] : rest, to_end * rk, a.scale * rq * pi, p4);
     c[2] = make_float4(second[0], second[1], second[2], second[3]);
   }
 }
@@ -503,6 +535,7 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
           static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (second ? 1 : 0)] = from_float<Tio>(o);
         }
       }
+      const uint64_t p4 = f2_pack(tail.w, tail.w), rest = f2_pack(st.c[g][1].x, st.c[g][1].x);
       float e4[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) e4[i] = st.c[g + i][1].y;
@@ -514,7 +547,7 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
 #pragma unroll
         for (int e = 0; e < NE / 2; ++e)
           x[w][e] = f2_fma(uu[3], k[3][e], f2_fma(uu[2], k[2][e], f2_fma(uu[1], k[1][e],
-                    f2_fma(uu[0], k[0][e], f2_fma(f2_pack(tail.w, tail.w), x[w][e], 0ull)))));
+                    f2_fma(uu[0], k[0][e], f2_fma(p4, x[w][e], f2_fma(rest, x[w][e], 0ull))))));
       }
     }
     mbar_arrive_warp(bars + 8 * (W::STAGES + b % W::STAGES));

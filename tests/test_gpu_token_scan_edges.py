@@ -234,3 +234,28 @@ def test_keys_of_zero_with_the_smallest_eps(dtype, d, n):
             vda.token_scan(**x, l2_eps=eps)
         with pytest.raises(binding.VdnError, match="l2_eps"):
             vda.token_step(**step, state=pool, l2_eps=eps)
+
+
+@pytest.mark.parametrize("dtype,d,flags", [("f32", 64, 0), ("f32", 128, 0), ("bf16", 64, 0), ("bf16", 128, 0),
+                                           ("bf16", 128, binding.VDN_FLAG_FORCE_SIMT)])
+@pytest.mark.parametrize("gate", [-1e-4, -1e-6, -1e-7, -4e-8, -2e-8, -0.02, -0.5, 0.0])
+def test_constant_gates_near_one(dtype, d, flags, gate):
+    """A gate that is the same for every token and head: what rounding does to it must not add up over the tokens.  A state's element is
+    rounded at most five times in four tokens, and what is written (a 1/sqrt(d)-th of the state or so) by its dot product: three
+    halves of a step a token, independent, 3 sqrt(n) u32; on the tensor cores 4 * 2^-16 besides."""
+    n, h = 3000, 4
+    x = draw(n, h, h, d, dtype, seed=42, decay=False)
+    x["log_alpha"] = torch.full((n, h), gate, device=DEV)
+    tol = 3 * n ** 0.5 * 2.0 ** -24
+    vda = binding.Vda(d, dtype, flags=flags)
+    vda.profile(True)
+    _, state = vda.token_scan(**x)
+    chunks = "token_chain" in kernels(vda)
+    want = in_chunks(*(x[m] for m in ("q", "k", "v", "beta", "log_alpha")), None, 1.0, 0.0, tol)[2]
+    far = (state[0].double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)
+    assert float(far.max()) <= tol + (4 * 2.0 ** -16 if chunks else 0)
+    # as one request of as many tokens
+    pool = torch.zeros(1, h, d, d, device=DEV)
+    vda.token_step(**{m: t[None] for m, t in x.items()}, state=pool)
+    far = (pool[0].double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)
+    assert float(far.max()) <= tol
