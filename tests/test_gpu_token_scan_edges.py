@@ -1,6 +1,7 @@
 """token_scan where its decays, its cuts and its inputs are at their edges, against the 64-bit statement of tests/test_gpu_token_ops.py's
 tolerances."""
-import numpy as np
+import ctypes
+
 import pytest
 import torch
 
@@ -259,3 +260,36 @@ def test_constant_gates_near_one(dtype, d, flags, gate):
     vda.token_step(**{m: t[None] for m, t in x.items()}, state=pool)
     far = (pool[0].double() - want).flatten(1).norm(dim=1) / want.flatten(1).norm(dim=1)
     assert float(far.max()) <= tol
+
+
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("f32", 128), ("bf16", 128)])
+def test_a_long_sequence_among_single_tokens(dtype, d):
+    """Few tokens a sequence on average: each sequence goes token by token, the long one too."""
+    lens = [1] * 150 + [700] + [1, 0, 2] * 20
+    x = draw(sum(lens), 2, 1, d, dtype, seed=43)
+    s0 = 0.3 * torch.randn(len(lens), 2, d, d, generator=torch.Generator().manual_seed(44)).to(DEV)
+    vda = binding.Vda(d, dtype)
+    vda.profile(True)
+    check_scan(vda, x, lens, dtype, d, False, s0, scale=0.5)
+    assert kernels(vda) == ["token_few"]
+
+
+@pytest.mark.parametrize("n", [5, 40, 300, 3000])
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("bf16", 128)])
+def test_a_state_that_nobody_wants(dtype, d, n):
+    """The C entry point takes NULL for the last states: the read-outs are the same."""
+    x = draw(n, 2, 2, d, dtype, seed=45)
+    s0 = torch.randn(1, 2, d, d, device=DEV)
+    vda = binding.Vda(d, dtype)
+    want, _ = vda.token_scan(**x, s0=s0)
+    prm = binding.VdnTokenParams(ctypes.sizeof(binding.VdnTokenParams), 2, 2, 1, 1.0, 0.0, None, None, x["log_alpha"].data_ptr(),
+                                 s0.data_ptr(), None)
+    need = vda.lib.vdn_vda_token_scan_workspace_bytes(vda.h, n, ctypes.byref(prm))
+    ws, out = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty_like(x["v"])
+    stream = torch.cuda.current_stream().cuda_stream
+    args = (vda.h, x["q"].data_ptr(), x["k"].data_ptr(), x["v"].data_ptr(), x["beta"].data_ptr(), out.data_ptr(), n, ctypes.byref(prm))
+    assert vda.lib.vdn_vda_token_scan(*args, ws.data_ptr() if need else None, need, stream) == binding.VDN_OK
+    torch.cuda.synchronize()
+    assert vda.status() == binding.VDN_OK and torch.equal(out, want)
+    if need:
+        assert binding.STATUS_NAMES[vda.lib.vdn_vda_token_scan(*args, ws.data_ptr(), need - 1, stream)] == "VDN_ERR_WORKSPACE"
