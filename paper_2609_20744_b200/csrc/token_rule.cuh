@@ -235,7 +235,7 @@ __device__ __forceinline__ int token_seq_of(const TokenArgs& t, long long x, int
 // fifth of the time.)
 //   [0] beta P r, beta, (i,0), (i,1) of the first sum;  [1] (i,2), A_4i r_i, scale r_q P, P_4;  [2] (i,0) .. (i,3) of the second, times scale
 // The first of the four has no (i,2): there stands what P_4 lost when it was rounded (slow_decay).  (A branch on the size, as below, is
-// slower here: 9000 tokens, 36 heads, f32, d = 128 1.94 ms instead of 1.86.)
+// slower here by 4 %: 9000 tokens, 36 heads, f32, d = 128.  As it is it costs 4 % there, 1 to 2 % with fewer heads.)
 constexpr int kCoefFloats = 12;
 
 template <typename Tio, int D>
@@ -340,8 +340,8 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c) {
 // Measured, one sequence of 1024 tokens, 2 heads, d = 128, bf16: 119 us, both kernels (R = 2: 150); a token at a time it took 289.
 // Long sequences of few (sequence, head)s: with COMPOSE the kernel makes, side by side, of each part what it writes by itself (J) and
 // what it makes of an entering state (M, rows of the identity walked without values); token_join_kernel passes the states along, and
-// the parts are walked from those.  9000 tokens, 1 head, d = 128, f32: 921 us whole, 167 in 33 parts (compose 62, join 51, walk 55).
-// Many heads (9000 tokens, 36, d = 128, f32): 1540 us; 1720 with queries fetched one by one and single fp32 instructions, about 60 % of
+// the parts are walked from those.  9000 tokens, 1 head, d = 128, f32: 921 us whole, 170 in 33 parts (compose 70, join 51, walk 55).
+// Many heads (9000 tokens, 36, d = 128, f32): 1620 us (1540 with decays rounded to one number); 1720 with queries fetched one by one and single fp32 instructions, about 60 % of
 // the issue slots and of the shared-memory pipe either way.
 template <typename Tio, int D, int R, bool COMPOSE = false>
 struct TokenWalk {
@@ -529,9 +529,15 @@ __global__ void __launch_bounds__(160) token_walk_kernel(const __grid_constant__
         const bool second = R == 2 && (what & 8);        // of the lane's two rows
         if ((what & 4) && (R == 2 || !(l16 & 1)) && i < n) {
           const float4 c = st.c[i][2];
-          // (what the tokens behind this one write has coefficients of zero, but need not be finite: left out, not multiplied)
-          auto from = [&](int t) { return t > (what & 3) ? 0.f : second ? u[R - 1][t] : u[0][t]; };
-          const float o = fmaf(st.c[i][1].z, mine, fmaf(c.x, from(0), fmaf(c.y, from(1), fmaf(c.z, from(2), c.w * from(3)))));
+          // Tokens behind this one have coefficients of zero, but what they write need not be finite: left out, not multiplied.
+          // (As predicated steps it costs nothing; with zeros selected for what they write, 9000 tokens, 36 heads, f32, d = 128 took
+          // 1.87 ms instead of 1.62.)
+          auto from = [&](int t) { return second ? u[R - 1][t] : u[0][t]; };
+          float o = 0.f;
+          if ((what & 3) == 3) o = c.w * from(3);
+          if (what & 2) o = fmaf(c.z, from(2), o);
+          if (what & 3) o = fmaf(c.y, from(1), o);
+          o = fmaf(st.c[i][1].z, mine, fmaf(c.x, from(0), o));
           static_cast<Tio*>(a.out)[(size_t)(start + t0 + i) * a.out_stride + h * D + row0 + r + (second ? 1 : 0)] = from_float<Tio>(o);
         }
       }

@@ -1303,7 +1303,7 @@ TokenPlainLayout make_plain_layout(const vdn_vda_s* h, long long n_tokens, int n
   // where a walk of the whole sequence was.  Microseconds, fitted to graph replays of 1 .. 20 sequences of 256 .. 9000 tokens and
   // 1 .. 36 heads, d = 64 and 128: 0.1 for a token of a walk, 0.0025 (d = 128) for each token and head besides; cut, 0.01
   // (d = 128; 0.0037, d = 64) for each token and head, and 1.7 / 0.85 to join a part.  The length of a part balances its walk with the
-  // joins.  9000 tokens, f32: 1 head 921 us whole, 167 cut (d = 64: 834, 94); 12 heads 1300, 1190 (854, 442); 36 heads 1540,
+  // joins.  9000 tokens, f32: 1 head 921 us whole, 170 cut (d = 64: 834, 94); 12 heads 1320, 1190 (854, 453); 36 heads 1620,
   // 3300; 256 tokens, 2 heads, d = 64: 31, 23.
   // (several sequences: the longest is taken to be twice the average.  8 of 512 tokens, 2 heads, d = 128: 82 us whole, 124 cut;
   // one of them four times the average: 227 whole.)
