@@ -310,7 +310,7 @@ vdn_status vdn_vda_prepare(vdn_vda_t h, const void* q_in, const void* k_in, cons
  *   fp32: against a 64-bit evaluation the state is off by 3e-6 .. 8e-6 of its norm (measured: unit keys, a third of them near
  *   shared directions; 1e-5 where few tokens are left after many resets, 4e-5 with one key throughout and beta = 1), the read-out by
  *   3e-4 at most before its rounding.  All else, and VDN_FLAG_FORCE_SIMT, runs in plain fp32, a few long sequences in parts as
- *   well: 1e-7 .. 6e-7 off.  The choice goes by sizes, so what is packed beside a sequence can change its last bits;
+ *   well: 1e-7 .. 1e-6 off.  The choice goes by sizes, so what is packed beside a sequence can change its last bits;
  *   VDN_FLAG_FORCE_SIMT keeps to plain fp32.
  *   A value that is not finite reaches its token and those after it, in v only its own channel; on the tensor cores the tokens
  *   before it in its chunk of 64 too.

@@ -99,3 +99,24 @@ def test_channels_that_are_not_turned_are_copied(dtype, d, half, pairs, frames):
     nan = x.isnan()
     bits = torch.int32 if dtype == "f32" else torch.int16
     assert torch.equal(got.isnan(), nan) and torch.equal(got[~nan].view(bits), x[~nan].view(bits))
+
+
+@pytest.mark.parametrize("dtype,d,half", [("f32", 64, True), ("bf16", 128, False)])
+@pytest.mark.parametrize("h,hk", [(1, None), (4, 2)])
+def test_given_positions_in_tiles_of_several_tokens(dtype, d, half, h, hk):
+    """Two clips of 1571 tokens, any positions, one pair on no axis, turned and turned back."""
+    B, T, F = 2, 1571, 1
+    n = B * T * F
+    g = torch.Generator().manual_seed(h)
+    q, k = (None if m is None else torch.randn(B, T, F, m, d, generator=g).to(TYPES[dtype]).to(DEV) for m in (h, hk))
+    freq, axis = binding.rotary_tables((8, 8, 8), theta=500.0)
+    axis[9] = 3
+    pos = torch.randint(-200000, 200000, (3, n), generator=g, dtype=torch.int32)
+    vda = binding.Vda(d, dtype)
+    for inverse in (False, True):
+        got = vda.rotate(q, k, freq.to(DEV), axis.to(DEV), positions=pos.to(DEV), half=half, inverse=inverse)
+        for x, y in zip((q, k), got):
+            if x is None:
+                continue
+            want = tok.rotary(x.double().cpu().numpy().reshape(n, -1, d), pos.numpy(), freq.tolist(), axis.tolist(), half, inverse)
+            assert (np.abs(y.double().cpu().numpy().reshape(n, -1, d) - want) <= allowed(dtype, want)).all()
