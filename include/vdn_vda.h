@@ -384,6 +384,86 @@ typedef struct {
 vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void* q_out, void* k_out, int B, int T, int F,
                           int H, int d, const vdn_vda_rotary_params* p, void* cuda_stream);
 
+/* Around the layer in its transformer block: the projections that make q, k, v and take the read-out back (Eq. 1d), in 8-bit floating
+ * point as the paper serves them (Sec. 5, "Other optimizations"), and the attention of the video tokens to an encoder's states.
+ *
+ * Cast to 8 bits (e4m3: 4-bit exponent, 3-bit mantissa, no infinity) with a scale for each block of 128 channels:
+ *      scale_b = the smallest power of two with max |x_b| <= 448 scale_b   (1 for a block of zeros),   x8 = rn(x / scale_b)
+ * Dividing by a power of two is exact; the cast rounds to nearest even.  What is not finite becomes NaN and leaves the scale of its
+ * block to the others.  (scale_b is 2^-126 at least: blocks of magnitudes below 2^-117 lose what that leaves behind.)
+ *   x       [rows, cols] of cfg.io_dtype, DEVICE.  Any alignment of its elements; rows that begin at multiples of 16 bytes are faster.
+ *   x8      [rows, cols], one byte an element, DEVICE, 16-byte aligned.  Bytes between its rows are not written.
+ *   scale   float, DEVICE, dense.  block_rows = 1: [rows, ceil(cols / 128)], a block is 128 channels of a row (activations).
+ *           block_rows = 128: [ceil(rows / 128), ceil(cols / 128)], a block is 128 x 128 (weights).
+ *   x_stride, out_stride   elements from one row to the next, 0 = dense.  x8's is a multiple of 16 (with 0, so is cols).
+ * rows = 0 is no error.  Needs no workspace.  Enqueues on cuda_stream and returns; does not synchronise. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(vdn_vda_quantize_params), checked */
+  int32_t block_rows;        /* 1 or 128 */
+  int64_t x_stride, out_stride;
+} vdn_vda_quantize_params;
+vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, long long rows, long long cols,
+                            const vdn_vda_quantize_params* p, void* cuda_stream);
+
+/* Product of 8-bit (e4m3) operands with a scale for each block of 128, a projection out = a w^T:
+ *      out[m,n] = sum_b a_scale[m,b] w_scale[n/128,b] (sum_{k in block b} a[m,k] w[n,k])  + bias[n] + add[m,n]
+ *   a       [M, K], w [N, K]: one byte an element, DEVICE, 16-byte aligned, rows at multiples of 16 bytes; K need not be one.
+ *   out     [M, N] of cfg.io_dtype, DEVICE, any alignment of its elements (16-byte aligned rows are faster).  May be add, and
+ *           must not alias another input.
+ *   p->a_scale  float [M, ceil(K / 128)], p->w_scale float [ceil(N / 128), ceil(K / 128)]: any values, not only those of vdn_vda_quantize.
+ *   p->bias     float [N] or NULL;   p->add [M, N] of cfg.io_dtype or NULL: Eq. 1d's other branch, or a residual.
+ *   strides     elements from one row to the next, 0 = dense.
+ * Products of 8-bit numbers are exact; a block's sum is formed on the tensor cores, scaled and added to the others in fp32;
+ * bias and add are added in fp32 before the one rounding to io_dtype.  VDN_FLAG_FORCE_SIMT: plain fp32 arithmetic throughout.
+ * M = 0 is no error.  Needs no workspace.  Enqueues on cuda_stream and returns; does not synchronise. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(vdn_vda_matmul_params), checked */
+  uint32_t reserved;         /* 0 */
+  const float* a_scale;
+  const float* w_scale;
+  const float* bias;
+  const void* add;
+  int64_t a_stride, w_stride, add_stride, out_stride;
+} vdn_vda_matmul_params;
+vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void* out, long long M, long long N, long long K,
+                                 const vdn_vda_matmul_params* p, void* cuda_stream);
+
+/* Attention of a batch's queries to an encoder's states, of another length.  Per batch row, query and head, over the keys that count:
+ *      z_j = scale q . k_j,    lse = log sum_j exp(z_j),    out = sum_j exp(z_j - lse) v_j
+ * A row without keys that count gives out = 0 and lse = -infinity.
+ *   q, out  [batch, queries, heads, d] of cfg.io_dtype, DEVICE, 16-byte aligned, d = cfg.d.  out must not alias an input.
+ *   k, v    [batch, keys, key_heads, d]; with p->cu_seqlens packed, [keys, key_heads, d].  Head h reads key head
+ *           h / (heads / key_heads); key_heads divides heads.
+ *   p->cu_seqlens int32 [batch + 1], DEVICE, or NULL: batch row b has the rows cu_seqlens[b] .. cu_seqlens[b+1]-1 of k and v (any
+ *           number, none too).  Offsets beyond the tensor are clamped to it (wrong rows, but no access outside).
+ *   p->lengths int32 [batch], DEVICE, or NULL (not with cu_seqlens): batch row b has its first lengths[b] keys (clamped to 0 .. keys).
+ *   p->mask    uint8 [batch, keys], packed [keys], DEVICE, or NULL: keys with 0 do not count.  Values of keys that do not count may be
+ *           anything, NaN too: they are not read into a result.
+ *   p->lse     float [batch, queries, heads], DEVICE, or NULL.
+ *   p->q_stride, k_stride, v_stride, out_stride   elements from one token to the next (also from the last of a batch row to the first
+ *           of the next), 0 = dense; heads of a token are always dense.  Multiples of 16 bytes.
+ *   workspace  DEVICE, 256-byte aligned, at least vdn_vda_cross_attention_workspace_bytes (0 where none is needed; NULL is fine
+ *           then): long encoders are cut into parts where there are few queries.  An argument and not the handle's, so that
+ *           calls that may overlap, or captured graphs, can each have their own; nothing in it outlives the call.
+ * bf16 runs on the tensor cores (weights exp(z_j - max) rounded to bf16, sums fp32), single tokens in plain fp32, as does f32 and all
+ * with VDN_FLAG_FORCE_SIMT.  Kernels and parts are chosen by sizes alone; lengths stay on the device.
+ * Enqueues on cuda_stream and returns; does not synchronise. */
+typedef struct {
+  uint32_t struct_size;      /* sizeof(vdn_vda_cross_params), checked */
+  int32_t batch, heads, key_heads;
+  float scale;
+  uint32_t reserved;         /* 0 */
+  const int32_t* cu_seqlens;
+  const int32_t* lengths;
+  const uint8_t* mask;
+  float* lse;
+  int64_t q_stride, k_stride, v_stride, out_stride;
+} vdn_vda_cross_params;
+size_t vdn_vda_cross_attention_workspace_bytes(vdn_vda_t h, long long queries, long long keys, const vdn_vda_cross_params* p);
+vdn_status vdn_vda_cross_attention(vdn_vda_t h, const void* q, const void* k, const void* v, void* out, long long queries,
+                                   long long keys, const vdn_vda_cross_params* p, void* workspace, size_t workspace_bytes,
+                                   void* cuda_stream);
+
 /* The same layer for callers whose tensors live in HOST memory (pinned memory recommended; with pageable
  * memory the copies are not asynchronous).  All six tensor pointers are HOST pointers.  The staging buffer is a
  * caller-owned DEVICE buffer of at least vdn_vda_staging_bytes, set beforehand.  The copies in run on an input

@@ -32,6 +32,7 @@ EXPORTS = (
     "vdn_vda_create", "vdn_vda_workspace_bytes", "vdn_vda_set_workspace", "vdn_vda_forward", "vdn_vda_forward_ex",
     "vdn_vda_forward_opt", "vdn_vda_workspace_bytes_opt", "vdn_vda_prepare",
     "vdn_vda_token_scan_workspace_bytes", "vdn_vda_token_scan", "vdn_vda_token_step", "vdn_vda_rotate",
+    "vdn_vda_quantize", "vdn_vda_scaled_matmul", "vdn_vda_cross_attention_workspace_bytes", "vdn_vda_cross_attention",
     "vdn_vda_staging_bytes", "vdn_vda_staging_bytes_opt", "vdn_vda_set_staging", "vdn_vda_forward_host",
     "vdn_vda_forward_host_opt", "vdn_vda_workspace_view",
     "vdn_vda_last_launch_count", "vdn_vda_profile", "vdn_vda_kernel_times", "vdn_vda_scan_static", "vdn_vda_status",
@@ -76,9 +77,31 @@ class VdnRotaryParams(ctypes.Structure):
                 ("k_out_stride", ctypes.c_int64)]
 
 
-# the same two structs as packed bytes (the header's layout, no padding anywhere): a third of the time of filling a Structure
+class VdnQuantizeParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("block_rows", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64)]
+
+
+class VdnMatmulParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("a_scale", ctypes.c_void_p),
+                ("w_scale", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("add", ctypes.c_void_p), ("a_stride", ctypes.c_int64),
+                ("w_stride", ctypes.c_int64), ("add_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+class VdnCrossParams(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("batch", ctypes.c_int32), ("heads", ctypes.c_int32), ("key_heads", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("reserved", ctypes.c_uint32), ("cu_seqlens", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("lse", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64)]
+
+
+# the same structs as packed bytes (the header's layout, no padding anywhere): a third of the time of filling a Structure
 _TOKEN_PARAMS = struct.Struct("=IiiiffQQQQQqqqqq")
 _ROTARY_PARAMS = struct.Struct("=IIiiiiifQQQQQqqqq")
+_QUANTIZE_PARAMS = struct.Struct("=Iiqq")
+_MATMUL_PARAMS = struct.Struct("=IIQQQQqqqq")
+_CROSS_PARAMS = struct.Struct("=IiiifIQQQQqqqq")
+SCALE_BLOCK = 128
 
 
 class VdnError(RuntimeError):
@@ -132,6 +155,14 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     lib.vdn_vda_token_step.restype = ci
     lib.vdn_vda_rotate.argtypes = [vp, vp, vp, vp, vp, *shape, vp, vp]
     lib.vdn_vda_rotate.restype = ci
+    lib.vdn_vda_quantize.argtypes = [vp, vp, vp, vp, i64, i64, vp, vp]
+    lib.vdn_vda_quantize.restype = ci
+    lib.vdn_vda_scaled_matmul.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp]
+    lib.vdn_vda_scaled_matmul.restype = ci
+    lib.vdn_vda_cross_attention_workspace_bytes.argtypes = [vp, i64, i64, vp]
+    lib.vdn_vda_cross_attention_workspace_bytes.restype = sz
+    lib.vdn_vda_cross_attention.argtypes = [vp, vp, vp, vp, vp, i64, i64, vp, vp, sz, vp]
+    lib.vdn_vda_cross_attention.restype = ci
     lib.vdn_vda_forward_host.argtypes = fwd_args
     lib.vdn_vda_forward_host.restype = ci
     lib.vdn_vda_forward_host_opt.argtypes = [vp, vp, vp, vp, vp, vp, vp, *shape, ctypes.POINTER(VdnOptions), vp]
@@ -315,6 +346,97 @@ def validate_token_args(io_dtype, d_handle, device_index, q, k, v, beta, out=Non
     if log_alpha is not None:
         _dense("log_alpha", log_alpha, gates, f32, on_cuda, device_index)
     return lead, H, Hk, strides
+
+
+def _matrix(name, x, shape, dtype, on_cuda, device_index, step_bytes=0):
+    """A tensor [..., columns] taken as rows that may lie apart: the elements of a row dense, one distance between all rows, with
+    step_bytes a multiple of so many bytes.  Returns that distance in elements."""
+    if x is None:
+        raise ValueError(f"{name} is missing")
+    if bool(x.is_cuda) != on_cuda:
+        raise ValueError(f"{name} must be a {'CUDA' if on_cuda else 'host'} tensor")
+    if on_cuda and (x.device.index or 0) != device_index:
+        raise ValueError(f"{name} is on cuda:{x.device.index}, the handle is bound to cuda:{device_index}")
+    if x.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+    if tuple(x.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(x.shape)}")
+    cols, step, n = shape[-1], None, 1
+    ok = cols == 1 or x.stride(-1) == 1
+    if not x.is_contiguous():
+        for size, stride in zip(reversed(shape[:-1]), reversed(x.stride()[:-1])):
+            if size != 1:
+                step = stride if step is None else step
+                ok = ok and stride == step * n
+            n *= size
+    # (a single row has no distance: the next multiple that covers it)
+    only = all(size == 1 for size in shape[:-1]) or x.numel() == 0
+    unit = max(1, step_bytes // x.element_size())
+    step = -(-cols // unit) * unit if only else cols if step is None else step
+    if not ok or step < cols or (step_bytes and (step * x.element_size()) % step_bytes):
+        raise ValueError(f"{name}: the elements of a row must be contiguous and its rows evenly spaced"
+                         + (f", by a multiple of {step_bytes} bytes" if step_bytes else ""))
+    return step
+
+
+def validate_matmul_args(io_dtype, device_index, a, a_scale, w, w_scale, bias=None, add=None, out=None, on_cuda=True):
+    """Checks the tensors of scaled_matmul: a [..., K], w [N, K] (float8_e4m3fn), a_scale [..., blocks], w_scale [.., blocks], bias [N],
+    add and out [..., N].  Returns (M, N, K, strides of a, w, add, out)."""
+    import torch
+    if a is None or a.dim() < 1 or w is None or w.dim() != 2:
+        raise ValueError("a must have shape [..., K] and w [N, K]")
+    lead, k, n = tuple(a.shape[:-1]), a.shape[-1], w.shape[0]
+    blocks = -(-k // SCALE_BLOCK)
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    sa = _matrix("a", a, (*lead, k), e4m3, on_cuda, device_index, 16)
+    sw = _matrix("w", w, (n, k), e4m3, on_cuda, device_index, 16)
+    _dense("a_scale", a_scale, (*lead, blocks), f32, on_cuda, device_index)
+    _dense("w_scale", w_scale, (-(-n // SCALE_BLOCK), blocks), f32, on_cuda, device_index)
+    if bias is not None:
+        _dense("bias", bias, (n,), f32, on_cuda, device_index)
+    sd = 0 if add is None else _matrix("add", add, (*lead, n), io_dtype, on_cuda, device_index)
+    so = n if out is None else _matrix("out", out, (*lead, n), io_dtype, on_cuda, device_index)
+    m = 1
+    for x in lead:
+        m *= x
+    return m, n, k, (sa, sw, sd, so)
+
+
+def validate_cross_args(io_dtype, d_handle, device_index, q, k, v, cu_seqlens=None, lengths=None, mask=None, out=None, lse=None,
+                        on_cuda=True):
+    """Checks the tensors of cross_attention: q, out [B, ..., H, d], k, v [B, Lk, Hk, d] or, with cu_seqlens [B + 1], packed [N, Hk, d];
+    lengths [B], mask [B, Lk] or [N], lse [B, ..., H].  Returns (B, queries, keys, H, Hk, strides of q, k, v, out)."""
+    import torch
+    if q is None or q.dim() < 3:
+        raise ValueError("q must have shape [batch, ..., heads, d]")
+    packed = cu_seqlens is not None
+    if k is None or k.dim() != (3 if packed else 4):
+        raise ValueError("k must have shape " + ("[keys, key_heads, d] with cu_seqlens" if packed else "[batch, keys, key_heads, d]"))
+    qs, ks = tuple(q.shape), tuple(k.shape)
+    B, H, d, Hk = qs[0], qs[-2], qs[-1], ks[-2]
+    if d != d_handle:
+        raise ValueError(f"q must have head dimension {d_handle}, got {d}")
+    if H == 0 or Hk == 0 or H % Hk:
+        raise ValueError(f"k must have a number of heads that divides the {H} of q, got {Hk}")
+    lead = ks[:1] if packed else (B, ks[1])
+    ks = (*lead, Hk, d)
+    strides = (_rows("q", q, qs, io_dtype, on_cuda, device_index), _rows("k", k, ks, io_dtype, on_cuda, device_index),
+               _rows("v", v, ks, io_dtype, on_cuda, device_index),
+               H * d if out is None else _rows("out", out, qs, io_dtype, on_cuda, device_index))
+    if packed:
+        _dense("cu_seqlens", cu_seqlens, (B + 1,), torch.int32, on_cuda, device_index)
+        if lengths is not None:
+            raise ValueError("lengths belong to keys that are not packed")
+    if lengths is not None:
+        _dense("lengths", lengths, (B,), torch.int32, on_cuda, device_index)
+    if mask is not None:
+        _dense("mask", mask, lead, torch.bool, on_cuda, device_index)
+    if lse is not None:
+        _dense("lse", lse, qs[:-1], torch.float32, on_cuda, device_index)
+    n = 1
+    for x in qs[1:-2]:
+        n *= x
+    return B, n, lead[-1], H, Hk, strides
 
 
 def _float32():
@@ -622,6 +744,85 @@ class Vda:
         if r:
             self._check(r)
         return qo, ko
+
+    # -- around the layer: 8-bit projections, attention to an encoder's states ------------------
+    def quantize(self, x, rows=1, out=None, scale=None, stream=None):
+        """vdn_vda_quantize: x [..., K] to (x8 [..., K] float8_e4m3fn, scale), a power of two for each block of 128 channels.
+
+        rows = 1: a block is 128 channels of a row, scale [..., ceil(K/128)] (activations); rows = 128: 128 x 128 of x [N, K],
+        scale [ceil(N/128), ceil(K/128)] (weights).  Rows of a fresh x8 begin at multiples of 16 bytes, as scaled_matmul wants them.
+        """
+        torch, dev = self._torch, self.device
+        if rows not in (1, SCALE_BLOCK):
+            raise ValueError("rows must be 1 or 128")
+        if x is None or x.dim() < 1 or (rows != 1 and x.dim() != 2):
+            raise ValueError("x must have shape " + ("[..., K]" if rows == 1 else "[N, K]"))
+        shape = tuple(x.shape)
+        k = shape[-1]
+        xs = _matrix("x", x, shape, self.torch_dtype, True, dev)
+        n = 1
+        for s in shape[:-1]:
+            n *= s
+        blocks = -(-k // SCALE_BLOCK)
+        streams = self._streams(stream)
+        pitch = -(-k // 16) * 16
+        if out is None:
+            out = self._new(streams, (*shape[:-1], pitch), torch.float8_e4m3fn)
+            if pitch != k:
+                out = out[..., :k]
+        else:
+            pitch = _matrix("out", out, shape, torch.float8_e4m3fn, True, dev, 16)
+        want = (*shape[:-1], blocks) if rows == 1 else (-(-n // SCALE_BLOCK), blocks)
+        if scale is None:
+            scale = self._new(streams, want, torch.float32)
+        else:
+            _dense("scale", scale, want, torch.float32, True, dev)
+        prm = _QUANTIZE_PARAMS.pack(_QUANTIZE_PARAMS.size, rows, xs, pitch)
+        r = self.lib.vdn_vda_quantize(self.h, x.data_ptr(), out.data_ptr(), scale.data_ptr(), n, k, prm, streams[0])
+        if r:
+            self._check(r)
+        return out, scale
+
+    def scaled_matmul(self, a, a_scale, w, w_scale, bias=None, add=None, out=None, stream=None):
+        """vdn_vda_scaled_matmul: a w^T + bias + add of 8-bit operands with a scale for each block of 128; [..., N] in the handle's type.
+
+        a [..., K] and w [N, K] float8_e4m3fn, rows at multiples of 16 bytes (quantize makes them so); a_scale [..., ceil(K/128)],
+        w_scale [ceil(N/128), ceil(K/128)], bias [N] (float); add [..., N] in the handle's type, `out` may be `add`.
+        """
+        m, n, k, st = validate_matmul_args(self.torch_dtype, self.device, a, a_scale, w, w_scale, bias, add, out)
+        streams = self._streams(stream)
+        if out is None:
+            out = self._new(streams, (*a.shape[:-1], n), self.torch_dtype)
+        prm = _MATMUL_PARAMS.pack(_MATMUL_PARAMS.size, 0, a_scale.data_ptr(), w_scale.data_ptr(), _ptr(bias), _ptr(add), *st)
+        r = self.lib.vdn_vda_scaled_matmul(self.h, a.data_ptr(), w.data_ptr(), out.data_ptr(), m, n, k, prm, streams[0])
+        if r:
+            self._check(r)
+        return out
+
+    def cross_attention(self, q, k, v, cu_seqlens=None, lengths=None, mask=None, scale=None, out=None, lse=False, stream=None):
+        """vdn_vda_cross_attention: softmax(scale q k^T) v of q [B, ..., H, d] over an encoder's states k, v [B, Lk, Hk, d].
+
+        lengths int32 [B]: keys of each batch row (None: Lk); or cu_seqlens int32 [B + 1] with k, v packed [N, Hk, d]; mask bool
+        [B, Lk] or [N]: False keys do not count, whatever they hold.  scale: None is d ** -0.5.  lse: True, or a float tensor
+        [B, ..., H], returns (out, lse), the logarithm of the sum of exponentials (-inf, and out = 0, for a row without keys).
+        """
+        dev = self.device
+        given = lse if hasattr(lse, "data_ptr") else None
+        B, n, keys, H, Hk, st = validate_cross_args(self.torch_dtype, self.d, dev, q, k, v, cu_seqlens, lengths, mask, out, given)
+        streams = self._streams(stream)
+        if out is None:
+            out = self._new_like(streams, q)
+        if given is None and lse:
+            given = self._new(streams, q.shape[:-1], self._torch.float32)
+        prm = _CROSS_PARAMS.pack(_CROSS_PARAMS.size, B, H, Hk, self.d ** -0.5 if scale is None else scale, 0, _ptr(cu_seqlens),
+                                 _ptr(lengths), _ptr(mask), _ptr(given), *st)
+        need = self.lib.vdn_vda_cross_attention_workspace_bytes(self.h, n, keys, prm)
+        ws = self._new(streams, (need,), self._torch.uint8) if need else None
+        r = self.lib.vdn_vda_cross_attention(self.h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), n, keys, prm,
+                                             _ptr(ws), need, streams[0])
+        if r:
+            self._check(r)
+        return out if given is None else (out, given)
 
     def forward_host(self, q, k, v, beta, gate, out, stream=None, alpha=None, s0=None, chunk=1, radius=0,
                      anchors=False, gate_elem=None, norm_weight=None, q_l2_eps=0.0):

@@ -91,6 +91,14 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = raw;
 }
 
+// 2^x, two units in the last place.  Arguments are at most a little above zero where this is used, and below -126 the result does
+// not matter.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // 16-byte asynchronous global->shared copy (LDGSTS) and its group fences.
 __device__ __forceinline__ void cp_async16(void* smem_dst, const void* gmem_src) {
   uint32_t s = (uint32_t)__cvta_generic_to_shared(smem_dst);

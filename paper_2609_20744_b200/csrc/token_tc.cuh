@@ -206,13 +206,6 @@ __device__ __forceinline__ void tile_store(float* D, int pd, float sign, const f
   *reinterpret_cast<float2*>(D + (g + 8) * pd + 2 * t) = make_float2(sign * c[2], sign * c[3]);
 }
 
-// 2^x.  Its argument is at most a little above zero here, and below -126 the result does not matter.
-__device__ __forceinline__ float exp2_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
 __global__ void __launch_bounds__(TokenPrep::THREADS, TokenPrep::CTAS)
 token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmQ, const TokenTcArgs a,
                   tc::DevStatus ds) {

@@ -6,6 +6,7 @@
 #include <cudaTypedefs.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstdio>
@@ -17,9 +18,12 @@
 #include <utility>
 
 #include "common.cuh"
+#include "cross_simt.cuh"
 #include "gram_simt.cuh"
 #include "gram_tc.cuh"
+#include "matmul_simt.cuh"
 #include "prep.cuh"
+#include "quantize.cuh"
 #include "readout_simt.cuh"
 #include "readout_tc.cuh"
 #include "resolve.cuh"
@@ -1667,6 +1671,258 @@ vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void*
   h->launches = 1;
   VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------------
+// Around the layer: casts to 8 bits, block-scaled products, attention to an encoder's states.
+
+namespace {
+
+int scale_blocks(long long n) { return (int)((n + vdn::kScaleBlock - 1) / vdn::kScaleBlock); }
+
+// Rows of single elements (no token heads): a stride covers the row.
+bool row_stride_ok(int64_t stride, long long dense) { return stride == 0 || (stride >= dense && stride <= (1LL << 40)); }
+
+bool rows_aligned16(const void* p, long long stride, long long rows, size_t es) {
+  return aligned16(p) && (rows <= 1 || (stride * (long long)es) % 16 == 0);
+}
+
+template <typename Tio, bool WIDE>
+void launch_quantize(const vdn::QuantizeArgs& a, int block_rows, cudaStream_t st) {
+  if (block_rows == 1) {
+    constexpr int per_cta = 4 * 256 / (vdn::kScaleBlock * (int)sizeof(Tio) / 16);
+    vdn::quantize_rows_kernel<Tio, WIDE><<<(a.items + per_cta - 1) / per_cta, 256, 0, st>>>(a);
+  } else {
+    vdn::quantize_square_kernel<Tio, WIDE><<<(unsigned)(scale_blocks(a.rows) * (long long)a.col_blocks), 512, 0, st>>>(a);
+  }
+}
+
+// What vdn_vda_cross_attention and its workspace query ask of their sizes; fills the kernel's arguments but for the tensors.
+vdn_status plan_cross(vdn_vda_t h, long long queries, long long keys, const vdn_vda_cross_params* p, vdn::CrossArgs& a) {
+  if (!p || p->struct_size != sizeof(vdn_vda_cross_params))
+    return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_cross_params missing or of the wrong struct_size");
+  if (p->reserved) return fail(h, VDN_ERR_INVALID_ARG, "reserved must be 0");
+  if (p->batch < 0 || queries < 0 || keys < 0) return fail(h, VDN_ERR_INVALID_ARG, "batch, queries and keys must not be negative");
+  if (p->heads <= 0 || p->key_heads <= 0 || p->heads % p->key_heads != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "key_heads must divide heads");
+  if (p->heads > 65535) return fail(h, VDN_ERR_UNSUPPORTED, "more than 65535 heads");
+  if (p->cu_seqlens && p->lengths) return fail(h, VDN_ERR_INVALID_ARG, "lengths belong to keys that are not packed");
+  const long long most = 1LL << 30;
+  if (queries > most || keys > most || p->batch * queries > most || (!p->cu_seqlens && p->batch * keys > most))
+    return fail(h, VDN_ERR_INVALID_ARG, "more than 2^30 query or key tokens");
+  if (queries * (p->heads / p->key_heads) > most) return fail(h, VDN_ERR_UNSUPPORTED, "more than 2^30 rows of a key head");
+  if (!std::isfinite(p->scale)) return fail(h, VDN_ERR_INVALID_ARG, "scale must be finite");
+  a = vdn::CrossArgs{};
+  a.B = p->batch; a.Lq = (int)queries; a.H = p->heads; a.Hk = p->key_heads; a.group = p->heads / p->key_heads;
+  a.Lk = p->cu_seqlens ? 0 : keys;
+  a.n_keys = p->cu_seqlens ? keys : p->batch * keys;
+  a.scale_log2 = p->scale * 1.4426950408889634f;
+  return VDN_OK;
+}
+
+// How a call runs: on which kernel, and in how many parts of the keys.
+struct CrossLayout {
+  int rows;                 // rows of a CTA's tile; up to 8: cross_few, 64: cross_plain
+  long long units;          // (batch row, key head, row tile)
+  int parts;
+  size_t o, ml, total;
+};
+CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
+  CrossLayout L = {};
+  L.parts = 1;
+  if (a.B == 0 || a.Lq == 0) return L;
+  const long long rows = (long long)a.Lq * a.group;
+  L.rows = rows <= 8 ? (rows <= 2 ? (int)rows : rows <= 4 ? 4 : 8) : vdn::CrossPlain<64>::ROWS;
+  L.units = (long long)a.B * a.Hk * ((rows + L.rows - 1) / L.rows);
+  // keys of a batch row, by which parts are chosen (packed: the average)
+  const long long keys = a.Lk ? a.Lk : a.n_keys / a.B;
+  const long long least = 128;                          // keys of a part
+  const long long wanted = (L.rows <= 8 ? 4LL : 2LL) * h->sm_count / L.units;
+  L.parts = (int)std::max(1LL, std::min({wanted, keys / least, 256LL}));
+  if (L.parts > 1) {
+    const size_t n = (size_t)a.B * a.Lq * a.H * L.parts;
+    L.o = 0;
+    L.ml = align_up(n * h->cfg.d * sizeof(float));
+    L.total = L.ml + align_up(n * sizeof(float2));
+  }
+  return L;
+}
+
+template <typename Tio, int D>
+vdn_status launch_cross_simt(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout& L, cudaStream_t st) {
+  const unsigned grid = (unsigned)(L.units * L.parts);
+  switch (L.rows) {
+    case 1: vdn::cross_few_kernel<Tio, D, 1><<<grid, 256, 0, st>>>(a); break;
+    case 2: vdn::cross_few_kernel<Tio, D, 2><<<grid, 256, 0, st>>>(a); break;
+    case 4: vdn::cross_few_kernel<Tio, D, 4><<<grid, 256, 0, st>>>(a); break;
+    case 8: vdn::cross_few_kernel<Tio, D, 8><<<grid, 256, 0, st>>>(a); break;
+    default:
+      VDN_CUDA(h, (cudaFuncSetAttribute(vdn::cross_plain_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        vdn::CrossPlain<D>::SMEM_BYTES)));
+      vdn::cross_plain_kernel<Tio, D><<<grid, 256, vdn::CrossPlain<D>::SMEM_BYTES, st>>>(a);
+  }
+  return VDN_OK;
+}
+
+template <typename Tio, int D>
+vdn_status launch_cross(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout& L, cudaStream_t st) {
+  prof_begin(h, st);
+  vdn_status r = launch_cross_simt<Tio, D>(h, a, L, st);
+  if (r != VDN_OK) return r;
+  prof_mark(h, st, 0, L.rows <= 8 ? "cross_few" : "cross_plain");
+  h->launches = 1;
+  if (L.parts > 1) {
+    const long long rows = (long long)a.B * a.Lq * a.H;
+    vdn::cross_join_kernel<Tio, D><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(a);
+    prof_mark(h, st, 1, "cross_join");
+    h->launches = 2;
+  }
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, long long rows, long long cols,
+                            const vdn_vda_quantize_params* p, void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  if (!p || p->struct_size != sizeof(vdn_vda_quantize_params))
+    return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_quantize_params missing or of the wrong struct_size");
+  if (p->block_rows != 1 && p->block_rows != vdn::kScaleBlock) return fail(h, VDN_ERR_INVALID_ARG, "block_rows must be 1 or 128");
+  if (rows < 0 || cols <= 0 || rows > (1LL << 30) || cols > (1LL << 30))
+    return fail(h, VDN_ERR_INVALID_ARG, "rows must lie between 0 and 2^30, cols between 1 and 2^30");
+  if (rows > 0 && (!x || !x8 || !scale)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
+  if (rows > 0 && x == x8) return fail(h, VDN_ERR_INVALID_ARG, "x8 must not alias x");
+  const size_t es = elem_size(h);
+  if (reinterpret_cast<uintptr_t>(x) % es != 0 || reinterpret_cast<uintptr_t>(scale) % sizeof(float) != 0 || !aligned16(x8))
+    return fail(h, VDN_ERR_INVALID_ARG, "x8 must be 16-byte aligned, x and scale aligned to their elements");
+  const long long out_stride = p->out_stride ? p->out_stride : cols;
+  if (!row_stride_ok(p->x_stride, cols) || !row_stride_ok(p->out_stride, cols) || out_stride % 16 != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "row strides must cover a row, that of x8 a multiple of 16");
+  vdn::QuantizeArgs a = {};
+  a.x = x; a.x8 = static_cast<uint8_t*>(x8); a.scale = scale;
+  a.rows = rows; a.cols = (int)cols;
+  a.x_stride = p->x_stride ? p->x_stride : cols;
+  a.out_stride = out_stride;
+  a.col_blocks = scale_blocks(cols);
+  const long long items = p->block_rows == 1 ? rows * a.col_blocks : (long long)scale_blocks(rows) * a.col_blocks;
+  if (items > 0x7fffffffLL) return fail(h, VDN_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks in one call");
+  a.items = (uint32_t)items;
+  a.per_row = vdn::fast_divide((uint32_t)a.col_blocks);
+  if (rows == 0) { h->launches = 0; return VDN_OK; }
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool wide = rows_aligned16(x, a.x_stride, rows, es);
+  prof_begin(h, st);
+  if (h->cfg.io_dtype == VDN_F32) {
+    if (wide) launch_quantize<float, true>(a, p->block_rows, st);
+    else launch_quantize<float, false>(a, p->block_rows, st);
+  } else {
+    if (wide) launch_quantize<__nv_bfloat16, true>(a, p->block_rows, st);
+    else launch_quantize<__nv_bfloat16, false>(a, p->block_rows, st);
+  }
+  prof_mark(h, st, 0, "quantize");
+  h->launches = 1;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
+vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void* out, long long M, long long N, long long K,
+                                 const vdn_vda_matmul_params* p, void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  if (!p || p->struct_size != sizeof(vdn_vda_matmul_params))
+    return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_matmul_params missing or of the wrong struct_size");
+  if (p->reserved) return fail(h, VDN_ERR_INVALID_ARG, "reserved must be 0");
+  if (M < 0 || M > (1LL << 30) || N <= 0 || K <= 0 || N > (1 << 22) || K > (1 << 22))
+    return fail(h, VDN_ERR_INVALID_ARG, "M must lie between 0 and 2^30, N and K between 1 and 2^22");
+  if (M > 0 && (!a || !w || !out || !p->a_scale || !p->w_scale)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
+  if (M > 0 && (out == a || out == w || out == p->a_scale || out == p->w_scale || out == p->bias))
+    return fail(h, VDN_ERR_INVALID_ARG, "out may only alias add");
+  const size_t es = elem_size(h);
+  if (!aligned16(a) || !aligned16(w)) return fail(h, VDN_ERR_INVALID_ARG, "a and w must be 16-byte aligned");
+  for (const void* x : {(const void*)p->a_scale, (const void*)p->w_scale, (const void*)p->bias})
+    if (reinterpret_cast<uintptr_t>(x) % sizeof(float) != 0) return fail(h, VDN_ERR_INVALID_ARG, "scales and bias must be aligned to their elements");
+  if (reinterpret_cast<uintptr_t>(out) % es != 0 || reinterpret_cast<uintptr_t>(p->add) % es != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "out and add must be aligned to their elements");
+  vdn::MatmulArgs g = {};
+  g.a = static_cast<const uint8_t*>(a); g.w = static_cast<const uint8_t*>(w); g.out = out;
+  g.a_scale = p->a_scale; g.w_scale = p->w_scale; g.bias = p->bias; g.add = p->add;
+  g.M = M; g.N = (int)N; g.K = (int)K; g.blocks = scale_blocks(K);
+  g.a_stride = p->a_stride ? p->a_stride : K;
+  g.w_stride = p->w_stride ? p->w_stride : K;
+  g.add_stride = p->add_stride ? p->add_stride : N;
+  g.out_stride = p->out_stride ? p->out_stride : N;
+  if (!row_stride_ok(p->a_stride, K) || !row_stride_ok(p->w_stride, K) || g.a_stride % 16 != 0 || g.w_stride % 16 != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "rows of a and w must cover K and begin at multiples of 16 bytes");
+  if (!row_stride_ok(p->add_stride, N) || !row_stride_ok(p->out_stride, N))
+    return fail(h, VDN_ERR_INVALID_ARG, "rows of out and add must cover N");
+  if (out == p->add && g.add_stride != g.out_stride)
+    return fail(h, VDN_ERR_INVALID_ARG, "in place, out and add need the same stride");
+  if (M == 0) { h->launches = 0; return VDN_OK; }
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  prof_begin(h, st);
+  const dim3 grid((unsigned)((M + 63) / 64), (unsigned)((N + 63) / 64));
+  if (h->cfg.io_dtype == VDN_F32) vdn::matmul_simt_kernel<float><<<grid, 256, 0, st>>>(g);
+  else vdn::matmul_simt_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(g);
+  prof_mark(h, st, 0, "matmul_simt");
+  h->launches = 1;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
+size_t vdn_vda_cross_attention_workspace_bytes(vdn_vda_t h, long long queries, long long keys, const vdn_vda_cross_params* p) {
+  vdn::CrossArgs a;
+  if (!h || plan_cross(h, queries, keys, p, a) != VDN_OK) return 0;
+  return make_cross_layout(h, a).total;
+}
+
+vdn_status vdn_vda_cross_attention(vdn_vda_t h, const void* q, const void* k, const void* v, void* out, long long queries,
+                                   long long keys, const vdn_vda_cross_params* p, void* workspace, size_t workspace_bytes,
+                                   void* cuda_stream) {
+  if (!h) return VDN_ERR_INVALID_ARG;
+  vdn::CrossArgs a;
+  vdn_status r = plan_cross(h, queries, keys, p, a);
+  if (r != VDN_OK) return r;
+  const bool some = a.B > 0 && a.Lq > 0;
+  if (some && (!q || !out || (a.n_keys > 0 && (!k || !v)))) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
+    return fail(h, VDN_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+  if (out && (out == q || out == k || out == v || out == p->mask)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias an input");
+  const size_t es = elem_size(h);
+  const long long dq = (long long)a.H * h->cfg.d, dk = (long long)a.Hk * h->cfg.d;
+  if (!stride_ok(p->q_stride, dq, es) || !stride_ok(p->k_stride, dk, es) || !stride_ok(p->v_stride, dk, es) ||
+      !stride_ok(p->out_stride, dq, es))
+    return fail(h, VDN_ERR_INVALID_ARG, "token strides must cover a token's heads and be multiples of 16 bytes");
+  a.q = q; a.k = k; a.v = v; a.out = out;
+  a.lse = p->lse; a.cu_seqlens = p->cu_seqlens; a.lengths = p->lengths; a.mask = p->mask;
+  a.q_stride = p->q_stride ? p->q_stride : dq;
+  a.k_stride = p->k_stride ? p->k_stride : dk;
+  a.v_stride = p->v_stride ? p->v_stride : dk;
+  a.out_stride = p->out_stride ? p->out_stride : dq;
+  const CrossLayout L = make_cross_layout(h, a);
+  if (L.total && (!workspace || workspace_bytes < L.total))
+    return fail(h, VDN_ERR_WORKSPACE, "workspace missing or smaller than vdn_vda_cross_attention_workspace_bytes");
+  if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
+    return fail(h, VDN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
+  if (L.units * L.parts > 0x7fffffffLL || (long long)a.B * a.Lq * a.H / 8 >= 0x7fffffffLL)
+    return fail(h, VDN_ERR_UNSUPPORTED, "too many (query, head) pairs for one call");
+  if (!some) { h->launches = 0; return VDN_OK; }
+  a.parts = L.parts;
+  a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + L.o);
+  a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + L.ml);
+  DeviceGuard guard(h->cfg.device);
+  if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const int d = h->cfg.d;
+  if (h->cfg.io_dtype == VDN_F32) return d == 64 ? launch_cross<float, 64>(h, a, L, st) : launch_cross<float, 128>(h, a, L, st);
+  return d == 64 ? launch_cross<__nv_bfloat16, 64>(h, a, L, st) : launch_cross<__nv_bfloat16, 128>(h, a, L, st);
 }
 
 }  // extern "C"
