@@ -1,0 +1,400 @@
+// Block-scaled 8-bit product on the tensor cores.
+//   out[m, n] = sum_b sa[m, b] sw[n / 128, b] sum_{k in block b} a[m, k] w[n, k]  + bias[n] + add[m, n]
+// The scales are any fp32 numbers, so a block's sum (128 channels: four instructions of 32) leaves tensor memory, is multiplied by
+// its scale and added to the others in fp32 registers, while the next block's sum is formed in another accumulator.
+#pragma once
+#include "matmul_simt.cuh"
+#include "tc_common.cuh"
+#include "token_rule.cuh"
+
+namespace vdn {
+
+// ---------------------------------------------------------------------------------------------- large
+// 256 x 256 outputs to a pair of CTAs (128 rows in either's tensor memory), persistent.  Per block of channels a CTA fetches 128 rows of
+// a and 128 of w (32 KB); one CTA alone would need 48 KB for as much work, more than L2 gives 148 SMs at the tensor
+// cores' rate.  Warps 0-7 take the block sums out, a thread a row and 128 of the 256 columns, and write the tile;
+// warp 8 issues the copies, warp 9 (of the even CTA) the products.  Registers: 384 threads start with 168 each; the four warps that
+// copy and issue keep 40, the eight others get 232 (128 of them sums): 256 * 232 + 128 * 40 = 384 * 168.
+struct MatmulPair {
+  static constexpr int ROWS = 128, COLS = 256, STAGES = 5, THREADS = 384;
+  static constexpr int A_BYTES = ROWS * 128, STAGE_BYTES = A_BYTES + COLS / 2 * 128;
+  static constexpr int OUT_BYTES = 32 * 128;                       // one warp's rows, 128 bytes of each
+  static constexpr int OFF_OUT = STAGES * STAGE_BYTES, OFF_BAR = OFF_OUT + 8 * 2 * OUT_BYTES;
+  static constexpr int USED_BYTES = OFF_BAR + 8 * (2 * STAGES + 4) + 16;
+  static constexpr int SMEM_BYTES = USED_BYTES + 1024;
+};
+static_assert(MatmulPair::SMEM_BYTES <= 232448, "shared memory of a CTA");
+
+__device__ __forceinline__ uint32_t bf16_word(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+// bias and add of columns n .. n+31 (of N) of row m.
+template <typename Tio>
+__device__ __forceinline__ void add_rest(const MatmulArgs& p, long long m, int n, bool add_wide, float (&x)[32]) {
+  if (p.bias) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) x[i] += n + i < p.N ? __ldg(p.bias + n + i) : 0.f;
+  }
+  if (p.add && m < p.M) {
+    const Tio* r = static_cast<const Tio*>(p.add) + m * p.add_stride + n;
+    if (add_wide && n + 32 <= p.N) {
+#pragma unroll
+      for (int i = 0; i < 32; i += 16 / (int)sizeof(Tio)) {
+#pragma unroll
+        for (int j = 0; j < 16 / (int)sizeof(Tio); j += 4) {
+          const float4 y = load4(r + i + j);
+          x[i + j] += y.x; x[i + j + 1] += y.y; x[i + j + 2] += y.z; x[i + j + 3] += y.w;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (n + i < p.N) x[i] += to_float(r[i]);
+    }
+  }
+}
+
+template <typename Tio>
+__global__ void __launch_bounds__(MatmulPair::THREADS, 1) __cluster_dims__(2, 1, 1)
+matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                   const __grid_constant__ CUtensorMap tmOut, const MatmulArgs p, const int out_tma, const int add_wide, tc::DevStatus ds) {
+  using namespace tc;
+  using G = MatmulPair;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  const uint32_t bar0 = base + G::OFF_BAR;
+  auto FULL = [&](int i) { return bar0 + 8u * i; };
+  auto EMPTY = [&](int i) { return bar0 + 8u * (G::STAGES + i); };
+  auto ACCFULL = [&](int i) { return bar0 + 8u * (2 * G::STAGES + i); };
+  auto ACCEMPTY = [&](int i) { return bar0 + 8u * (2 * G::STAGES + 2 + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * (2 * G::STAGES + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const WaitCtx wc(abort_flag, ds);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < G::STAGES; ++i) { mbar_init(FULL(i), 1); mbar_init(EMPTY(i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(ACCFULL(i), 1); mbar_init(ACCEMPTY(i), 16); }   // a warp an arrival, of both CTAs
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmW);
+  }
+  if (warp == 9) {
+    tmem_alloc_pair(smem_u32(tmem_slot), 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  const int tiles_n = (p.N + G::COLS - 1) / G::COLS;
+  const long long tiles = (p.M + 2 * G::ROWS - 1) / (2 * G::ROWS) * tiles_n;
+  const long long first = blockIdx.x / 2, step = gridDim.x / 2;
+
+  if (warp >= 8) {
+    registers_fewer<40>();
+    if (warp == 8) {
+      if (lane == 0) {
+        uint32_t it = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += step) {
+          const int m0 = (int)(t / tiles_n) * 2 * G::ROWS + (int)rank * G::ROWS;
+          const int n0 = (int)(t % tiles_n) * G::COLS + (int)rank * (G::COLS / 2);
+          for (int b = 0; b < p.blocks; ++b, ++it) {
+            const int st = it % G::STAGES;
+            if (!mbar_wait(EMPTY(st), ((it / G::STAGES) & 1) ^ 1, wc)) { ok = false; break; }
+            if (rank == 0) mbar_arrive_expect_tx(FULL(st), 2 * G::STAGE_BYTES);
+            const uint32_t dst = base + st * G::STAGE_BYTES, bar = rank_address(FULL(st), 0);
+            tma_load_2d_pair(dst, &tmA, bar, b * kScaleBlock, m0);
+            tma_load_2d_pair(dst + G::A_BYTES, &tmW, bar, b * kScaleBlock, n0);
+          }
+        }
+        // (the even CTA's barriers count the copies of both; the odd one leaves with it, at the cluster's barrier)
+        if (!ok && rank == 0) mbar_drain_ring(FULL(0), G::STAGES, it);
+      }
+    } else if (warp == 9) {
+      if (lane == 0 && rank == 0) {
+        constexpr uint32_t idesc = make_idesc_e4m3(2 * G::ROWS, G::COLS);
+        uint32_t it = 0;
+        bool ok = true;
+        for (long long t = first; t < tiles && ok; t += step) {
+          for (int b = 0; b < p.blocks; ++b, ++it) {
+            const int st = it % G::STAGES, a = it & 1;
+            if (!mbar_wait(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) || !mbar_wait(FULL(st), (it / G::STAGES) & 1, wc)) { ok = false; break; }
+            tc_fence_after_sync();
+            const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
+            const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES + G::A_BYTES, 16, 1024);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) mma_e4m3_pair(tmem + a * G::COLS, da + k * 2, dw + k * 2, idesc, k ? 1u : 0u);
+            mma_commit_pair(EMPTY(st));
+            mma_commit_pair(ACCFULL(a));
+          }
+        }
+      }
+    }
+  } else {
+    registers_more<232>();
+    const int qd = warp & 3, half = warp >> 2;
+    const uint32_t taddr = tmem + ((uint32_t)(qd * 32) << 16) + half * 128;
+    const uint32_t out_smem = base + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
+    unsigned char* out_ptr = base_ptr + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
+    uint32_t it = 0, slot = 0;
+    bool ok = true;
+    for (long long t = first; t < tiles && ok; t += step) {
+      const long long m = (t / tiles_n) * 2 * G::ROWS + rank * G::ROWS + qd * 32 + lane;
+      const int n0 = (int)(t % tiles_n) * G::COLS + half * 128;
+      const bool inside = m < p.M && n0 < p.N;
+      const float* sa = p.a_scale + (inside ? m * p.blocks : 0);
+      const float* sw = p.w_scale + (inside ? (long long)(n0 / kScaleBlock) * p.blocks : 0);
+      uint64_t acc[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i) acc[i] = 0ull;
+      float s = __ldg(sa) * __ldg(sw);
+      for (int b = 0; b < p.blocks; ++b, ++it) {
+        const int a = it & 1;
+        const uint64_t s2 = f2_pack(s, s);
+        if (b + 1 < p.blocks) s = __ldg(sa + b + 1) * __ldg(sw + b + 1);
+        if (!mbar_wait(ACCFULL(a), (it >> 1) & 1, wc)) { ok = false; break; }
+        tc_fence_after_sync();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          tmem_ld32(taddr + a * G::COLS + c * 32, v);
+          tmem_wait_ld();
+          if (c == 3) {
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(rank_address(ACCEMPTY(a), 0));
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c * 16 + i] = f2_fma(f2_pack(v[2 * i], v[2 * i + 1]), s2, acc[c * 16 + i]);
+        }
+      }
+      if (!ok) break;
+      // the tile: this warp's 32 rows, 128 bytes of each at a time through shared memory (16-byte pieces turned by the row, as the
+      // copy's swizzle has them), so that whole lines leave
+      constexpr int PER = 128 / (int)sizeof(Tio);
+#pragma unroll
+      for (int c = 0; c < 128 / PER; ++c, slot ^= 1) {
+        tma_store_wait_read<1>();                       // (only lane 0 has any) the store that last read this buffer
+        __syncwarp();
+        unsigned char* row = out_ptr + slot * G::OUT_BYTES + lane * 128;
+#pragma unroll
+        for (int g = 0; g < PER / 32; ++g) {
+          float x[32];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) f2_unpack(acc[(c * PER + g * 32) / 2 + i], x[2 * i], x[2 * i + 1]);
+          add_rest<Tio>(p, m, n0 + c * PER + g * 32, add_wide, x);
+          if constexpr (sizeof(Tio) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) *reinterpret_cast<float4*>(row + ((i ^ (lane & 7)) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<uint4*>(row + (((g * 4 + i) ^ (lane & 7)) * 16)) =
+                  make_uint4(bf16_word(x[8 * i], x[8 * i + 1]), bf16_word(x[8 * i + 2], x[8 * i + 3]), bf16_word(x[8 * i + 4], x[8 * i + 5]),
+                             bf16_word(x[8 * i + 6], x[8 * i + 7]));
+          }
+        }
+        const int n = n0 + c * PER;
+        const long long mw = m - lane;
+        if (out_tma) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (mw < p.M && n < p.N) tma_store_2d(&tmOut, out_smem + slot * G::OUT_BYTES, n, (int)mw);
+            tma_store_commit();
+          }
+        } else {
+          __syncwarp();
+          for (int r = 0; r < 32 && mw + r < p.M; ++r)
+            for (int j = lane; j < PER && n + j < p.N; j += 32) {
+              const int byte = j * (int)sizeof(Tio);
+              static_cast<Tio*>(p.out)[(mw + r) * p.out_stride + n + j] = *reinterpret_cast<const Tio*>(
+                  out_ptr + slot * G::OUT_BYTES + r * 128 + (((byte / 16) ^ (r & 7)) * 16) + byte % 16);
+            }
+        }
+      }
+    }
+    tma_store_wait_all<0>();
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 9) {
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem, 512);
+  }
+  cluster_sync();
+}
+
+// ---------------------------------------------------------------------------------------------- few rows
+// Few tokens: bound by the weights' bytes.  The weights take the place of A (128 features in the lanes of tensor memory), TOK tokens
+// that of B, so that a product's size goes with the tokens; the channels are cut among the CTAs of a cluster, which add their
+// sums through each other's shared memory, in the order of their ranks.  Warps 0-3: a thread a feature; warp 4 copies, warp 5 products.
+template <int TOK>
+struct MatmulSlim {
+  static constexpr int THREADS = 192, STAGE_BYTES = 128 * 128 + TOK * 128;
+  static constexpr int STAGES = TOK <= 32 ? 5 : TOK <= 64 ? 4 : 3;             // two CTAs to an SM
+  static constexpr int OFF_SCALE = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALE + 2 * TOK * 4;
+  static constexpr int USED_BYTES = OFF_BAR + 8 * (2 * STAGES + 4) + 16;
+  static constexpr int SMEM_BYTES = USED_BYTES + 1024;
+  static constexpr int TMEM_COLS = 2 * TOK < 32 ? 32 : 2 * TOK;
+  static_assert(TOK * 128 * 4 <= OFF_SCALE, "the partial sums take the place of the stages");
+};
+
+template <typename Tio, int TOK>
+__global__ void __launch_bounds__(192) matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
+                                                          const MatmulArgs p, const int parts, tc::DevStatus ds) {
+  using namespace tc;
+  using G = MatmulSlim<TOK>;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  const uint32_t bar0 = base + G::OFF_BAR;
+  auto FULL = [&](int i) { return bar0 + 8u * i; };
+  auto EMPTY = [&](int i) { return bar0 + 8u * (G::STAGES + i); };
+  auto ACCFULL = [&](int i) { return bar0 + 8u * (2 * G::STAGES + i); };
+  auto ACCEMPTY = [&](int i) { return bar0 + 8u * (2 * G::STAGES + 2 + i); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * (2 * G::STAGES + 4));
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  const WaitCtx wc(abort_flag, ds);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = (int)cluster_rank();
+  const int n0 = (int)(blockIdx.x / parts) * 128;
+  const long long m0 = (long long)blockIdx.y * TOK;
+  const int b_lo = (int)((long long)p.blocks * part / parts), b_hi = (int)((long long)p.blocks * (part + 1) / parts);
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < G::STAGES; ++i) { mbar_init(FULL(i), 1); mbar_init(EMPTY(i), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(ACCFULL(i), 1); mbar_init(ACCEMPTY(i), 4); }
+    *abort_flag = 0;
+    mbar_fence_init();
+    tma_prefetch_desc(&tmA);
+    tma_prefetch_desc(&tmW);
+  }
+  if (warp == 5) {
+    tmem_alloc(smem_u32(tmem_slot), G::TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *tmem_slot;
+
+  float* sums = reinterpret_cast<float*>(base_ptr);
+  if (warp == 4) {
+    if (lane == 0) {
+      uint32_t it = 0;
+      bool ok = true;
+      for (int b = b_lo; b < b_hi; ++b, ++it) {
+        const int st = it % G::STAGES;
+        if (!mbar_wait(EMPTY(st), ((it / G::STAGES) & 1) ^ 1, wc)) { ok = false; break; }
+        mbar_arrive_expect_tx(FULL(st), G::STAGE_BYTES);
+        const uint32_t dst = base + st * G::STAGE_BYTES;
+        tma_load_2d(dst, &tmW, FULL(st), b * kScaleBlock, n0);
+        tma_load_2d(dst + 128 * 128, &tmA, FULL(st), b * kScaleBlock, (int)m0);
+      }
+      if (!ok) mbar_drain_ring(FULL(0), G::STAGES, it);
+    }
+  } else if (warp == 5) {
+    if (lane == 0) {
+      constexpr uint32_t idesc = make_idesc_e4m3(128, TOK);
+      uint32_t it = 0;
+      for (int b = b_lo; b < b_hi; ++b, ++it) {
+        const int st = it % G::STAGES, a = it & 1;
+        if (!mbar_wait(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) || !mbar_wait(FULL(st), (it / G::STAGES) & 1, wc)) break;
+        tc_fence_after_sync();
+        const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
+        const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES + 128 * 128, 16, 1024);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mma_e4m3_ss(tmem + a * TOK, dw + k * 2, da + k * 2, idesc, k ? 1u : 0u);
+        mma_commit(EMPTY(st));
+        mma_commit(ACCFULL(a));
+      }
+    }
+  } else {
+    // The factors of a block, one for each token, go through shared memory: a thread brings one token's and reads all.
+    const uint32_t taddr = tmem + ((uint32_t)(warp * 32) << 16);
+    float* factors = reinterpret_cast<float*>(base_ptr + G::OFF_SCALE);
+    const bool mine = (int)threadIdx.x < TOK && m0 + threadIdx.x < p.M;
+    const float* sa = p.a_scale + (mine ? (m0 + threadIdx.x) * p.blocks : 0);
+    const float* sw = p.w_scale + (long long)(n0 / kScaleBlock) * p.blocks;
+    constexpr int W = TOK < 32 ? 16 : 32;                                 // columns read at a time
+    float acc[TOK];
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) acc[i] = 0.f;
+    float s = mine && b_lo < b_hi ? __ldg(sa + b_lo) * __ldg(sw + b_lo) : 0.f;
+    uint32_t it = 0;
+    bool ok = true;
+    for (int b = b_lo; b < b_hi; ++b, ++it) {
+      const int a = it & 1;
+      if ((int)threadIdx.x < TOK) factors[a * TOK + threadIdx.x] = s;
+      if (mine && b + 1 < b_hi) s = __ldg(sa + b + 1) * __ldg(sw + b + 1);
+      ok = mbar_wait(ACCFULL(a), (it >> 1) & 1, wc);
+      if (named_barrier_or(1, 128, !ok)) { ok = false; break; }
+      tc_fence_after_sync();
+#pragma unroll
+      for (int c = 0; c < TOK / W; ++c) {
+        float v[W];
+        if constexpr (W == 16) tmem_ld16(taddr + a * TOK + c * W, v);
+        else tmem_ld32(taddr + a * TOK + c * W, v);
+        tmem_wait_ld();
+        if (c == TOK / W - 1) {
+          tc_fence_before_sync();
+          mbar_arrive_warp(ACCEMPTY(a));
+        }
+#pragma unroll
+        for (int i = 0; i < W; i += 4) {
+          const float4 f = *reinterpret_cast<const float4*>(factors + a * TOK + c * W + i);
+          acc[c * W + i] = fmaf(v[i], f.x, acc[c * W + i]);
+          acc[c * W + i + 1] = fmaf(v[i + 1], f.y, acc[c * W + i + 1]);
+          acc[c * W + i + 2] = fmaf(v[i + 2], f.z, acc[c * W + i + 2]);
+          acc[c * W + i + 3] = fmaf(v[i + 3], f.w, acc[c * W + i + 3]);
+        }
+      }
+    }
+    // every product has been read, so nothing is on its way into the stages any more (after a wait that ran out something may be:
+    // nothing is put there then)
+    if (ok) {
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) sums[i * 128 + threadIdx.x] = acc[i];
+    }
+  }
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 5) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, G::TMEM_COLS);
+  }
+  if (warp < 4) {
+    const int n = n0 + (int)threadIdx.x;
+    const int lo = TOK * part / parts, hi = (int)min((long long)(TOK * (part + 1) / parts), p.M - m0);
+    const float bias = p.bias && n < p.N ? __ldg(p.bias + n) : 0.f;
+    for (int i = lo; i < hi; ++i) {
+      const uint32_t at = base + (uint32_t)(i * 128 + (int)threadIdx.x) * 4;
+      float y = 0.f;
+      for (int r = 0; r < parts; ++r) y += ld_cluster(rank_address(at, r));
+      if (n < p.N) {
+        y += bias;
+        if (p.add) y += to_float(static_cast<const Tio*>(p.add)[(m0 + i) * p.add_stride + n]);
+        static_cast<Tio*>(p.out)[(m0 + i) * p.out_stride + n] = from_float<Tio>(y);
+      }
+    }
+  }
+  __syncwarp();
+  cluster_sync();
+}
+
+}  // namespace vdn

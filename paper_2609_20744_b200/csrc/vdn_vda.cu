@@ -22,6 +22,7 @@
 #include "gram_simt.cuh"
 #include "gram_tc.cuh"
 #include "matmul_simt.cuh"
+#include "matmul_tc.cuh"
 #include "prep.cuh"
 #include "quantize.cuh"
 #include "readout_simt.cuh"
@@ -1689,6 +1690,101 @@ bool rows_aligned16(const void* p, long long stride, long long rows, size_t es) 
   return aligned16(p) && (rows <= 1 || (stride * (long long)es) % 16 == 0);
 }
 
+// Rows of bytes, or of results, as a 2-D map with a box of 128 bytes by `box_rows`, 16-byte pieces turned by the row.
+vdn_status make_bytes_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, CUtensorMapDataType type, size_t es, long long rows, long long width,
+                          long long stride, unsigned box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)width, (cuuint64_t)rows};
+  // (a single row has no stride to speak of, but the map wants a multiple of 16)
+  const cuuint64_t strides[1] = {rows > 1 ? (cuuint64_t)stride * es : ((cuuint64_t)width * es + 15) / 16 * 16};
+  const cuuint32_t box[2] = {(cuuint32_t)(128 / es), box_rows};
+  const cuuint32_t estr[2] = {1, 1};
+  CUresult r = h->encode(m, type, 2, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (matrix rows) failed: " + std::to_string((int)r));
+  return VDN_OK;
+}
+
+template <typename... P, typename... A>
+cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, unsigned cluster, int threads, int smem, cudaStream_t st, A&&... args) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = grid;
+  c.blockDim = dim3((unsigned)threads);
+  c.dynamicSmemBytes = (size_t)smem;
+  c.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cluster;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  c.attrs = at;
+  c.numAttrs = 1;
+  return cudaLaunchKernelEx(&c, kernel, std::forward<A>(args)...);
+}
+
+template <typename Tio>
+vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st) {
+  using G = vdn::MatmulPair;
+  CUtensorMap tmA, tmW, tmOut;
+  vdn_status r;
+  const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, G::ROWS)) != VDN_OK) return r;
+  if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, G::COLS / 2)) != VDN_OK) return r;
+  // results that no tile copy can write (rows at any address) leave by ordinary stores
+  const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio));
+  const bool wide = g.add && rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio));
+  if (!tma) tmOut = tmA;
+  else if ((r = make_bytes_map(h, &tmOut, g.out, sizeof(Tio) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                               sizeof(Tio), g.M, g.N, g.out_stride, 32)) != VDN_OK)
+    return r;
+  VDN_CUDA(h, (cudaFuncSetAttribute(vdn::matmul_pair_kernel<Tio>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES)));
+  const long long tiles = (g.M + 2 * G::ROWS - 1) / (2 * G::ROWS) * ((g.N + G::COLS - 1) / G::COLS);
+  const unsigned pairs = (unsigned)std::min<long long>(tiles, h->sm_count / 2);
+  prof_begin(h, st);
+  vdn::matmul_pair_kernel<Tio><<<2 * pairs, G::THREADS, G::SMEM_BYTES, st>>>(tmA, tmW, tmOut, g, tma ? 1 : 0, wide ? 1 : 0, dev_status(h));
+  prof_mark(h, st, 0, "matmul_pair");
+  return VDN_OK;
+}
+
+template <typename Tio, int TOK>
+vdn_status launch_matmul_slim(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st) {
+  using G = vdn::MatmulSlim<TOK>;
+  CUtensorMap tmA, tmW;
+  vdn_status r;
+  const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
+  if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, TOK)) != VDN_OK) return r;
+  if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, 128)) != VDN_OK) return r;
+  VDN_CUDA(h, (cudaFuncSetAttribute(vdn::matmul_slim_kernel<Tio, TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES)));
+  const long long tiles_n = scale_blocks(g.N), tiles_m = (g.M + TOK - 1) / TOK;
+  int parts = 1;
+  while (parts < 8 && 2 * parts <= g.blocks && 2 * parts * tiles_n * tiles_m <= 2LL * h->sm_count) parts *= 2;
+  prof_begin(h, st);
+  VDN_CUDA(h, launch_cluster(vdn::matmul_slim_kernel<Tio, TOK>, dim3((unsigned)(tiles_n * parts), (unsigned)tiles_m), (unsigned)parts, G::THREADS,
+                             G::SMEM_BYTES, st, tmA, tmW, g, parts, dev_status(h)));
+  prof_mark(h, st, 0, "matmul_slim");
+  return VDN_OK;
+}
+
+template <typename Tio>
+vdn_status launch_matmul(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st) {
+  vdn_status r = VDN_OK;
+  h->launches = 1;
+  if (h->cfg.flags & VDN_FLAG_FORCE_SIMT) {
+    prof_begin(h, st);
+    const dim3 grid((unsigned)((g.M + 63) / 64), (unsigned)((g.N + 63) / 64));
+    vdn::matmul_simt_kernel<Tio><<<grid, 256, 0, st>>>(g);
+    prof_mark(h, st, 0, "matmul_simt");
+  } else {
+    if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+    if (g.M <= 16) r = launch_matmul_slim<Tio, 16>(h, g, st);
+    else if (g.M <= 32) r = launch_matmul_slim<Tio, 32>(h, g, st);
+    else if (g.M <= 64) r = launch_matmul_slim<Tio, 64>(h, g, st);
+    else if (g.M <= 256) r = launch_matmul_slim<Tio, 128>(h, g, st);
+    else r = launch_matmul_pair<Tio>(h, g, st);
+  }
+  if (r != VDN_OK) return r;
+  VDN_CUDA(h, cudaGetLastError());
+  return VDN_OK;
+}
+
 template <typename Tio, bool WIDE>
 void launch_quantize(const vdn::QuantizeArgs& a, int block_rows, cudaStream_t st) {
   if (block_rows == 1) {
@@ -1867,14 +1963,7 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  prof_begin(h, st);
-  const dim3 grid((unsigned)((M + 63) / 64), (unsigned)((N + 63) / 64));
-  if (h->cfg.io_dtype == VDN_F32) vdn::matmul_simt_kernel<float><<<grid, 256, 0, st>>>(g);
-  else vdn::matmul_simt_kernel<__nv_bfloat16><<<grid, 256, 0, st>>>(g);
-  prof_mark(h, st, 0, "matmul_simt");
-  h->launches = 1;
-  VDN_CUDA(h, cudaGetLastError());
-  return VDN_OK;
+  return h->cfg.io_dtype == VDN_F32 ? launch_matmul<float>(h, g, st) : launch_matmul<__nv_bfloat16>(h, g, st);
 }
 
 size_t vdn_vda_cross_attention_workspace_bytes(vdn_vda_t h, long long queries, long long keys, const vdn_vda_cross_params* p) {
