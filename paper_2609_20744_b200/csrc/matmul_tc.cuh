@@ -154,9 +154,9 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       const bool inside = m < p.M && n0 < p.N;
       const float* sa = p.a_scale + (inside ? m * p.blocks : 0);
       const float* sw = p.w_scale + (inside ? (long long)(n0 / kScaleBlock) * p.blocks : 0);
-      float acc[128];
+      uint64_t acc[64];
 #pragma unroll
-      for (int i = 0; i < 128; ++i) acc[i] = 0.f;
+      for (int i = 0; i < 64; ++i) acc[i] = 0ull;
       float xa = __ldg(sa), xw = __ldg(sw);
       for (int b = 0; b < p.blocks; ++b, ++it) {
         const int a = it & 1;
@@ -164,22 +164,19 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         if (b + 1 < p.blocks) { xa = __ldg(sa + b + 1); xw = __ldg(sw + b + 1); }
         if (!mbar_wait(ACCFULL(a), (it >> 1) & 1, wc)) { ok = false; break; }
         tc_fence_after_sync();
-        // 32 columns are on their way while the 32 before them are added
-        float v[2][32];
-        tmem_ld32(taddr + a * G::COLS, v[0]);
+        // The accumulator is free once it has been read: half of it waits in registers (there is no room for all), and only that half
+        // is added before the rest has been fetched.
+        const uint64_t s2 = f2_pack(s, s);
+        uint64_t v[32];
+        tmem_ld64_pairs(taddr + a * G::COLS, v);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tmem_wait_ld();
-          if (c < 3) {
-            tmem_ld32(taddr + a * G::COLS + (c + 1) * 32, v[(c + 1) & 1]);
-          } else {
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(rank_address(ACCEMPTY(a), 0));
-          }
+        for (int i = 0; i < 32; ++i) acc[i] = f2_fma(v[i], s2, acc[i]);
+        tmem_ld64_pairs(taddr + a * G::COLS + 64, v);
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(rank_address(ACCEMPTY(a), 0));
 #pragma unroll
-          for (int i = 0; i < 32; ++i) acc[c * 32 + i] = fmaf(v[c & 1][i], s, acc[c * 32 + i]);
-        }
+        for (int i = 0; i < 32; ++i) acc[32 + i] = f2_fma(v[i], s2, acc[32 + i]);
       }
       if (!ok) break;
       // the tile: this warp's 32 rows, 128 bytes of each at a time through shared memory (16-byte pieces turned by the row, as the
@@ -194,7 +191,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         for (int g = 0; g < PER / 32; ++g) {
           float x[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = acc[c * PER + g * 32 + i];
+          for (int i = 0; i < 16; ++i) f2_unpack(acc[(c * PER + g * 32) / 2 + i], x[2 * i], x[2 * i + 1]);
           add_rest<Tio>(p, m, n0 + c * PER + g * 32, add_wide, x);
           if constexpr (sizeof(Tio) == 4) {
 #pragma unroll
