@@ -20,7 +20,7 @@ struct MatmulPair {
   static constexpr int A_BYTES = ROWS * 128, STAGE_BYTES = A_BYTES + COLS / 2 * 128;
   static constexpr int OUT_BYTES = 32 * 128;                       // one warp's rows, 128 bytes of each
   static constexpr int OFF_OUT = STAGES * STAGE_BYTES, OFF_BAR = OFF_OUT + 8 * 2 * OUT_BYTES;
-  static constexpr int USED_BYTES = OFF_BAR + 8 * (2 * STAGES + 4) + 16;
+  static constexpr int BARS = 2 * STAGES + 4 + 16, USED_BYTES = OFF_BAR + 8 * BARS + 16;
   static constexpr int SMEM_BYTES = USED_BYTES + 1024;
 };
 static_assert(MatmulPair::SMEM_BYTES <= 232448, "shared memory of a CTA");
@@ -31,36 +31,27 @@ __device__ __forceinline__ uint32_t bf16_word(float lo, float hi) {
   return r;
 }
 
-// bias and add of columns n .. n+31 (of N) of row m.
+// bias of columns n .. n+31 (of N), and add where it did not come by tile copies, element by element.
 template <typename Tio>
-__device__ __forceinline__ void add_rest(const MatmulArgs& p, long long m, int n, bool add_wide, float (&x)[32]) {
+__device__ __forceinline__ void add_rest(const MatmulArgs& p, long long m, int n, bool add, float (&x)[32]) {
   if (p.bias) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] += n + i < p.N ? __ldg(p.bias + n + i) : 0.f;
   }
-  if (p.add && m < p.M) {
+  if (add && m < p.M) {
     const Tio* r = static_cast<const Tio*>(p.add) + m * p.add_stride + n;
-    if (add_wide && n + 32 <= p.N) {
 #pragma unroll
-      for (int i = 0; i < 32; i += 16 / (int)sizeof(Tio)) {
-#pragma unroll
-        for (int j = 0; j < 16 / (int)sizeof(Tio); j += 4) {
-          const float4 y = load4(r + i + j);
-          x[i + j] += y.x; x[i + j + 1] += y.y; x[i + j + 2] += y.z; x[i + j + 3] += y.w;
-        }
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 32; ++i)
-        if (n + i < p.N) x[i] += to_float(r[i]);
-    }
+    for (int i = 0; i < 32; ++i)
+      if (n + i < p.N) x[i] += to_float(r[i]);
   }
 }
 
-template <typename Tio>
+// ADD: `add` comes by tile copies (a variant of its own: without it the same code takes 6 % longer, 753 -> 800 us at 32768 x 5120 x 5120).
+template <typename Tio, bool ADD>
 __global__ void __launch_bounds__(MatmulPair::THREADS, 1) __cluster_dims__(2, 1, 1)
 matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                   const __grid_constant__ CUtensorMap tmOut, const MatmulArgs p, const int out_tma, const int add_wide, tc::DevStatus ds) {
+                   const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmAdd, const MatmulArgs p,
+                   const int out_tma, tc::DevStatus ds) {
   using namespace tc;
   using G = MatmulPair;
   extern __shared__ unsigned char smem_dyn[];
@@ -71,7 +62,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   auto EMPTY = [&](int i) { return bar0 + 8u * (G::STAGES + i); };
   auto ACCFULL = [&](int i) { return bar0 + 8u * (2 * G::STAGES + i); };
   auto ACCEMPTY = [&](int i) { return bar0 + 8u * (2 * G::STAGES + 2 + i); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * (2 * G::STAGES + 4));
+  auto ADDED = [&](int i) { return bar0 + 8u * (2 * G::STAGES + 4 + i); };       // 16: a warp's two staging tiles
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * G::BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const WaitCtx wc(abort_flag, ds);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -80,6 +72,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   if (threadIdx.x == 0) {
     for (int i = 0; i < G::STAGES; ++i) { mbar_init(FULL(i), 1); mbar_init(EMPTY(i), 1); }
     for (int i = 0; i < 2; ++i) { mbar_init(ACCFULL(i), 1); mbar_init(ACCEMPTY(i), 16); }   // a warp an arrival, of both CTAs
+    for (int i = 0; i < 16; ++i) mbar_init(ADDED(i), 1);
     *abort_flag = 0;
     mbar_fence_init();
     tma_prefetch_desc(&tmA);
@@ -146,7 +139,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const uint32_t taddr = tmem + ((uint32_t)(qd * 32) << 16) + half * 128;
     const uint32_t out_smem = base + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
     unsigned char* out_ptr = base_ptr + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
-    uint32_t it = 0, slot = 0;
+    constexpr int PER = 128 / (int)sizeof(Tio), SLICES = 128 / PER;
+    uint32_t it = 0, phase = 0;                          // phase: of the two staging tiles' barriers, a bit each
     bool ok = true;
     for (long long t = first; t < tiles && ok; t += step) {
       const long long m = (t / tiles_n) * 2 * G::ROWS + rank * G::ROWS + qd * 32 + lane;
@@ -154,6 +148,20 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       const bool inside = m < p.M && n0 < p.N;
       const float* sa = p.a_scale + (inside ? m * p.blocks : 0);
       const float* sw = p.w_scale + (inside ? (long long)(n0 / kScaleBlock) * p.blocks : 0);
+      // What is to be added comes into the staging tiles the results will leave from, the first two slices while the sums are formed.
+      const bool here = m - lane < p.M;
+      auto fetch = [&](int c) {
+        const int n = n0 + c * PER, bar = warp * 2 + (c & 1);
+        if (!ADD || !here || n >= p.N || lane != 0) return;
+        mbar_arrive_expect_tx(ADDED(bar), G::OUT_BYTES);
+        tma_load_2d(out_smem + (c & 1) * G::OUT_BYTES, &tmAdd, ADDED(bar), n, (int)m);
+      };
+      if constexpr (ADD) {
+        tma_store_wait_read<0>();                        // (only lane 0 has any) the last tile's stores have read them
+        __syncwarp();
+        fetch(0);
+        fetch(1);
+      }
       uint64_t acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0ull;
@@ -178,33 +186,59 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[32 + i] = f2_fma(v[i], s2, acc[32 + i]);
       }
-      if (!ok) break;
+      if (!ok) {
+        if (ADD && here)                            // a bounded chance for copies under way to land
+          for (int c = 0; c < 2 && n0 + c * PER < p.N; ++c) mbar_drain(ADDED(warp * 2 + c), (phase >> c) & 1);
+        break;
+      }
       // the tile: this warp's 32 rows, 128 bytes of each at a time through shared memory (16-byte pieces turned by the row, as the
       // copy's swizzle has them), so that whole lines leave
-      constexpr int PER = 128 / (int)sizeof(Tio);
 #pragma unroll
-      for (int c = 0; c < 128 / PER; ++c, slot ^= 1) {
-        tma_store_wait_read<1>();                       // (only lane 0 has any) the store that last read this buffer
-        __syncwarp();
+      for (int c = 0; c < SLICES; ++c) {
+        const uint32_t slot = c & 1;
+        if (c >= 2 || !ADD) {
+          tma_store_wait_read<1>();                      // the store that last read this buffer
+          __syncwarp();
+          if (c >= 2) fetch(c);
+        }
+        const int n = n0 + c * PER;
+        const bool by_tile = ADD && here && n < p.N;
+        if (by_tile) {
+          if (!mbar_wait(ADDED(warp * 2 + slot), (phase >> slot) & 1, wc)) ok = false;
+          phase ^= 1u << slot;
+        }
         unsigned char* row = out_ptr + slot * G::OUT_BYTES + lane * 128;
 #pragma unroll
         for (int g = 0; g < PER / 32; ++g) {
           float x[32];
 #pragma unroll
           for (int i = 0; i < 16; ++i) f2_unpack(acc[(c * PER + g * 32) / 2 + i], x[2 * i], x[2 * i + 1]);
-          add_rest<Tio>(p, m, n0 + c * PER + g * 32, add_wide, x);
+          add_rest<Tio>(p, m, n + g * 32, !ADD && p.add, x);
           if constexpr (sizeof(Tio) == 4) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) *reinterpret_cast<float4*>(row + ((i ^ (lane & 7)) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) {
+              float4* at = reinterpret_cast<float4*>(row + ((i ^ (lane & 7)) * 16));
+              const float4 y = by_tile ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
+              *at = make_float4(x[4 * i] + y.x, x[4 * i + 1] + y.y, x[4 * i + 2] + y.z, x[4 * i + 3] + y.w);
+            }
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<uint4*>(row + (((g * 4 + i) ^ (lane & 7)) * 16)) =
-                  make_uint4(bf16_word(x[8 * i], x[8 * i + 1]), bf16_word(x[8 * i + 2], x[8 * i + 3]), bf16_word(x[8 * i + 4], x[8 * i + 5]),
-                             bf16_word(x[8 * i + 6], x[8 * i + 7]));
+            for (int i = 0; i < 4; ++i) {
+              uint4* at = reinterpret_cast<uint4*>(row + (((g * 4 + i) ^ (lane & 7)) * 16));
+              if (by_tile) {
+                const uint4 y = *at;
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  x[8 * i + 2 * e] += __uint_as_float(w[e] << 16);
+                  x[8 * i + 2 * e + 1] += __uint_as_float(w[e] & 0xFFFF0000u);
+                }
+              }
+              *at = make_uint4(bf16_word(x[8 * i], x[8 * i + 1]), bf16_word(x[8 * i + 2], x[8 * i + 3]), bf16_word(x[8 * i + 4], x[8 * i + 5]),
+                               bf16_word(x[8 * i + 6], x[8 * i + 7]));
+            }
           }
         }
-        const int n = n0 + c * PER;
         const long long mw = m - lane;
         if (out_tma) {
           fence_proxy_async_smem();
@@ -221,6 +255,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
               static_cast<Tio*>(p.out)[(mw + r) * p.out_stride + n + j] = *reinterpret_cast<const Tio*>(
                   out_ptr + slot * G::OUT_BYTES + r * 128 + (((byte / 16) ^ (r & 7)) * 16) + byte % 16);
             }
+          fence_proxy_async_smem();                      // (read before a copy may come here)
+          __syncwarp();
         }
       }
     }
@@ -240,7 +276,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // ---------------------------------------------------------------------------------------------- few rows
 // Few tokens: bound by the weights' bytes.  The weights take the place of A (128 features in the lanes of tensor memory), TOK tokens
 // that of B, so that a product's size goes with the tokens; the channels are cut among the CTAs of a cluster, which add their
-// sums through each other's shared memory, in the order of their ranks.  Warps 0-3: a thread a feature; warp 4 copies, warp 5 products.
+// sums through each other's shared memory, in the order of their ranks.  Warps 0-3 take the block sums out, a thread a feature; warp 4
+// copies, warp 5 issues products.
 template <int TOK>
 struct MatmulSlim {
   static constexpr int THREADS = 192, STAGE_BYTES = 128 * 128 + TOK * 128;
@@ -253,8 +290,9 @@ struct MatmulSlim {
 };
 
 template <typename Tio, int TOK>
-__global__ void __launch_bounds__(192) matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
-                                                          const MatmulArgs p, const int parts, tc::DevStatus ds) {
+__global__ void __launch_bounds__(192, 2)
+matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW, const MatmulArgs p, const int parts,
+                   const int wide, tc::DevStatus ds) {
   using namespace tc;
   using G = MatmulSlim<TOK>;
   extern __shared__ unsigned char smem_dyn[];
@@ -329,7 +367,7 @@ __global__ void __launch_bounds__(192) matmul_slim_kernel(const __grid_constant_
     const bool mine = (int)threadIdx.x < TOK && m0 + threadIdx.x < p.M;
     const float* sa = p.a_scale + (mine ? (m0 + threadIdx.x) * p.blocks : 0);
     const float* sw = p.w_scale + (long long)(n0 / kScaleBlock) * p.blocks;
-    constexpr int W = TOK < 32 ? 16 : 32;                                 // columns read at a time
+    constexpr int W = TOK < 32 || TOK > 64 ? 16 : 32;                     // columns read at a time (registers)
     float acc[TOK];
 #pragma unroll
     for (int i = 0; i < TOK; ++i) acc[i] = 0.f;
@@ -378,19 +416,36 @@ __global__ void __launch_bounds__(192) matmul_slim_kernel(const __grid_constant_
     tc_fence_after_sync();
     tmem_dealloc(tmem, G::TMEM_COLS);
   }
-  if (warp < 4) {
-    const int n = n0 + (int)threadIdx.x;
-    const int lo = TOK * part / parts, hi = (int)min((long long)(TOK * (part + 1) / parts), p.M - m0);
-    const float bias = p.bias && n < p.N ? __ldg(p.bias + n) : 0.f;
-    for (int i = lo; i < hi; ++i) {
-      const uint32_t at = base + (uint32_t)(i * 128 + (int)threadIdx.x) * 4;
-      float y = 0.f;
-      for (int r = 0; r < parts; ++r) y += ld_cluster(rank_address(at, r));
-      if (n < p.N) {
-        y += bias;
-        if (p.add) y += to_float(static_cast<const Tio*>(p.add)[(m0 + i) * p.add_stride + n]);
-        static_cast<Tio*>(p.out)[(m0 + i) * p.out_stride + n] = from_float<Tio>(y);
+  // A rank's share of the tokens: four neighbouring features of one to a thread, from all ranks.
+  const int lo = TOK * part / parts, hi = (int)min((long long)(TOK * (part + 1) / parts), p.M - m0);
+#pragma unroll 2
+  for (int t = (int)threadIdx.x; t < (hi - lo) * 32; t += G::THREADS) {
+    const int i = lo + t / 32, n = n0 + (t % 32) * 4;
+    const uint32_t at = base + (uint32_t)(i * 128 + (t % 32) * 4) * 4;
+    float4 x[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+      if (r < parts) x[r] = ld_cluster4(rank_address(at, r));
+    float y[4] = {x[0].x, x[0].y, x[0].z, x[0].w};
+#pragma unroll
+    for (int r = 1; r < 8; ++r)
+      if (r < parts) { y[0] += x[r].x; y[1] += x[r].y; y[2] += x[r].z; y[3] += x[r].w; }
+    Tio* out = static_cast<Tio*>(p.out) + (m0 + i) * p.out_stride + n;
+    const Tio* add = static_cast<const Tio*>(p.add) + (m0 + i) * p.add_stride + n;
+    if (p.bias) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] += n + j < p.N ? __ldg(p.bias + n + j) : 0.f;
+    }
+    if (wide && n + 4 <= p.N) {
+      if (p.add) {
+        const float4 z = load4(add);
+        y[0] += z.x; y[1] += z.y; y[2] += z.z; y[3] += z.w;
       }
+      store4(out, make_float4(y[0], y[1], y[2], y[3]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (n + j < p.N) out[j] = from_float<Tio>(y[j] + (p.add ? to_float(add[j]) : 0.f));
     }
   }
   __syncwarp();

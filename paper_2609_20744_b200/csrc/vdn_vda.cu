@@ -1723,23 +1723,24 @@ cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, unsigned cluster, in
 template <typename Tio>
 vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st) {
   using G = vdn::MatmulPair;
-  CUtensorMap tmA, tmW, tmOut;
+  CUtensorMap tmA, tmW, tmOut, tmAdd;
   vdn_status r;
   const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
   if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, G::ROWS)) != VDN_OK) return r;
   if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, G::COLS / 2)) != VDN_OK) return r;
   // results that no tile copy can write (rows at any address) leave by ordinary stores
   const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio));
-  const bool wide = g.add && rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio));
-  if (!tma) tmOut = tmA;
-  else if ((r = make_bytes_map(h, &tmOut, g.out, sizeof(Tio) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
-                               sizeof(Tio), g.M, g.N, g.out_stride, 32)) != VDN_OK)
-    return r;
-  VDN_CUDA(h, (cudaFuncSetAttribute(vdn::matmul_pair_kernel<Tio>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES)));
+  const bool add_tma = g.add && rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio));
+  const CUtensorMapDataType io = sizeof(Tio) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  tmOut = tmAdd = tmA;
+  if (tma && (r = make_bytes_map(h, &tmOut, g.out, io, sizeof(Tio), g.M, g.N, g.out_stride, 32)) != VDN_OK) return r;
+  if (add_tma && (r = make_bytes_map(h, &tmAdd, g.add, io, sizeof(Tio), g.M, g.N, g.add_stride, 32)) != VDN_OK) return r;
+  auto kernel = add_tma ? vdn::matmul_pair_kernel<Tio, true> : vdn::matmul_pair_kernel<Tio, false>;
+  VDN_CUDA(h, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES));
   const long long tiles = (g.M + 2 * G::ROWS - 1) / (2 * G::ROWS) * ((g.N + G::COLS - 1) / G::COLS);
   const unsigned pairs = (unsigned)std::min<long long>(tiles, h->sm_count / 2);
   prof_begin(h, st);
-  vdn::matmul_pair_kernel<Tio><<<2 * pairs, G::THREADS, G::SMEM_BYTES, st>>>(tmA, tmW, tmOut, g, tma ? 1 : 0, wide ? 1 : 0, dev_status(h));
+  kernel<<<2 * pairs, G::THREADS, G::SMEM_BYTES, st>>>(tmA, tmW, tmOut, tmAdd, g, tma ? 1 : 0, dev_status(h));
   prof_mark(h, st, 0, "matmul_pair");
   return VDN_OK;
 }
@@ -1756,9 +1757,10 @@ vdn_status launch_matmul_slim(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   const long long tiles_n = scale_blocks(g.N), tiles_m = (g.M + TOK - 1) / TOK;
   int parts = 1;
   while (parts < 8 && 2 * parts <= g.blocks && 2 * parts * tiles_n * tiles_m <= 2LL * h->sm_count) parts *= 2;
+  const bool wide = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio)) && (!g.add || rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio)));
   prof_begin(h, st);
   VDN_CUDA(h, launch_cluster(vdn::matmul_slim_kernel<Tio, TOK>, dim3((unsigned)(tiles_n * parts), (unsigned)tiles_m), (unsigned)parts, G::THREADS,
-                             G::SMEM_BYTES, st, tmA, tmW, g, parts, dev_status(h)));
+                             G::SMEM_BYTES, st, tmA, tmW, g, parts, wide ? 1 : 0, dev_status(h)));
   prof_mark(h, st, 0, "matmul_slim");
   return VDN_OK;
 }
@@ -1788,7 +1790,7 @@ vdn_status launch_matmul(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st)
 template <typename Tio, bool WIDE>
 void launch_quantize(const vdn::QuantizeArgs& a, int block_rows, cudaStream_t st) {
   if (block_rows == 1) {
-    constexpr int per_cta = 4 * 256 / (vdn::kScaleBlock * (int)sizeof(Tio) / 16);
+    constexpr int per_cta = vdn::kQuantizeItems * 256 / vdn::kQuantizeLanes;
     vdn::quantize_rows_kernel<Tio, WIDE><<<(a.items + per_cta - 1) / per_cta, 256, 0, st>>>(a);
   } else {
     vdn::quantize_square_kernel<Tio, WIDE><<<(unsigned)(scale_blocks(a.rows) * (long long)a.col_blocks), 512, 0, st>>>(a);
