@@ -202,7 +202,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantizeArgs a) {
 
 // One scale for 128 rows of 128 channels: a CTA to a block, its elements in registers between the maximum and the cast.
 template <typename Tio, bool WIDE>
-__global__ void __launch_bounds__(512, 2) quantize_square_kernel(QuantizeArgs a) {
+__global__ void __launch_bounds__(512, sizeof(Tio) == 4 ? 2 : 1) quantize_square_kernel(QuantizeArgs a) {
   constexpr int GROUPS = 512 / kQuantizeLanes, ITEMS = kScaleBlock / GROUPS;
   const long long row0 = (long long)(blockIdx.x / a.col_blocks) * kScaleBlock;
   const int col = (int)(blockIdx.x % a.col_blocks) * kScaleBlock + (int)(threadIdx.x % kQuantizeLanes) * 16;

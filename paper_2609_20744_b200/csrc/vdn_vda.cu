@@ -19,6 +19,7 @@
 
 #include "common.cuh"
 #include "cross_simt.cuh"
+#include "cross_tc.cuh"
 #include "gram_simt.cuh"
 #include "gram_tc.cuh"
 #include "matmul_simt.cuh"
@@ -1822,23 +1823,41 @@ vdn_status plan_cross(vdn_vda_t h, long long queries, long long keys, const vdn_
 
 // How a call runs: on which kernel, and in how many parts of the keys.
 struct CrossLayout {
-  int rows;                 // rows of a CTA's tile; up to 8: cross_few, 64: cross_plain
-  long long units;          // (batch row, key head, row tile)
+  bool tc;
+  int rows;                 // plain kernels: rows of a CTA's tile; up to 8: cross_few, 64: cross_plain
+  long long units;          // plain kernels: (batch row, key head, row tile); tensor cores: pairs of tiles
   int parts;
   size_t o, ml, total;
+  vdn::CrossTcShape shape;
 };
 CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
   CrossLayout L = {};
   L.parts = 1;
   if (a.B == 0 || a.Lq == 0) return L;
   const long long rows = (long long)a.Lq * a.group;
-  L.rows = rows <= 8 ? (rows <= 2 ? (int)rows : rows <= 4 ? 4 : 8) : vdn::CrossPlain<64>::ROWS;
-  L.units = (long long)a.B * a.Hk * ((rows + L.rows - 1) / L.rows);
+  // (the tensor-core kernel finds a row's maximum before it scales)
+  L.tc = h->cfg.io_dtype == VDN_BF16 && !(h->cfg.flags & VDN_FLAG_FORCE_SIMT) && a.scale_log2 > 0.f && rows > 8;
   // keys of a batch row, by which parts are chosen (packed: the average)
   const long long keys = a.Lk ? a.Lk : a.n_keys / a.B;
-  const long long least = 128;                          // keys of a part
-  const long long wanted = (L.rows <= 8 ? 4LL : 2LL) * h->sm_count / L.units;
+  long long wanted, least;                              // parts, keys of a part
+  if (L.tc) {
+    vdn::CrossTcShape& s = L.shape;
+    s.hb = std::min(a.group, 32);
+    s.tb = 32 / s.hb;
+    s.head_blocks = (a.group + s.hb - 1) / s.hb;
+    const long long blocks = (long long)((a.Lq + s.tb - 1) / s.tb) * s.head_blocks;
+    s.pairs = (int)((blocks + 7) / 8);
+    L.units = (long long)a.B * a.Hk * s.pairs;
+    wanted = h->sm_count / L.units;
+    least = 256;
+  } else {
+    L.rows = rows <= 8 ? (rows <= 2 ? (int)rows : rows <= 4 ? 4 : 8) : vdn::CrossPlain<64>::ROWS;
+    L.units = (long long)a.B * a.Hk * ((rows + L.rows - 1) / L.rows);
+    wanted = (L.rows <= 8 ? 4LL : 2LL) * h->sm_count / L.units;
+    least = 128;
+  }
   L.parts = (int)std::max(1LL, std::min({wanted, keys / least, 256LL}));
+  L.shape.items = L.units * L.parts;
   if (L.parts > 1) {
     const size_t n = (size_t)a.B * a.Lq * a.H * L.parts;
     L.o = 0;
@@ -1846,6 +1865,47 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     L.total = L.ml + align_up(n * sizeof(float2));
   }
   return L;
+}
+
+// Rows of one key head as the tensor-core kernel takes them: [B, Lq, Hk, group, d] with a box of a row block, 64 channels wide.
+vdn_status make_query_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, const vdn::CrossArgs& a, const vdn::CrossTcShape& s, int d, long long stride) {
+  const cuuint64_t es = 2, dims[5] = {(cuuint64_t)d, (cuuint64_t)a.group, (cuuint64_t)a.Hk, (cuuint64_t)a.Lq, (cuuint64_t)a.B};
+  const cuuint64_t strides[4] = {d * es, (cuuint64_t)a.group * d * es, (cuuint64_t)stride * es,
+                                 (cuuint64_t)stride * (a.B > 1 ? a.Lq : 1) * es};
+  const cuuint32_t box[5] = {64, (cuuint32_t)s.hb, 1, (cuuint32_t)s.tb, 1}, estr[5] = {1, 1, 1, 1, 1};
+  CUresult r = h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (queries) failed: " + std::to_string((int)r));
+  return VDN_OK;
+}
+// Keys or values [n_keys, Hk, d] with a box of 128 keys, 64 channels of one head.
+vdn_status make_key_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, const vdn::CrossArgs& a, int d, long long stride) {
+  const cuuint64_t es = 2, dims[3] = {(cuuint64_t)d, (cuuint64_t)a.Hk, (cuuint64_t)a.n_keys};
+  const cuuint64_t strides[2] = {d * es, (cuuint64_t)stride * es};
+  const cuuint32_t box[3] = {64, 1, 128}, estr[3] = {1, 1, 1};
+  CUresult r = h->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(ptr), dims, strides, box, estr,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled (keys) failed: " + std::to_string((int)r));
+  return VDN_OK;
+}
+
+template <int D>
+vdn_status launch_cross_tc(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout& L, cudaStream_t st) {
+  using G = vdn::CrossTc<D>;
+  if (!h->encode) return fail(h, VDN_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+  CUtensorMap tmQ, tmK, tmV, tmOut;
+  vdn_status r;
+  if ((r = make_query_map(h, &tmQ, a.q, a, L.shape, D, a.q_stride)) != VDN_OK) return r;
+  if ((r = make_query_map(h, &tmOut, a.out, a, L.shape, D, a.out_stride)) != VDN_OK) return r;
+  tmK = tmV = tmQ;                                      // (no keys at all: never used)
+  if (a.n_keys > 0 && ((r = make_key_map(h, &tmK, a.k, a, D, a.k_stride)) != VDN_OK || (r = make_key_map(h, &tmV, a.v, a, D, a.v_stride)) != VDN_OK))
+    return r;
+  VDN_CUDA(h, cudaFuncSetAttribute(vdn::cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES));
+  const unsigned grid = (unsigned)std::min<long long>(L.shape.items, h->sm_count);
+  vdn::cross_tc_kernel<D><<<grid, G::THREADS, G::SMEM_BYTES, st>>>(tmQ, tmK, tmV, tmOut, a, L.shape, dev_status(h));
+  return VDN_OK;
 }
 
 template <typename Tio, int D>
@@ -1867,9 +1927,9 @@ vdn_status launch_cross_simt(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLa
 template <typename Tio, int D>
 vdn_status launch_cross(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout& L, cudaStream_t st) {
   prof_begin(h, st);
-  vdn_status r = launch_cross_simt<Tio, D>(h, a, L, st);
+  vdn_status r = L.tc ? launch_cross_tc<D>(h, a, L, st) : launch_cross_simt<Tio, D>(h, a, L, st);
   if (r != VDN_OK) return r;
-  prof_mark(h, st, 0, L.rows <= 8 ? "cross_few" : "cross_plain");
+  prof_mark(h, st, 0, L.tc ? "cross_tc" : L.rows <= 8 ? "cross_few" : "cross_plain");
   h->launches = 1;
   if (L.parts > 1) {
     const long long rows = (long long)a.B * a.Lq * a.H;
