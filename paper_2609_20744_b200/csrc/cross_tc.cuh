@@ -32,7 +32,7 @@ struct CrossTc {
   static constexpr int STAGES = D == 128 ? 2 : 4;                       // of keys, and of values
   static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + STAGES * TILE_BYTES, OFF_OUT = OFF_V + STAGES * TILE_BYTES;
   static constexpr int OFF_BAR = OFF_OUT + 8 * OUT_BYTES;
-  static constexpr int BARS = 2 + 2 + 5 * STAGES + 2 + 2 + 2 + 2;
+  static constexpr int BARS = 2 + 2 + 5 * STAGES + 2 + 4 + 2 + 2;
   static constexpr int USED_BYTES = OFF_BAR + 8 * BARS + 16, SMEM_BYTES = USED_BYTES + 1024;
   static constexpr int COL_S = 0, COL_O = 256, COLS = 512;              // tensor memory: S of both tiles, O of both
 };
@@ -78,8 +78,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   auto V_EMPTY = [&](int i) { return bar0 + 8u * (4 + 4 * G::STAGES + i); };
   auto S_FULL = [&](int c) { return bar0 + 8u * (4 + 5 * G::STAGES + c); };
   auto P_READY = [&](int c) { return bar0 + 8u * (6 + 5 * G::STAGES + c); };
-  auto O_FULL = [&](int c) { return bar0 + 8u * (8 + 5 * G::STAGES + c); };
-  auto O_EMPTY = [&](int c) { return bar0 + 8u * (10 + 5 * G::STAGES + c); };
+  auto O_FULL = [&](int c) { return bar0 + 8u * (10 + 5 * G::STAGES + c); };
+  auto O_EMPTY = [&](int c) { return bar0 + 8u * (12 + 5 * G::STAGES + c); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * G::BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const WaitCtx wc(abort_flag, ds);
@@ -88,7 +88,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   if (threadIdx.x == 0) {
     for (int c = 0; c < 2; ++c) {
       mbar_init(Q_FULL(c), 1); mbar_init(Q_EMPTY(c), 1);
-      mbar_init(S_FULL(c), 1); mbar_init(P_READY(c), 4);           // a warp an arrival
+      mbar_init(S_FULL(c), 1);
+      mbar_init(P_READY(2 * c), 4); mbar_init(P_READY(2 * c + 1), 4);   // a warp an arrival
       mbar_init(O_FULL(c), 1); mbar_init(O_EMPTY(c), 4);
     }
     for (int i = 0; i < G::STAGES; ++i) {
@@ -158,60 +159,75 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
     } else if (warp == 9) {
       // ------------------------------------------------------------------ products
-      if (lane == 0) {
-        constexpr uint32_t id_s = make_idesc_bf16(128, 128, false, false), id_o = make_idesc_bf16(128, D, false, true);
-        uint32_t kv = 0, n_item[2] = {0, 0}, n_p[2] = {0, 0};
-        bool ok = true;
-        for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
-          const CrossItem x = cross_item(a, s, item);
-          if (x.tiles == 0) continue;
-          const int chains = x.second ? 2 : 1;
-          auto scores = [&](int c, uint32_t at) {
-            const uint32_t st = at % G::STAGES;
-            const uint64_t dq = make_smem_desc(base + G::OFF_Q + c * G::TILE_BYTES, 16, 1024);
-            const uint64_t dk = make_smem_desc(base + G::OFF_K + st * G::TILE_BYTES, 16, 1024);
+      constexpr uint32_t id_s = make_idesc_bf16(128, 128, false, false), id_o = make_idesc_bf16(128, D, false, true);
+      uint32_t kv = 0, n_item[2] = {0, 0}, n_p[2] = {0, 0};
+      bool ok = true;
+      auto scores = [&](int c, uint32_t at) {
+        const uint32_t st = at % G::STAGES;
+        const uint64_t dq = make_smem_desc(base + G::OFF_Q + c * G::TILE_BYTES, 16, 1024);
+        const uint64_t dk = make_smem_desc(base + G::OFF_K + st * G::TILE_BYTES, 16, 1024);
+        if (elect_one()) {
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (k >> 2) * (G::CHUNK_BYTES >> 4) + (k & 3) * 2;
-              mma_bf16_ss(tmem + G::COL_S + c * 128, dq + off, dk + off, id_s, k ? 1u : 0u);
-            }
-            mma_commit(S_FULL(c));
-          };
-          for (int c = 0; c < chains && ok; ++c) {
-            ok = mbar_wait(Q_FULL(c), n_item[c] & 1, wc) && mbar_wait(K_FULL(kv % G::STAGES), (kv / G::STAGES) & 1, wc);
-            if (!ok) break;
-            tc_fence_after_sync();
-            scores(c, kv);
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = (k >> 2) * (G::CHUNK_BYTES >> 4) + (k & 3) * 2;
+            mma_bf16_ss(tmem + G::COL_S + c * 128, dq + off, dk + off, id_s, k ? 1u : 0u);
           }
-          if (!ok) break;
-          mma_commit(K_EMPTY(kv % G::STAGES));
-          if (x.tiles == 1)
-            for (int c = 0; c < chains; ++c) mma_commit(Q_EMPTY(c));
-          for (int j = 0; j < x.tiles && ok; ++j, ++kv) {
-            const uint32_t st = kv % G::STAGES, next = kv + 1;
-            for (int c = 0; c < chains; ++c) {
-              ok = mbar_wait(P_READY(c), n_p[c] & 1, wc) && mbar_wait(V_READY(st), (kv / G::STAGES) & 1, wc) &&
-                   (j > 0 || mbar_wait(O_EMPTY(c), (n_item[c] & 1) ^ 1, wc));
-              if (!ok) break;
-              ++n_p[c];
-              tc_fence_after_sync();
-              const uint64_t dv = make_smem_desc(base + G::OFF_V + st * G::TILE_BYTES, G::CHUNK_BYTES, 1024);
-#pragma unroll
-              for (int k = 0; k < 8; ++k)
-                mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, (j | k) ? 1u : 0u);
-              if (j + 1 == x.tiles) mma_commit(O_FULL(c));
-              if (c + 1 == chains) mma_commit(V_EMPTY(st));
-              if (j + 1 < x.tiles) {
-                if (!mbar_wait(K_FULL(next % G::STAGES), (next / G::STAGES) & 1, wc)) { ok = false; break; }
-                tc_fence_after_sync();
-                scores(c, next);
-                if (c + 1 == chains) mma_commit(K_EMPTY(next % G::STAGES));
-                if (j + 2 == x.tiles) mma_commit(Q_EMPTY(c));
-              }
-            }
-          }
-          for (int c = 0; c < chains; ++c) ++n_item[c];
+          mma_commit(S_FULL(c));
         }
+        __syncwarp();
+      };
+      auto commit = [&](uint32_t bar) {
+        if (elect_one()) mma_commit(bar);
+        __syncwarp();
+      };
+      for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
+        const CrossItem x = cross_item(a, s, item);
+        if (x.tiles == 0) continue;
+        const int chains = x.second ? 2 : 1;
+        for (int c = 0; c < chains && ok; ++c) {
+          ok = mbar_wait_warp(Q_FULL(c), n_item[c] & 1, wc) && mbar_wait_warp(K_FULL(kv % G::STAGES), (kv / G::STAGES) & 1, wc);
+          if (!ok) break;
+          tc_fence_after_sync();
+          scores(c, kv);
+        }
+        if (!ok) break;
+        commit(K_EMPTY(kv % G::STAGES));
+        if (x.tiles == 1)
+          for (int c = 0; c < chains; ++c) commit(Q_EMPTY(c));
+        for (int j = 0; j < x.tiles && ok; ++j, ++kv) {
+          const uint32_t st = kv % G::STAGES, next = kv + 1;
+          const uint64_t dv = make_smem_desc(base + G::OFF_V + st * G::TILE_BYTES, G::CHUNK_BYTES, 1024);
+          for (int c = 0; c < chains; ++c) {
+            ok = mbar_wait_warp(V_READY(st), (kv / G::STAGES) & 1, wc) && (j > 0 || mbar_wait_warp(O_EMPTY(c), (n_item[c] & 1) ^ 1, wc));
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              ok = ok && mbar_wait_warp(P_READY(2 * c + half), n_p[c] & 1, wc);
+              if (!ok) break;
+              tc_fence_after_sync();
+              if (elect_one()) {
+#pragma unroll
+                for (int k = half * 4; k < half * 4 + 4; ++k)
+                  mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, k || j ? 1u : 0u);
+                if (half == 1) {
+                  if (j + 1 == x.tiles) mma_commit(O_FULL(c));
+                  if (c + 1 == chains) mma_commit(V_EMPTY(st));
+                }
+              }
+              __syncwarp();
+            }
+            if (!ok) break;
+            ++n_p[c];
+            if (j + 1 < x.tiles) {
+              ok = mbar_wait_warp(K_FULL(next % G::STAGES), (next / G::STAGES) & 1, wc);
+              if (!ok) break;
+              tc_fence_after_sync();
+              scores(c, next);
+              if (c + 1 == chains) commit(K_EMPTY(next % G::STAGES));
+              if (j + 2 == x.tiles) commit(Q_EMPTY(c));
+            }
+          }
+        }
+        for (int c = 0; c < chains; ++c) ++n_item[c];
       }
     } else if (warp == 10) {
       // ------------------------------------------------------------------ values that do not count become zeros
@@ -272,19 +288,26 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (!mbar_wait(S_FULL(c), n_s & 1, wc)) { ok = false; break; }
         tc_fence_after_sync();
-        float v[128];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) tmem_ld32(ts + i * 32, *reinterpret_cast<float (*)[32]>(v + i * 32));
-        tmem_wait_ld();
+        uint64_t v[64];                                        // two neighbouring scores each
+        tmem_ld128_pairs(ts, v);
         if (!all) {
 #pragma unroll
-          for (int i = 0; i < 128; ++i)
-            if (!((on[i >> 5] >> (i & 31)) & 1u)) v[i] = -INFINITY;
+          for (int i = 0; i < 64; ++i) {
+            float x0, x1;
+            f2_unpack(v[i], x0, x1);
+            if (!((on[i >> 4] >> (2 * i & 31)) & 1u)) x0 = -INFINITY;
+            if (!((on[i >> 4] >> ((2 * i + 1) & 31)) & 1u)) x1 = -INFINITY;
+            v[i] = f2_pack(x0, x1);
+          }
         }
-        float top = v[0];
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int i = 1; i < 127; i += 2) top = fmaxf(fmaxf(top, v[i]), v[i + 1]);
-        top = fmaxf(top, v[127]) * sl;
+        for (int i = 0; i < 64; ++i) {
+          float x0, x1;
+          f2_unpack(v[i], x0, x1);
+          tops[i & 3] = fmaxf(fmaxf(tops[i & 3], x0), x1);
+        }
+        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * sl;
         // the first finite maximum is taken over as it is (O is zero, or about to be overwritten), a later one if it is much larger
         const bool grown = ms != -INFINITY && top > ms + 8.f;
         if (__any_sync(0xffffffffu, grown)) {
@@ -303,23 +326,30 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (ms == -INFINITY || grown) ms = fmaxf(ms, top);
         const float neg = -finite_max(ms);
-        float sum[4] = {};
+        const uint64_t sl2 = f2_pack(sl, sl), neg2 = f2_pack(neg, neg);
+        uint64_t sum[2] = {0ull, 0ull};
 #pragma unroll
-        for (int h = 0; h < 4; ++h) {
+        for (int h = 0; h < 4; ++h) {                          // 32 keys; the products may begin with the first 64
           uint32_t p[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float p0 = exp2_fast(fmaf(v[h * 32 + 2 * i], sl, neg)), p1 = exp2_fast(fmaf(v[h * 32 + 2 * i + 1], sl, neg));
-            sum[2 * (i & 1)] += p0;
-            sum[2 * (i & 1) + 1] += p1;
+            float p0, p1;
+            f2_unpack(f2_fma(v[h * 16 + i], sl2, neg2), p0, p1);
+            p0 = exp2_fast(p0);
+            p1 = exp2_fast(p1);
+            sum[i & 1] = f2_add(sum[i & 1], f2_pack(p0, p1));
             p[i] = bf16_pair(p0, p1);
           }
           tmem_st16(ts + h * 16, *reinterpret_cast<float (*)[16]>(p));
+          if (h & 1) {
+            tmem_wait_st();
+            tc_fence_before_sync();
+            mbar_arrive_warp(P_READY(c * 2 + (h >> 1)));
+          }
         }
-        tmem_wait_st();
-        tc_fence_before_sync();
-        mbar_arrive_warp(P_READY(c));
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        float s0, s1;
+        f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
+        l += s0 + s1;
       }
       if (!ok) break;
       if (x.tiles > 0) {

@@ -1836,7 +1836,7 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
   if (a.B == 0 || a.Lq == 0) return L;
   const long long rows = (long long)a.Lq * a.group;
   // (the tensor-core kernel finds a row's maximum before it scales)
-  L.tc = h->cfg.io_dtype == VDN_BF16 && !(h->cfg.flags & VDN_FLAG_FORCE_SIMT) && a.scale_log2 > 0.f && rows > 8;
+  L.tc = h->cfg.io_dtype == VDN_BF16 && !(h->cfg.flags & VDN_FLAG_FORCE_SIMT) && a.scale_log2 > 0.f && rows > 2;
   // keys of a batch row, by which parts are chosen (packed: the average)
   const long long keys = a.Lk ? a.Lk : a.n_keys / a.B;
   long long wanted, least;                              // parts, keys of a part
