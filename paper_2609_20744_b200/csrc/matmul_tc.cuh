@@ -113,23 +113,25 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         // (the even CTA's barriers count the copies of both; the odd one leaves with it, at the cluster's barrier)
         if (!ok && rank == 0) mbar_drain_ring(FULL(0), G::STAGES, it);
       }
-    } else if (warp == 9) {
-      if (lane == 0 && rank == 0) {
-        constexpr uint32_t idesc = make_idesc_e4m3(2 * G::ROWS, G::COLS);
-        uint32_t it = 0;
-        bool ok = true;
-        for (long long t = first; t < tiles && ok; t += step) {
-          for (int b = 0; b < p.blocks; ++b, ++it) {
-            const int st = it % G::STAGES, a = it & 1;
-            if (!mbar_wait(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) || !mbar_wait(FULL(st), (it / G::STAGES) & 1, wc)) { ok = false; break; }
-            tc_fence_after_sync();
-            const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
-            const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES + G::A_BYTES, 16, 1024);
+    } else if (warp == 9 && rank == 0) {
+      constexpr uint32_t idesc = make_idesc_e4m3(2 * G::ROWS, G::COLS);
+      uint32_t it = 0;
+      bool ok = true;
+      for (long long t = first; t < tiles && ok; t += step) {
+        for (int b = 0; b < p.blocks; ++b, ++it) {
+          const int st = it % G::STAGES, a = it & 1;
+          ok = mbar_wait_warp(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) && mbar_wait_warp(FULL(st), (it / G::STAGES) & 1, wc);
+          if (!ok) break;
+          tc_fence_after_sync();
+          const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
+          const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES + G::A_BYTES, 16, 1024);
+          if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) mma_e4m3_pair(tmem + a * G::COLS, da + k * 2, dw + k * 2, idesc, k ? 1u : 0u);
             mma_commit_pair(EMPTY(st));
             mma_commit_pair(ACCFULL(a));
           }
+          __syncwarp();
         }
       }
     }
@@ -345,20 +347,21 @@ matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       if (!ok) mbar_drain_ring(FULL(0), G::STAGES, it);
     }
   } else if (warp == 5) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = make_idesc_e4m3(128, TOK);
-      uint32_t it = 0;
-      for (int b = b_lo; b < b_hi; ++b, ++it) {
-        const int st = it % G::STAGES, a = it & 1;
-        if (!mbar_wait(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) || !mbar_wait(FULL(st), (it / G::STAGES) & 1, wc)) break;
-        tc_fence_after_sync();
-        const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
-        const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES + 128 * 128, 16, 1024);
+    constexpr uint32_t idesc = make_idesc_e4m3(128, TOK);
+    uint32_t it = 0;
+    for (int b = b_lo; b < b_hi; ++b, ++it) {
+      const int st = it % G::STAGES, a = it & 1;
+      if (!mbar_wait_warp(ACCEMPTY(a), ((it >> 1) & 1) ^ 1, wc) || !mbar_wait_warp(FULL(st), (it / G::STAGES) & 1, wc)) break;
+      tc_fence_after_sync();
+      const uint64_t dw = make_smem_desc(base + st * G::STAGE_BYTES, 16, 1024);
+      const uint64_t da = make_smem_desc(base + st * G::STAGE_BYTES + 128 * 128, 16, 1024);
+      if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) mma_e4m3_ss(tmem + a * TOK, dw + k * 2, da + k * 2, idesc, k ? 1u : 0u);
         mma_commit(EMPTY(st));
         mma_commit(ACCFULL(a));
       }
+      __syncwarp();
     }
   } else {
     // The factors of a block, one for each token, go through shared memory: a thread brings one token's and reads all.
