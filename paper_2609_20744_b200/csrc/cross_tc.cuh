@@ -11,7 +11,10 @@
 // Keys that do not count: their scores are replaced by -inf, their rows of V by zeros in shared memory (zero times what may
 // be anything is not zero).
 #pragma once
+#include <type_traits>
+
 #include "cross_simt.cuh"
+#include "quantize.cuh"
 #include "tc_common.cuh"
 #include "token_rule.cuh"
 #include "token_tc.cuh"
@@ -21,18 +24,19 @@ namespace vdn {
 struct CrossTcShape {
   int hb, tb;                 // heads and tokens of a row block
   int head_blocks;            // ceil(group / hb)
-  int pairs;                  // pairs of tiles of a (batch row, key head)
-  long long items;            // B * Hk * pairs * parts
+  int blocks, pairs;          // row blocks, and pairs of tiles, of a (batch row, key head)
+  FastDivide by_parts, by_pairs, by_heads, by_head_blocks;
+  uint32_t items;             // B * Hk * pairs * parts
 };
 
 template <int D>
 struct CrossTc {
   static constexpr int KEYS = 128, THREADS = 384, CHUNKS = D / 64;
   static constexpr int TILE_BYTES = 128 * D * 2, CHUNK_BYTES = 128 * 128, OUT_BYTES = 32 * 128;
-  static constexpr int STAGES = D == 128 ? 2 : 4;                       // of keys, and of values
-  static constexpr int OFF_Q = 0, OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + STAGES * TILE_BYTES, OFF_OUT = OFF_V + STAGES * TILE_BYTES;
-  static constexpr int OFF_BAR = OFF_OUT + 8 * OUT_BYTES;
-  static constexpr int BARS = 2 + 2 + 5 * STAGES + 2 + 4 + 2 + 2;
+  static constexpr int STAGES = D == 128 ? 3 : 6;                       // tiles of keys and values in turn
+  static constexpr int OFF_Q = 0, OFF_KV = 2 * TILE_BYTES, OFF_OUT = OFF_KV + STAGES * TILE_BYTES;
+  static constexpr int OFF_BAR = OFF_OUT + 8 * CHUNKS * OUT_BYTES;      // a warp's results: 32 rows, 64 channels at a time
+  static constexpr int BARS = 2 + 2 + 3 * STAGES + 2 + 4 + 2 + 2;
   static constexpr int USED_BYTES = OFF_BAR + 8 * BARS + 16, SMEM_BYTES = USED_BYTES + 1024;
   static constexpr int COL_S = 0, COL_O = 256, COLS = 512;              // tensor memory: S of both tiles, O of both
 };
@@ -44,18 +48,19 @@ struct CrossItem {
   long long start;
   bool second;                                  // the pair's second tile has rows
 };
-__device__ __forceinline__ CrossItem cross_item(const CrossArgs& a, const CrossTcShape& s, long long item) {
+__device__ __forceinline__ CrossItem cross_item(const CrossArgs& a, const CrossTcShape& s, uint32_t item) {
   CrossItem x;
-  x.part = (int)(item % a.parts); item /= a.parts;
-  x.pair = (int)(item % s.pairs); item /= s.pairs;
-  x.hk = (int)(item % a.Hk);
-  x.b = (int)(item / a.Hk);
+  uint32_t q = quotient(item, s.by_parts);
+  x.part = (int)(item - q * s.by_parts.d);
+  item = quotient(q, s.by_pairs);
+  x.pair = (int)(q - item * s.by_pairs.d);
+  x.b = (int)quotient(item, s.by_heads);
+  x.hk = (int)(item - (uint32_t)x.b * s.by_heads.d);
   int len;
   cross_range(a, x.b, x.start, len);
   cross_part(len, x.part, a.parts, 128, x.lo, x.hi);
   x.tiles = (x.hi - x.lo + 127) / 128;
-  const long long blocks = (long long)((a.Lq + s.tb - 1) / s.tb) * s.head_blocks;
-  x.second = ((long long)x.pair * 2 + 1) * 4 < blocks;
+  x.second = ((uint32_t)x.pair * 2 + 1) * 4 < (uint32_t)s.blocks;
   return x;
 }
 
@@ -71,15 +76,13 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   const uint32_t bar0 = base + G::OFF_BAR;
   auto Q_FULL = [&](int c) { return bar0 + 8u * c; };
   auto Q_EMPTY = [&](int c) { return bar0 + 8u * (2 + c); };
-  auto K_FULL = [&](int i) { return bar0 + 8u * (4 + i); };
-  auto K_EMPTY = [&](int i) { return bar0 + 8u * (4 + G::STAGES + i); };
-  auto V_FULL = [&](int i) { return bar0 + 8u * (4 + 2 * G::STAGES + i); };
-  auto V_READY = [&](int i) { return bar0 + 8u * (4 + 3 * G::STAGES + i); };
-  auto V_EMPTY = [&](int i) { return bar0 + 8u * (4 + 4 * G::STAGES + i); };
-  auto S_FULL = [&](int c) { return bar0 + 8u * (4 + 5 * G::STAGES + c); };
-  auto P_READY = [&](int c) { return bar0 + 8u * (6 + 5 * G::STAGES + c); };
-  auto O_FULL = [&](int c) { return bar0 + 8u * (10 + 5 * G::STAGES + c); };
-  auto O_EMPTY = [&](int c) { return bar0 + 8u * (12 + 5 * G::STAGES + c); };
+  auto FULL = [&](int i) { return bar0 + 8u * (4 + i); };
+  auto READY = [&](int i) { return bar0 + 8u * (4 + G::STAGES + i); };
+  auto EMPTY = [&](int i) { return bar0 + 8u * (4 + 2 * G::STAGES + i); };
+  auto S_FULL = [&](int c) { return bar0 + 8u * (4 + 3 * G::STAGES + c); };
+  auto P_READY = [&](int c) { return bar0 + 8u * (6 + 3 * G::STAGES + c); };
+  auto O_FULL = [&](int c) { return bar0 + 8u * (10 + 3 * G::STAGES + c); };
+  auto O_EMPTY = [&](int c) { return bar0 + 8u * (12 + 3 * G::STAGES + c); };
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(base_ptr + G::OFF_BAR + 8 * G::BARS);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const WaitCtx wc(abort_flag, ds);
@@ -93,8 +96,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       mbar_init(O_FULL(c), 1); mbar_init(O_EMPTY(c), 4);
     }
     for (int i = 0; i < G::STAGES; ++i) {
-      mbar_init(K_FULL(i), 1); mbar_init(K_EMPTY(i), 1);
-      mbar_init(V_FULL(i), 1); mbar_init(V_READY(i), 1); mbar_init(V_EMPTY(i), 1);
+      mbar_init(FULL(i), 1); mbar_init(READY(i), 1); mbar_init(EMPTY(i), 1);
     }
     *abort_flag = 0;
     mbar_fence_init();
@@ -117,55 +119,52 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     if (warp == 8) {
       // ------------------------------------------------------------------ copies
       if (lane == 0) {
-        uint32_t kv = 0, q[2] = {0, 0};
+        uint32_t n = 0, q[2] = {0, 0};                       // tiles so far: keys and values in turn
         bool ok = true;
-        for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
+        for (uint32_t item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
           const CrossItem x = cross_item(a, s, item);
           if (x.tiles == 0) continue;
           auto load_q = [&](int c) {
             if (!mbar_wait(Q_EMPTY(c), (q[c] & 1) ^ 1, wc)) return false;
             mbar_arrive_expect_tx(Q_FULL(c), 4 * G::CHUNKS * block_rows * 128);
             for (int w = 0; w < 4; ++w) {
-              const int rb = (x.pair * 2 + c) * 4 + w;
-              const int tok = rb / s.head_blocks * s.tb, head = rb % s.head_blocks * s.hb;
+              const uint32_t rb = (uint32_t)(x.pair * 2 + c) * 4 + w, tb = quotient(rb, s.by_head_blocks);
               for (int i = 0; i < G::CHUNKS; ++i)
-                tma_load_5d(base + G::OFF_Q + c * G::TILE_BYTES + i * G::CHUNK_BYTES + w * 32 * 128, &tmQ, Q_FULL(c), i * 64, head, x.hk, tok, x.b);
+                tma_load_5d(base + G::OFF_Q + c * G::TILE_BYTES + i * G::CHUNK_BYTES + w * 32 * 128, &tmQ, Q_FULL(c), i * 64,
+                            (int)(rb - tb * s.head_blocks) * s.hb, x.hk, (int)tb * s.tb, x.b);
             }
             ++q[c];
             return true;
           };
-          auto load = [&](const CUtensorMap* m, uint32_t full, uint32_t empty, int off, int j) {
-            if (!mbar_wait(empty, ((kv / G::STAGES) & 1) ^ 1, wc)) return false;
-            mbar_arrive_expect_tx(full, G::TILE_BYTES);
+          auto load = [&](const CUtensorMap* m, int j) {
+            const uint32_t st = n % G::STAGES;
+            if (!mbar_wait(EMPTY(st), ((n / G::STAGES) & 1) ^ 1, wc)) return false;
+            mbar_arrive_expect_tx(FULL(st), G::TILE_BYTES);
             for (int i = 0; i < G::CHUNKS; ++i)
-              tma_load_3d(base + off + (kv % G::STAGES) * G::TILE_BYTES + i * G::CHUNK_BYTES, m, full, i * 64, x.hk, (int)(x.start + x.lo + j * 128));
+              tma_load_3d(base + G::OFF_KV + st * G::TILE_BYTES + i * G::CHUNK_BYTES, m, FULL(st), i * 64, x.hk, (int)(x.start + x.lo + j * 128));
+            ++n;
             return true;
           };
           ok = load_q(0);
-          for (int j = 0; j < x.tiles && ok; ++j, ++kv) {
-            const int st = kv % G::STAGES;
-            ok = load(&tmK, K_FULL(st), K_EMPTY(st), G::OFF_K, j);
-            if (ok && j == 0 && x.second) ok = load_q(1);
-            if (ok) ok = load(&tmV, V_FULL(st), V_EMPTY(st), G::OFF_V, j);
-          }
+          for (int j = 0; j < x.tiles && ok; ++j)
+            ok = load(&tmK, j) && (j > 0 || !x.second || load_q(1)) && load(&tmV, j);
         }
-        if (!ok) {
-          // a bounded chance for what is under way to land (the last tile of values may not have been asked for: bounded all the same)
+        if (!ok) {                                             // a bounded chance for what is under way to land
           for (int c = 0; c < 2; ++c)
             if (q[c]) mbar_drain(Q_FULL(c), (q[c] - 1) & 1);
-          mbar_drain_ring(K_FULL(0), G::STAGES, kv);
-          mbar_drain_ring(V_FULL(0), G::STAGES, kv);
+          mbar_drain_ring(FULL(0), G::STAGES, n);
         }
       }
     } else if (warp == 9) {
       // ------------------------------------------------------------------ products
       constexpr uint32_t id_s = make_idesc_bf16(128, 128, false, false), id_o = make_idesc_bf16(128, D, false, true);
-      uint32_t kv = 0, n_item[2] = {0, 0}, n_p[2] = {0, 0};
+      uint32_t n = 0, n_item[2] = {0, 0}, n_p[2] = {0, 0};
       bool ok = true;
-      auto scores = [&](int c, uint32_t at) {
-        const uint32_t st = at % G::STAGES;
+      auto arrived = [&](uint32_t r) { return mbar_wait_warp(READY(r % G::STAGES), (r / G::STAGES) & 1, wc); };
+      auto scores = [&](int c, uint32_t r, bool last_of_k, bool last_of_q) {
+        const uint32_t st = r % G::STAGES;
         const uint64_t dq = make_smem_desc(base + G::OFF_Q + c * G::TILE_BYTES, 16, 1024);
-        const uint64_t dk = make_smem_desc(base + G::OFF_K + st * G::TILE_BYTES, 16, 1024);
+        const uint64_t dk = make_smem_desc(base + G::OFF_KV + st * G::TILE_BYTES, 16, 1024);
         if (elect_one()) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
@@ -173,32 +172,30 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             mma_bf16_ss(tmem + G::COL_S + c * 128, dq + off, dk + off, id_s, k ? 1u : 0u);
           }
           mma_commit(S_FULL(c));
+          if (last_of_k) mma_commit(EMPTY(st));
+          if (last_of_q) mma_commit(Q_EMPTY(c));
         }
         __syncwarp();
       };
-      auto commit = [&](uint32_t bar) {
-        if (elect_one()) mma_commit(bar);
-        __syncwarp();
-      };
-      for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
+      for (uint32_t item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
         const CrossItem x = cross_item(a, s, item);
         if (x.tiles == 0) continue;
         const int chains = x.second ? 2 : 1;
+        ok = arrived(n);
         for (int c = 0; c < chains && ok; ++c) {
-          ok = mbar_wait_warp(Q_FULL(c), n_item[c] & 1, wc) && mbar_wait_warp(K_FULL(kv % G::STAGES), (kv / G::STAGES) & 1, wc);
+          ok = mbar_wait_warp(Q_FULL(c), n_item[c] & 1, wc);
           if (!ok) break;
           tc_fence_after_sync();
-          scores(c, kv);
+          scores(c, n, c + 1 == chains, x.tiles == 1);
         }
-        if (!ok) break;
-        commit(K_EMPTY(kv % G::STAGES));
-        if (x.tiles == 1)
-          for (int c = 0; c < chains; ++c) commit(Q_EMPTY(c));
-        for (int j = 0; j < x.tiles && ok; ++j, ++kv) {
-          const uint32_t st = kv % G::STAGES, next = kv + 1;
-          const uint64_t dv = make_smem_desc(base + G::OFF_V + st * G::TILE_BYTES, G::CHUNK_BYTES, 1024);
-          for (int c = 0; c < chains; ++c) {
-            ok = mbar_wait_warp(V_READY(st), (kv / G::STAGES) & 1, wc) && (j > 0 || mbar_wait_warp(O_EMPTY(c), (n_item[c] & 1) ^ 1, wc));
+        for (int j = 0; j < x.tiles && ok; ++j, n += 2) {
+          const uint32_t st = (n + 1) % G::STAGES;
+          const uint64_t dv = make_smem_desc(base + G::OFF_KV + st * G::TILE_BYTES, G::CHUNK_BYTES, 1024);
+          const bool more = j + 1 < x.tiles;
+          // all else that the products wait for comes before P, and once: a wait takes about as long as what is queued lasts
+          ok = arrived(n + 1) && (!more || arrived(n + 2));
+          for (int c = 0; c < chains && ok; ++c) {
+            if (j == 0) ok = mbar_wait_warp(O_EMPTY(c), (n_item[c] & 1) ^ 1, wc);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
               ok = ok && mbar_wait_warp(P_READY(2 * c + half), n_p[c] & 1, wc);
@@ -209,50 +206,45 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 for (int k = half * 4; k < half * 4 + 4; ++k)
                   mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, k || j ? 1u : 0u);
                 if (half == 1) {
-                  if (j + 1 == x.tiles) mma_commit(O_FULL(c));
-                  if (c + 1 == chains) mma_commit(V_EMPTY(st));
+                  if (!more) mma_commit(O_FULL(c));
+                  if (c + 1 == chains) mma_commit(EMPTY(st));
                 }
               }
               __syncwarp();
             }
             if (!ok) break;
             ++n_p[c];
-            if (j + 1 < x.tiles) {
-              ok = mbar_wait_warp(K_FULL(next % G::STAGES), (next / G::STAGES) & 1, wc);
-              if (!ok) break;
-              tc_fence_after_sync();
-              scores(c, next);
-              if (c + 1 == chains) commit(K_EMPTY(next % G::STAGES));
-              if (j + 2 == x.tiles) commit(Q_EMPTY(c));
-            }
+            if (more) scores(c, n + 2, c + 1 == chains, j + 2 == x.tiles);
           }
         }
         for (int c = 0; c < chains; ++c) ++n_item[c];
       }
     } else if (warp == 10) {
       // ------------------------------------------------------------------ values that do not count become zeros
-      uint32_t kv = 0;
+      uint32_t n = 0;
       bool ok = true;
-      for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
+      for (uint32_t item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
         const CrossItem x = cross_item(a, s, item);
-        for (int j = 0; j < x.tiles && ok; ++j, ++kv) {
-          const uint32_t st = kv % G::STAGES;
-          uint32_t on[4];
+        for (int j = 0; j < 2 * x.tiles && ok; ++j, ++n) {
+          const uint32_t st = n % G::STAGES;
+          uint32_t on[4] = {~0u, ~0u, ~0u, ~0u};
+          if (j & 1) {                                             // (tiles of keys pass)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int key = x.lo + j * 128 + i * 32 + lane;
-            on[i] = __ballot_sync(0xffffffffu, key < x.hi && key_counts(a, x.start + key));
+            for (int i = 0; i < 4; ++i) {
+              const int key = x.lo + (j >> 1) * 128 + i * 32 + lane;
+              on[i] = __ballot_sync(0xffffffffu, key < x.hi && key_counts(a, x.start + key));
+            }
           }
-          ok = __all_sync(0xffffffffu, mbar_wait(V_FULL(st), (kv / G::STAGES) & 1, wc));
+          ok = mbar_wait_warp(FULL(st), (n / G::STAGES) & 1, wc);
           if (!ok) break;
           if ((on[0] & on[1] & on[2] & on[3]) != 0xffffffffu) {
-            unsigned char* v = base_ptr + G::OFF_V + st * G::TILE_BYTES;
+            unsigned char* v = base_ptr + G::OFF_KV + st * G::TILE_BYTES;
             for (int r = lane / 8; r < 128; r += 4)                 // eight lanes to a row's 128 bytes
               if (!((on[r >> 5] >> (r & 31)) & 1u))
                 for (int i = 0; i < G::CHUNKS; ++i) *reinterpret_cast<uint4*>(v + i * G::CHUNK_BYTES + r * 128 + (lane & 7) * 16) = make_uint4(0, 0, 0, 0);
             fence_proxy_async_smem();
           }
-          mbar_arrive_warp(V_READY(st));
+          mbar_arrive_warp(READY(st));
         }
       }
     }
@@ -261,19 +253,21 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     registers_more<216>();
     const int c = warp >> 2, qd = warp & 3;
     const uint32_t ts = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_S + c * 128, to = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_O + c * D;
-    const uint32_t out_smem = base + G::OFF_OUT + warp * G::OUT_BYTES;
-    unsigned char* out_row = base_ptr + G::OFF_OUT + warp * G::OUT_BYTES + lane * 128;
     const float sl = a.scale_log2;
+    const int lane_head = lane % s.hb, lane_tok = lane / s.hb;
+    const uint32_t out_smem = base + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES;
+    unsigned char* out_row = base_ptr + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES + lane * 128;
     uint32_t n_s = 0, n_item = 0;
     bool ok = true;
-    for (long long item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
+    for (uint32_t item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
       const CrossItem x = cross_item(a, s, item);
       if (c == 1 && !x.second) continue;
-      const int rb = (x.pair * 2 + c) * 4 + qd;
-      const int tok0 = rb / s.head_blocks * s.tb, head0 = rb % s.head_blocks * s.hb;
-      const int head_in = head0 + lane % s.hb, tok = tok0 + lane / s.hb;
+      const uint32_t rb = (uint32_t)(x.pair * 2 + c) * 4 + qd, block = quotient(rb, s.by_head_blocks);
+      const int tok0 = (int)block * s.tb, head0 = (int)(rb - block * s.head_blocks) * s.hb;
+      const int head_in = head0 + lane_head, tok = tok0 + lane_tok;
       const bool row_on = lane < block_rows && head_in < a.group && tok < a.Lq;
-      float ms = -INFINITY, l = 0.f;                           // the maximum times sl, the sum relative to it
+      float ms = -INFINITY;                                    // the maximum times sl,
+      uint64_t sum[2] = {0ull, 0ull};                          // and the sum relative to it, in four parts
       for (int j = 0; j < x.tiles; ++j, ++n_s) {
         const int key0 = x.lo + j * 128;
         uint32_t on[4];
@@ -288,68 +282,78 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (!mbar_wait(S_FULL(c), n_s & 1, wc)) { ok = false; break; }
         tc_fence_after_sync();
-        uint64_t v[64];                                        // two neighbouring scores each
-        tmem_ld128_pairs(ts, v);
-        if (!all) {
+        // (twice, so that a tile whose keys all count has no branch in it: those cost 6 % of a long encoder's time)
+        auto weights = [&](auto cut) {
+          constexpr bool CUT = decltype(cut)::value;
+          uint64_t v[64];                                      // two neighbouring scores each
+          tmem_ld128_pairs(ts, v);
+          float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 64; ++i) {
-            float x0, x1;
-            f2_unpack(v[i], x0, x1);
-            if (!((on[i >> 4] >> (2 * i & 31)) & 1u)) x0 = -INFINITY;
-            if (!((on[i >> 4] >> ((2 * i + 1) & 31)) & 1u)) x1 = -INFINITY;
-            v[i] = f2_pack(x0, x1);
+          for (int g = 0; g < 4; ++g) {
+            if (CUT && on[g] != 0xffffffffu) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float x0, x1;
+                f2_unpack(v[g * 16 + i], x0, x1);
+                v[g * 16 + i] = f2_pack((on[g] >> (2 * i)) & 1u ? x0 : -INFINITY, (on[g] >> (2 * i + 1)) & 1u ? x1 : -INFINITY);
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x0, x1;
+              f2_unpack(v[g * 16 + i], x0, x1);
+              tops[i & 3] = fmaxf(fmaxf(tops[i & 3], x0), x1);
+            }
           }
-        }
-        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-        for (int i = 0; i < 64; ++i) {
-          float x0, x1;
-          f2_unpack(v[i], x0, x1);
-          tops[i & 3] = fmaxf(fmaxf(tops[i & 3], x0), x1);
-        }
-        const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * sl;
-        // the first finite maximum is taken over as it is (O is zero, or about to be overwritten), a later one if it is much larger
-        const bool grown = ms != -INFINITY && top > ms + 8.f;
-        if (__any_sync(0xffffffffu, grown)) {
-          const float keep = grown ? exp2_fast(ms - top) : 1.f;
-          l *= keep;
+          const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * sl;
+          // the first finite maximum is taken over as it is (O is zero, or about to be overwritten), a later one if it is much larger
+          const bool grown = ms != -INFINITY && top > ms + 8.f;
+          if (__any_sync(0xffffffffu, grown)) {
+            const float keep = grown ? exp2_fast(ms - top) : 1.f;
+            const uint64_t keep2 = f2_pack(keep, keep);
+            sum[0] = f2_fma(sum[0], keep2, 0ull);
+            sum[1] = f2_fma(sum[1], keep2, 0ull);
 #pragma unroll 1
-          for (int i = 0; i < D; i += 16) {
-            float o[16];
-            tmem_ld16(to + i, o);
-            tmem_wait_ld();
+            for (int i = 0; i < D; i += 16) {
+              float o[16];
+              tmem_ld16(to + i, o);
+              tmem_wait_ld();
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] *= keep;
-            tmem_st16(to + i, o);
-          }
-          tmem_wait_st();
-        }
-        if (ms == -INFINITY || grown) ms = fmaxf(ms, top);
-        const float neg = -finite_max(ms);
-        const uint64_t sl2 = f2_pack(sl, sl), neg2 = f2_pack(neg, neg);
-        uint64_t sum[2] = {0ull, 0ull};
-#pragma unroll
-        for (int h = 0; h < 4; ++h) {                          // 32 keys; the products may begin with the first 64
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float p0, p1;
-            f2_unpack(f2_fma(v[h * 16 + i], sl2, neg2), p0, p1);
-            p0 = exp2_fast(p0);
-            p1 = exp2_fast(p1);
-            sum[i & 1] = f2_add(sum[i & 1], f2_pack(p0, p1));
-            p[i] = bf16_pair(p0, p1);
-          }
-          tmem_st16(ts + h * 16, *reinterpret_cast<float (*)[16]>(p));
-          if (h & 1) {
+              for (int e = 0; e < 16; ++e) o[e] *= keep;
+              tmem_st16(to + i, o);
+            }
             tmem_wait_st();
-            tc_fence_before_sync();
-            mbar_arrive_warp(P_READY(c * 2 + (h >> 1)));
           }
-        }
-        float s0, s1;
-        f2_unpack(f2_add(sum[0], sum[1]), s0, s1);
-        l += s0 + s1;
+          if (ms == -INFINITY || grown) ms = fmaxf(ms, top);
+          const float neg = -finite_max(ms);
+          const uint64_t sl2 = f2_pack(sl, sl), neg2 = f2_pack(neg, neg);
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {                        // 32 keys; the products may begin with the first 64
+            uint32_t p[16];
+            if (!CUT || on[g] != 0) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float p0, p1;
+                f2_unpack(f2_fma(v[g * 16 + i], sl2, neg2), p0, p1);
+                p0 = exp2_fast(p0);
+                p1 = exp2_fast(p1);
+                sum[i & 1] = f2_add(sum[i & 1], f2_pack(p0, p1));
+                p[i] = bf16_pair(p0, p1);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) p[i] = 0u;
+            }
+            tmem_st16(ts + g * 16, *reinterpret_cast<float (*)[16]>(p));
+            if (g & 1) {
+              tmem_wait_st();
+              tc_fence_before_sync();
+              mbar_arrive_warp(P_READY(c * 2 + (g >> 1)));
+            }
+          }
+        };
+        if (all) weights(std::false_type{});
+        else weights(std::true_type{});
       }
       if (!ok) break;
       if (x.tiles > 0) {
@@ -357,17 +361,27 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         ++n_item;
         tc_fence_after_sync();
       }
+      float l, l1;
+      f2_unpack(f2_add(sum[0], sum[1]), l, l1);
+      l += l1;
       const long long token = (long long)x.b * a.Lq + tok;
-      const int head = x.hk * a.group + head_in;
-      const long long at = token * a.H + head;
-      const float r = a.parts > 1 ? 1.f : l == 0.f ? 0.f : 1.f / l;
-#pragma unroll 1
+      const long long at = token * a.H + x.hk * a.group + head_in;
+      const float r = l == 0.f ? 0.f : 1.f / l;
+      if (a.parts == 1) {
+        tma_store_wait_read<0>();                              // (only lane 0 has any) the last item's stores
+        __syncwarp();
+      }
+#pragma unroll
       for (int i = 0; i < G::CHUNKS; ++i) {
         float o[64];
         if (x.tiles > 0) {
           tmem_ld32(to + i * 64, *reinterpret_cast<float (*)[32]>(o));
           tmem_ld32(to + i * 64 + 32, *reinterpret_cast<float (*)[32]>(o + 32));
           tmem_wait_ld();
+          if (i + 1 == G::CHUNKS) {
+            tc_fence_before_sync();
+            mbar_arrive_warp(O_EMPTY(c));
+          }
         } else {
 #pragma unroll
           for (int e = 0; e < 64; ++e) o[e] = 0.f;
@@ -379,24 +393,21 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             for (int e = 0; e < 64; e += 4) store4(dst + e, make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]));
           }
         } else {
-          tma_store_wait_read<0>();                            // (only lane 0 has any) the store that last read this buffer
-          __syncwarp();
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            *reinterpret_cast<uint4*>(out_row + ((e ^ (lane & 7)) * 16)) =
+            *reinterpret_cast<uint4*>(out_row + i * G::OUT_BYTES + ((e ^ (lane & 7)) * 16)) =
                 make_uint4(bf16_pair(o[8 * e] * r, o[8 * e + 1] * r), bf16_pair(o[8 * e + 2] * r, o[8 * e + 3] * r),
                            bf16_pair(o[8 * e + 4] * r, o[8 * e + 5] * r), bf16_pair(o[8 * e + 6] * r, o[8 * e + 7] * r));
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            if (tok0 < a.Lq) tma_store_5d(&tmOut, out_smem, i * 64, head0, x.hk, tok0, x.b);
-            tma_store_commit();
-          }
         }
       }
-      if (x.tiles > 0) {
-        tc_fence_before_sync();
-        mbar_arrive_warp(O_EMPTY(c));
+      if (a.parts == 1) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (tok0 < a.Lq)
+            for (int i = 0; i < G::CHUNKS; ++i) tma_store_5d(&tmOut, out_smem + i * G::OUT_BYTES, i * 64, head0, x.hk, tok0, x.b);
+          tma_store_commit();
+        }
       }
       if (row_on) {
         if (a.parts > 1) a.part_ml[at * a.parts + x.part] = make_float2(ms, l);

@@ -1846,7 +1846,11 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     s.tb = 32 / s.hb;
     s.head_blocks = (a.group + s.hb - 1) / s.hb;
     const long long blocks = (long long)((a.Lq + s.tb - 1) / s.tb) * s.head_blocks;
+    s.blocks = (int)blocks;
     s.pairs = (int)((blocks + 7) / 8);
+    s.by_pairs = vdn::fast_divide((uint32_t)s.pairs);
+    s.by_heads = vdn::fast_divide((uint32_t)a.Hk);
+    s.by_head_blocks = vdn::fast_divide((uint32_t)s.head_blocks);
     L.units = (long long)a.B * a.Hk * s.pairs;
     wanted = h->sm_count / L.units;
     least = 256;
@@ -1857,7 +1861,8 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     least = 128;
   }
   L.parts = (int)std::max(1LL, std::min({wanted, keys / least, 256LL}));
-  L.shape.items = L.units * L.parts;
+  L.shape.items = (uint32_t)(L.units * L.parts);         // (refused where that does not fit)
+  L.shape.by_parts = vdn::fast_divide((uint32_t)L.parts);
   if (L.parts > 1) {
     const size_t n = (size_t)a.B * a.Lq * a.H * L.parts;
     L.o = 0;
