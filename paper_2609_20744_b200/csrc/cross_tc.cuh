@@ -38,6 +38,9 @@ struct CrossTc {
   static constexpr int OFF_BAR = OFF_OUT + 8 * CHUNKS * OUT_BYTES;      // a warp's results: 32 rows, 64 channels at a time
   static constexpr int BARS = 2 + 2 + 3 * STAGES + 2 + 4 + 2 + 2;
   static constexpr int USED_BYTES = OFF_BAR + 8 * BARS + 16, SMEM_BYTES = USED_BYTES + 1024;
+  // P is handed over as a whole (d = 128), or in halves (d = 64: products are short, and waiting for the second half costs less than
+  // starting late).  16384 x 16384: d = 128 1679 us whole, 1733 in halves; d = 64 1528, 1435.
+  static constexpr int P_PARTS = D == 128 ? 1 : 2;
   static constexpr int COL_S = 0, COL_O = 256, COLS = 512;              // tensor memory: S of both tiles, O of both
 };
 static_assert(CrossTc<128>::SMEM_BYTES <= 232448, "shared memory of a CTA");
@@ -192,20 +195,21 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           const uint32_t st = (n + 1) % G::STAGES;
           const uint64_t dv = make_smem_desc(base + G::OFF_KV + st * G::TILE_BYTES, G::CHUNK_BYTES, 1024);
           const bool more = j + 1 < x.tiles;
-          // all else that the products wait for comes before P, and once: a wait takes about as long as what is queued lasts
-          ok = arrived(n + 1) && (!more || arrived(n + 2));
+          // (a tile is waited for once; the next keys early only where there are stages for them to have come long ago)
+          constexpr bool EARLY = G::STAGES > 3;
+          ok = arrived(n + 1) && (!EARLY || !more || arrived(n + 2));
           for (int c = 0; c < chains && ok; ++c) {
             if (j == 0) ok = mbar_wait_warp(O_EMPTY(c), (n_item[c] & 1) ^ 1, wc);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              ok = ok && mbar_wait_warp(P_READY(2 * c + half), n_p[c] & 1, wc);
+            for (int part = 0; part < G::P_PARTS; ++part) {
+              ok = ok && mbar_wait_warp(P_READY(2 * c + part), n_p[c] & 1, wc);
               if (!ok) break;
               tc_fence_after_sync();
               if (elect_one()) {
 #pragma unroll
-                for (int k = half * 4; k < half * 4 + 4; ++k)
+                for (int k = part * (8 / G::P_PARTS); k < (part + 1) * (8 / G::P_PARTS); ++k)
                   mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, k || j ? 1u : 0u);
-                if (half == 1) {
+                if (part + 1 == G::P_PARTS) {
                   if (!more) mma_commit(O_FULL(c));
                   if (c + 1 == chains) mma_commit(EMPTY(st));
                 }
@@ -214,7 +218,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             }
             if (!ok) break;
             ++n_p[c];
-            if (more) scores(c, n + 2, c + 1 == chains, j + 2 == x.tiles);
+            if (!EARLY && more && c == 0) ok = arrived(n + 2);
+            if (more && ok) scores(c, n + 2, c + 1 == chains, j + 2 == x.tiles);
           }
         }
         for (int c = 0; c < chains; ++c) ++n_item[c];
@@ -328,7 +333,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           const float neg = -finite_max(ms);
           const uint64_t sl2 = f2_pack(sl, sl), neg2 = f2_pack(neg, neg);
 #pragma unroll
-          for (int g = 0; g < 4; ++g) {                        // 32 keys; the products may begin with the first 64
+          for (int g = 0; g < 4; ++g) {                        // 32 keys
             uint32_t p[16];
             if (!CUT || on[g] != 0) {
 #pragma unroll
@@ -345,10 +350,10 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
               for (int i = 0; i < 16; ++i) p[i] = 0u;
             }
             tmem_st16(ts + g * 16, *reinterpret_cast<float (*)[16]>(p));
-            if (g & 1) {
+            if ((g + 1) % (4 / G::P_PARTS) == 0) {
               tmem_wait_st();
               tc_fence_before_sync();
-              mbar_arrive_warp(P_READY(c * 2 + (g >> 1)));
+              mbar_arrive_warp(P_READY(c * 2 + g / (4 / G::P_PARTS)));
             }
           }
         };
