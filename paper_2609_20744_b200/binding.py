@@ -379,23 +379,35 @@ def _matrix(name, x, shape, dtype, on_cuda, device_index, step_bytes=0):
     return step
 
 
+def _glance(x, shape, dtype, on_cuda, device_index):
+    """Whether x is dense and just so, as in all likelihood it is."""
+    return x is not None and x.dtype is dtype and x.shape == shape and x.get_device() == (device_index if on_cuda else -1) and x.is_contiguous()
+
+
 def validate_matmul_args(io_dtype, device_index, a, a_scale, w, w_scale, bias=None, add=None, out=None, on_cuda=True):
     """Checks the tensors of scaled_matmul: a [..., K], w [N, K] (float8_e4m3fn), a_scale [..., blocks], w_scale [.., blocks], bias [N],
     add and out [..., N].  Returns (M, N, K, strides of a, w, add, out)."""
-    import torch
     if a is None or a.dim() < 1 or w is None or w.dim() != 2:
         raise ValueError("a must have shape [..., K] and w [N, K]")
-    lead, k, n = tuple(a.shape[:-1]), a.shape[-1], w.shape[0]
+    e4m3, f32 = _e4m3(), _float32()
+    sa_, sw_ = a.shape, w.shape
+    lead, k, n = tuple(sa_[:-1]), sa_[-1], sw_[0]
     blocks = -(-k // SCALE_BLOCK)
-    e4m3, f32 = torch.float8_e4m3fn, torch.float32
-    sa = _matrix("a", a, (*lead, k), e4m3, on_cuda, device_index, 16)
-    sw = _matrix("w", w, (n, k), e4m3, on_cuda, device_index, 16)
+    dense = k % 16 == 0
+    sa = k if dense and _glance(a, sa_, e4m3, on_cuda, device_index) else _matrix("a", a, (*lead, k), e4m3, on_cuda, device_index, 16)
+    sw = k if dense and _glance(w, (n, k), e4m3, on_cuda, device_index) else _matrix("w", w, (n, k), e4m3, on_cuda, device_index, 16)
     _dense("a_scale", a_scale, (*lead, blocks), f32, on_cuda, device_index)
     _dense("w_scale", w_scale, (-(-n // SCALE_BLOCK), blocks), f32, on_cuda, device_index)
     if bias is not None:
         _dense("bias", bias, (n,), f32, on_cuda, device_index)
-    sd = 0 if add is None else _matrix("add", add, (*lead, n), io_dtype, on_cuda, device_index)
-    so = n if out is None else _matrix("out", out, (*lead, n), io_dtype, on_cuda, device_index)
+    shape = (*lead, n)
+    sd = so = n
+    if add is None:
+        sd = 0
+    elif not _glance(add, shape, io_dtype, on_cuda, device_index):
+        sd = _matrix("add", add, shape, io_dtype, on_cuda, device_index)
+    if out is not None and not _glance(out, shape, io_dtype, on_cuda, device_index):
+        so = _matrix("out", out, shape, io_dtype, on_cuda, device_index)
     m = 1
     for x in lead:
         m *= x
@@ -437,6 +449,17 @@ def validate_cross_args(io_dtype, d_handle, device_index, q, k, v, cu_seqlens=No
     for x in qs[1:-2]:
         n *= x
     return B, n, lead[-1], H, Hk, strides
+
+
+_E4M3 = None
+
+
+def _e4m3():
+    global _E4M3
+    if _E4M3 is None:
+        import torch
+        _E4M3 = torch.float8_e4m3fn
+    return _E4M3
 
 
 def _float32():
@@ -757,9 +780,9 @@ class Vda:
             raise ValueError("rows must be 1 or 128")
         if x is None or x.dim() < 1 or (rows != 1 and x.dim() != 2):
             raise ValueError("x must have shape " + ("[..., K]" if rows == 1 else "[N, K]"))
-        shape = tuple(x.shape)
+        shape = x.shape
         k = shape[-1]
-        xs = _matrix("x", x, shape, self.torch_dtype, True, dev)
+        xs = k if _glance(x, shape, self.torch_dtype, True, dev) else _matrix("x", x, tuple(shape), self.torch_dtype, True, dev)
         n = 1
         for s in shape[:-1]:
             n *= s
@@ -767,11 +790,14 @@ class Vda:
         streams = self._streams(stream)
         pitch = -(-k // 16) * 16
         if out is None:
-            out = self._new(streams, (*shape[:-1], pitch), torch.float8_e4m3fn)
-            if pitch != k:
-                out = out[..., :k]
+            if pitch == k and streams[1] is None and x.is_contiguous():
+                out = torch.empty_like(x, dtype=torch.float8_e4m3fn)
+            else:
+                out = self._new(streams, (*shape[:-1], pitch), torch.float8_e4m3fn)
+                if pitch != k:
+                    out = out[..., :k]
         else:
-            pitch = _matrix("out", out, shape, torch.float8_e4m3fn, True, dev, 16)
+            pitch = _matrix("out", out, tuple(shape), torch.float8_e4m3fn, True, dev, 16)
         want = (*shape[:-1], blocks) if rows == 1 else (-(-n // SCALE_BLOCK), blocks)
         if scale is None:
             scale = self._new(streams, want, torch.float32)
@@ -792,7 +818,7 @@ class Vda:
         m, n, k, st = validate_matmul_args(self.torch_dtype, self.device, a, a_scale, w, w_scale, bias, add, out)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, (*a.shape[:-1], n), self.torch_dtype)
+            out = self._new(streams, (*a.shape[:-1], n), self.torch_dtype) if add is None else self._new_like(streams, add)
         prm = _MATMUL_PARAMS.pack(_MATMUL_PARAMS.size, 0, a_scale.data_ptr(), w_scale.data_ptr(), _ptr(bias), _ptr(add), *st)
         r = self.lib.vdn_vda_scaled_matmul(self.h, a.data_ptr(), w.data_ptr(), out.data_ptr(), m, n, k, prm, streams[0])
         if r:

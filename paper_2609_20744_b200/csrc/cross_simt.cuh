@@ -11,6 +11,7 @@
 // behind a sequence or under the mask may be anything, NaN too.
 #pragma once
 #include "common.cuh"
+#include "token_rule.cuh"
 
 namespace vdn {
 
@@ -86,6 +87,7 @@ __global__ void __launch_bounds__(256) cross_few_kernel(CrossArgs a) {
   constexpr int STEP = WARPS * SLOTS * U;
   __shared__ float so[WARPS][R][D];
   __shared__ float2 sml[WARPS][R];
+  if (a.parts > 1) let_next_kernel_start();
   const int tiles = (a.Lq * a.group + R - 1) / R;
   long long unit = blockIdx.x;
   const int part = (int)(unit % a.parts); unit /= a.parts;
@@ -206,6 +208,7 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
   extern __shared__ __align__(16) float smem[];
   float *sq = smem, *sk = smem + S::OFF_K, *sv = smem + S::OFF_V, *sp = smem + S::OFF_P;
   int* son = reinterpret_cast<int*>(smem + S::OFF_ON);
+  if (a.parts > 1) let_next_kernel_start();
   const int tiles = (int)(((long long)a.Lq * a.group + S::ROWS - 1) / S::ROWS);
   long long unit = blockIdx.x;
   const int part = (int)(unit % a.parts); unit /= a.parts;
@@ -313,10 +316,11 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- parts
-// A warp to a (token, head).
+// A warp to a (token, head).  Starts while its predecessor runs.
 template <typename Tio, int D>
 __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs a) {
   constexpr int N = D / 32;
+  wait_for_kernel_before();
   const long long at = (long long)blockIdx.x * 8 + threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
   if (at >= (long long)a.B * a.Lq * a.H) return;

@@ -90,6 +90,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   const WaitCtx wc(abort_flag, ds);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (a.parts > 1) let_next_kernel_start();
 
   if (threadIdx.x == 0) {
     for (int c = 0; c < 2; ++c) {

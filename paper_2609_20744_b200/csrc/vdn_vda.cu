@@ -110,6 +110,7 @@ struct vdn_vda_s {
   bool attrs_set = false;
   bool tc_attrs_set = false;
   bool token_attrs_set = false;
+  unsigned block_attrs_set = 0;    // kernels around the layer whose shared-memory attribute has been set
   unsigned ro_attrs_set = 0;       // read-out instantiations whose shared-memory attribute has been set
   int ro_short = 1;                // use the short-frame read-out layout where it applies (VDN_RO_SHORT=0 turns it off)
   // More scan chains than SMs: the surplus chains run on a side stream beside the read-out of the others
@@ -1705,6 +1706,16 @@ vdn_status make_bytes_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, CUtensor
   return VDN_OK;
 }
 
+// Lets a kernel have its shared memory, once for a handle: `which` numbers the kernels of these entry points.
+enum BlockKernel { kMatmulPair, kMatmulPairAdd, kMatmulSlim, kCrossTc = kMatmulSlim + 4, kCrossPlain };
+template <typename... P>
+vdn_status allow_smem(vdn_vda_t h, int which, void (*kernel)(P...), int bytes) {
+  if (h->block_attrs_set & (1u << which)) return VDN_OK;
+  VDN_CUDA(h, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+  h->block_attrs_set |= 1u << which;
+  return VDN_OK;
+}
+
 template <typename... P, typename... A>
 cudaError_t launch_cluster(void (*kernel)(P...), dim3 grid, unsigned cluster, int threads, int smem, cudaStream_t st, A&&... args) {
   cudaLaunchConfig_t c = {};
@@ -1737,7 +1748,7 @@ vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   if (tma && (r = make_bytes_map(h, &tmOut, g.out, io, sizeof(Tio), g.M, g.N, g.out_stride, 32)) != VDN_OK) return r;
   if (add_tma && (r = make_bytes_map(h, &tmAdd, g.add, io, sizeof(Tio), g.M, g.N, g.add_stride, 32)) != VDN_OK) return r;
   auto kernel = add_tma ? vdn::matmul_pair_kernel<Tio, true> : vdn::matmul_pair_kernel<Tio, false>;
-  VDN_CUDA(h, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES));
+  if ((r = allow_smem(h, add_tma ? kMatmulPairAdd : kMatmulPair, kernel, G::SMEM_BYTES)) != VDN_OK) return r;
   const long long tiles = (g.M + 2 * G::ROWS - 1) / (2 * G::ROWS) * ((g.N + G::COLS - 1) / G::COLS);
   const unsigned pairs = (unsigned)std::min<long long>(tiles, h->sm_count / 2);
   prof_begin(h, st);
@@ -1754,7 +1765,8 @@ vdn_status launch_matmul_slim(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
   if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, TOK)) != VDN_OK) return r;
   if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, 128)) != VDN_OK) return r;
-  VDN_CUDA(h, (cudaFuncSetAttribute(vdn::matmul_slim_kernel<Tio, TOK>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES)));
+  if ((r = allow_smem(h, kMatmulSlim + (TOK == 16 ? 0 : TOK == 32 ? 1 : TOK == 64 ? 2 : 3), vdn::matmul_slim_kernel<Tio, TOK>, G::SMEM_BYTES)) != VDN_OK)
+    return r;
   const long long tiles_n = scale_blocks(g.N), tiles_m = (g.M + TOK - 1) / TOK;
   int parts = 1;
   while (parts < 8 && 2 * parts <= g.blocks && 2 * parts * tiles_n * tiles_m <= 2LL * h->sm_count) parts *= 2;
@@ -1907,7 +1919,7 @@ vdn_status launch_cross_tc(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayo
   tmK = tmV = tmQ;                                      // (no keys at all: never used)
   if (a.n_keys > 0 && ((r = make_key_map(h, &tmK, a.k, a, D, a.k_stride)) != VDN_OK || (r = make_key_map(h, &tmV, a.v, a, D, a.v_stride)) != VDN_OK))
     return r;
-  VDN_CUDA(h, cudaFuncSetAttribute(vdn::cross_tc_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::SMEM_BYTES));
+  if ((r = allow_smem(h, kCrossTc, vdn::cross_tc_kernel<D>, G::SMEM_BYTES)) != VDN_OK) return r;
   const unsigned grid = (unsigned)std::min<long long>(L.shape.items, h->sm_count);
   vdn::cross_tc_kernel<D><<<grid, G::THREADS, G::SMEM_BYTES, st>>>(tmQ, tmK, tmV, tmOut, a, L.shape, dev_status(h));
   return VDN_OK;
@@ -1921,10 +1933,11 @@ vdn_status launch_cross_simt(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLa
     case 2: vdn::cross_few_kernel<Tio, D, 2><<<grid, 256, 0, st>>>(a); break;
     case 4: vdn::cross_few_kernel<Tio, D, 4><<<grid, 256, 0, st>>>(a); break;
     case 8: vdn::cross_few_kernel<Tio, D, 8><<<grid, 256, 0, st>>>(a); break;
-    default:
-      VDN_CUDA(h, (cudaFuncSetAttribute(vdn::cross_plain_kernel<Tio, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                        vdn::CrossPlain<D>::SMEM_BYTES)));
+    default: {
+      vdn_status r = allow_smem(h, kCrossPlain, vdn::cross_plain_kernel<Tio, D>, vdn::CrossPlain<D>::SMEM_BYTES);
+      if (r != VDN_OK) return r;
       vdn::cross_plain_kernel<Tio, D><<<grid, 256, vdn::CrossPlain<D>::SMEM_BYTES, st>>>(a);
+    }
   }
   return VDN_OK;
 }
@@ -1938,7 +1951,7 @@ vdn_status launch_cross(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout&
   h->launches = 1;
   if (L.parts > 1) {
     const long long rows = (long long)a.B * a.Lq * a.H;
-    vdn::cross_join_kernel<Tio, D><<<(unsigned)((rows + 7) / 8), 256, 0, st>>>(a);
+    VDN_CUDA(h, launch_overlapped(vdn::cross_join_kernel<Tio, D>, (unsigned)((rows + 7) / 8), 256, 0, st, a));
     prof_mark(h, st, 1, "cross_join");
     h->launches = 2;
   }
