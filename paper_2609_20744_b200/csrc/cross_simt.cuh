@@ -193,20 +193,23 @@ __global__ void __launch_bounds__(256) cross_few_kernel(CrossArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- many rows
-// 64 rows of one key head against 64 keys at a time, both in shared memory as fp32.  A thread has 4 x 4 scores (rows of its own,
-// keys 16 apart: reads without bank conflicts) and 4 x D/16 results; the 16 threads of a row lie side by side in a warp.
+// 64 rows of one key head against 64 keys at a time, in shared memory as fp32; keys and then values in the same place, so that two
+// CTAs fit on an SM with d = 128.  A thread has 4 x 4 scores (rows of its own, keys 16 apart: reads without bank conflicts) and
+// 4 x D/16 results, both as pairs for packed arithmetic (scores: sums over even and odd channels); the 16 threads of a row lie side
+// by side in a warp.  Bound by the multiply-adds.
 template <int D>
 struct CrossPlain {
   static constexpr int ROWS = 64, KEYS = 64, PITCH = D + 4, P_PITCH = KEYS + 4;
-  static constexpr int OFF_K = ROWS * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * D, OFF_ON = OFF_P + ROWS * P_PITCH;
+  static constexpr int OFF_KV = ROWS * PITCH, OFF_P = OFF_KV + KEYS * PITCH, OFF_ON = OFF_P + ROWS * P_PITCH;
   static constexpr int SMEM_BYTES = (OFF_ON + KEYS) * 4;
 };
 
 template <typename Tio, int D>
-__global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
+__global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
+  using namespace tc;
   using S = CrossPlain<D>;
   extern __shared__ __align__(16) float smem[];
-  float *sq = smem, *sk = smem + S::OFF_K, *sv = smem + S::OFF_V, *sp = smem + S::OFF_P;
+  float *sq = smem, *skv = smem + S::OFF_KV, *sp = smem + S::OFF_P;
   int* son = reinterpret_cast<int*>(smem + S::OFF_ON);
   if (a.parts > 1) let_next_kernel_start();
   const int tiles = (int)(((long long)a.Lq * a.group + S::ROWS - 1) / S::ROWS);
@@ -227,42 +230,50 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
     x.x *= a.scale_log2; x.y *= a.scale_log2; x.z *= a.scale_log2; x.w *= a.scale_log2;
     store4(sq + r * S::PITCH + c, x);
   }
-  float o[4][D / 16] = {}, m[4], l[4] = {};
+  uint64_t o[4][D / 32];
+  float m[4], l[4] = {};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) m[i] = -INFINITY;
+  for (int i = 0; i < 4; ++i) {
+    m[i] = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) o[i][c] = 0ull;
+  }
   for (int j0 = lo; j0 < hi; j0 += S::KEYS) {
     __syncthreads();
     if (threadIdx.x < S::KEYS) son[threadIdx.x] = j0 + (int)threadIdx.x < hi && key_counts(a, start + j0 + threadIdx.x);
     __syncthreads();
-    for (int t = threadIdx.x; t < S::KEYS * (D / 4); t += 256) {
-      const int r = t / (D / 4), c = (t % (D / 4)) * 4;
-      const long long row = start + j0 + r;
-      const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-      store4(sk + r * S::PITCH + c, son[r] ? load4(static_cast<const Tio*>(a.k) + row * a.k_stride + (long long)hk * D + c) : zero);
-      store4(sv + r * D + c, son[r] ? load4(static_cast<const Tio*>(a.v) + row * a.v_stride + (long long)hk * D + c) : zero);
-    }
-    __syncthreads();
-    float z[4][4] = {};
+    auto fetch = [&](const void* from, long long stride) {
+#pragma unroll 4
+      for (int t = threadIdx.x; t < S::KEYS * (D / 4); t += 256) {
+        const int r = t / (D / 4), c = (t % (D / 4)) * 4;
+        store4(skv + r * S::PITCH + c, son[r] ? load4(static_cast<const Tio*>(from) + (start + j0 + r) * stride + (long long)hk * D + c)
+                                              : make_float4(0.f, 0.f, 0.f, 0.f));
+      }
+      __syncthreads();
+    };
+    fetch(a.k, a.k_stride);
+    uint64_t z2[4][4] = {};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
-      float4 x[4], y[4];
+      ulonglong2 x[4], y[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = load4(sq + (ty * 4 + i) * S::PITCH + c);
+      for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(sq + (ty * 4 + i) * S::PITCH + c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = load4(sk + (tx + 16 * j) * S::PITCH + c);
+      for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const ulonglong2*>(skv + (tx + 16 * j) * S::PITCH + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          z[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, z[i][j]))));
+        for (int j = 0; j < 4; ++j) z2[i][j] = f2_fma(x[i].y, y[j].y, f2_fma(x[i].x, y[j].x, z2[i][j]));
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float top = m[i];
+      float z[4], top = m[i];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (!son[tx + 16 * j]) z[i][j] = -INFINITY;
-        top = fmaxf(top, z[i][j]);
+        float z0, z1;
+        f2_unpack(z2[i][j], z0, z1);
+        z[j] = son[tx + 16 * j] ? z0 + z1 : -INFINITY;
+        top = fmaxf(top, z[j]);
       }
 #pragma unroll
       for (int s = 8; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
@@ -271,14 +282,16 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
       l[i] *= keep;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = exp2_fast(z[i][j] - base);
+        const float p = exp2_fast(z[j] - base);
         l[i] += p;                                                       // (this thread's keys; the row's 16 are added at the end)
         sp[(ty * 4 + i) * S::P_PITCH + tx + 16 * j] = p;
       }
+      const uint64_t keep2 = f2_pack(keep, keep);
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c) o[i][c] *= keep;
+      for (int c = 0; c < D / 32; ++c) o[i][c] = f2_fma(o[i][c], keep2, 0ull);
     }
-    __syncwarp();                                                        // a row's 16 threads are lanes of one warp
+    __syncthreads();                                                     // all have read the keys
+    fetch(a.v, a.v_stride);
 #pragma unroll 2
     for (int j = 0; j < S::KEYS; j += 4) {
       float4 p[4];
@@ -288,14 +301,13 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
-          const float4 y = load4(sv + (j + u) * D + c * 64 + tx * 4);
+          const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(skv + (j + u) * S::PITCH + c * 64 + tx * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float w = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
-            o[i][4 * c] = fmaf(w, y.x, o[i][4 * c]);
-            o[i][4 * c + 1] = fmaf(w, y.y, o[i][4 * c + 1]);
-            o[i][4 * c + 2] = fmaf(w, y.z, o[i][4 * c + 2]);
-            o[i][4 * c + 3] = fmaf(w, y.w, o[i][4 * c + 3]);
+            const uint64_t w2 = f2_pack(w, w);
+            o[i][2 * c] = f2_fma(w2, y.x, o[i][2 * c]);
+            o[i][2 * c + 1] = f2_fma(w2, y.y, o[i][2 * c + 1]);
           }
         }
     }
@@ -309,7 +321,9 @@ __global__ void __launch_bounds__(256) cross_plain_kernel(CrossArgs a) {
     const int row = row0 + r, t = row / a.group;
 #pragma unroll
     for (int c = 0; c < D / 64; ++c) {
-      const float x[4] = {o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]};
+      float x[4];
+      f2_unpack(o[i][2 * c], x[0], x[1]);
+      f2_unpack(o[i][2 * c + 1], x[2], x[3]);
       cross_put<Tio>(a, (long long)b * a.Lq + t, hk * a.group + row - t * a.group, c * 64 + tx * 4, x, m[i], l[i], part, D);
     }
   }

@@ -1824,7 +1824,7 @@ vdn_status plan_cross(vdn_vda_t h, long long queries, long long keys, const vdn_
   if (queries > most || keys > most || p->batch * queries > most || (!p->cu_seqlens && p->batch * keys > most))
     return fail(h, VDN_ERR_INVALID_ARG, "more than 2^30 query or key tokens");
   if (queries * (p->heads / p->key_heads) > most) return fail(h, VDN_ERR_UNSUPPORTED, "more than 2^30 rows of a key head");
-  if (!std::isfinite(p->scale)) return fail(h, VDN_ERR_INVALID_ARG, "scale must be finite");
+  if (!(std::fabs(p->scale) <= 1e30f)) return fail(h, VDN_ERR_INVALID_ARG, "scale must lie between -1e30 and 1e30");
   a = vdn::CrossArgs{};
   a.B = p->batch; a.Lq = (int)queries; a.H = p->heads; a.Hk = p->key_heads; a.group = p->heads / p->key_heads;
   a.Lk = p->cu_seqlens ? 0 : keys;
@@ -2014,8 +2014,8 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
   if (!p || p->struct_size != sizeof(vdn_vda_matmul_params))
     return fail(h, VDN_ERR_INVALID_ARG, "vdn_vda_matmul_params missing or of the wrong struct_size");
   if (p->reserved) return fail(h, VDN_ERR_INVALID_ARG, "reserved must be 0");
-  if (M < 0 || M > (1LL << 30) || N <= 0 || K <= 0 || N > (1 << 22) || K > (1 << 22))
-    return fail(h, VDN_ERR_INVALID_ARG, "M must lie between 0 and 2^30, N and K between 1 and 2^22");
+  if (M < 0 || M > (1LL << 30) || N <= 0 || K <= 0 || N > (1 << 21) || K > (1 << 21))
+    return fail(h, VDN_ERR_INVALID_ARG, "M must lie between 0 and 2^30, N and K between 1 and 2^21");
   if (M > 0 && (!a || !w || !out || !p->a_scale || !p->w_scale)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
   if (M > 0 && (out == a || out == w || out == p->a_scale || out == p->w_scale || out == p->bias))
     return fail(h, VDN_ERR_INVALID_ARG, "out may only alias add");

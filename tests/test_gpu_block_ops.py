@@ -258,7 +258,7 @@ def check_attention(vda, x, rows, dtype, scale=None, **kw):
         assert (np.abs(got[b] - want) <= bound).all()
         some = np.isfinite(wlse)
         assert np.array_equal(glse[b][~some], wlse[~some])
-        assert (np.abs(glse[b] - wlse)[some] <= (dz + 4 * U32 * np.abs(wlse))[some]).all()
+        assert (np.abs(glse[b][some] - wlse[some]) <= dz[some] + 4 * U32 * np.abs(wlse[some])).all()
     return out, lse
 
 
