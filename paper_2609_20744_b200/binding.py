@@ -642,6 +642,10 @@ class Vda:
             return self._torch.empty_like(x)
         return self._new(streams, x.shape, x.dtype)
 
+    def _new_beside(self, streams, x, shape, dtype):
+        """_new where a checked input lies (a little less to work out)."""
+        return x.new_empty(shape, dtype=dtype) if streams[1] is None else self._new(streams, shape, dtype)
+
     def token_scan(self, q, k, v, beta, log_alpha=None, cu_seqlens=None, s0=None, out=None, state=None, scale=1.0,
                    l2_eps=0.0, stream=None):
         """vdn_vda_token_scan: the gated delta rule over packed sequences.  Returns (out, state).
@@ -800,7 +804,7 @@ class Vda:
             pitch = _matrix("out", out, tuple(shape), torch.float8_e4m3fn, True, dev, 16)
         want = (*shape[:-1], blocks) if rows == 1 else (-(-n // SCALE_BLOCK), blocks)
         if scale is None:
-            scale = self._new(streams, want, torch.float32)
+            scale = self._new_beside(streams, x, want, torch.float32)
         else:
             _dense("scale", scale, want, torch.float32, True, dev)
         prm = _QUANTIZE_PARAMS.pack(_QUANTIZE_PARAMS.size, rows, xs, pitch)
@@ -818,7 +822,7 @@ class Vda:
         m, n, k, st = validate_matmul_args(self.torch_dtype, self.device, a, a_scale, w, w_scale, bias, add, out)
         streams = self._streams(stream)
         if out is None:
-            out = self._new(streams, (*a.shape[:-1], n), self.torch_dtype) if add is None else self._new_like(streams, add)
+            out = self._new_beside(streams, a, (*a.shape[:-1], n), self.torch_dtype) if add is None else self._new_like(streams, add)
         prm = _MATMUL_PARAMS.pack(_MATMUL_PARAMS.size, 0, a_scale.data_ptr(), w_scale.data_ptr(), _ptr(bias), _ptr(add), *st)
         r = self.lib.vdn_vda_scaled_matmul(self.h, a.data_ptr(), w.data_ptr(), out.data_ptr(), m, n, k, prm, streams[0])
         if r:
@@ -839,7 +843,7 @@ class Vda:
         if out is None:
             out = self._new_like(streams, q)
         if given is None and lse:
-            given = self._new(streams, q.shape[:-1], self._torch.float32)
+            given = self._new_beside(streams, q, q.shape[:-1], self._torch.float32)
         prm = _CROSS_PARAMS.pack(_CROSS_PARAMS.size, B, H, Hk, self.d ** -0.5 if scale is None else scale, 0, _ptr(cu_seqlens),
                                  _ptr(lengths), _ptr(mask), _ptr(given), *st)
         need = self.lib.vdn_vda_cross_attention_workspace_bytes(self.h, n, keys, prm)
