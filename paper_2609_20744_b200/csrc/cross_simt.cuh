@@ -77,6 +77,21 @@ __device__ __forceinline__ void cross_put(const CrossArgs& a, long long token, i
   }
 }
 
+// 16 bytes as floats.
+template <typename Tio>
+__device__ __forceinline__ void piece_floats(const uint4& r, float (&x)[16 / sizeof(Tio)]) {
+  const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(Tio) == 4) {
+      x[i] = __uint_as_float(w[i]);
+    } else {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+}
+
 // ---------------------------------------------------------------------------------------------- few rows
 // R rows of one key head, a CTA of eight warps over a part of the keys.  A key's channels lie across as many lanes as 16-byte
 // pieces make them up, so a warp holds 1 to 4 keys at once, U of them one behind another in flight; every such slot keeps its own
@@ -114,20 +129,31 @@ __global__ void __launch_bounds__(256) cross_few_kernel(CrossArgs a) {
   }
   const Tio* kp = static_cast<const Tio*>(a.k) + start * a.k_stride + (long long)hk * D + c;
   const Tio* vp = static_cast<const Tio*>(a.v) + start * a.v_stride + (long long)hk * D + c;
-  for (int j0 = lo + (warp * SLOTS + slot); j0 - (warp * SLOTS + slot) < hi; j0 += STEP) {
-    float k[U][N], v[U][N];
-    bool on[U];
+  struct Step { uint4 k[U], v[U]; bool on[U]; };
+  auto fetch = [&](int first, Step& x) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int j = j0 + u * WARPS * SLOTS;
-      on[u] = j < hi && key_counts(a, start + j);
-#pragma unroll
-      for (int i = 0; i < N; i += 4) {
-        const float4 x = on[u] ? load4(kp + j * a.k_stride + i) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float4 y = on[u] ? load4(vp + j * a.v_stride + i) : make_float4(0.f, 0.f, 0.f, 0.f);
-        k[u][i] = x.x; k[u][i + 1] = x.y; k[u][i + 2] = x.z; k[u][i + 3] = x.w;
-        v[u][i] = y.x; v[u][i + 1] = y.y; v[u][i + 2] = y.z; v[u][i + 3] = y.w;
+      const int j = first + u * WARPS * SLOTS;
+      x.on[u] = j < hi && key_counts(a, start + j);
+      x.k[u] = x.v[u] = make_uint4(0, 0, 0, 0);
+      if (x.on[u]) {
+        x.k[u] = *reinterpret_cast<const uint4*>(kp + j * a.k_stride);
+        x.v[u] = *reinterpret_cast<const uint4*>(vp + j * a.v_stride);
       }
+    }
+  };
+  const int mine = warp * SLOTS + slot;
+  Step next;
+  fetch(lo + mine, next);
+  for (int j0 = lo; j0 < hi; j0 += STEP) {
+    const Step x = next;
+    if (j0 + STEP < hi) fetch(j0 + STEP + mine, next);                    // while these are worked on
+    float k[U][N], v[U][N];
+    const bool (&on)[U] = x.on;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      piece_floats<Tio>(x.k[u], k[u]);
+      piece_floats<Tio>(x.v[u], v[u]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -193,24 +219,29 @@ __global__ void __launch_bounds__(256) cross_few_kernel(CrossArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- many rows
-// 64 rows of one key head against 64 keys at a time, in shared memory as fp32; keys and then values in the same place, so that two
-// CTAs fit on an SM with d = 128.  A thread has 4 x 4 scores (rows of its own, keys 16 apart: reads without bank conflicts) and
-// 4 x D/16 results, both as pairs for packed arithmetic (scores: sums over even and odd channels); the 16 threads of a row lie side
-// by side in a warp.  Bound by the multiply-adds.
-template <int D>
+// 128 rows of one key head (64 where that leaves SMs without work) against 64 keys at a time, in shared memory as fp32; values arrive while scores are formed, the next keys
+// while the values are summed (f32: by asynchronous copies).  A thread has 4 x 4 scores (rows of its own, keys 16 apart: reads
+// without bank conflicts) and 4 x D/16 results, both as pairs for packed arithmetic (scores: sums over even and odd channels); the
+// 16 threads of a row lie side by side in a warp.  Bound by the multiply-adds and the shared-memory reads that feed them.
+template <int D, int TILE>
 struct CrossPlain {
-  static constexpr int ROWS = 64, KEYS = 64, PITCH = D + 4, P_PITCH = KEYS + 4;
-  static constexpr int OFF_KV = ROWS * PITCH, OFF_P = OFF_KV + KEYS * PITCH, OFF_ON = OFF_P + ROWS * P_PITCH;
-  static constexpr int SMEM_BYTES = (OFF_ON + KEYS) * 4;
+  static constexpr int ROWS = TILE, KEYS = 64, THREADS = 4 * ROWS, PITCH = D + 4, P_PITCH = KEYS + 4;
+  static constexpr int OFF_K = ROWS * PITCH, OFF_V = OFF_K + KEYS * PITCH, OFF_P = OFF_V + KEYS * PITCH;
+  static constexpr int SMEM_BYTES = (OFF_P + ROWS * P_PITCH) * 4;
 };
 
-template <typename Tio, int D>
-__global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
+// 16 bytes of shared memory from global memory, or zeros.
+__device__ __forceinline__ void cp_async16_or_zero(void* smem_dst, const void* gmem_src, bool on) {
+  const uint32_t s = (uint32_t)__cvta_generic_to_shared(smem_dst);
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(s), "l"(gmem_src), "r"(on ? 16 : 0) : "memory");
+}
+
+template <typename Tio, int D, int TILE>
+__global__ void __launch_bounds__(CrossPlain<D, TILE>::THREADS, 512 / CrossPlain<D, TILE>::THREADS) cross_plain_kernel(CrossArgs a) {
   using namespace tc;
-  using S = CrossPlain<D>;
+  using S = CrossPlain<D, TILE>;
   extern __shared__ __align__(16) float smem[];
-  float *sq = smem, *skv = smem + S::OFF_KV, *sp = smem + S::OFF_P;
-  int* son = reinterpret_cast<int*>(smem + S::OFF_ON);
+  float *sq = smem, *sk = smem + S::OFF_K, *sv = smem + S::OFF_V, *sp = smem + S::OFF_P;
   if (a.parts > 1) let_next_kernel_start();
   const int tiles = (int)(((long long)a.Lq * a.group + S::ROWS - 1) / S::ROWS);
   long long unit = blockIdx.x;
@@ -224,7 +255,19 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
   cross_range(a, b, start, len);
   cross_part(len, part, a.parts, S::KEYS, lo, hi);
 
-  for (int t = threadIdx.x; t < S::ROWS * (D / 4); t += 256) {
+  auto fetch = [&](float* to, const void* from, long long stride, int j0) {
+#pragma unroll
+    for (int t = threadIdx.x; t < S::KEYS * (D / 4); t += S::THREADS) {
+      const int r = t / (D / 4), c = (t % (D / 4)) * 4;
+      const bool on = j0 + r < hi && key_counts(a, start + j0 + r);
+      const Tio* p = static_cast<const Tio*>(from) + (on ? (start + j0 + r) * stride + (long long)hk * D + c : 0);
+      if constexpr (sizeof(Tio) == 4) cp_async16_or_zero(to + r * S::PITCH + c, p, on);
+      else store4(to + r * S::PITCH + c, on ? load4(p) : make_float4(0.f, 0.f, 0.f, 0.f));
+    }
+    cp_async_commit();
+  };
+  if (lo < hi) fetch(sk, a.k, a.k_stride, lo);
+  for (int t = threadIdx.x; t < S::ROWS * (D / 4); t += S::THREADS) {
     const int r = t / (D / 4), c = (t % (D / 4)) * 4, row = row0 + min(r, rows - 1), i = row / a.group;
     float4 x = load4(static_cast<const Tio*>(a.q) + ((long long)b * a.Lq + i) * a.q_stride + (long long)(hk * a.group + row - i * a.group) * D + c);
     x.x *= a.scale_log2; x.y *= a.scale_log2; x.z *= a.scale_log2; x.w *= a.scale_log2;
@@ -239,19 +282,12 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
     for (int c = 0; c < D / 32; ++c) o[i][c] = 0ull;
   }
   for (int j0 = lo; j0 < hi; j0 += S::KEYS) {
+    fetch(sv, a.v, a.v_stride, j0);
+    bool on[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) on[j] = j0 + tx + 16 * j < hi && key_counts(a, start + j0 + tx + 16 * j);
+    cp_async_wait<1>();                                                  // the keys
     __syncthreads();
-    if (threadIdx.x < S::KEYS) son[threadIdx.x] = j0 + (int)threadIdx.x < hi && key_counts(a, start + j0 + threadIdx.x);
-    __syncthreads();
-    auto fetch = [&](const void* from, long long stride) {
-#pragma unroll 4
-      for (int t = threadIdx.x; t < S::KEYS * (D / 4); t += 256) {
-        const int r = t / (D / 4), c = (t % (D / 4)) * 4;
-        store4(skv + r * S::PITCH + c, son[r] ? load4(static_cast<const Tio*>(from) + (start + j0 + r) * stride + (long long)hk * D + c)
-                                              : make_float4(0.f, 0.f, 0.f, 0.f));
-      }
-      __syncthreads();
-    };
-    fetch(a.k, a.k_stride);
     uint64_t z2[4][4] = {};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
@@ -259,7 +295,7 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const ulonglong2*>(sq + (ty * 4 + i) * S::PITCH + c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const ulonglong2*>(skv + (tx + 16 * j) * S::PITCH + c);
+      for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const ulonglong2*>(sk + (tx + 16 * j) * S::PITCH + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -272,7 +308,7 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
       for (int j = 0; j < 4; ++j) {
         float z0, z1;
         f2_unpack(z2[i][j], z0, z1);
-        z[j] = son[tx + 16 * j] ? z0 + z1 : -INFINITY;
+        z[j] = on[j] ? z0 + z1 : -INFINITY;
         top = fmaxf(top, z[j]);
       }
 #pragma unroll
@@ -291,7 +327,10 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
       for (int c = 0; c < D / 32; ++c) o[i][c] = f2_fma(o[i][c], keep2, 0ull);
     }
     __syncthreads();                                                     // all have read the keys
-    fetch(a.v, a.v_stride);
+    if (j0 + S::KEYS < hi) fetch(sk, a.k, a.k_stride, j0 + S::KEYS);
+    else cp_async_commit();
+    cp_async_wait<1>();                                                  // the values
+    __syncthreads();
 #pragma unroll 2
     for (int j = 0; j < S::KEYS; j += 4) {
       float4 p[4];
@@ -301,7 +340,7 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
-          const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(skv + (j + u) * S::PITCH + c * 64 + tx * 4);
+          const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(sv + (j + u) * S::PITCH + c * 64 + tx * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float w = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
@@ -311,7 +350,9 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
           }
         }
     }
+    __syncthreads();                                                     // ... and the values
   }
+  cp_async_wait<0>();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -330,35 +371,42 @@ __global__ void __launch_bounds__(256, 2) cross_plain_kernel(CrossArgs a) {
 }
 
 // ---------------------------------------------------------------------------------------------- parts
-// A warp to a (token, head).  Starts while its predecessor runs.
+// A warp to 32 channels of a (token, head), eight parts in flight (rows are few where parts are many).  Starts while its predecessor runs.
 template <typename Tio, int D>
 __global__ void __launch_bounds__(256) cross_join_kernel(CrossArgs a) {
-  constexpr int N = D / 32;
+  constexpr int PER = D / 32, BATCH = 8;
   wait_for_kernel_before();
-  const long long at = (long long)blockIdx.x * 8 + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
+  const long long unit = (long long)blockIdx.x * 8 + threadIdx.x / 32, at = unit / PER;
+  const int lane = threadIdx.x % 32, c = (int)(unit % PER) * 32 + lane;
   if (at >= (long long)a.B * a.Lq * a.H) return;
   const float2* ml = a.part_ml + at * a.parts;
-  const float* o = a.part_o + at * a.parts * D + lane * N;
-  float top = -INFINITY, sum = 0.f, x[N] = {};
+  const float* o = a.part_o + at * a.parts * D + c;
+  float top = -INFINITY, sum = 0.f, x = 0.f;
   for (int p = lane; p < a.parts; p += 32) top = fmaxf(top, ml[p].x);
 #pragma unroll
   for (int s = 16; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
   const float base = finite_max(top);
-  for (int p = 0; p < a.parts; ++p) {
-    const float2 y = ml[p];
-    const float f = exp2_fast(y.x - base);
-    sum = fmaf(y.y, f, sum);
+  for (int p0 = 0; p0 < a.parts; p0 += BATCH) {
+    float2 y[BATCH];
+    float z[BATCH];
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) {
+      const bool on = p0 + i < a.parts;
+      y[i] = on ? ml[p0 + i] : make_float2(-INFINITY, 0.f);
+      z[i] = on ? o[(long long)(p0 + i) * D] : 0.f;
+    }
     // (a part without a key that counts has left zeros)
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaf(o[(long long)p * D + i], f, x[i]);
+    for (int i = 0; i < BATCH; ++i) {
+      const float f = exp2_fast(y[i].x - base);
+      sum = fmaf(y[i].y, f, sum);
+      x = fmaf(z[i], f, x);
+    }
   }
   const float r = sum == 0.f ? 0.f : 1.f / sum;
   const long long token = at / a.H;
-  Tio* out = static_cast<Tio*>(a.out) + token * a.out_stride + (at - token * a.H) * D + lane * N;
-#pragma unroll
-  for (int i = 0; i < N; ++i) out[i] = from_float<Tio>(x[i] * r);
-  if (lane == 0 && a.lse) a.lse[at] = lse_of(top, sum);
+  static_cast<Tio*>(a.out)[token * a.out_stride + (at - token * a.H) * D + c] = from_float<Tio>(x * r);
+  if (c == 0 && a.lse) a.lse[at] = lse_of(top, sum);
 }
 
 }  // namespace vdn

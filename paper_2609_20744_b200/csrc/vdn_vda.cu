@@ -1707,7 +1707,7 @@ vdn_status make_bytes_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, CUtensor
 }
 
 // Lets a kernel have its shared memory, once for a handle: `which` numbers the kernels of these entry points.
-enum BlockKernel { kMatmulPair, kMatmulPairAdd, kMatmulSlim, kCrossTc = kMatmulSlim + 4, kCrossPlain };
+enum BlockKernel { kMatmulPair, kMatmulPairAdd, kMatmulSlim, kCrossTc = kMatmulSlim + 4, kCrossPlain /* two */ };
 template <typename... P>
 vdn_status allow_smem(vdn_vda_t h, int which, void (*kernel)(P...), int bytes) {
   if (h->block_attrs_set & (1u << which)) return VDN_OK;
@@ -1836,7 +1836,7 @@ vdn_status plan_cross(vdn_vda_t h, long long queries, long long keys, const vdn_
 // How a call runs: on which kernel, and in how many parts of the keys.
 struct CrossLayout {
   bool tc;
-  int rows;                 // plain kernels: rows of a CTA's tile; up to 8: cross_few, 64: cross_plain
+  int rows;                 // plain kernels: rows of a CTA's tile; up to 8: cross_few, 64 or 128: cross_plain
   long long units;          // plain kernels: (batch row, key head, row tile); tensor cores: pairs of tiles
   int parts;
   size_t o, ml, total;
@@ -1867,10 +1867,14 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     wanted = h->sm_count / L.units;
     least = 256;
   } else {
-    L.rows = rows <= 8 ? (rows <= 2 ? (int)rows : rows <= 4 ? 4 : 8) : vdn::CrossPlain<64>::ROWS;
-    L.units = (long long)a.B * a.Hk * ((rows + L.rows - 1) / L.rows);
-    wanted = (L.rows <= 8 ? 4LL : 2LL) * h->sm_count / L.units;
     least = 128;
+    // 128 rows a CTA read keys and values half as often as 64 and keep an SM busier (4096 x 4096 x 8 heads, f32, d = 128: 1850 us instead of
+    // 2182), if they and the parts that the keys can be cut into are CTAs for half of the SMs (256 queries of 2 heads, 77 keys: 21 us, with 64
+    // rows 14) and no half of them is empty (16 batch rows of 40 queries: 64 us, 42).
+    const long long tall = (long long)a.B * a.Hk * ((rows + 127) / 128), cuts = std::max(1LL, std::min(h->sm_count / tall, keys / least));
+    L.rows = rows <= 8 ? (rows <= 2 ? (int)rows : rows <= 4 ? 4 : 8) : rows > 64 && 2 * tall * cuts >= h->sm_count ? 128 : 64;
+    L.units = (long long)a.B * a.Hk * ((rows + L.rows - 1) / L.rows);
+    wanted = (L.rows <= 8 ? 4LL : 1LL) * h->sm_count / L.units;
   }
   L.parts = (int)std::max(1LL, std::min({wanted, keys / least, 256LL}));
   L.shape.items = (uint32_t)(L.units * L.parts);         // (refused where that does not fit)
@@ -1925,6 +1929,15 @@ vdn_status launch_cross_tc(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayo
   return VDN_OK;
 }
 
+template <typename Tio, int D, int TILE>
+vdn_status launch_cross_plain(vdn_vda_t h, const vdn::CrossArgs& a, unsigned grid, int which, cudaStream_t st) {
+  using S = vdn::CrossPlain<D, TILE>;
+  vdn_status r = allow_smem(h, which, vdn::cross_plain_kernel<Tio, D, TILE>, S::SMEM_BYTES);
+  if (r != VDN_OK) return r;
+  vdn::cross_plain_kernel<Tio, D, TILE><<<grid, S::THREADS, S::SMEM_BYTES, st>>>(a);
+  return VDN_OK;
+}
+
 template <typename Tio, int D>
 vdn_status launch_cross_simt(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout& L, cudaStream_t st) {
   const unsigned grid = (unsigned)(L.units * L.parts);
@@ -1933,11 +1946,8 @@ vdn_status launch_cross_simt(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLa
     case 2: vdn::cross_few_kernel<Tio, D, 2><<<grid, 256, 0, st>>>(a); break;
     case 4: vdn::cross_few_kernel<Tio, D, 4><<<grid, 256, 0, st>>>(a); break;
     case 8: vdn::cross_few_kernel<Tio, D, 8><<<grid, 256, 0, st>>>(a); break;
-    default: {
-      vdn_status r = allow_smem(h, kCrossPlain, vdn::cross_plain_kernel<Tio, D>, vdn::CrossPlain<D>::SMEM_BYTES);
-      if (r != VDN_OK) return r;
-      vdn::cross_plain_kernel<Tio, D><<<grid, 256, vdn::CrossPlain<D>::SMEM_BYTES, st>>>(a);
-    }
+    case 64: return launch_cross_plain<Tio, D, 64>(h, a, grid, kCrossPlain, st);
+    default: return launch_cross_plain<Tio, D, 128>(h, a, grid, kCrossPlain + 1, st);
   }
   return VDN_OK;
 }
@@ -1950,8 +1960,8 @@ vdn_status launch_cross(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayout&
   prof_mark(h, st, 0, L.tc ? "cross_tc" : L.rows <= 8 ? "cross_few" : "cross_plain");
   h->launches = 1;
   if (L.parts > 1) {
-    const long long rows = (long long)a.B * a.Lq * a.H;
-    VDN_CUDA(h, launch_overlapped(vdn::cross_join_kernel<Tio, D>, (unsigned)((rows + 7) / 8), 256, 0, st, a));
+    const long long warps = (long long)a.B * a.Lq * a.H * (D / 32);
+    VDN_CUDA(h, launch_overlapped(vdn::cross_join_kernel<Tio, D>, (unsigned)((warps + 7) / 8), 256, 0, st, a));
     prof_mark(h, st, 1, "cross_join");
     h->launches = 2;
   }
@@ -2080,7 +2090,7 @@ vdn_status vdn_vda_cross_attention(vdn_vda_t h, const void* q, const void* k, co
     return fail(h, VDN_ERR_WORKSPACE, "workspace missing or smaller than vdn_vda_cross_attention_workspace_bytes");
   if (reinterpret_cast<uintptr_t>(workspace) % kAlign != 0)
     return fail(h, VDN_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  if (L.units * L.parts > 0x7fffffffLL || (long long)a.B * a.Lq * a.H / 8 >= 0x7fffffffLL)
+  if (L.units * L.parts > 0x7fffffffLL || (long long)a.B * a.Lq * a.H / 2 >= 0x7fffffffLL)
     return fail(h, VDN_ERR_UNSUPPORTED, "too many (query, head) pairs for one call");
   if (!some) { h->launches = 0; return VDN_OK; }
   a.parts = L.parts;
