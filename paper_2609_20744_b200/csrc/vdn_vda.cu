@@ -1707,7 +1707,7 @@ vdn_status make_bytes_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, CUtensor
 }
 
 // Lets a kernel have its shared memory, once for a handle: `which` numbers the kernels of these entry points.
-enum BlockKernel { kMatmulPair, kMatmulPairAdd, kMatmulSlim, kCrossTc = kMatmulSlim + 4, kCrossPlain /* two */ };
+enum BlockKernel { kMatmulPair /* three */, kMatmulSlim = kMatmulPair + 3, kCrossTc = kMatmulSlim + 4, kCrossPlain /* two */ };
 template <typename... P>
 vdn_status allow_smem(vdn_vda_t h, int which, void (*kernel)(P...), int bytes) {
   if (h->block_attrs_set & (1u << which)) return VDN_OK;
@@ -1740,19 +1740,19 @@ vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
   if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, G::ROWS)) != VDN_OK) return r;
   if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, G::COLS / 2)) != VDN_OK) return r;
-  // results that no tile copy can write (rows at any address) leave by ordinary stores
-  const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio));
-  const bool add_tma = g.add && rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio));
+  const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio)) && (!g.add || rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio)));
+  const bool add_tma = tma && g.add;
   const CUtensorMapDataType io = sizeof(Tio) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   tmOut = tmAdd = tmA;
   if (tma && (r = make_bytes_map(h, &tmOut, g.out, io, sizeof(Tio), g.M, g.N, g.out_stride, 32)) != VDN_OK) return r;
   if (add_tma && (r = make_bytes_map(h, &tmAdd, g.add, io, sizeof(Tio), g.M, g.N, g.add_stride, 32)) != VDN_OK) return r;
-  auto kernel = add_tma ? vdn::matmul_pair_kernel<Tio, true> : vdn::matmul_pair_kernel<Tio, false>;
-  if ((r = allow_smem(h, add_tma ? kMatmulPairAdd : kMatmulPair, kernel, G::SMEM_BYTES)) != VDN_OK) return r;
+  auto kernel = !tma ? vdn::matmul_pair_kernel<Tio, vdn::kOutElements>
+                     : add_tma ? vdn::matmul_pair_kernel<Tio, vdn::kOutTilesAdd> : vdn::matmul_pair_kernel<Tio, vdn::kOutTiles>;
+  if ((r = allow_smem(h, kMatmulPair + (!tma ? 2 : add_tma ? 1 : 0), kernel, G::SMEM_BYTES)) != VDN_OK) return r;
   const long long tiles = (g.M + 2 * G::ROWS - 1) / (2 * G::ROWS) * ((g.N + G::COLS - 1) / G::COLS);
   const unsigned pairs = (unsigned)std::min<long long>(tiles, h->sm_count / 2);
   prof_begin(h, st);
-  kernel<<<2 * pairs, G::THREADS, G::SMEM_BYTES, st>>>(tmA, tmW, tmOut, tmAdd, g, tma ? 1 : 0, dev_status(h));
+  kernel<<<2 * pairs, G::THREADS, G::SMEM_BYTES, st>>>(tmA, tmW, tmOut, tmAdd, g, dev_status(h));
   prof_mark(h, st, 0, "matmul_pair");
   return VDN_OK;
 }
