@@ -415,7 +415,7 @@ vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, 
  *   strides     elements from one row to the next, 0 = dense.
  * Products of 8-bit numbers are exact; a block's sum is formed on the tensor cores, scaled and added to the others in fp32;
  * bias and add are added in fp32 before the one rounding to io_dtype.  VDN_FLAG_FORCE_SIMT: plain fp32 arithmetic throughout.
- * M = 0 is no error.  Needs no workspace.  Enqueues on cuda_stream and returns; does not synchronise. */
+ * M up to 2^30 (0 is no error), N and K up to 2^21.  Needs no workspace.  Enqueues on cuda_stream and returns; does not synchronise. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(vdn_vda_matmul_params), checked */
   uint32_t reserved;         /* 0 */
@@ -445,8 +445,11 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
  *   workspace  DEVICE, 256-byte aligned, at least vdn_vda_cross_attention_workspace_bytes (0 where none is needed; NULL is fine
  *           then): long encoders are cut into parts where there are few queries.  An argument and not the handle's, so that
  *           calls that may overlap, or captured graphs, can each have their own; nothing in it outlives the call.
- * bf16 runs on the tensor cores (weights exp(z_j - max) rounded to bf16, sums fp32), single tokens in plain fp32, as does f32 and all
- * with VDN_FLAG_FORCE_SIMT.  Kernels and parts are chosen by sizes alone; lengths stay on the device.
+ *   p->scale   -1e30 .. 1e30.
+ * bf16 with three or more rows to a key head (queries times heads of its group) and a scale above zero runs on the tensor cores (weights
+ * exp(z_j - max) rounded to bf16, sums fp32: out is off by about 2.3e-3 in the 2-norm, 1.7e-3 of it its own rounding); one or two rows,
+ * other scales, f32, and all with VDN_FLAG_FORCE_SIMT in plain fp32.  Kernels and parts are chosen by sizes alone (packed: by the average
+ * length); lengths stay on the device.  What is not finite among q, k, v that count reaches its own rows of the result only.
  * Enqueues on cuda_stream and returns; does not synchronise. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(vdn_vda_cross_params), checked */

@@ -44,7 +44,7 @@ __device__ __forceinline__ void add_bias(const MatmulArgs& p, int n, float (&x)[
 }
 
 // How results leave: by tile copies; by tile copies, `add` coming the same way; or element by element, where one of them has rows that no tile
-// copy can reach.  Variants of their own: in common code the first takes 6 % longer with the second's (753 -> 800 us at
+// copy can reach, or that end inside 16 bytes.  Variants of their own: in common code the first takes 6 % longer with the second's (753 -> 800 us at
 // 32768 x 5120 x 5120), and spills with the third's.
 enum MatmulOut { kOutTiles, kOutTilesAdd, kOutElements };
 template <typename Tio, int MODE>

@@ -1740,7 +1740,9 @@ vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   const CUtensorMapDataType byte = CU_TENSOR_MAP_DATA_TYPE_UINT8;
   if ((r = make_bytes_map(h, &tmA, g.a, byte, 1, g.M, g.K, g.a_stride, G::ROWS)) != VDN_OK) return r;
   if ((r = make_bytes_map(h, &tmW, g.w, byte, 1, g.N, g.K, g.w_stride, G::COLS / 2)) != VDN_OK) return r;
-  const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio)) && (!g.add || rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio)));
+  // (a tile copy writes whole pieces of 16 bytes: with a row that ends inside one it would write what lies behind it)
+  const bool tma = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio)) && (size_t)g.N * sizeof(Tio) % 16 == 0 &&
+                   (!g.add || rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio)));
   const bool add_tma = tma && g.add;
   const CUtensorMapDataType io = sizeof(Tio) == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   tmOut = tmAdd = tmA;

@@ -36,6 +36,42 @@ def test_key_counts_around_tiles(handle, dtype, d, flags, lq):
     check_attention(handle(dtype, d, flags), x, rows, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(300, 200, 208), (1031, 333, 130), (520, 127, 640)])
+def test_products_of_many_rows_at_any_address(handle, dtype, m, n, k):
+    """Results and what is added to them: both where tile copies reach, one of them, neither; apart and in place; without add."""
+    vda = handle(dtype)
+    x = operands(m, n, k, dtype, seed=m)
+    first = check_product(vda, x, dtype)
+    for pad_out in (-n % 8, 5, 1):
+        room = torch.full((m, n + pad_out), 7.0, device=DEV, dtype=TYPES[dtype])
+        check_product(vda, dict(x, add=None), dtype, out=room[:, :n])
+        for pad_add in (-n % 8 + 8, 3):
+            add = torch.full((m, n + pad_add), 9.0, device=DEV, dtype=TYPES[dtype])
+            add[:, :n] = x["add"]
+            got = vda.scaled_matmul(x["a"], x["a_scale"], x["w"], x["w_scale"], bias=x["bias"], add=add[:, :n], out=room[:, :n])
+            assert got.equal(first) and (room[:, n:] == 7).all() and (add[:, n:] == 9).all()
+        room[:, :n] = x["add"]
+        got = vda.scaled_matmul(x["a"], x["a_scale"], x["w"], x["w_scale"], bias=x["bias"], add=room[:, :n], out=room[:, :n])
+        assert got.equal(first) and (room[:, n:] == 7).all()
+    shifted = torch.full((m * n + 8,), 7.0, device=DEV, dtype=TYPES[dtype])          # dense, but not from a multiple of 16 bytes on
+    got = vda.scaled_matmul(x["a"], x["a_scale"], x["w"], x["w_scale"], bias=x["bias"], add=x["add"], out=shifted[1: 1 + m * n].view(m, n))
+    assert got.equal(first) and (shifted[:1] == 7).all() and (shifted[1 + m * n:] == 7).all()
+
+
+@pytest.mark.parametrize("m", [1, 40, 140, 300])
+@pytest.mark.parametrize("k", [1, 17, 130, 255, 391])
+def test_what_lies_between_rows_is_not_read(handle, m, k):
+    """NaN in the bytes behind the channels of every row."""
+    x = operands(m, 150, k, "bf16", seed=k)
+    for name in ("a", "w"):
+        room = torch.full((x[name].shape[0], -(-k // 16) * 16 + 16), float("nan"), device=DEV).to(x[name].dtype)
+        room[:, :k] = x[name]
+        x[name] = room[:, :k]
+    check_product(handle("bf16"), x, "bf16")
+    check_product(handle("bf16", flags=SIMT), x, "bf16")
+
+
 def test_more_items_than_run_at_once(handle):
     """Persistent CTAs: batch rows of very uneven lengths one after another, some of them empty, odd numbers of tiles."""
     r = np.random.default_rng(0)
