@@ -415,6 +415,7 @@ vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, 
  *   strides     elements from one row to the next, 0 = dense.
  * Products of 8-bit numbers are exact; a block's sum is formed on the tensor cores, scaled and added to the others in fp32;
  * bias and add are added in fp32 before the one rounding to io_dtype.  VDN_FLAG_FORCE_SIMT: plain fp32 arithmetic throughout.
+ * The kernel, and with it the order of a sum, goes by M, N and K: a row's last bits may change with the number of rows beside it.
  * M up to 2^30 (0 is no error), N and K up to 2^21.  Needs no workspace.  Enqueues on cuda_stream and returns; does not synchronise. */
 typedef struct {
   uint32_t struct_size;      /* sizeof(vdn_vda_matmul_params), checked */

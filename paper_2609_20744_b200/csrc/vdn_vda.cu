@@ -1759,6 +1759,28 @@ vdn_status launch_matmul_pair(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   return VDN_OK;
 }
 
+// The channels of a product of few rows are cut among so many CTAs of a cluster: as many as fill two CTAs an SM, each with a block at least.
+int slim_parts(const vdn_vda_s* h, const vdn::MatmulArgs& g, int tok) {
+  const long long tiles = scale_blocks(g.N) * ((g.M + tok - 1) / tok);
+  int parts = 1;
+  while (parts < 8 && 2 * parts <= g.blocks && 2 * parts * tiles <= 2LL * h->sm_count) parts *= 2;
+  return parts;
+}
+
+// Whether more than 64 rows go as few (128 tokens to a tile, the channels cut among CTAs) or as many (pairs of CTAs with 256 x 256 tiles).
+// Microseconds, fitted to graph replays: 6 and 0.8 for each block that a CTA has, times the CTAs on an SM; 4.7 and 0.46 for each block
+// of each round of pairs.  5120 x 5120: 100 rows 16.6 as few, 22.6 as many, 256 rows 26.1 and 23.0; 300 x 9000: 512 rows 13.6 and 37.9;
+// 9000 x 2000: 200 rows 18.7 and 14.2.
+bool matmul_as_few(const vdn_vda_s* h, const vdn::MatmulArgs& g) {
+  if (g.M > 1024) return false;
+  const int parts = slim_parts(h, g, 128);
+  const double ctas = (double)scale_blocks(g.N) * ((g.M + 127) / 128) * parts, blocks = g.blocks;
+  const double tiles = (double)((g.M + 255) / 256) * ((g.N + 255) / 256);
+  const double few = 6.0 + 0.8 * blocks / parts * std::max(1.0, ctas / h->sm_count);
+  const double many = 4.7 + 0.46 * blocks * std::ceil(tiles / (h->sm_count / 2));
+  return few < many;
+}
+
 template <typename Tio, int TOK>
 vdn_status launch_matmul_slim(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st) {
   using G = vdn::MatmulSlim<TOK>;
@@ -1770,8 +1792,7 @@ vdn_status launch_matmul_slim(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_
   if ((r = allow_smem(h, kMatmulSlim + (TOK == 16 ? 0 : TOK == 32 ? 1 : TOK == 64 ? 2 : 3), vdn::matmul_slim_kernel<Tio, TOK>, G::SMEM_BYTES)) != VDN_OK)
     return r;
   const long long tiles_n = scale_blocks(g.N), tiles_m = (g.M + TOK - 1) / TOK;
-  int parts = 1;
-  while (parts < 8 && 2 * parts <= g.blocks && 2 * parts * tiles_n * tiles_m <= 2LL * h->sm_count) parts *= 2;
+  const int parts = slim_parts(h, g, TOK);
   const bool wide = rows_aligned16(g.out, g.out_stride, g.M, sizeof(Tio)) && (!g.add || rows_aligned16(g.add, g.add_stride, g.M, sizeof(Tio)));
   prof_begin(h, st);
   VDN_CUDA(h, launch_cluster(vdn::matmul_slim_kernel<Tio, TOK>, dim3((unsigned)(tiles_n * parts), (unsigned)tiles_m), (unsigned)parts, G::THREADS,
@@ -1794,7 +1815,7 @@ vdn_status launch_matmul(vdn_vda_t h, const vdn::MatmulArgs& g, cudaStream_t st)
     if (g.M <= 16) r = launch_matmul_slim<Tio, 16>(h, g, st);
     else if (g.M <= 32) r = launch_matmul_slim<Tio, 32>(h, g, st);
     else if (g.M <= 64) r = launch_matmul_slim<Tio, 64>(h, g, st);
-    else if (g.M <= 256) r = launch_matmul_slim<Tio, 128>(h, g, st);
+    else if (matmul_as_few(h, g)) r = launch_matmul_slim<Tio, 128>(h, g, st);
     else r = launch_matmul_pair<Tio>(h, g, st);
   }
   if (r != VDN_OK) return r;
@@ -1849,7 +1870,9 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
   L.parts = 1;
   if (a.B == 0 || a.Lq == 0) return L;
   const long long rows = (long long)a.Lq * a.group;
-  // (the tensor-core kernel finds a row's maximum before it scales)
+  // One or two rows of a key head: bytes, not products.  40 heads, 512 keys: 1 row 7.1 us on cross_few, 12.6 on the tensor cores, 2 rows 8.4 and
+  // 12.9, 4 rows 12.5 and 10.7; 32 requests of 4 rows, 8 key heads, 1500 keys: 84 and 53.  (The tensor-core kernel finds a row's maximum
+  // before it scales, hence a scale above zero.)
   L.tc = h->cfg.io_dtype == VDN_BF16 && !(h->cfg.flags & VDN_FLAG_FORCE_SIMT) && a.scale_log2 > 0.f && rows > 2;
   // keys of a batch row, by which parts are chosen (packed: the average)
   const long long keys = a.Lk ? a.Lk : a.n_keys / a.B;
@@ -1866,7 +1889,7 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     s.by_heads = vdn::fast_divide((uint32_t)a.Hk);
     s.by_head_blocks = vdn::fast_divide((uint32_t)s.head_blocks);
     L.units = (long long)a.B * a.Hk * s.pairs;
-    wanted = h->sm_count / L.units;
+    wanted = h->sm_count / L.units;                     // (a CTA an SM: twice or four times as many were slower, 32 requests 53 -> 59 us)
     least = 256;
   } else {
     least = 128;

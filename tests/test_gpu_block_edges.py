@@ -102,15 +102,16 @@ def test_kernels_go_by_sizes(handle):
         vda.profile(False)
         return name
 
-    def product(m):
-        x = operands(m, 256, 256, "bf16")
+    def product(m, n=256, k=256):
+        x = operands(m, n, k, "bf16")
         return kernel(lambda: vda.scaled_matmul(**x))
 
     def attention(lq, H, Hk, scale=None):
         x, _ = states(1, lq, H, Hk, 128, "bf16", [100])
         return kernel(lambda: vda.cross_attention(**x, scale=scale))
 
-    assert [product(m) for m in (1, 64, 256, 257, 2000)] == ["matmul_slim"] * 3 + ["matmul_pair"] * 2
+    assert [product(m) for m in (1, 64, 300, 2000)] == ["matmul_slim"] * 2 + ["matmul_pair"] * 2
+    assert product(300, 130, 5000) == "matmul_slim" and product(1025, 130, 5000) == "matmul_pair"
     assert attention(1, 2, 2) == attention(2, 2, 2) == attention(1, 4, 2) == "cross_few"
     assert attention(3, 2, 2) == attention(1, 3, 1) == attention(500, 2, 2) == "cross_tc"
     assert attention(50, 2, 2, scale=-1.0) == "cross_plain" and attention(50, 2, 2, scale=1.0) == "cross_tc"
