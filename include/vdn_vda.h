@@ -444,11 +444,13 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
  *   p->q_stride, k_stride, v_stride, out_stride   elements from one token to the next (also from the last of a batch row to the first
  *           of the next), 0 = dense; heads of a token are always dense.  Multiples of 16 bytes.
  *   workspace  DEVICE, 256-byte aligned, at least vdn_vda_cross_attention_workspace_bytes (0 where none is needed; NULL is fine
- *           then): long encoders are cut into parts where there are few queries.  An argument and not the handle's, so that
+ *           then): long encoders are cut into parts where there are few queries, and sums over more than 32768 keys in one part
+ *           (on the tensor cores) are kept there.  An argument and not the handle's, so that
  *           calls that may overlap, or captured graphs, can each have their own; nothing in it outlives the call.
  *   p->scale   -1e30 .. 1e30.
  * bf16 with three or more rows to a key head (queries times heads of its group) and a scale above zero runs on the tensor cores (weights
- * exp(z_j - max) rounded to bf16, sums fp32: out is off by about 2.3e-3 in the 2-norm, 1.7e-3 of it its own rounding); one or two rows,
+ * exp(z_j - max) rounded to bf16, sums fp32: out is off by about 2.3e-3 in the 2-norm, 1.7e-3 of it its own rounding, whatever
+ * the number of keys); one or two rows,
  * other scales, f32, and all with VDN_FLAG_FORCE_SIMT in plain fp32.  Kernels and parts are chosen by sizes alone (packed: by the average
  * length); lengths stay on the device.  What is not finite among q, k, v that count reaches its own rows of the result only.
  * Enqueues on cuda_stream and returns; does not synchronise. */

@@ -13,6 +13,9 @@
 // in the warps, 1400 in products and signals), two chains side by side.  Three exponentials in eight on the
 // multiply-add pipe: 8 % slower; 64 keys at a time with two S for each tile: 963 TFLOP/s (products of 64 columns take as long to issue
 // as those of 128); results stored by the threads instead of by tile copies: 1400 us at 87720 x 512.
+// The tensor cores cut off what an addition leaves over instead of rounding it, so a long sum of values of one sign falls short by about
+// 2^-27 for each of its keys: 5e-4 at 65536 keys, 7e-3 at 2^20, a tenth at 2^24.  Every FOLD tiles O and the sum of weights therefore
+// move to fp32 sums of their own (O's in the workspace), at most 3e-4 short, and start anew.  2^20 keys, 19456 rows, d = 128: 14.9 ms, 14.7 without.
 // Keys that do not count: their scores are replaced by -inf, their rows of V by zeros in shared memory (zero times what may
 // be anything is not zero).
 #pragma once
@@ -47,6 +50,7 @@ struct CrossTc {
   // starting late).  16384 x 16384: d = 128 1679 us whole, 1733 in halves; d = 64 1528, 1435.
   static constexpr int P_PARTS = D == 128 ? 1 : 2;
   static constexpr int COL_S = 0, COL_O = 256, COLS = 512;              // tensor memory: S of both tiles, O of both
+  static constexpr int FOLD = 256, ROWS = 256;                          // tiles between two moves of O; rows, a thread each
 };
 static_assert(CrossTc<128>::SMEM_BYTES <= 232448, "shared memory of a CTA");
 
@@ -72,7 +76,8 @@ __device__ __forceinline__ CrossItem cross_item(const CrossArgs& a, const CrossT
   return x;
 }
 
-template <int D>
+// LONG: some run of keys is longer than FOLD tiles.  (A variant of its own: in common code 87720 x 512 x 40 heads takes 1055 to 1100 us.)
+template <int D, bool LONG>
 __global__ void __launch_bounds__(CrossTc<D>::THREADS, 1)
 cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                 const __grid_constant__ CUtensorMap tmOut, const CrossArgs a, const CrossTcShape s, tc::DevStatus ds) {
@@ -214,7 +219,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
               if (elect_one()) {
 #pragma unroll
                 for (int k = part * (8 / G::P_PARTS); k < (part + 1) * (8 / G::P_PARTS); ++k)
-                  mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, k || j ? 1u : 0u);
+                  mma_bf16_ts(tmem + G::COL_O + c * D, tmem + G::COL_S + c * 128 + k * 8, dv + k * (2048 >> 4), id_o, k || (LONG ? j % G::FOLD : j) ? 1u : 0u);
                 if (part + 1 == G::P_PARTS) {
                   if (!more) mma_commit(O_FULL(c));
                   if (c + 1 == chains) mma_commit(EMPTY(st));
@@ -265,6 +270,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const int c = warp >> 2, qd = warp & 3;
     const uint32_t ts = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_S + c * 128, to = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_O + c * D;
     const float sl = a.scale_log2;
+    [[maybe_unused]] float* long_o = a.long_o + (size_t)blockIdx.x * (D * G::ROWS) + threadIdx.x;
     const int lane_head = lane % s.hb, lane_tok = lane / s.hb;
     const uint32_t out_smem = base + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES;
     unsigned char* out_row = base_ptr + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES + lane * 128;
@@ -279,6 +285,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       const bool row_on = lane < block_rows && head_in < a.group && tok < a.Lq;
       float ms = -INFINITY;                                    // the maximum times sl,
       uint64_t sum[2] = {0ull, 0ull};                          // and the sum relative to it, in four parts
+      float ms_long = -INFINITY, l_long = 0.f;                 // the same of the sums in the workspace
       for (int j = 0; j < x.tiles; ++j, ++n_s) {
         const int key0 = x.lo + j * 128;
         uint32_t on[4];
@@ -293,6 +300,25 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (!mbar_wait(S_FULL(c), n_s & 1, wc)) { ok = false; break; }
         tc_fence_after_sync();
+        if (LONG && j % G::FOLD == 0 && j > 0) {                       // (these scores follow the last product into O, and the next one waits for P)
+          const float keep = exp2_fast(ms_long - finite_max(ms));
+#pragma unroll 1
+          for (int i = 0; i < D; i += 16) {
+            float o[16];
+            tmem_ld16(to + i, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              float* at = long_o + (i + e) * G::ROWS;
+              *at = j == G::FOLD ? o[e] : fmaf(*at, keep, o[e]);
+            }
+          }
+          float l0, l1;
+          f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
+          l_long = fmaf(l_long, keep, l0 + l1);
+          sum[0] = sum[1] = 0ull;
+          ms_long = ms;
+        }
         // (twice, so that a tile whose keys all count has no branch in it: those cost 6 % of a long encoder's time)
         auto weights = [&](auto cut) {
           constexpr bool CUT = decltype(cut)::value;
@@ -375,6 +401,8 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       float l, l1;
       f2_unpack(f2_add(sum[0], sum[1]), l, l1);
       l += l1;
+      const float keep_long = LONG && x.tiles > G::FOLD ? exp2_fast(ms_long - finite_max(ms)) : 0.f;
+      if (LONG) l = fmaf(l_long, keep_long, l);
       const long long token = (long long)x.b * a.Lq + tok;
       const long long at = token * a.H + x.hk * a.group + head_in;
       const float r = l == 0.f ? 0.f : 1.f / l;
@@ -392,6 +420,10 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           if (i + 1 == G::CHUNKS) {
             tc_fence_before_sync();
             mbar_arrive_warp(O_EMPTY(c));
+          }
+          if (LONG && x.tiles > G::FOLD) {
+#pragma unroll
+            for (int e = 0; e < 64; ++e) o[e] = fmaf(long_o[(i * 64 + e) * G::ROWS], keep_long, o[e]);
           }
         } else {
 #pragma unroll

@@ -1707,7 +1707,7 @@ vdn_status make_bytes_map(vdn_vda_t h, CUtensorMap* m, const void* ptr, CUtensor
 }
 
 // Lets a kernel have its shared memory, once for a handle: `which` numbers the kernels of these entry points.
-enum BlockKernel { kMatmulPair /* three */, kMatmulSlim = kMatmulPair + 3, kCrossTc = kMatmulSlim + 4, kCrossPlain /* two */ };
+enum BlockKernel { kMatmulPair /* three */, kMatmulSlim = kMatmulPair + 3, kCrossTc = kMatmulSlim + 4 /* two */, kCrossPlain = kCrossTc + 2 /* two */ };
 template <typename... P>
 vdn_status allow_smem(vdn_vda_t h, int which, void (*kernel)(P...), int bytes) {
   if (h->block_attrs_set & (1u << which)) return VDN_OK;
@@ -1862,7 +1862,7 @@ struct CrossLayout {
   int rows;                 // plain kernels: rows of a CTA's tile; up to 8: cross_few, 64 or 128: cross_plain
   long long units;          // plain kernels: (batch row, key head, row tile); tensor cores: pairs of tiles
   int parts;
-  size_t o, ml, total;
+  size_t o, ml, long_o, long_bytes, total;
   vdn::CrossTcShape shape;
 };
 CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
@@ -1910,6 +1910,14 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     L.ml = align_up(n * h->cfg.d * sizeof(float));
     L.total = L.ml + align_up(n * sizeof(float2));
   }
+  // sums over more tiles than tensor memory may hold (packed: one batch row may have all keys)
+  using G = vdn::CrossTc<128>;
+  const long long tiles = ((a.Lk ? a.Lk : a.n_keys) + G::KEYS - 1) / G::KEYS;
+  if (L.tc && (tiles + L.parts - 1) / L.parts > G::FOLD) {
+    L.long_o = L.total;
+    L.long_bytes = align_up((size_t)std::min<long long>(L.units * L.parts, h->sm_count) * G::ROWS * h->cfg.d * sizeof(float));
+    L.total += L.long_bytes;
+  }
   return L;
 }
 
@@ -1948,9 +1956,11 @@ vdn_status launch_cross_tc(vdn_vda_t h, const vdn::CrossArgs& a, const CrossLayo
   tmK = tmV = tmQ;                                      // (no keys at all: never used)
   if (a.n_keys > 0 && ((r = make_key_map(h, &tmK, a.k, a, D, a.k_stride)) != VDN_OK || (r = make_key_map(h, &tmV, a.v, a, D, a.v_stride)) != VDN_OK))
     return r;
-  if ((r = allow_smem(h, kCrossTc, vdn::cross_tc_kernel<D>, G::SMEM_BYTES)) != VDN_OK) return r;
+  const bool is_long = L.long_bytes > 0;
+  auto kernel = is_long ? vdn::cross_tc_kernel<D, true> : vdn::cross_tc_kernel<D, false>;
+  if ((r = allow_smem(h, kCrossTc + (is_long ? 1 : 0), kernel, G::SMEM_BYTES)) != VDN_OK) return r;
   const unsigned grid = (unsigned)std::min<long long>(L.shape.items, h->sm_count);
-  vdn::cross_tc_kernel<D><<<grid, G::THREADS, G::SMEM_BYTES, st>>>(tmQ, tmK, tmV, tmOut, a, L.shape, dev_status(h));
+  kernel<<<grid, G::THREADS, G::SMEM_BYTES, st>>>(tmQ, tmK, tmV, tmOut, a, L.shape, dev_status(h));
   return VDN_OK;
 }
 
@@ -2121,6 +2131,7 @@ vdn_status vdn_vda_cross_attention(vdn_vda_t h, const void* q, const void* k, co
   a.parts = L.parts;
   a.part_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + L.o);
   a.part_ml = reinterpret_cast<float2*>(static_cast<unsigned char*>(workspace) + L.ml);
+  a.long_o = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + L.long_o);
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
