@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(256) cross_few_kernel(CrossArgs a) {
 // while the values are summed (f32: by asynchronous copies).  A thread has 4 x 4 scores (rows of its own, keys 16 apart: reads
 // without bank conflicts) and 4 x D/16 results, both as pairs for packed arithmetic (scores: sums over even and odd channels); the
 // 16 threads of a row lie side by side in a warp.  Bound by the multiply-adds and the shared-memory reads that feed them: 4096 x 4096 x
-// 8 heads, f32: d = 128 1850 us, 37 TFLOP/s, d = 64 1045 us, 33 TFLOP/s.  (8 x 4 scores a thread, half as many threads: 2890 us.)
+// 8 heads, f32: d = 128 1825 us, 38 TFLOP/s, d = 64 1053 us, 33 TFLOP/s.  (8 x 4 scores a thread, half as many threads: 2890 us.)
 template <int D, int TILE>
 struct CrossPlain {
   static constexpr int ROWS = TILE, KEYS = 64, THREADS = 4 * ROWS, PITCH = D + 4, P_PITCH = KEYS + 4;
@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(CrossPlain<D, TILE>::THREADS, 512 / CrossPlain
     for (int j = 0; j < 4; ++j) on[j] = j0 + tx + 16 * j < hi && key_counts(a, start + j0 + tx + 16 * j);
     cp_async_wait<1>();                                                  // the keys
     __syncthreads();
+    float keep[4];
     uint64_t z2[4][4] = {};
 #pragma unroll 4
     for (int c = 0; c < D; c += 4) {
@@ -316,24 +317,25 @@ __global__ void __launch_bounds__(CrossPlain<D, TILE>::THREADS, 512 / CrossPlain
       }
 #pragma unroll
       for (int s = 8; s > 0; s /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
-      const float base = finite_max(top), keep = exp2_fast(m[i] - base);
+      const float base = finite_max(top);
+      keep[i] = exp2_fast(m[i] - base);
       m[i] = top;
-      l[i] *= keep;
+      float sum = 0.f;                                                   // (this thread's keys; the row's 16 are added at the end)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float p = exp2_fast(z[j] - base);
-        l[i] += p;                                                       // (this thread's keys; the row's 16 are added at the end)
+        sum += p;
         sp[(ty * 4 + i) * S::P_PITCH + tx + 16 * j] = p;
       }
-      const uint64_t keep2 = f2_pack(keep, keep);
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) o[i][c] = f2_fma(o[i][c], keep2, 0ull);
+      l[i] = fmaf(l[i], keep[i], sum);
     }
     __syncthreads();                                                     // all have read the keys
     if (j0 + S::KEYS < hi) fetch(sk, a.k, a.k_stride, j0 + S::KEYS);
     else cp_async_commit();
     cp_async_wait<1>();                                                  // the values
     __syncthreads();
+    // a tile's values by themselves first: what is small beside a long sum would get lost in it
+    uint64_t t[4][D / 32] = {};
 #pragma unroll 2
     for (int j = 0; j < S::KEYS; j += 4) {
       float4 p[4];
@@ -348,11 +350,15 @@ __global__ void __launch_bounds__(CrossPlain<D, TILE>::THREADS, 512 / CrossPlain
           for (int i = 0; i < 4; ++i) {
             const float w = u == 0 ? p[i].x : u == 1 ? p[i].y : u == 2 ? p[i].z : p[i].w;
             const uint64_t w2 = f2_pack(w, w);
-            o[i][2 * c] = f2_fma(w2, y.x, o[i][2 * c]);
-            o[i][2 * c + 1] = f2_fma(w2, y.y, o[i][2 * c + 1]);
+            t[i][2 * c] = f2_fma(w2, y.x, t[i][2 * c]);
+            t[i][2 * c + 1] = f2_fma(w2, y.y, t[i][2 * c + 1]);
           }
         }
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[i][c] = f2_fma(o[i][c], f2_pack(keep[i], keep[i]), t[i][c]);
     __syncthreads();                                                     // ... and the values
   }
   cp_async_wait<0>();

@@ -72,6 +72,23 @@ def test_mean_of_ones_over_a_million_keys(d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+def test_mean_of_ones_over_a_million_keys_in_f32(d):
+    """Sum and weighted values take 64 + n / 64 additions, each off by at most u32 of a sum that grows to its end: u32 / 3 for each in the
+    mean square, 8 sqrt(64 + n / 64) sqrt(2) u32 / 3 < 8 sqrt(64 + n / 64) u32 / 2 between the two."""
+    n = 1 << 20
+    g = torch.Generator(device=DEV).manual_seed(d)
+    q = torch.randn(1, 128 * 148, 1, d, generator=g, device=DEV)
+    k = torch.randn(1, n, 1, d, generator=g, device=DEV)
+    vda = binding.Vda(d, "f32")
+    out, lse = vda.cross_attention(q, k, torch.ones_like(k), lse=True)
+    assert vda.launch_count() == 1
+    assert float((out - 1).abs().max()) <= 8 * math.sqrt(64 + n / 64) * U32 / 2
+    for i in range(0, q.shape[1], 2377):
+        want = torch.logsumexp(k[0, :, 0].double() @ q[0, i, 0].double() * d ** -0.5, 0)
+        assert abs(float(lse[0, i, 0]) - float(want)) <= 2.0 ** -18                        # 2 d u32 of a score of about 10, and the above
+
+
+@pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n", [32768, 32769, 65536, 70001])
 @pytest.mark.parametrize("louder", [False, True])
 def test_keys_around_where_sums_move(d, n, louder):
