@@ -410,7 +410,8 @@ vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, 
  *   a       [M, K], w [N, K]: one byte an element, DEVICE, 16-byte aligned, rows at multiples of 16 bytes; K need not be one.
  *   out     [M, N] of cfg.io_dtype, DEVICE, any alignment of its elements (16-byte aligned rows are faster).  May be add, and
  *           must not alias another input.
- *   p->a_scale  float [M, ceil(K / 128)], p->w_scale float [ceil(N / 128), ceil(K / 128)]: any values, not only those of vdn_vda_quantize.
+ *   p->a_scale  float [M, ceil(K / 128)], p->w_scale float [ceil(N / 128), ceil(K / 128)]: any values, not only those of vdn_vda_quantize; a
+ *           pair whose product leaves the normal fp32 numbers is applied one after the other, so that only the terms have to be in range.
  *   p->bias     float [N] or NULL;   p->add [M, N] of cfg.io_dtype or NULL: Eq. 1d's other branch, or a residual.
  *   strides     elements from one row to the next, 0 = dense.
  * Products of 8-bit numbers are exact; a block's sum is formed on the tensor cores, scaled and added to the others in fp32;

@@ -23,6 +23,19 @@ __device__ __forceinline__ float2 from_e4m3x2(uint32_t x) {
   return __half22float2(__half2(h));
 }
 
+// The two scales of a block as one factor: the result, with `first` = 1.  Where their product is no normal number although what it stands
+// for may well be (a block's sum is 0 or 2^-18 .. 2^24.6), it is two: the sum times `first`, then times the result.  The larger goes first
+// where the product is too small, the smaller where it is too large, so that the step between leaves the range only if the end does.
+__device__ __forceinline__ bool normal_number(float x) { return (__float_as_uint(x) & 0x7FFFFFFFu) - 0x00800000u < 0x7F000000u; }
+__device__ __forceinline__ float join_scales(float sa, float sw, float& first) {
+  const float s = sa * sw;
+  first = 1.f;
+  if (normal_number(s) || sa == 0.f || sw == 0.f) return s;
+  const bool a_first = (fabsf(sa) > fabsf(sw)) == (fabsf(s) < 1.f);
+  first = a_first ? sa : sw;
+  return a_first ? sw : sa;
+}
+
 template <typename Tio>
 __global__ void __launch_bounds__(256) matmul_simt_kernel(MatmulArgs p) {
   constexpr int TILE = 64, KC = 32;
@@ -56,9 +69,9 @@ __global__ void __launch_bounds__(256) matmul_simt_kernel(MatmulArgs p) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const long long m = m0 + ty * 4 + i;
-      const float s = m < p.M ? p.a_scale[m * p.blocks + b] * ws : 0.f;
+      float first, s = join_scales(m < p.M ? p.a_scale[m * p.blocks + b] : 0.f, ws, first);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(part[i][j], s, acc[i][j]);
+      for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(part[i][j] * first, s, acc[i][j]);
     }
   }
 #pragma unroll

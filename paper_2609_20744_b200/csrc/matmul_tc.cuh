@@ -43,6 +43,22 @@ __device__ __forceinline__ void add_bias(const MatmulArgs& p, int n, float (&x)[
   }
 }
 
+// An accumulator's sums times `factor(column)`, where they lie: what blocks need whose scales do not make one factor, out of the way of
+// those that the rest of the loop is laid out for (the same in its registers: 32768 x 5120 x 5120 3 % slower, 128 rows 18.9 -> 23.1 us).
+template <int COLS, typename F>
+__device__ __forceinline__ void scale_in_place(uint32_t taddr, F factor) {
+#pragma unroll 1
+  for (int c = 0; c < COLS; c += 16) {
+    float v[16];
+    tc::tmem_ld16(taddr + c, v);
+    tc::tmem_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] *= factor(c + i);
+    tc::tmem_st16(taddr + c, v);
+    tc::tmem_wait_st();
+  }
+}
+
 // How results leave: by tile copies; by tile copies, `add` coming the same way; or element by element, where one of them has rows that no tile
 // copy can reach, or that end inside 16 bytes.  Variants of their own: in common code the first takes 6 % longer with the second's (753 -> 800 us at
 // 32768 x 5120 x 5120), and spills with the third's.
@@ -168,13 +184,18 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       uint64_t acc[64];
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0ull;
-      float xa = __ldg(sa), xw = __ldg(sw);
+      float s = __ldg(sa) * __ldg(sw), xa = 0.f, xw = 0.f;
+      bool odd = __any_sync(0xffffffffu, !normal_number(s));
       for (int b = 0; b < p.blocks; ++b, ++it) {
         const int a = it & 1;
-        const float s = xa * xw;
         if (b + 1 < p.blocks) { xa = __ldg(sa + b + 1); xw = __ldg(sw + b + 1); }
         if (!mbar_wait(ACCFULL(a), (it >> 1) & 1, wc)) { ok = false; break; }
         tc_fence_after_sync();
+        if (odd) {
+          float first;
+          s = join_scales(__ldg(sa + b), __ldg(sw + b), first);
+          if (__any_sync(0xffffffffu, first != 1.f)) scale_in_place<128>(taddr + a * G::COLS, [&](int) { return first; });
+        }
         // The accumulator is free once it has been read: half of it waits in registers (there is no room for all), and only that half
         // is added before the rest has been fetched.
         const uint64_t s2 = f2_pack(s, s);
@@ -186,6 +207,8 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(rank_address(ACCEMPTY(a), 0));
+        s = xa * xw;                                       // the next block's
+        odd = __any_sync(0xffffffffu, !normal_number(s));
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[32 + i] = f2_fma(v[i], s2, acc[32 + i]);
       }
@@ -313,7 +336,7 @@ template <int TOK>
 struct MatmulSlim {
   static constexpr int THREADS = 192, STAGE_BYTES = 128 * 128 + TOK * 128;
   static constexpr int STAGES = TOK <= 32 ? 5 : TOK <= 64 ? 4 : 3;             // two CTAs to an SM
-  static constexpr int OFF_SCALE = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALE + 2 * TOK * 4;
+  static constexpr int OFF_SCALE = STAGES * STAGE_BYTES, OFF_BAR = OFF_SCALE + 3 * TOK * 4;
   static constexpr int USED_BYTES = OFF_BAR + 8 * (2 * STAGES + 4) + 16;
   static constexpr int SMEM_BYTES = USED_BYTES + 1024;
   static constexpr int TMEM_COLS = 2 * TOK < 32 ? 32 : 2 * TOK;
@@ -395,7 +418,8 @@ matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   } else {
     // The factors of a block, one for each token, go through shared memory: a thread brings one token's and reads all.
     const uint32_t taddr = tmem + ((uint32_t)(warp * 32) << 16);
-    float* factors = reinterpret_cast<float*>(base_ptr + G::OFF_SCALE);
+    float* factors = reinterpret_cast<float*>(base_ptr + G::OFF_SCALE);    // [2][TOK]
+    float* firsts = factors + 2 * TOK;                                     // [TOK], where a token's are two
     const bool mine = (int)threadIdx.x < TOK && m0 + threadIdx.x < p.M;
     const float* sa = p.a_scale + (mine ? (m0 + threadIdx.x) * p.blocks : 0);
     const float* sw = p.w_scale + (long long)(n0 / kScaleBlock) * p.blocks;
@@ -403,15 +427,23 @@ matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     float acc[TOK];
 #pragma unroll
     for (int i = 0; i < TOK; ++i) acc[i] = 0.f;
-    float s = mine && b_lo < b_hi ? __ldg(sa + b_lo) * __ldg(sw + b_lo) : 0.f;
+    float xa = mine && b_lo < b_hi ? __ldg(sa + b_lo) : 0.f, xw = mine && b_lo < b_hi ? __ldg(sw + b_lo) : 0.f;
     uint32_t it = 0;
     bool ok = true;
     for (int b = b_lo; b < b_hi; ++b, ++it) {
       const int a = it & 1;
+      float first;
+      const float s = join_scales(xa, xw, first);
       if ((int)threadIdx.x < TOK) factors[a * TOK + threadIdx.x] = s;
-      if (mine && b + 1 < b_hi) s = __ldg(sa + b + 1) * __ldg(sw + b + 1);
+      if (mine && b + 1 < b_hi) { xa = __ldg(sa + b + 1); xw = __ldg(sw + b + 1); }
       ok = mbar_wait(ACCFULL(a), (it >> 1) & 1, wc);
-      if (named_barrier_or(1, 128, !ok)) { ok = false; break; }
+      // (one barrier for both pieces of news; which of them it is, a second one tells)
+      if (named_barrier_or(1, 128, !ok || first != 1.f)) {
+        if ((int)threadIdx.x < TOK) firsts[threadIdx.x] = first;
+        if (named_barrier_or(1, 128, !ok)) { ok = false; break; }
+        tc_fence_after_sync();
+        scale_in_place<TOK>(taddr + a * TOK, [&](int i) { return firsts[i]; });
+      }
       tc_fence_after_sync();
 #pragma unroll
       for (int c = 0; c < TOK / W; ++c) {
