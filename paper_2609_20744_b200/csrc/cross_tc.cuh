@@ -298,7 +298,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           }
           all = (on[0] & on[1] & on[2] & on[3]) == 0xffffffffu;
         }
-        if (!mbar_wait(S_FULL(c), n_s & 1, wc)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(S_FULL(c), n_s & 1, wc))) { ok = false; break; }
         tc_fence_after_sync();
         if (LONG && j % G::FOLD == 0 && j > 0) {                       // (these scores follow the last product into O, and the next one waits for P)
           const float keep = exp2_fast(ms_long - finite_max(ms));
@@ -394,7 +394,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       }
       if (!ok) break;
       if (x.tiles > 0) {
-        if (!mbar_wait(O_FULL(c), n_item & 1, wc)) { ok = false; break; }
+        if (!__all_sync(0xffffffffu, mbar_wait(O_FULL(c), n_item & 1, wc))) { ok = false; break; }
         ++n_item;
         tc_fence_after_sync();
       }

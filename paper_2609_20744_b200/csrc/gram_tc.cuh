@@ -174,7 +174,7 @@ gram_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
     uint32_t ai = 0;
     for (long long item = blockIdx.x; item < nitems; item += gridDim.x, ++ai) {
       const int a = ai & 1;
-      if (!mbar_wait(ACCFULL(a), (ai >> 1) & 1, wc)) break;
+      if (!mbar_wait_warp(ACCFULL(a), (ai >> 1) & 1, wc)) break;
       tc_fence_after_sync();
       const uint32_t taddr = tmem_base + ((uint32_t)(qd * 32) << 16) + a * 256;
       int b, h, t;
@@ -222,10 +222,10 @@ gram_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ 
         const float bu[2] = {bnext[0], bnext[1]};
         if (tile + 1 < ntiles) load_beta(item, tile + 1, bnext);
         else load_beta(item + gridDim.x, 0, bnext);
-        if (!mbar_wait(FULL(st), (it / G::STAGES) & 1, wc)) { ok = false; break; }
+        if (!mbar_wait_warp(FULL(st), (it / G::STAGES) & 1, wc)) { ok = false; break; }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          if (!mbar_wait(KPFREE(half), (it & 1) ^ 1, wc)) { ok = false; break; }
+          if (!mbar_wait_warp(KPFREE(half), (it & 1) ^ 1, wc)) { ok = false; break; }
           const unsigned char* src = base_ptr + st * G::STAGE_BYTES + c * G::BOX_BYTES + (half * 64 + r) * 128;
           unsigned char* dst = base_ptr + G::OFF_KP + half * G::KP_HALF_BYTES + c * (64 * 128) + r * 128;
           // beta rounded to bf16, then one packed bf16 multiply per channel pair (round to nearest): the

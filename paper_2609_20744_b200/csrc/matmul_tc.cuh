@@ -159,6 +159,10 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     const uint32_t out_smem = base + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
     unsigned char* out_ptr = base_ptr + G::OFF_OUT + warp * 2 * G::OUT_BYTES;
     constexpr int PER = 128 / (int)sizeof(Tio), SLICES = 128 / PER;
+    // Whether this lane's waits for sums have all ended in time.  No lane acts on that by itself: the vote on the next block's scales carries
+    // it, and until then sums that are not there are added like others.  (A vote of its own at the wait: 1 % longer; one for both there: 1 to
+    // 3 %, 10 % where results and add leave element by element.)
+    bool in_time = true;
     uint32_t it = 0, phase = 0;                          // phase: of the two staging tiles' barriers, a bit each
     bool ok = true;
     for (long long t = first; t < tiles && ok; t += step) {
@@ -185,13 +189,14 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
 #pragma unroll
       for (int i = 0; i < 64; ++i) acc[i] = 0ull;
       float s = __ldg(sa) * __ldg(sw), xa = 0.f, xw = 0.f;
-      bool odd = __any_sync(0xffffffffu, !normal_number(s));
+      bool odd = __any_sync(0xffffffffu, !normal_number(s));   // anything out of the ordinary
       for (int b = 0; b < p.blocks; ++b, ++it) {
         const int a = it & 1;
         if (b + 1 < p.blocks) { xa = __ldg(sa + b + 1); xw = __ldg(sw + b + 1); }
-        if (!mbar_wait(ACCFULL(a), (it >> 1) & 1, wc)) { ok = false; break; }
+        in_time = mbar_wait(ACCFULL(a), (it >> 1) & 1, wc) && in_time;
         tc_fence_after_sync();
         if (odd) {
+          if (__any_sync(0xffffffffu, !in_time)) break;
           float first;
           s = join_scales(__ldg(sa + b), __ldg(sw + b), first);
           if (__any_sync(0xffffffffu, first != 1.f)) scale_in_place<128>(taddr + a * G::COLS, [&](int) { return first; });
@@ -208,10 +213,11 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(rank_address(ACCEMPTY(a), 0));
         s = xa * xw;                                       // the next block's
-        odd = __any_sync(0xffffffffu, !normal_number(s));
+        odd = __any_sync(0xffffffffu, !normal_number(s) || !in_time);
 #pragma unroll
         for (int i = 0; i < 32; ++i) acc[32 + i] = f2_fma(v[i], s2, acc[32 + i]);
       }
+      if (odd) ok = !__any_sync(0xffffffffu, !in_time);
       if (!ok) {
         if (ADD && here)                            // a bounded chance for copies under way to land
           for (int c = 0; c < 2 && n0 + c * PER < p.N; ++c) mbar_drain(ADDED(warp * 2 + c), (phase >> c) & 1);
@@ -268,7 +274,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           const int n = n0 + c * PER;
           const bool by_tile = ADD && here && n < p.N;
           if (by_tile) {
-            if (!mbar_wait(ADDED(warp * 2 + slot), (phase >> slot) & 1, wc)) ok = false;
+            if (!mbar_wait_warp(ADDED(warp * 2 + slot), (phase >> slot) & 1, wc)) { ok = false; break; }
             phase ^= 1u << slot;
           }
           unsigned char* row = out_ptr + slot * G::OUT_BYTES + lane * 128;

@@ -208,7 +208,7 @@ readout_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (lane == 0) ok = mbar_wait(QFULL(st), (qi / R::QSTAGES) & 1, wc);
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
-        if (!mbar_wait(QFULL(st), (qi / R::QSTAGES) & 1, wc)) { ok = false; break; }
+        if (!mbar_wait_warp(QFULL(st), (qi / R::QSTAGES) & 1, wc)) { ok = false; break; }
         const unsigned char* qrowp = base_ptr + R::OFF_Q + st * R::TILE_BYTES + qrow * 128;
         // packed fp32 pairs: these warps share their schedulers with the epilogue warps, whose per-tile chain sets
         // the pace of the kernel, so every instruction here counts
@@ -239,7 +239,7 @@ readout_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         // the read (a later tile cannot have completed that barrier again: it needs this slot first).  The Q stage
         // goes back only after this wait: measured, handing it back before the wait is slower (768p clip, 148
         // CTAs: 1.39 instead of 1.25 ms) -- the producer running further ahead of the epilogue does not help.
-        if (qi >= QS && !mbar_wait(ACCEMPTY((qi - QS) & 3), ((qi - QS) >> 2) & 1, wc)) { ok = false; break; }
+        if (qi >= QS && !mbar_wait_warp(ACCEMPTY((qi - QS) & 3), ((qi - QS) >> 2) & 1, wc)) { ok = false; break; }
         qn[(qi % QS) * 128 + qrow] = rsqrtf(ss + q_l2_eps);
         mbar_arrive_warp(QEMPTY(st));
         mbar_arrive_warp(QNFULL(qi % QS));
@@ -292,11 +292,11 @@ readout_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
       }
       for (int tile = 0; tile < ntiles; ++tile, ++qi) {
         const int a = qi & 3;
-        if (!mbar_wait(ACCFULL(a), (qi >> 2) & 1, wc)) { give_up(); break; }
+        if (!mbar_wait_warp(ACCFULL(a), (qi >> 2) & 1, wc)) { give_up(); break; }
         tc_fence_after_sync();
         float qrs = 1.0f;
         if constexpr (QNORM) {
-          if (!mbar_wait(QNFULL(qi % QS), (qi / QS) & 1, wc)) { give_up(); break; }
+          if (!mbar_wait_warp(QNFULL(qi % QS), (qi / QS) & 1, wc)) { give_up(); break; }
           qrs = reinterpret_cast<const float*>(base_ptr + R::OFF_QN)[(qi % QS) * 128 + row];
         }
         const uint32_t taddr = tmem_base + ((uint32_t)(qd * 32) << 16) + a * 128;
@@ -326,7 +326,7 @@ readout_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
         if (use_ge) {
           // the gate tile sits in the staging tile (its copy was issued after the store that last used the tile
           // had been read)
-          if (!mbar_wait(GFULL(ob), (qi / R::NOUT) & 1, wc)) { give_up(); break; }
+          if (!mbar_wait_warp(GFULL(ob), (qi / R::NOUT) & 1, wc)) { give_up(); break; }
         } else {
           if (et == 0) tma_store_wait_read<R::NOUT - 1>();   // the store that last used this staging tile has read it
           if (named_barrier_or(1, 128, false)) { ok = false; break; }

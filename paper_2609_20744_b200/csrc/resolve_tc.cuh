@@ -305,7 +305,7 @@ resolve_tc_kernel(const float* __restrict__ stats, __nv_bfloat16* __restrict__ c
       mbar_arrive_warp(XREADY);
 
       // ---- coefficients: c = -M[i][P] Gi = -+(Y Gi) from the tensor cores; a pivot row a takes Gi[a]
-      if (!mbar_wait(CDONE, step & 1, wc)) { ok = false; continue; }
+      if (!mbar_wait_warp(CDONE, step & 1, wc)) { ok = false; continue; }
       tc_fence_after_sync();
       float c[16];
       tmem_ld16(trow + p0, c);
@@ -331,7 +331,7 @@ resolve_tc_kernel(const float* __restrict__ stats, __nv_bfloat16* __restrict__ c
       fence_proxy_async_smem();
       tc_fence_before_sync();
       mbar_arrive_warp(OPREADY);
-      if (!mbar_wait(MMADONE, step & 1, wc)) { ok = false; continue; }
+      if (!mbar_wait_warp(MMADONE, step & 1, wc)) { ok = false; continue; }
       tc_fence_after_sync();
       // ---- column fix: M[i][P] = c (for a pivot row: Gi[a])
       tmem_st16(trow + p0, c);

@@ -377,7 +377,7 @@ scan_tc_kernel(const __grid_constant__ CUtensorMap tmC, const ScanTcArgs a, tc::
     if (!additive && writes && nsteps > 1) load_bt(1, bt);
     float a_next = nsteps > 1 ? step_decay(1) : 1.0f;
     for (int s = 0; s < nsteps; ++s) {
-      if (!mbar_wait(ACCFULL, s & 1, wc)) break;
+      if (!mbar_wait_warp(ACCFULL, s & 1, wc)) break;
       tc_fence_after_sync();
       float z[CW];
       tmem_ld32(taddr, z);

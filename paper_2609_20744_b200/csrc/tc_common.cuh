@@ -84,6 +84,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const W
   }
 }
 
+// The wait of a whole warp.  mbar_wait answers each lane by itself, and a barrier may complete between one lane's giving up and another's
+// look at it; lanes that disagreed and met in an instruction of the whole warp (tensor memory, votes, __syncwarp) would stand there
+// for ever.  So a warp that goes on as a whole decides as a whole.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtx& w) {
+  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
+}
+
 // After a wait gave up: the copy last issued on `bar` completes the phase of parity `parity`; give it a bounded
 // chance to land before the CTA retires and its shared memory goes to another CTA.  (Asking for either parity would
 // return at once: the phase before the current one always counts as complete.)
@@ -325,11 +333,6 @@ __device__ __forceinline__ bool elect_one() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
   return p != 0;
 }
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const WaitCtx& w) {
-  if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-  return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
-}
-
 // mbarrier arrive once every MMA issued so far by this thread has completed.
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
