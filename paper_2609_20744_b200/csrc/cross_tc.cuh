@@ -463,6 +463,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 9) {
+    settle(bar0 + 8u * G::BARS + 4u);
     tc_fence_after_sync();
     tmem_dealloc(tmem, G::COLS);
   }

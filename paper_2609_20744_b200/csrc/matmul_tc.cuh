@@ -127,7 +127,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             tma_load_2d_pair(dst + G::A_BYTES, &tmW, bar, b * kScaleBlock, n0);
           }
         }
-        // (the even CTA's barriers count the copies of both; the odd one leaves with it, at the cluster's barrier)
+        // (the even CTA's barriers count the copies of both)
         if (!ok && rank == 0) mbar_drain_ring(FULL(0), G::STAGES, it);
       }
     } else if (warp == 9 && rank == 0) {
@@ -325,6 +325,7 @@ matmul_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   __syncthreads();
   cluster_sync();
   if (warp == 9) {
+    settle(bar0 + 8u * G::BARS + 4u);
     tc_fence_after_sync();
     tmem_dealloc_pair(tmem, 512);
   }
@@ -482,10 +483,6 @@ matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   tc_fence_before_sync();
   __syncthreads();
   cluster_sync();
-  if (warp == 5) {
-    tc_fence_after_sync();
-    tmem_dealloc(tmem, G::TMEM_COLS);
-  }
   // A rank's share of the tokens: four neighbouring features of one to a thread, from all ranks.
   const int lo = TOK * part / parts, hi = (int)min((long long)(TOK * (part + 1) / parts), p.M - m0);
 #pragma unroll 2
@@ -519,6 +516,11 @@ matmul_slim_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     }
   }
   __syncwarp();
+  if (warp == 5) {
+    settle(bar0 + 8u * (2 * G::STAGES + 4) + 4u);
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, G::TMEM_COLS);
+  }
   cluster_sync();
 }
 

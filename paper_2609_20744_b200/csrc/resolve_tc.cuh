@@ -365,6 +365,7 @@ resolve_tc_kernel(const float* __restrict__ stats, __nv_bfloat16* __restrict__ c
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 4) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 128);
   }

@@ -418,6 +418,7 @@ scan_tc_kernel(const __grid_constant__ CUtensorMap tmC, const ScanTcArgs a, tc::
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 1) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 128);
   }

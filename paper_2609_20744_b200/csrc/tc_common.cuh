@@ -107,6 +107,20 @@ __device__ __forceinline__ void mbar_drain_ring(uint32_t first, uint32_t stages,
   }
 }
 
+// Between a CTA's last barrier and its end, by the warp that gives the tensor memory back: where a wait ran out, copies, products and their
+// signals may still be on their way into this CTA (or, of a pair, into the other), also those of roles that had nothing left to wait
+// for.  Milliseconds are more than any of them takes.  `flag` is the abort flag's shared-memory address.
+__device__ __forceinline__ void settle(uint32_t flag) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b32 f;\n\t"
+      "ld.volatile.shared.b32 f, [%0];\n\t"
+      "setp.ne.u32 p, f, 0;\n\t"
+      "@p nanosleep.u32 1000000;\n\t@p nanosleep.u32 1000000;\n\t@p nanosleep.u32 1000000;\n\t}"
+      ::"r"(flag)
+      : "memory");
+  __syncwarp();
+}
+
 // ---------------------------------------------------------------------------------------------- proxies
 __device__ __forceinline__ void fence_proxy_async_smem() {
   asm volatile("fence.proxy.async.shared::cta;" ::: "memory");

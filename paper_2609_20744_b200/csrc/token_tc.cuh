@@ -586,6 +586,7 @@ token_prep_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 0) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(*tmem_slot, 128);
   }
@@ -974,6 +975,7 @@ token_chain_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constan
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 1) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
   }
@@ -1242,6 +1244,7 @@ token_compose_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_const
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 1) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
   }

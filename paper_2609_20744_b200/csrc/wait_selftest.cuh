@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(64, 1) wait_expiry_selftest_kernel(tc::DevStat
   tc_fence_before_sync();
   __syncthreads();
   if (warp == 1) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 32);
   }

@@ -83,3 +83,15 @@ def test_the_rule_tells_them_apart():
     assert lonely_waits("{ if (lane == 0) { for (;;) { if (!%s) break; } } }" % wait) == []
     assert lonely_waits("{ if (!__all_sync(0xffffffffu, %s)) break; }" % wait) == []
     assert lonely_waits("{ if (!mbar_wait_warp(FULL, 0, wc)) break; tmem_ld16(a, b); }") == []
+
+
+@pytest.mark.parametrize("path", sorted(glob.glob(os.path.join(CSRC, "*.cuh"))), ids=os.path.basename)
+def test_a_block_that_gave_up_settles_before_it_goes(path):
+    """What is on its way into a block's shared and tensor memory is given time before either goes to another: between the last barrier
+    and the return of tensor memory (which a cluster's last barrier follows)."""
+    text = source(path)
+    for m in re.finditer(r"\btmem_dealloc(_pair)?\(", text):
+        if re.search(r"\bvoid\s+$", text[: m.start()]):                       # the definition
+            continue
+        end = text[text.rindex("__syncthreads();", 0, m.start()): m.start()]
+        assert "settle(" in end, text[: m.start()].count("\n") + 1
