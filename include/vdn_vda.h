@@ -42,7 +42,7 @@
  * synchronising cuda_stream still covers everything.
  *
  * Errors.  Every call returns a vdn_status; nothing throws, aborts or traps.  Problems the host can see
- * (null or misaligned pointers, non-positive sizes, d != cfg.d, workspace too small, 32-bit index overflow,
+ * (null or misaligned pointers -- small operands are aligned to their elements --, non-positive sizes, d != cfg.d, workspace too small, 32-bit index overflow,
  * wrong device architecture) are reported synchronously and nothing is enqueued.  Every wait inside a
  * kernel is bounded (vdn_vda_set_wait_limit_us); a wait that runs out records VDN_ERR_TIMEOUT in the handle's
  * status word, which vdn_vda_status returns once the caller has synchronised the stream and which stays set

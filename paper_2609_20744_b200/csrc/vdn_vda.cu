@@ -557,6 +557,9 @@ vdn_status launch_scan_static(const float* stats, const float* inv, float* read,
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+// (what is read element by element; null is aligned)
+template <typename T>
+bool aligned(const T* p) { return reinterpret_cast<uintptr_t>(p) % alignof(T) == 0; }
 
 // Feature preparation: the spatial filter of K and V (when filters are passed), their temporal half in place, Q.
 template <typename Tio, int D>
@@ -1230,6 +1233,8 @@ vdn_status plan_token(vdn_vda_t h, const void* q, const void* k, const void* v, 
   if (n_tokens > 0 && (!q || !k || !v || !beta || !out)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(p->s0) || !aligned16(p->state))
     return fail(h, VDN_ERR_INVALID_ARG, "q, k, v, out and the states must be 16-byte aligned");
+  if (!aligned(beta) || !aligned(p->log_alpha) || !aligned(p->cu_seqlens) || !aligned(p->index))
+    return fail(h, VDN_ERR_INVALID_ARG, "beta, log_alpha, cu_seqlens and index must be aligned to their elements");
   if (out && (out == q || out == k || out == v)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias an input");
   // (two keys of zero have the factor 1 / l2_eps, which must be finite: times their product, zero, it would be NaN)
   if (!(p->l2_eps >= 0.f) || p->l2_eps > 1e30f || (p->l2_eps > 0.f && p->l2_eps < FLT_MIN) || !std::isfinite(p->scale))
@@ -1610,6 +1615,8 @@ vdn_status vdn_vda_rotate(vdn_vda_t h, const void* q_in, const void* k_in, void*
     return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
   if (!aligned16(q_in) || !aligned16(k_in) || !aligned16(q_out) || !aligned16(k_out))
     return fail(h, VDN_ERR_INVALID_ARG, "q and k must be 16-byte aligned");
+  if (!aligned(p->freq) || !aligned(p->axis) || !aligned(p->positions) || !aligned(p->q_weight) || !aligned(p->k_weight))
+    return fail(h, VDN_ERR_INVALID_ARG, "freq, axis, positions and the norm weights must be aligned to their elements");
   if (k_in && (q_out == k_in || k_out == q_in || q_out == k_out))
     return fail(h, VDN_ERR_INVALID_ARG, "an output may only alias its own input");
   if (d != h->cfg.d) return fail(h, VDN_ERR_INVALID_ARG, "d differs from the handle's configured head dimension");
@@ -2019,7 +2026,7 @@ vdn_status vdn_vda_quantize(vdn_vda_t h, const void* x, void* x8, float* scale, 
   if (rows > 0 && (!x || !x8 || !scale)) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
   if (rows > 0 && x == x8) return fail(h, VDN_ERR_INVALID_ARG, "x8 must not alias x");
   const size_t es = elem_size(h);
-  if (reinterpret_cast<uintptr_t>(x) % es != 0 || reinterpret_cast<uintptr_t>(scale) % sizeof(float) != 0 || !aligned16(x8))
+  if (reinterpret_cast<uintptr_t>(x) % es != 0 || !aligned(scale) || !aligned16(x8))
     return fail(h, VDN_ERR_INVALID_ARG, "x8 must be 16-byte aligned, x and scale aligned to their elements");
   const long long out_stride = p->out_stride ? p->out_stride : cols;
   if (!row_stride_ok(p->x_stride, cols) || !row_stride_ok(p->out_stride, cols) || out_stride % 16 != 0)
@@ -2066,8 +2073,8 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
     return fail(h, VDN_ERR_INVALID_ARG, "out may only alias add");
   const size_t es = elem_size(h);
   if (!aligned16(a) || !aligned16(w)) return fail(h, VDN_ERR_INVALID_ARG, "a and w must be 16-byte aligned");
-  for (const void* x : {(const void*)p->a_scale, (const void*)p->w_scale, (const void*)p->bias})
-    if (reinterpret_cast<uintptr_t>(x) % sizeof(float) != 0) return fail(h, VDN_ERR_INVALID_ARG, "scales and bias must be aligned to their elements");
+  if (!aligned(p->a_scale) || !aligned(p->w_scale) || !aligned(p->bias))
+    return fail(h, VDN_ERR_INVALID_ARG, "scales and bias must be aligned to their elements");
   if (reinterpret_cast<uintptr_t>(out) % es != 0 || reinterpret_cast<uintptr_t>(p->add) % es != 0)
     return fail(h, VDN_ERR_INVALID_ARG, "out and add must be aligned to their elements");
   vdn::MatmulArgs g = {};
@@ -2108,6 +2115,8 @@ vdn_status vdn_vda_cross_attention(vdn_vda_t h, const void* q, const void* k, co
   if (some && (!q || !out || (a.n_keys > 0 && (!k || !v)))) return fail(h, VDN_ERR_INVALID_ARG, "null tensor pointer");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out))
     return fail(h, VDN_ERR_INVALID_ARG, "q, k, v and out must be 16-byte aligned");
+  if (!aligned(p->lse) || !aligned(p->cu_seqlens) || !aligned(p->lengths))
+    return fail(h, VDN_ERR_INVALID_ARG, "lse, cu_seqlens and lengths must be aligned to their elements");
   if (out && (out == q || out == k || out == v || out == p->mask)) return fail(h, VDN_ERR_INVALID_ARG, "out must not alias an input");
   const size_t es = elem_size(h);
   const long long dq = (long long)a.H * h->cfg.d, dk = (long long)a.Hk * h->cfg.d;
