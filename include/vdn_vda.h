@@ -42,9 +42,9 @@
  * synchronising cuda_stream still covers everything.
  *
  * Errors.  Every call returns a vdn_status; nothing throws, aborts or traps.  Problems the host can see
- * (null or misaligned pointers -- small operands are aligned to their elements --, non-positive sizes, d != cfg.d, workspace too small, 32-bit index overflow,
- * wrong device architecture) are reported synchronously and nothing is enqueued.  Every wait inside a
- * kernel is bounded (vdn_vda_set_wait_limit_us); a wait that runs out records VDN_ERR_TIMEOUT in the handle's
+ * (null pointers, pointers misaligned to 16 bytes or, small operands, to their elements, non-positive sizes,
+ * d != cfg.d, workspace too small, 32-bit index overflow, wrong device architecture) are reported synchronously and
+ * nothing is enqueued.  Every wait inside a kernel is bounded (vdn_vda_set_wait_limit_us); a wait that runs out records VDN_ERR_TIMEOUT in the handle's
  * status word, which vdn_vda_status returns once the caller has synchronised the stream and which stays set
  * until vdn_vda_clear_status.
  *
@@ -445,14 +445,13 @@ vdn_status vdn_vda_scaled_matmul(vdn_vda_t h, const void* a, const void* w, void
  *   p->q_stride, k_stride, v_stride, out_stride   elements from one token to the next (also from the last of a batch row to the first
  *           of the next), 0 = dense; heads of a token are always dense.  Multiples of 16 bytes.
  *   workspace  DEVICE, 256-byte aligned, at least vdn_vda_cross_attention_workspace_bytes (0 where none is needed; NULL is fine
- *           then): long encoders are cut into parts where there are few queries, and sums over more than 32768 keys in one part
- *           (on the tensor cores) are kept there.  An argument and not the handle's, so that
- *           calls that may overlap, or captured graphs, can each have their own; nothing in it outlives the call.
- *   p->scale   -1e30 .. 1e30.
+ *           then): long encoders are cut into parts where there are few queries, and on the tensor cores sums over more than
+ *           32768 keys in one part are kept there (packed: asked for where there are as many in all).  An argument and not the
+ *           handle's, so that calls that may overlap, or captured graphs, can each have their own; nothing in it outlives the call.
+ *   p->scale   -1e30 .. 1e30.  q . k_j, scale q and scale q . k_j have to stay within fp32's range.
  * bf16 with three or more rows to a key head (queries times heads of its group) and a scale above zero runs on the tensor cores (weights
  * exp(z_j - max) rounded to bf16, sums fp32: out is off by about 2.3e-3 in the 2-norm, 1.7e-3 of it its own rounding, whatever
- * the number of keys); one or two rows,
- * other scales, f32, and all with VDN_FLAG_FORCE_SIMT in plain fp32.  Kernels and parts are chosen by sizes alone (packed: by the average
+ * the number of keys); one or two rows, other scales, f32, and all with VDN_FLAG_FORCE_SIMT in plain fp32.  Kernels and parts are chosen by sizes alone (packed: by the average
  * length); lengths stay on the device.  What is not finite among q, k, v that count reaches its own rows of the result only.
  * Enqueues on cuda_stream and returns; does not synchronise. */
 typedef struct {
@@ -564,7 +563,8 @@ vdn_status vdn_vda_clear_status(vdn_vda_t h);
 
 /* Plumbing.  The longest any single wait inside a kernel of this handle may take before its CTA gives up
  * (default 2 s = 2 000 000 microseconds; 1 microsecond .. 1 hour).  A wait covers one pipeline hand-over (a tile
- * arriving, an accumulator being drained), never a whole kernel, so the default is generous for any shape. */
+ * arriving, an accumulator being drained), never a whole kernel, so the default is generous for any shape.  The longest is
+ * vdn_vda_cross_attention's: the keys of a tile of rows, where the other tile of its CTA has none (1 us for each 128 keys). */
 vdn_status vdn_vda_set_wait_limit_us(vdn_vda_t h, unsigned long long microseconds);
 
 /* Test support (no counterpart in the paper): exercises the give-up path of the bounded waits without touching

@@ -91,8 +91,8 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = raw;
 }
 
-// 2^x, two units in the last place.  Arguments are at most a little above zero where this is used, and below -126 the result does
-// not matter.
+// 2^x, two units in the last place.  Where this is used arguments are at most a little above zero, up to 8 on the tensor cores of
+// cross_attention (whose running maximum may lag by as much), and below -126 the result does not matter.
 __device__ __forceinline__ float exp2_fast(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

@@ -1777,7 +1777,9 @@ int slim_parts(const vdn_vda_s* h, const vdn::MatmulArgs& g, int tok) {
 // Whether more than 64 rows go as few (128 tokens to a tile, the channels cut among CTAs) or as many (pairs of CTAs with 256 x 256 tiles).
 // Microseconds, fitted to graph replays: 6 and 0.8 for each block that a CTA has, times the CTAs on an SM; 4.7 and 0.46 for each block
 // of each round of pairs.  5120 x 5120: 100 rows 16.6 as few, 22.6 as many, 256 rows 26.1 and 23.0; 300 x 9000: 512 rows 13.6 and 37.9;
-// 9000 x 2000: 200 rows 18.7 and 14.2.
+// 9000 x 2000: 200 rows 18.7 and 14.2.  Above 1024 rows always as many, which is as good where there are tiles for half of the pairs
+// (8000 x 256 x 4096 22.6 either way, 3000 x 512 x 5120 24.8) and up to twice as long for narrow results of long sums: 1025 x 130 x 5000 25.1,
+// 14.7 as few; 1500 x 300 x 9000 39.0 and 30.2; 4096 x 128 x 9000 37.3 and 20.9.
 bool matmul_as_few(const vdn_vda_s* h, const vdn::MatmulArgs& g) {
   if (g.M > 1024) return false;
   const int parts = slim_parts(h, g, 128);
@@ -1896,7 +1898,10 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
     s.by_heads = vdn::fast_divide((uint32_t)a.Hk);
     s.by_head_blocks = vdn::fast_divide((uint32_t)s.head_blocks);
     L.units = (long long)a.B * a.Hk * s.pairs;
-    wanted = h->sm_count / L.units;                     // (a CTA an SM: twice or four times as many were slower, 32 requests 53 -> 59 us)
+    // A CTA an SM.  Up to twice as many are slower for short keys (8 requests of 1500 keys 21.8 -> 24.9 us, 300 queries x 8192 x 4 heads 29.1 ->
+    // 37.2; 32 requests: as they are) and faster for long ones where the SMs are no multiple of the units (1560 x 32760 x 4 key heads, masked:
+    // 52 units, so 104 items for 148 SMs, 282 us; 208 items 255, 416 items 251).
+    wanted = h->sm_count / L.units;
     least = 256;
   } else {
     least = 128;
