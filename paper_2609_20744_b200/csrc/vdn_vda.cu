@@ -1142,8 +1142,10 @@ vdn_status vdn_vda_selftest_wait_expiry(vdn_vda_t h, unsigned long long limit_us
   DeviceGuard guard(h->cfg.device);
   if (!guard.ok) return fail(h, VDN_ERR_CUDA, "cannot make the handle's device current");
   const_cast<volatile int*>(h->status_host)[1] = 0;
-  vdn::wait_expiry_selftest_kernel<<<1, 64, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-      vdn::tc::DevStatus{h->status_dev, limit_us * 1000ull}, h->status_dev + 1);
+  const vdn::tc::DevStatus ds{h->status_dev, limit_us * 1000ull};
+  vdn::pair_wait_expiry_selftest_kernel<<<2, 64, 0, static_cast<cudaStream_t>(cuda_stream)>>>(ds, h->status_dev + 1);
+  VDN_CUDA(h, cudaGetLastError());
+  vdn::wait_expiry_selftest_kernel<<<1, 64, 0, static_cast<cudaStream_t>(cuda_stream)>>>(ds, h->status_dev + 1);
   VDN_CUDA(h, cudaGetLastError());
   return VDN_OK;
 }

@@ -1,4 +1,4 @@
-// A stand-alone check of the error path every tensor-core kernel shares: a bounded wait that runs out.
+// Stand-alone checks of the error path every tensor-core kernel shares: a bounded wait that runs out.
 //
 // One CTA, two warps, set up exactly like the pipeline kernels (mbarrier in shared memory, tensor memory
 // allocated by warp 1, the same WaitCtx).  Warp 0 waits on a barrier that nothing ever arrives at and that no
@@ -10,6 +10,53 @@
 #include "tc_common.cuh"
 
 namespace vdn {
+
+// Before it a pair of CTAs that share tensor memory, as those of matmul_pair: a whole warp of the odd one waits for what never comes and
+// leaves as one; the even one has nothing to wait for.  Both meet at the cluster's barriers and give the tensor memory back.  Leaves
+// `kPairLeft` in the marker.
+constexpr int kPairLeft = 1 << 16;
+__global__ void __launch_bounds__(64, 1) __cluster_dims__(2, 1, 1) pair_wait_expiry_selftest_kernel(tc::DevStatus ds, int* left_cleanly) {
+  using namespace tc;
+  __shared__ __align__(8) unsigned long long bar_storage;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag_storage;
+  volatile int* abort_flag = &abort_flag_storage;
+  const uint32_t bar = smem_u32(&bar_storage);
+  const WaitCtx wc(abort_flag, ds);
+  const int warp = threadIdx.x >> 5;
+  const uint32_t rank = cluster_rank();
+
+  if (threadIdx.x == 0) {
+    mbar_init(bar, 1);
+    *abort_flag = 0;
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc_pair(smem_u32(&tmem_slot), 32);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after_sync();
+  const uint32_t tmem_base = tmem_slot;
+
+  bool ok = true;
+  if (warp == 0 && rank == 1) ok = mbar_wait_warp(bar, 0, wc);
+
+  // ---- teardown, as in matmul_pair
+  __syncwarp();
+  tc_fence_before_sync();
+  __syncthreads();
+  cluster_sync();
+  if (warp == 1) {
+    settle(smem_u32(const_cast<int*>(abort_flag)));
+    tc_fence_after_sync();
+    tmem_dealloc_pair(tmem_base, 32);
+  }
+  cluster_sync();
+  if (threadIdx.x == 0 && rank == 1 && !ok) *left_cleanly = kPairLeft;
+}
 
 __global__ void __launch_bounds__(64, 1) wait_expiry_selftest_kernel(tc::DevStatus ds, int* left_cleanly) {
   using namespace tc;
@@ -54,8 +101,11 @@ __global__ void __launch_bounds__(64, 1) wait_expiry_selftest_kernel(tc::DevStat
     tc_fence_after_sync();
     tmem_dealloc(tmem_base, 32);
   }
-  // bit 0: the wait gave up and the CTA got here; bit 1: the warp that had not waited was told at the barrier
-  if (threadIdx.x == 0 && left_cleanly) *left_cleanly = (ok ? 0 : 1) | (told_storage ? 2 : 0);
+  // bit 0: the wait gave up and the CTA got here, and the pair of CTAs before; bit 1: the warp that had not waited was told at the barrier
+  if (threadIdx.x == 0) {
+    const bool pair_left = *(volatile int*)left_cleanly == kPairLeft;
+    *left_cleanly = (!ok && pair_left ? 1 : 0) | (told_storage ? 2 : 0);
+  }
 }
 
 }  // namespace vdn
