@@ -1779,7 +1779,7 @@ int slim_parts(const vdn_vda_s* h, const vdn::MatmulArgs& g, int tok) {
 // Whether more than 64 rows go as few (128 tokens to a tile, the channels cut among CTAs) or as many (pairs of CTAs with 256 x 256 tiles).
 // Microseconds, fitted to graph replays: 6 and 0.8 for each block that a CTA has, times the CTAs on an SM; 4.7 and 0.46 for each block
 // of each round of pairs.  5120 x 5120: 100 rows 16.6 as few, 22.6 as many, 256 rows 26.1 and 23.0; 300 x 9000: 512 rows 13.6 and 37.9;
-// 9000 x 2000: 200 rows 18.7 and 14.2.  Above 1024 rows always as many, which is as good where there are tiles for half of the pairs
+// 9000 x 2000: 200 rows 18.7 and 14.2.  Above 1024 rows always as many, which is as good where there are tiles for a third of the pairs
 // (8000 x 256 x 4096 22.6 either way, 3000 x 512 x 5120 24.8) and up to twice as long for narrow results of long sums: 1025 x 130 x 5000 25.1,
 // 14.7 as few; 1500 x 300 x 9000 39.0 and 30.2; 4096 x 128 x 9000 37.3 and 20.9.
 bool matmul_as_few(const vdn_vda_s* h, const vdn::MatmulArgs& g) {
