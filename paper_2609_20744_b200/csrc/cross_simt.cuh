@@ -26,7 +26,7 @@ struct CrossArgs {
   const uint8_t* mask;        // [keys of all rows] or null; zero: does not count
   float* part_o;              // [B * Lq * H][parts][d]
   float2* part_ml;            // [B * Lq * H][parts] maximum (base 2) and sum
-  float* long_o;              // tensor cores, long parts: sums of the keys so far, [CTA][d][256]
+  float* long_o;              // tensor cores, long parts: sums of the keys so far, [CTA][d + 2][256]
   long long q_stride, k_stride, v_stride, out_stride;
   long long n_keys;           // rows of k and v in all
   long long Lk;               // keys of a batch row (not packed)

@@ -19,7 +19,7 @@
 // as those of 128); results stored by the threads instead of by tile copies: 1400 us at 87720 x 512.
 // The tensor cores cut off what an addition leaves over instead of rounding it, so a long sum of values of one sign falls short by about
 // 2^-27 for each of its keys: 5e-4 at 65536 keys, 7e-3 at 2^20, a tenth at 2^24.  Every FOLD tiles O and the sum of weights therefore
-// move to fp32 sums of their own (O's in the workspace), at most 3e-4 short, and start anew.  2^20 keys, 19456 rows, d = 128: 14.9 ms, 14.7 without.
+// move to fp32 sums of their own (O's in the workspace), at most 3e-4 short, and start anew.  2^20 keys, 19456 rows, d = 128: 15.2 ms, 14.7 without.
 // Keys that do not count: their scores are replaced by -inf, their rows of V by zeros in shared memory (zero times what may
 // be anything is not zero).
 #pragma once
@@ -80,7 +80,45 @@ __device__ __forceinline__ CrossItem cross_item(const CrossArgs& a, const CrossT
   return x;
 }
 
-// LONG: some run of keys is longer than FOLD tiles.  (A variant of its own: in common code 87720 x 512 x 40 heads takes 1055 to 1100 us.)
+// A thread's sums of the tiles so far, and back: O's channels, what the weights add up to, and the maximum that both are relative to, ROWS
+// apart.  Functions of their own, with all of it in memory, so that nothing of it lives in registers on the way.
+template <int D>
+__device__ __noinline__ void cross_fold(float* at, uint32_t to, float ms, float l, bool first) {
+  using namespace tc;
+  constexpr int ROWS = CrossTc<D>::ROWS;
+  const float keep = first ? 0.f : exp2_fast(at[(D + 1) * ROWS] - finite_max(ms));
+#pragma unroll 1
+  for (int i = 0; i < D; i += 16) {
+    float o[16];
+    tmem_ld16(to + i, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) at[(i + e) * ROWS] = first ? o[e] : fmaf(at[(i + e) * ROWS], keep, o[e]);
+  }
+  at[D * ROWS] = first ? l : fmaf(at[D * ROWS], keep, l);
+  at[(D + 1) * ROWS] = ms;
+}
+// (returns what is to be added to the sum of weights)
+template <int D>
+__device__ __noinline__ float cross_unfold(const float* at, uint32_t to, float ms) {
+  using namespace tc;
+  constexpr int ROWS = CrossTc<D>::ROWS;
+  const float keep = exp2_fast(at[(D + 1) * ROWS] - finite_max(ms));
+#pragma unroll 1
+  for (int i = 0; i < D; i += 16) {
+    float o[16];
+    tmem_ld16(to + i, o);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[e] = fmaf(at[(i + e) * ROWS], keep, o[e]);
+    tmem_st16(to + i, o);
+  }
+  tmem_wait_st();
+  return at[D * ROWS] * keep;
+}
+
+// LONG: some run of keys may be longer than FOLD tiles.  A variant of its own: what has none that long takes 1 to 3 % longer with it, as a
+// packed batch with so many keys in all does (100 x 512 keys, 1000 queries, 8 heads 264 -> 272 us; with the two functions above in line 295).
 template <int D, bool LONG>
 __global__ void __launch_bounds__(CrossTc<D>::THREADS, 1)
 cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -274,12 +312,12 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const int c = warp >> 2, qd = warp & 3;
     const uint32_t ts = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_S + c * 128, to = tmem + ((uint32_t)(qd * 32) << 16) + G::COL_O + c * D;
     const float sl = a.scale_log2;
-    [[maybe_unused]] float* long_o = a.long_o + (size_t)blockIdx.x * (D * G::ROWS) + threadIdx.x;
     const int lane_head = lane % s.hb, lane_tok = lane / s.hb;
     const uint32_t out_smem = base + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES;
     unsigned char* out_row = base_ptr + G::OFF_OUT + warp * G::CHUNKS * G::OUT_BYTES + lane * 128;
     uint32_t n_s = 0, n_item = 0;
     bool ok = true;
+    [[maybe_unused]] auto long_at = [&] { return a.long_o + (size_t)blockIdx.x * ((D + 2) * G::ROWS) + threadIdx.x; };
     for (uint32_t item = blockIdx.x; item < s.items && ok; item += gridDim.x) {
       const CrossItem x = cross_item(a, s, item);
       if (c == 1 && !x.second) continue;
@@ -289,7 +327,6 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       const bool row_on = lane < block_rows && head_in < a.group && tok < a.Lq;
       float ms = -INFINITY;                                    // the maximum times sl,
       uint64_t sum[2] = {0ull, 0ull};                          // and the sum relative to it, in four parts
-      float ms_long = -INFINITY, l_long = 0.f;                 // the same of the sums in the workspace
       for (int j = 0; j < x.tiles; ++j, ++n_s) {
         const int key0 = x.lo + j * 128;
         uint32_t on[4];
@@ -304,24 +341,12 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         if (!__all_sync(0xffffffffu, mbar_wait(S_FULL(c), n_s & 1, wc))) { ok = false; break; }
         tc_fence_after_sync();
-        if (LONG && j % G::FOLD == 0 && j > 0) {                       // (these scores follow the last product into O, and the next one waits for P)
-          const float keep = exp2_fast(ms_long - finite_max(ms));
-#pragma unroll 1
-          for (int i = 0; i < D; i += 16) {
-            float o[16];
-            tmem_ld16(to + i, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              float* at = long_o + (i + e) * G::ROWS;
-              *at = j == G::FOLD ? o[e] : fmaf(*at, keep, o[e]);
-            }
-          }
+        // (these scores follow the last product into O, and the next one waits for P)
+        if (LONG && j % G::FOLD == 0 && j > 0) {
           float l0, l1;
           f2_unpack(f2_add(sum[0], sum[1]), l0, l1);
-          l_long = fmaf(l_long, keep, l0 + l1);
+          cross_fold<D>(long_at(), to, ms, l0 + l1, j == G::FOLD);
           sum[0] = sum[1] = 0ull;
-          ms_long = ms;
         }
         // (twice, so that a tile whose keys all count has no branch in it: those cost 6 % of a long encoder's time)
         auto weights = [&](auto cut) {
@@ -405,8 +430,7 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
       float l, l1;
       f2_unpack(f2_add(sum[0], sum[1]), l, l1);
       l += l1;
-      const float keep_long = LONG && x.tiles > G::FOLD ? exp2_fast(ms_long - finite_max(ms)) : 0.f;
-      if (LONG) l = fmaf(l_long, keep_long, l);
+      if (LONG && x.tiles > G::FOLD) l += cross_unfold<D>(long_at(), to, ms);
       const long long token = (long long)x.b * a.Lq + tok;
       const long long at = token * a.H + x.hk * a.group + head_in;
       const float r = l == 0.f ? 0.f : 1.f / l;
@@ -424,10 +448,6 @@ cross_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
           if (i + 1 == G::CHUNKS) {
             tc_fence_before_sync();
             mbar_arrive_warp(O_EMPTY(c));
-          }
-          if (LONG && x.tiles > G::FOLD) {
-#pragma unroll
-            for (int e = 0; e < 64; ++e) o[e] = fmaf(long_o[(i * 64 + e) * G::ROWS], keep_long, o[e]);
           }
         } else {
 #pragma unroll

@@ -1929,7 +1929,7 @@ CrossLayout make_cross_layout(const vdn_vda_s* h, const vdn::CrossArgs& a) {
   const long long tiles = ((a.Lk ? a.Lk : a.n_keys) + G::KEYS - 1) / G::KEYS;
   if (L.tc && (tiles + L.parts - 1) / L.parts > G::FOLD) {
     L.long_o = L.total;
-    L.long_bytes = align_up((size_t)std::min<long long>(L.units * L.parts, h->sm_count) * G::ROWS * h->cfg.d * sizeof(float));
+    L.long_bytes = align_up((size_t)std::min<long long>(L.units * L.parts, h->sm_count) * G::ROWS * (h->cfg.d + 2) * sizeof(float));
     L.total += L.long_bytes;
   }
   return L;
